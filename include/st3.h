@@ -483,6 +483,127 @@ ST3_EXPORT st3_status st3_cosine_similarity(const float* va, const int32_t* ids_
                                             int32_t n_b, int32_t batch, int32_t id_space, float* cosine, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Grouped heads, packed prompts, 8-bit caches in blocks.  The calls below serve decoders whose key
+ * heads are shared by groups of query heads, over batches of sequences of different lengths: prompts
+ * that lie one behind the other (st3_packed_attention), a cache of 8-bit codes with a scale for each
+ * block of tokens and key head (st3_block_store, st3_block_decode), and an eviction by the attention
+ * weight that a token has received so far (st3_block_evict; Sec. 3.2's score, added up over the steps,
+ * for each key head).  They stand beside the calls above and share no state with them.
+ * The conventions at the top of this header hold.  None of these calls changes a length: `len` is
+ * read, and the caller advances it once a step for all layers that share it.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t batch;          /* sequences, 1 to 65535 */
+    int32_t heads;          /* H, query heads, up to 1024 */
+    int32_t kv_heads;       /* Hk; divides H: query head h reads key head h / (H / Hk) */
+    int32_t head_dim;       /* d: 64 or 128 */
+    int32_t dtype;          /* st3_dtype of q/k/v/out (the block calls: ST3_BF16) */
+    float   softmax_scale;  /* as in st3_attn_shape */
+} st3_gqa_shape;
+
+/* Rows [T, heads, d] on the DEVICE: element (t,h,c) at data + t*stride_t + h*stride_h + c (strides in elements).
+ * Rows are 16-byte aligned; a slice of a fused projection's output is one. */
+typedef struct {
+    void*   data;
+    int64_t stride_t, stride_h;
+} st3_rows;
+
+/* Bytes of DEVICE workspace that st3_packed_attention needs for `total` packed rows when it leaves scores. */
+ST3_EXPORT size_t st3_packed_workspace_bytes(const st3_gqa_shape* shape, int32_t total);
+
+/* ---------------------------------------------------------------------------------------------
+ * Causal attention over whole prompts (Eq. 2) with grouped heads and packed sequences.
+ * Sequence b owns the rows cu_len[b] .. cu_len[b+1] - 1 of q, k, v and out (cu_len: DEVICE int32
+ * [batch + 1], ascending, cu_len[batch] <= total); n_b is their number, 0 allowed.
+ *   A_h[i,:]     = softmax over j <= i of (q_h[i] . k_{h/G}[j]) * scale,   G = heads / kv_heads
+ *   out[i,h,:]   = sum_j A_h[i,j] v_{h/G}[j]
+ *   score[b,kh,j] = sum_{h in group kh} sum_{i in last `window` rows, i >= j} A_h[i,j],  j in [0, n_b)
+ * total: rows that q, k, v and out have.  max_len: HOST upper bound of n_b; rows of a sequence past it
+ * are not attended.  score: DEVICE float32, row (b,kh) at score + b*score_stride_b + kh*score_stride_h,
+ * or NULL; entries from n_b on are left untouched; the caller's rows hold max_len entries at least.  window >= 1 when a
+ * score is wanted (a prompt shorter than the window counts all of its rows).  out shares no memory with q, k or v (rows of one buffer may
+ * alternate where the strides are equal).  workspace: scratch, read and written only when score is not NULL.
+ * ------------------------------------------------------------------------------------------- */
+ST3_EXPORT st3_status st3_packed_attention(const st3_gqa_shape* shape, const st3_rows* q, const st3_rows* k, const st3_rows* v,
+                                           const int32_t* cu_len, int32_t total, int32_t max_len, const st3_rows* out,
+                                           int32_t window, float* score, int64_t score_stride_b, int64_t score_stride_h,
+                                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* How a block's 8-bit codes stand for values: value = code * scale, one scale for the 64 rows of a block and key head.
+ * ST3_BLOCK_INT8: two's complement in [-127, 127], scale = max|x| / 127.  ST3_BLOCK_E4M3: OCP FP8 E4M3 (see
+ * st3_kv_format), scale = max|x| / 448.  Codes are x / scale in float32 (one correctly rounded division), rounded to nearest, ties
+ * to even, saturated; a block of zeros has scale 0 and codes 0.  The maximum is over finite entries; an infinity saturates,
+ * a NaN becomes code 0 (INT8) or the format's NaN (E4M3). */
+typedef enum { ST3_BLOCK_INT8 = 0, ST3_BLOCK_E4M3 = 1 } st3_block_code;
+
+#define ST3_BLOCK_TOKENS 64
+
+/* One layer's cache in blocks, on the DEVICE.  Row r of sequence b lies in block r / 64: page table[b*table_stride + r/64]
+ * as long as that block is whole (r/64 < len[b]/64); the rows of the last, partial block are kept in 16 bits, in the tail.
+ *   k_codes [n_pages][Hk][64][d]   v_codes [n_pages][Hk][d][64]  (the 64 values of a column side by side)
+ *   k_scale, v_scale float32 [n_pages][Hk]
+ *   k_tail bf16 [batch][Hk][64][d]  v_tail bf16 [batch][Hk][d][64]
+ * Codes and tails are 16-byte aligned.  table holds table_blocks entries a sequence; a block behind them, or one whose entry lies outside
+ * [0, n_pages), does not exist: its rows are not attended and nothing is written for it.  No two sequences share a page that a
+ * call writes.  len: DEVICE int32 [batch], rows that a sequence has; a negative one marks an empty place in the batch:
+ * it gets out = 0 and nothing else happens for it. */
+typedef struct {
+    void*    k_codes;
+    void*    v_codes;
+    float*   k_scale;
+    float*   v_scale;
+    void*    k_tail;
+    void*    v_tail;
+    const int32_t* table;
+    int64_t  table_stride;
+    const int32_t* len;
+    int32_t  table_blocks;
+    int32_t  n_pages;
+    int32_t  code;          /* st3_block_code */
+} st3_block_cache;
+
+/* Writes packed prompts (as for st3_packed_attention) into a cache: rows 0 .. n_b - 1 of sequence b, whole blocks coded into their
+ * pages, the rest into the tail.  cache->len is not read. */
+ST3_EXPORT st3_status st3_block_store(const st3_gqa_shape* shape, const st3_rows* k, const st3_rows* v, const int32_t* cu_len,
+                                      int32_t total, int32_t max_len, const st3_block_cache* cache, void* stream);
+
+/* Bytes of DEVICE workspace that st3_block_decode needs for caches of at most max_len rows. */
+ST3_EXPORT size_t st3_block_workspace_bytes(const st3_gqa_shape* shape, int32_t max_len);
+
+/* ---------------------------------------------------------------------------------------------
+ * One token of every sequence: appended, attended, and the weight it gives added to what each row has received.
+ * With r = len[b] (at most max_len, a HOST bound):
+ *   row r <- k_new[b], v_new[b], in the tail; a block that is whole now (r % 64 == 63) is coded into its page, for later calls
+ *   p_h = softmax over rows 0 .. r of (q_h . k_{h/G}) * scale,   out[b,h,:] = sum_j p_h[j] v_{h/G}[j]
+ *   score[b,kh,j] += sum_{h in group kh} p_h[j]  for j < r,   score[b,kh,r] = that sum at r
+ * q, out: [batch, H, d] rows, k_new, v_new: [batch, Hk, d].  k_new and v_new NULL: rows 0 .. r - 1 are attended and nothing is appended
+ * (no rows: out = 0).  score may be NULL; its rows hold max_len + 1 entries at least.
+ * The cache's `len` still says r behind the call.
+ * ------------------------------------------------------------------------------------------- */
+ST3_EXPORT st3_status st3_block_decode(const st3_gqa_shape* shape, const st3_rows* q, const st3_rows* k_new, const st3_rows* v_new,
+                                       const st3_block_cache* cache, int32_t max_len, const st3_rows* out, float* score,
+                                       int64_t score_stride_b, int64_t score_stride_h, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Eviction by accumulated weight: each key head of a sequence with more than `keep` rows keeps its first n_sink, its last
+ * n_recent and the best of the rest by score (order of st3_select_topk, ties by the lower row; a NaN ranks last), `keep` in all, in
+ * ascending order; a sequence with fewer keeps them all.  With kept[b,kh,0..k_b) the rows kept, k_b = min(len[b], keep):
+ *   row i of `to`     = row kept[i] of `from`        to_score[b,kh,i] = score[b,kh,kept[i]]
+ * to_score may be score itself.  kept (DEVICE int32) is padded with -1 up to keep entries.  A block of `to` that is one whole block of
+ * `from` keeps its codes and scale; others are coded anew from the values that their rows stand for (rounded to bf16 in
+ * the tail), so a value moves by half a step of its new block's scale at most.
+ * `to` shares codes' format with `from` and may share its pools; its table names pages that `from` does not use and its tails are other
+ * buffers, so nothing that is read is written, and `from` stays as it is (but for score).  len of `from` is read, that of `to` is not:
+ * the caller sets lengths to min(len, keep).  0 <= n_sink, n_recent; n_sink + n_recent <= keep; keep >= 1.
+ * ------------------------------------------------------------------------------------------- */
+ST3_EXPORT st3_status st3_block_evict(const st3_gqa_shape* shape, const st3_block_cache* from, const st3_block_cache* to,
+                                      int32_t max_len, int32_t keep, int32_t n_sink, int32_t n_recent, const float* score,
+                                      int64_t score_stride_b, int64_t score_stride_h, float* to_score,
+                                      int64_t to_score_stride_b, int64_t to_score_stride_h, int32_t* kept,
+                                      int64_t kept_stride_b, int64_t kept_stride_h, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Diagnostic block.  Compiled into every build, inert by default: unless the environment held
  * ST3_DEBUG=1 when the library was loaded, every call below returns ST3_ERR_UNSUPPORTED and
  * changes nothing (st3_debug_enabled tells which).  The switches are process-wide and meant for

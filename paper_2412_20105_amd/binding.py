@@ -23,6 +23,8 @@ ST3_ERR_HIP = 4
 ST3_F32, ST3_BF16, ST3_E4M3 = 0, 1, 2
 ST3_KV_PLAIN, ST3_KV_E4M3 = 0, 1
 ST3_STABLE, ST3_HOLE_FILL = 0, 1
+ST3_BLOCK_INT8, ST3_BLOCK_E4M3 = 0, 1
+ST3_BLOCK_TOKENS = 64
 ST3_ANNEAL_COS, ST3_ANNEAL_LINEAR, ST3_ANNEAL_EXP, ST3_ANNEAL_DROP, ST3_ANNEAL_NONE = 0, 1, 2, 3, 4
 
 EXPORTED = [
@@ -33,7 +35,8 @@ EXPORTED = [
     "st3_decode_layer_attend", "st3_decode_plans", "st3_select_columns", "st3_select_compact_layers",
     "st3_schedule_pvtp", "st3_schedule_linear", "st3_schedule_anneal", "st3_kv_bytes",
     "st3_debug_enabled", "st3_debug_set_prefill_path", "st3_debug_set_attend_tile", "st3_profile_enable", "st3_profile_read", "st3_overlap_topk",
-    "st3_cosine_similarity",
+    "st3_cosine_similarity", "st3_packed_workspace_bytes", "st3_packed_attention", "st3_block_store", "st3_block_workspace_bytes",
+    "st3_block_decode", "st3_block_evict",
 ]
 
 
@@ -72,6 +75,21 @@ class GatherPair(C.Structure):
     _fields_ = [("src", C.c_void_p), ("src_stride_b", C.c_int64), ("src_stride_inner", C.c_int64),
                 ("src_stride_row", C.c_int64), ("dst", C.c_void_p), ("dst_stride_b", C.c_int64),
                 ("dst_stride_inner", C.c_int64), ("dst_stride_row", C.c_int64)]
+
+
+class GqaShape(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("softmax_scale", C.c_float)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
+
+
+class BlockCache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("k_tail", C.c_void_p), ("v_tail", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int64),
+                ("len", C.c_void_p), ("table_blocks", C.c_int32), ("n_pages", C.c_int32), ("code", C.c_int32)]
 
 
 ST3_MAX_GATHER = 4
@@ -165,6 +183,21 @@ def lib() -> C.CDLL:
                                             C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                                             C.c_void_p, C.c_void_p]
         L.st3_cosine_similarity.restype = C.c_int
+        L.st3_packed_workspace_bytes.restype = C.c_size_t
+        L.st3_packed_workspace_bytes.argtypes = [P(GqaShape), C.c_int32]
+        L.st3_packed_attention.argtypes = [P(GqaShape), P(Rows), P(Rows), P(Rows), C.c_void_p, C.c_int32, C.c_int32, P(Rows), C.c_int32,
+                                           C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.st3_packed_attention.restype = C.c_int
+        L.st3_block_store.argtypes = [P(GqaShape), P(Rows), P(Rows), C.c_void_p, C.c_int32, C.c_int32, P(BlockCache), C.c_void_p]
+        L.st3_block_store.restype = C.c_int
+        L.st3_block_workspace_bytes.restype = C.c_size_t
+        L.st3_block_workspace_bytes.argtypes = [P(GqaShape), C.c_int32]
+        L.st3_block_decode.argtypes = [P(GqaShape), P(Rows), P(Rows), P(Rows), P(BlockCache), C.c_int32, P(Rows), C.c_void_p, C.c_int64,
+                                       C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.st3_block_decode.restype = C.c_int
+        L.st3_block_evict.argtypes = [P(GqaShape), P(BlockCache), P(BlockCache), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                                      C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]
+        L.st3_block_evict.restype = C.c_int
         L.st3_profile_enable.argtypes = [C.c_int32]
         L.st3_profile_enable.restype = C.c_int
         L.st3_profile_read.argtypes = [P(C.c_double), P(C.c_int64), P(C.c_double), P(C.c_double)]
@@ -225,6 +258,86 @@ def segments(sys_len: int, max_vis_len: int, max_kv_len: int, vis_len: torch.Ten
                  vis_len_hint, tail_start_hint)
     s._refs = (vis_len, kv_len, tail_start)
     return s
+
+
+def gqa_shape(batch: int, heads: int, kv_heads: int, head_dim: int, dtype: int = ST3_BF16, softmax_scale: float = 0.0) -> GqaShape:
+    return GqaShape(batch, heads, kv_heads, head_dim, dtype, softmax_scale)
+
+
+_DTYPE_OF_CODE = {ST3_F32: torch.float32, ST3_BF16: torch.bfloat16}
+
+
+def _rows(shape: GqaShape, t: torch.Tensor, heads: int, total: int) -> Rows:
+    """t [total, heads, d] of the shape's element type, as the library takes it (the caller keeps t alive)."""
+    if tuple(t.shape) != (total, heads, shape.head_dim):
+        raise ValueError(f"rows {tuple(t.shape)}: ({total}, {heads}, {shape.head_dim}) expected")
+    if t.dtype != _DTYPE_OF_CODE.get(shape.dtype) or not t.is_cuda:
+        raise TypeError(f"rows of {t.dtype} on {t.device}: the shape says {_DTYPE_OF_CODE.get(shape.dtype)}, on the device")
+    st, sh, sc = t.stride()
+    if sc != 1 and t.numel():
+        raise ValueError("the elements of a row follow each other")
+    # (a dimension of one element has any stride)
+    d = shape.head_dim
+    if heads == 1:
+        sh = d
+    if total <= 1:
+        st = max(st, heads * sh)
+    return Rows(t.data_ptr(), st, sh)
+
+
+def _ints(t: torch.Tensor, what: str) -> int:
+    if t.dtype != torch.int32 or not t.is_cuda:
+        raise TypeError(f"{what}: int32 on the device expected, {t.dtype} on {t.device} given")
+    return t.data_ptr()
+
+
+def _scores(shape: GqaShape, t: Optional[torch.Tensor], what: str, width: int, dtype=torch.float32):
+    """(address, stride of a sequence, of a key head) of a [batch, kv_heads, >= width] tensor; None stays none."""
+    if t is None:
+        return None, 0, 0
+    if t.dtype != dtype or not t.is_cuda:
+        raise TypeError(f"{what}: {dtype} on the device expected, {t.dtype} on {t.device} given")
+    if t.dim() != 3 or t.shape[0] != shape.batch or t.shape[1] != shape.kv_heads or t.shape[2] < width or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise ValueError(f"{what}: [{shape.batch}, {shape.kv_heads}, {width} or more] expected, entries side by side; {tuple(t.shape)} given")
+    sb, sh = t.stride(0), t.stride(1)
+    if shape.kv_heads == 1:
+        sh = max(sh, width)
+    return t.data_ptr(), sb, sh
+
+
+def block_cache(k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, k_tail: torch.Tensor,
+                v_tail: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor) -> BlockCache:
+    """One layer's cache in blocks of 64 rows.  k_codes [pages, Hk, 64, d] and v_codes [pages, Hk, d, 64]: int8 tensors are
+    INT8 codes, uint8 (or float8_e4m3fn) ones E4M3; scales float32 [pages, Hk]; tails bf16 [batch, Hk, 64, d] and
+    [batch, Hk, d, 64]; table int32 [batch, blocks]; kv_len int32 [batch]."""
+    pages, hk, blk, d = k_codes.shape
+    batch = kv_len.shape[0]
+    want = {"k_codes": (k_codes, (pages, hk, blk, d)), "v_codes": (v_codes, (pages, hk, d, blk)), "k_scale": (k_scale, (pages, hk)),
+            "v_scale": (v_scale, (pages, hk)), "k_tail": (k_tail, (batch, hk, blk, d)), "v_tail": (v_tail, (batch, hk, d, blk))}
+    if blk != ST3_BLOCK_TOKENS or table.dim() != 2 or table.shape[0] != batch:
+        raise ValueError(f"blocks of {ST3_BLOCK_TOKENS} rows and a table for each of {batch} sequences expected")
+    for name, (t, shape) in want.items():
+        if tuple(t.shape) != shape or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"{name}: {shape}, contiguous, on the device expected; {tuple(t.shape)} given")
+    code = {torch.int8: ST3_BLOCK_INT8, torch.uint8: ST3_BLOCK_E4M3, torch.float8_e4m3fn: ST3_BLOCK_E4M3}.get(k_codes.dtype)
+    if code is None or v_codes.dtype != k_codes.dtype:
+        raise TypeError(f"codes of {k_codes.dtype} and {v_codes.dtype}")
+    if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or k_tail.dtype != torch.bfloat16 or v_tail.dtype != torch.bfloat16:
+        raise TypeError("scales are float32, tails bfloat16")
+    if table.shape[1] > 1 and table.stride(1) != 1:
+        raise ValueError("the blocks of a sequence follow each other in the table")
+    if kv_len.dim() != 1 or not (kv_len.is_contiguous()):
+        raise ValueError("kv_len: [batch], contiguous, expected")
+    c = BlockCache(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_tail.data_ptr(), v_tail.data_ptr(),
+                   _ints(table, "table"), max(table.stride(0), table.shape[1]), _ints(kv_len, "kv_len"), table.shape[1], pages, code)
+    c._refs = (k_codes, v_codes, k_scale, v_scale, k_tail, v_tail, table, kv_len)
+    c._dims = (batch, hk, d)
+    return c
+
+
+def _check_cache(shape: GqaShape, cache: BlockCache) -> None:
+    if cache._dims != (shape.batch, shape.kv_heads, shape.head_dim):
+        raise ValueError(f"a cache of (batch, key heads, d) = {cache._dims} for a shape of {(shape.batch, shape.kv_heads, shape.head_dim)}")
 
 
 # The current stream's handle alone (a Stream object around it takes 2.8 us a call, of 13 for the smallest step), where this build
@@ -395,6 +508,63 @@ def st3_decode_plans(shape, layer_steps, n_layers, mode, stream=None):
 
 def st3_select_compact_layers(shape, layer_steps, n_layers, mode, stream=None):
     _check(lib().st3_select_compact_layers(C.byref(shape), n_layers, layer_steps, mode, _stream(stream)), "st3_select_compact_layers")
+
+
+# -- grouped heads, packed prompts, caches in blocks --------------------------------------------
+def st3_packed_workspace_bytes(shape: GqaShape, total: int) -> int:
+    return lib().st3_packed_workspace_bytes(C.byref(shape), total)
+
+
+def st3_packed_attention(shape: GqaShape, q, k, v, cu_len, max_len: int, out, window: int = 0, score=None, workspace=None, stream=None) -> None:
+    """q, out [T, H, d]; k, v [T, Hk, d]; cu_len int32 [batch + 1]; score float32 [batch, Hk, >= max_len] or None."""
+    total = q.shape[0]
+    H, Hk = shape.heads, shape.kv_heads
+    if cu_len.shape != (shape.batch + 1,) or not cu_len.is_contiguous():
+        raise ValueError(f"cu_len: [{shape.batch + 1}], contiguous, expected")
+    sp, sb, sh = _scores(shape, score, "score", max_len)
+    _check(lib().st3_packed_attention(C.byref(shape), C.byref(_rows(shape, q, H, total)), C.byref(_rows(shape, k, Hk, total)),
+                                      C.byref(_rows(shape, v, Hk, total)), _ints(cu_len, "cu_len"), total, max_len,
+                                      C.byref(_rows(shape, out, H, total)), window, sp, sb, sh, _ptr(workspace),
+                                      0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)),
+           "st3_packed_attention")
+
+
+def st3_block_store(shape: GqaShape, k, v, cu_len, max_len: int, cache: BlockCache, stream=None) -> None:
+    """Packed prompts [T, Hk, d] into the cache's pages and tails."""
+    _check_cache(shape, cache)
+    total = k.shape[0]
+    if cu_len.shape != (shape.batch + 1,) or not cu_len.is_contiguous():
+        raise ValueError(f"cu_len: [{shape.batch + 1}], contiguous, expected")
+    _check(lib().st3_block_store(C.byref(shape), C.byref(_rows(shape, k, shape.kv_heads, total)), C.byref(_rows(shape, v, shape.kv_heads, total)),
+                                 _ints(cu_len, "cu_len"), total, max_len, C.byref(cache), _stream(stream)), "st3_block_store")
+
+
+def st3_block_workspace_bytes(shape: GqaShape, max_len: int) -> int:
+    return lib().st3_block_workspace_bytes(C.byref(shape), max_len)
+
+
+def st3_block_decode(shape: GqaShape, q, k_new, v_new, cache: BlockCache, max_len: int, out, score, workspace, stream=None) -> None:
+    """q, out [batch, H, d]; k_new, v_new [batch, Hk, d] or None; score float32 [batch, Hk, > max_len] or None."""
+    _check_cache(shape, cache)
+    B, H, Hk = shape.batch, shape.heads, shape.kv_heads
+    sp, sb, sh = _scores(shape, score, "score", max_len + 1)
+    kn = None if k_new is None else C.byref(_rows(shape, k_new, Hk, B))
+    vn = None if v_new is None else C.byref(_rows(shape, v_new, Hk, B))
+    _check(lib().st3_block_decode(C.byref(shape), C.byref(_rows(shape, q, H, B)), kn, vn, C.byref(cache), max_len,
+                                  C.byref(_rows(shape, out, H, B)), sp, sb, sh, workspace.data_ptr(),
+                                  workspace.numel() * workspace.element_size(), _stream(stream)), "st3_block_decode")
+
+
+def st3_block_evict(shape: GqaShape, src: BlockCache, dst: BlockCache, max_len: int, keep: int, n_sink: int, n_recent: int, score, to_score, kept,
+                    stream=None) -> None:
+    """score float32 [batch, Hk, >= max_len], to_score [batch, Hk, >= min(max_len, keep)], kept int32 [batch, Hk, >= keep]."""
+    _check_cache(shape, src)
+    _check_cache(shape, dst)
+    s = _scores(shape, score, "score", max_len)
+    t = _scores(shape, to_score, "to_score", min(max_len, keep))
+    i = _scores(shape, kept, "kept", keep, torch.int32)
+    _check(lib().st3_block_evict(C.byref(shape), C.byref(src), C.byref(dst), max_len, keep, n_sink, n_recent, *s, *t, *i, _stream(stream)),
+           "st3_block_evict")
 
 
 # -- host-only schedule helpers ---------------------------------------------------------------

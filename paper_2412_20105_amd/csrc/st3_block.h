@@ -1,0 +1,124 @@
+// Shared by the calls for grouped heads: argument checks, the cache of 8-bit blocks as kernels see it, its quantiser.
+#pragma once
+
+#include "st3_mfma.h"
+
+namespace st3 {
+
+constexpr int kBlk = ST3_BLOCK_TOKENS;      // rows of a block
+
+inline st3_status check_gqa_shape(const st3_gqa_shape* s) {
+    if (!s) return ST3_ERR_INVALID_ARG;
+    if (s->batch <= 0 || s->heads <= 0 || s->kv_heads <= 0) return ST3_ERR_INVALID_ARG;
+    if (s->dtype != ST3_F32 && s->dtype != ST3_BF16) return ST3_ERR_UNSUPPORTED;
+    if (s->head_dim != 64 && s->head_dim != 128) return ST3_ERR_UNSUPPORTED;
+    if (s->heads > 1024 || s->batch > 65535) return ST3_ERR_UNSUPPORTED;
+    if (s->heads % s->kv_heads != 0) return ST3_ERR_INVALID_ARG;
+    if (!(s->softmax_scale >= 0.0f)) return ST3_ERR_INVALID_ARG;
+    return ST3_OK;
+}
+
+inline float gqa_scale_log2(const st3_gqa_shape* s) {
+    const float sc = s->softmax_scale > 0.0f ? s->softmax_scale : 1.0f / sqrtf((float)s->head_dim);
+    return sc * kLog2e;
+}
+
+// Rows of eb-byte elements: 16-byte aligned, heads and rows far enough apart not to overlap themselves.
+inline st3_status check_rows(const st3_rows* r, int heads, int D, int eb) {
+    if (!r || !r->data) return ST3_ERR_INVALID_ARG;
+    if (r->stride_h < D || r->stride_t < (heads - 1) * r->stride_h + D) {
+        // (heads outside rows: [H, T, d] seen as [T, H, d])
+        if (r->stride_t < D || r->stride_h < D) return ST3_ERR_INVALID_ARG;
+    }
+    if (!aligned16(r->data) || r->stride_t * eb % 16 != 0 || r->stride_h * eb % 16 != 0) return ST3_ERR_INVALID_ARG;
+    return ST3_OK;
+}
+
+// Whether a row of x meets a row of y.  Of tensors with equal strides it is told exactly (slices of one buffer may
+// alternate); of others, all that lies between the first byte and the last counts.
+inline bool packed_rows_meet(const st3_rows* x, int hx, const st3_rows* y, int hy, int64_t T, int D, int eb) {
+    const int64_t row = (int64_t)D * eb, d = (int64_t)(reinterpret_cast<intptr_t>(y->data) - reinterpret_cast<intptr_t>(x->data));
+    auto extent = [&](const st3_rows* t, int h) { return ((h - 1) * t->stride_h + (T - 1) * t->stride_t) * eb + row; };
+    if (d >= extent(x, hx) || -d >= extent(y, hy)) return false;
+    if (x->stride_t != y->stride_t || x->stride_h != y->stride_h) return true;
+    const int64_t sh = x->stride_h * eb, st = x->stride_t * eb;
+    for (int64_t h = 1 - hx; h < hy; ++h) {
+        // rows i of x and j of y begin gap + (j - i) * st apart; the two nearest values of j - i on either side of -gap / st
+        const int64_t gap = d + h * sh, near = -gap / st;
+        for (int64_t k = near - 1; k <= near + 1; ++k)
+            if (k > -T && k < T && gap + k * st < row && -(gap + k * st) < row) return true;
+    }
+    return false;
+}
+
+inline st3_status check_block_cache(const st3_gqa_shape* s, const st3_block_cache* c) {
+    if (!c || !c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !c->k_tail || !c->v_tail || !c->table || !c->len) return ST3_ERR_INVALID_ARG;
+    if (s->dtype != ST3_BF16) return ST3_ERR_UNSUPPORTED;
+    if (c->code != ST3_BLOCK_INT8 && c->code != ST3_BLOCK_E4M3) return ST3_ERR_INVALID_ARG;
+    if (c->n_pages <= 0 || c->table_blocks <= 0 || c->table_stride < c->table_blocks) return ST3_ERR_INVALID_ARG;
+    if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->k_tail) || !aligned16(c->v_tail)) return ST3_ERR_INVALID_ARG;
+    return ST3_OK;
+}
+
+// The cache as kernels take it.
+struct BlockPages {
+    uint8_t* k_codes; uint8_t* v_codes;
+    float* k_scale; float* v_scale;
+    uint16_t* k_tail; uint16_t* v_tail;
+    const int32_t* table; int64_t table_stride;
+    const int32_t* len;
+    int32_t table_blocks, n_pages;
+};
+
+inline BlockPages block_pages(const st3_block_cache* c) {
+    return BlockPages{reinterpret_cast<uint8_t*>(c->k_codes), reinterpret_cast<uint8_t*>(c->v_codes), c->k_scale, c->v_scale,
+                      reinterpret_cast<uint16_t*>(c->k_tail), reinterpret_cast<uint16_t*>(c->v_tail), c->table, c->table_stride, c->len,
+                      c->table_blocks, c->n_pages};
+}
+
+#if defined(__HIPCC__)
+
+// Page of block j of sequence b; -1: there is none.
+__device__ __forceinline__ int page_of(const BlockPages& c, int b, int j) {
+    if (j >= c.table_blocks) return -1;
+    const int p = c.table[b * c.table_stride + j];
+    return p >= 0 && p < c.n_pages ? p : -1;
+}
+
+template <int CODE> struct BlockCode;
+template <> struct BlockCode<ST3_BLOCK_INT8> {
+    static constexpr float kTop = 127.0f;
+    // x / scale as the format defines it
+    __device__ static __forceinline__ uint32_t code(float x, float scale) {
+        const float y = scale > 0.f ? __fdiv_rn(x, scale) : 0.f;
+        if (!(y == y)) return 0;
+        return (uint32_t)(int)rintf(fminf(fmaxf(y, -kTop), kTop)) & 0xffu;
+    }
+    __device__ static __forceinline__ float value(uint32_t byte) { return (float)(int8_t)byte; }
+    // four codes as four bf16 (exact: at most seven bits)
+    __device__ static __forceinline__ uint2 to_bf16(uint32_t w) {
+        const float f0 = (float)(int8_t)w, f1 = (float)(int8_t)(w >> 8), f2 = (float)(int8_t)(w >> 16), f3 = (float)(int8_t)(w >> 24);
+        return make_uint2(__builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u),
+                          __builtin_amdgcn_perm(__float_as_uint(f3), __float_as_uint(f2), 0x07060302u));
+    }
+};
+template <> struct BlockCode<ST3_BLOCK_E4M3> {
+    static constexpr float kTop = 448.0f;
+    __device__ static __forceinline__ uint32_t code(float x, float scale) {
+        return f32_to_e4m3(scale > 0.f ? __fdiv_rn(x, scale) : x == x ? 0.f : x);
+    }
+    __device__ static __forceinline__ float value(uint32_t byte) { return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0); }
+    __device__ static __forceinline__ uint2 to_bf16(uint32_t w) {
+        const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+        return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+    }
+};
+
+__device__ __forceinline__ float finite_abs(float x) {
+    const float a = fabsf(x);
+    return a <= 3.402823466e38f ? a : 0.f;
+}
+
+#endif  // __HIPCC__
+
+}  // namespace st3

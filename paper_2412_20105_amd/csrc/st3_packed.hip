@@ -1,0 +1,464 @@
+// Causal attention over packed prompts with grouped heads (Eq. 2), and the weight that the last W rows of each prompt give to every key.
+//
+// Rows.  The G query heads that share a key head are rows of ONE matrix: row x of a (sequence, key head) pair is head x % G of position x / G,
+// so a group's queries meet a K and V tile together, any G fills the MFMA's columns, and a tile of rows spans few positions (the
+// causal edge wastes little).  A workgroup takes kRows such rows of a pair and walks the key tiles up to its last position.
+#include <algorithm>
+#include <utility>
+
+#include "st3_block.h"
+
+namespace st3 {
+namespace {
+
+struct PackedArgs {
+    const void* q; const void* k; const void* v; void* out;
+    int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh, o_st, o_sh;     // strides in elements
+    const int32_t* cu;
+    int32_t B, total, max_len, H, Hk, G;
+    int32_t levels;                 // row tiles of the longest prompt that may come
+    float scale_l2;
+    float* score; int64_t s_sb, s_sh;
+    float2* ml;                     // [total][H] maximum and sum of the rows whose weights count; null: no score
+    int32_t window;
+};
+
+struct Seq { int start, n; };
+__device__ __forceinline__ Seq sequence(const PackedArgs& a, int b) {
+    const int s = max(0, min(a.cu[b], a.total)), e = max(s, min(a.cu[b + 1], a.total));
+    return Seq{s, min(e - s, a.max_len)};
+}
+
+// Workgroup -> (sequence, key head, row tile).  A tile costs in proportion to its index, and lengths differ: tiles are dealt in
+// descending order of their index over all sequences, so the launch ends with its shortest workgroups.  Lengths are known to the device
+// only: every wave finds its place with a search over S(t), the number of tiles (of all sequences) with index t or more.  Key heads run fastest:
+// workgroups go round-robin to the 8 XCDs, so with a multiple of 8 key heads a pair's K and V stay in one XCD's L2.
+template <int ROWS>
+__device__ __forceinline__ bool place(const PackedArgs& a, int lane, int& b, int& kh, int& tile, Seq& sq) {
+    kh = blockIdx.x % a.Hk;
+    const int x = blockIdx.x / a.Hk;
+    auto tiles_of = [&](int i) { return i < a.B ? (int)(((int64_t)sequence(a, i).n * a.G + ROWS - 1) / ROWS) : 0; };
+    const int mine = tiles_of(lane);
+    auto from = [&](int t) {            // S(t)
+        int s = max(0, mine - t);
+        for (int i = lane + kWave; i < a.B; i += kWave) s += max(0, tiles_of(i) - t);
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
+        return __builtin_amdgcn_readfirstlane(s);
+    };
+    int lo = 0, hi = a.levels;          // S(lo) > x >= S(hi)
+    if (from(0) <= x) return false;
+    int above = 0;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2, s = from(mid);
+        if (s > x) lo = mid;
+        else { hi = mid; above = s; }
+    }
+    tile = lo;
+    int rank = x - above;               // among the sequences with more than `tile` tiles
+    for (int i0 = 0; i0 < a.B; i0 += kWave) {
+        const bool has = (i0 == 0 ? mine : tiles_of(i0 + lane)) > tile;
+        const uint64_t who = __ballot(has);
+        const int cnt = __popcll(who);
+        if (rank < cnt) {
+            const uint64_t me = __ballot(has && __popcll(who & ((1ull << lane) - 1)) == rank);
+            b = __builtin_amdgcn_readfirstlane(i0 + __ffsll((unsigned long long)me) - 1);
+            sq = sequence(a, b);
+            return true;
+        }
+        rank -= cnt;
+    }
+    return false;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// bf16
+// ---------------------------------------------------------------------------------------------------------------------------------
+
+// A wave's 16 QC rows, as QC columns of 16: lane (c, g) holds row 16 qc + c of each, and of its output the columns 16 dt + 4 g .. + 3.
+template <int D, int QC>
+struct Rows {
+    f32x4 o[D / 16][QC];
+    float m[QC];
+    float l[QC];
+    int pos[QC];            // position of the row: the last key that it sees
+    __device__ __forceinline__ void init() {
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) {
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) o[dt][qc] = f32x4{0.f, 0.f, 0.f, 0.f};
+            m[qc] = -3.402823466e38f; l[qc] = 0.f;
+        }
+    }
+};
+
+// 32 keys for one wave: S^T = K Q^T, one online-softmax update, O^T += V^T P^T.  MASKED: some row does not see some of the keys.
+template <int D, int QC, bool MASKED>
+__device__ __forceinline__ void packed_step(uint32_t Kt, uint32_t Vt, const Frag (&qf)[QC][D / 32], Rows<D, QC>& st, float scale_l2, int g, int k0) {
+    constexpr int KS = D / 32, DT = D / 16;
+    f32x4 s[2][QC];
+    Frag ka[2][KS];
+    auto load_k = [&](int half) {
+#pragma unroll
+        for (int x = 0; x < KS; ++x) ka[half][x].u4 = lds_read16((Kt ^ (64 * x)) + 32 * half * D);
+    };
+    __builtin_amdgcn_s_setprio(1);
+    load_k(0);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        if (half == 0) load_k(1);
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) {
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[half][i].v, qf[qc][i].v, x, 0, 0, 0);
+            s[half][qc] = x;
+        }
+    }
+    constexpr int VB = DT < 4 ? DT : 4;
+    Frag va[VB];
+    auto load_v = [&](int dt) {
+        const uint32_t at = Vt ^ (32 * dt);
+        va[dt % VB].h[0] = lds_read_tr(at);
+        va[dt % VB].h[1] = lds_read_tr(at + 32 * D);
+    };
+#pragma unroll
+    for (int i = 0; i < VB; ++i) load_v(i);
+    __builtin_amdgcn_s_setprio(0);
+    if (MASKED) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int qc = 0; qc < QC; ++qc)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (k0 + 16 * half + 4 * g + r > st.pos[qc]) s[half][qc][r] = -INFINITY;
+    }
+    // the reference point of the exponents follows the maximum only when that has moved by more than kLazy (probabilities reach 2^kLazy at most)
+    constexpr float kLazy = 8.0f;
+    float mx[QC];
+    bool moved = false;
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc) {
+        mx[qc] = fmaxf(fmaxf(fmaxf(s[0][qc][0], s[0][qc][1]), fmaxf(s[0][qc][2], s[0][qc][3])),
+                       fmaxf(fmaxf(s[1][qc][0], s[1][qc][1]), fmaxf(s[1][qc][2], s[1][qc][3]))) * scale_l2;
+        moved |= mx[qc] - st.m[qc] > kLazy;
+    }
+    if (__any(moved)) {
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) {
+            const float cand = fmaxf(st.m[qc], wave_max_from<16>(mx[qc]));
+            const float m_new = cand - st.m[qc] > kLazy ? cand : st.m[qc];
+            const float alpha = exp2_fast(st.m[qc] - m_new);
+            st.m[qc] = m_new;
+            st.l[qc] *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) st.o[dt][qc] *= alpha;
+        }
+    }
+    // P is rounded to bf16 once, to nearest: an error of 2^-9 of a probability at most and without bias, beside the output's own rounding by as much;
+    // the sum is of the unrounded ones
+    Frag pb[QC];
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const f32x2 p = {exp2_fast(fmaf(s[j / 2][qc][2 * (j & 1)], scale_l2, -st.m[qc])),
+                             exp2_fast(fmaf(s[j / 2][qc][2 * (j & 1) + 1], scale_l2, -st.m[qc]))};
+            st.l[qc] += p.x + p.y;
+            pb[qc].w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+        }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+        if (dt > 0 && dt + VB - 1 < DT) load_v(dt + VB - 1);
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) st.o[dt][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[dt % VB].v, pb[qc].v, st.o[dt][qc], 0, 0, 0);
+    }
+}
+
+// Starts the direct loads of the tile of 32 keys at k0 (rows past the last are clamped: no row sees them).
+template <int D>
+__device__ __forceinline__ void load_tile(uint32_t lds, const uint16_t* K, const uint16_t* V, int64_t k_st, int64_t v_st, int k0, int n, int lane, int wave,
+                                          int wave_s) {
+    using L = TileLayout<D, 32>;
+    const int row0 = wave * L::RPI + lane / L::UPR, u = lane % L::UPR;
+    const uint32_t ku = 16 * (u ^ L::k_swz(row0)), vu = 16 * (u ^ L::v_swz(row0));
+    const uint16_t* kp = uniform_ptr(K + k0 * k_st);
+    const uint16_t* vp = uniform_ptr(V + k0 * v_st);
+#pragma unroll
+    for (int i = 0; i < L::NI; ++i) {
+        const uint32_t dst = lds + (4 * i + wave_s) * 1024;
+        const uint32_t row = (uint32_t)min(row0 + 4 * i * L::RPI, n - 1 - k0);
+        direct_load16(kp, ku + row * (uint32_t)(2 * k_st), dst);
+        direct_load16(vp, vu + row * (uint32_t)(2 * v_st), dst + 2 * L::TILE);
+    }
+}
+
+template <int D, int QC>
+__global__ __launch_bounds__(256, 3) void packed_kernel(PackedArgs a) {
+    using L = TileLayout<D, 32>;
+    constexpr int kRows = 64 * QC, KS = D / 32, DT = D / 16, kRing = 3;
+    __shared__ __attribute__((aligned(1024))) uint16_t buf[kRing * 2 * L::TILE];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wave_s = __builtin_amdgcn_readfirstlane(wave);
+    const int g = lane >> 4, c = lane & 15;
+    int b, kh, tile;
+    Seq sq;
+    if (!place<kRows>(a, lane, b, kh, tile, sq)) return;
+    const int n = sq.n, rows = n * a.G;
+    // row tiles are cut from the end, in whole columns: a prompt's first tile, the cheapest, is the one that is not full
+    const int tiles = (rows + kRows - 1) / kRows, shift = (tiles * kRows - rows) / (16 * QC) * (16 * QC);
+    const int r0 = tile * kRows - shift + wave * 16 * QC;            // the wave's first row; < 0 or >= rows: it has none
+    const uint16_t* K = reinterpret_cast<const uint16_t*>(a.k) + (int64_t)sq.start * a.k_st + kh * a.k_sh;
+    const uint16_t* V = reinterpret_cast<const uint16_t*>(a.v) + (int64_t)sq.start * a.v_st + kh * a.v_sh;
+    const uint32_t lds0 = lds_addr(buf);
+    constexpr int kBuf = 4 * L::TILE;
+    const int last = min(rows, (tile + 1) * kRows - shift) - 1;      // the workgroup's last row
+    const int nt = last / a.G / 32 + 1;
+    auto issue = [&](int t, int slot) { load_tile<D>(lds0 + slot * kBuf, K, V, a.k_st, a.v_st, t * 32, n, lane, wave, wave_s); };
+    issue(0, 0);
+    Rows<D, QC> st;
+    st.init();
+    Frag qf[QC][KS];
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc) {
+        const int r = max(0, min(r0 + 16 * qc + c, rows - 1)), p = r / a.G;
+        st.pos[qc] = p;
+        const uint16_t* row = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(sq.start + p) * a.q_st + (int64_t)(kh * a.G + r - p * a.G) * a.q_sh;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[qc][s].u4 = *reinterpret_cast<const u32x4*>(row + 32 * s + 8 * g);
+    }
+    const bool live = r0 >= 0 && r0 < rows;
+    const int p_first = __builtin_amdgcn_readfirstlane(max(r0, 0) / a.G), p_last = __builtin_amdgcn_readfirstlane(min(r0 + 16 * QC, rows) - 1) / a.G;
+    uint32_t k_at, v_at;                                             // this lane's operands in a tile (as in the prefill's kernel)
+    {
+        k_at = (uint32_t)(2 * (c * D + (g ^ L::k_swz(c)) * 8));
+        const int row = 4 * g + (c >> 2);
+        v_at = (uint32_t)(2 * (row * D + (((c & 3) >> 1) ^ L::v_swz(row)) * 8 + 4 * (c & 1))) + 2 * L::TILE;
+    }
+    if (nt > 1) { issue(1, 1); wait_direct_loads_but<2 * L::NI>(); }
+    else wait_direct_loads();
+    __syncthreads();
+    int slot = 0, next = 2;
+    for (int t = 0; t < nt; ++t) {
+        const int k0 = 32 * t;
+        const uint32_t at = lds0 + slot * kBuf;
+        if (live && k0 <= p_last) {
+            if (k0 + 31 <= p_first) packed_step<D, QC, false>(at + k_at, at + v_at, qf, st, a.scale_l2, g, k0);
+            else packed_step<D, QC, true>(at + k_at, at + v_at, qf, st, a.scale_l2, g, k0);
+        }
+        if (t + 2 < nt) { issue(t + 2, next); wait_direct_loads_but<2 * L::NI>(); }
+        else wait_direct_loads();
+        __syncthreads();
+        slot = slot == kRing - 1 ? 0 : slot + 1;
+        next = next == kRing - 1 ? 0 : next + 1;
+    }
+    // ---- normalise; the block of outputs goes through LDS and leaves as whole rows ----------------------------------------------
+    constexpr int OSTR = D + 8, VPR = D / 8, RPI = 64 / VPR;
+    static_assert(4 * 16 * QC * OSTR <= kRing * 2 * L::TILE, "the waves' output blocks fit the tile buffers");
+    uint16_t* ob = buf + wave * 16 * QC * OSTR;
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc) {
+        const float l = wave_sum_from<16>(st.l[qc]), rl = 1.0f / l;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const f32x4 o = st.o[dt][qc] * rl;
+            const f32x2 o01 = {o[0], o[1]}, o23 = {o[2], o[3]};
+            uint2 pk;
+            pk.x = __builtin_bit_cast(uint32_t, __builtin_convertvector(o01, bf16x2));
+            pk.y = __builtin_bit_cast(uint32_t, __builtin_convertvector(o23, bf16x2));
+            *reinterpret_cast<uint2*>(ob + (16 * qc + c) * OSTR + 16 * dt + 4 * g) = pk;
+        }
+        const int r = r0 + 16 * qc + c;
+        if (a.ml != nullptr && g == 0 && r >= 0 && r < rows && st.pos[qc] >= n - a.window)
+            a.ml[(int64_t)(sq.start + st.pos[qc]) * a.H + kh * a.G + r - st.pos[qc] * a.G] = make_float2(st.m[qc], rl);
+    }
+    uint16_t* O = reinterpret_cast<uint16_t*>(a.out);
+#pragma unroll
+    for (int i = 0; i < 16 * QC / RPI; ++i) {
+        const int x = i * RPI + lane / VPR, r = r0 + x;
+        const u32x4 val = *reinterpret_cast<const u32x4*>(ob + x * OSTR + (lane % VPR) * 8);
+        if (r >= 0 && r < rows) {
+            const int p = r / a.G;
+            *reinterpret_cast<u32x4*>(O + (int64_t)(sq.start + p) * a.o_st + (int64_t)(kh * a.G + r - p * a.G) * a.o_sh + (lane % VPR) * 8) = val;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// A row's operand of a product over d, straight from memory: lane (c, g) holds elements of row c, in the same order for both operands.
+// ---------------------------------------------------------------------------------------------------------------------------------
+template <typename T, int D> struct RowFrag;
+template <int D> struct RowFrag<bf16_t, D> {
+    Frag f[D / 32];
+    __device__ __forceinline__ void load(const bf16_t* row, int g) {
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) f[s].u4 = *reinterpret_cast<const u32x4*>(row + 32 * s + 8 * g);
+    }
+    __device__ __forceinline__ f32x4 dot(const RowFrag& o) const {      // [row of this][row of o]
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[s].v, o.f[s].v, x, 0, 0, 0);
+        return x;
+    }
+};
+template <int D> struct RowFrag<float, D> {
+    f32x4 f[D / 16];
+    __device__ __forceinline__ void load(const float* row, int g) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) f[s] = *reinterpret_cast<const f32x4*>(row + 16 * s + 4 * g);
+    }
+    __device__ __forceinline__ f32x4 dot(const RowFrag& o) const {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(f[s][e], o.f[s][e], x, 0, 0, 0);
+        return x;
+    }
+};
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// float32: the same rows on v_mfma_f32_16x16x4f32 (A: lane (c, g) holds A[c][g]), 16 rows a wave, 64 a workgroup, operands straight from memory.
+// ---------------------------------------------------------------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256) void packed_f32_kernel(PackedArgs a) {
+    constexpr int DT = D / 16, kRows = 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c = lane & 15;
+    int b, kh, tile;
+    Seq sq;
+    if (!place<kRows>(a, lane, b, kh, tile, sq)) return;
+    const int n = sq.n, rows = n * a.G, r0 = tile * kRows + wave * 16;
+    if (r0 >= rows) return;
+    const float* K = reinterpret_cast<const float*>(a.k) + (int64_t)sq.start * a.k_st + kh * a.k_sh;
+    const float* V = reinterpret_cast<const float*>(a.v) + (int64_t)sq.start * a.v_st + kh * a.v_sh;
+    const int r = min(r0 + c, rows - 1), pos = r / a.G, head = kh * a.G + r - pos * a.G;
+    RowFrag<float, D> qf;
+    qf.load(reinterpret_cast<const float*>(a.q) + (int64_t)(sq.start + pos) * a.q_st + (int64_t)head * a.q_sh, g);
+    f32x4 o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -3.402823466e38f, l = 0.f;
+    const int p_last = min(r0 + 15, rows - 1) / a.G;
+    for (int k0 = 0; k0 <= p_last; k0 += 16) {
+        RowFrag<float, D> kf;
+        kf.load(K + (int64_t)min(k0 + c, n - 1) * a.k_st, g);
+        f32x4 s = kf.dot(qf) * a.scale_l2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k0 + 4 * g + i > pos) s[i] = -INFINITY;
+        const float mx = fmaxf(m, wave_max_from<16>(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
+        const float alpha = exp2_fast(m - mx);
+        m = mx;
+        l *= alpha;
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { p[i] = exp2_fast(s[i] - m); l += p[i]; }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            o[dt] *= alpha;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)         // contraction slot g of product i is key 4 g + i, the one whose weight this lane holds
+                o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(V[(int64_t)min(k0 + 4 * g + i, n - 1) * a.v_st + 16 * dt + c], p[i], o[dt], 0, 0, 0);
+        }
+    }
+    const float rl = 1.0f / wave_sum_from<16>(l);
+    if (r0 + c >= rows) return;
+    float* out = reinterpret_cast<float*>(a.out) + (int64_t)(sq.start + pos) * a.o_st + (int64_t)head * a.o_sh;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(out + 16 * dt + 4 * g) = o[dt] * rl;
+    if (a.ml != nullptr && g == 0 && pos >= n - a.window) a.ml[(int64_t)(sq.start + pos) * a.H + head] = make_float2(m, rl);
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// score[b,kh,j] = sum over the rows of the window of exp2(logit - maximum) / sum: the logits are formed again, 16 keys a wave against 16 rows at a
+// time, and a lane adds up what its four keys get.
+// ---------------------------------------------------------------------------------------------------------------------------------
+template <typename T, int D>
+__global__ __launch_bounds__(256) void packed_score_kernel(PackedArgs a) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c = lane & 15;
+    const int kh = blockIdx.x, b = blockIdx.z;
+    const Seq sq = sequence(a, b);
+    const int n = sq.n, k0 = blockIdx.y * 64 + wave * 16;
+    if (k0 >= n) return;
+    RowFrag<T, D> kf;
+    kf.load(reinterpret_cast<const T*>(a.k) + (int64_t)(sq.start + min(k0 + c, n - 1)) * a.k_st + kh * a.k_sh, g);
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    const int first = max(max(0, n - a.window), k0) * a.G, rows = n * a.G;
+    for (int r0 = first; r0 < rows; r0 += 16) {
+        const int r = min(r0 + c, rows - 1), pos = r / a.G, head = kh * a.G + r - pos * a.G;
+        RowFrag<T, D> qf;
+        qf.load(reinterpret_cast<const T*>(a.q) + (int64_t)(sq.start + pos) * a.q_st + (int64_t)head * a.q_sh, g);
+        const float2 ml = a.ml[(int64_t)(sq.start + pos) * a.H + head];
+        const f32x4 s = kf.dot(qf);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float p = exp2_fast(fmaf(s[i], a.scale_l2, -ml.x)) * ml.y;
+            sum[i] += r0 + c < rows && k0 + 4 * g + i <= pos ? p : 0.f;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = group_sum<16>(sum[i]);
+    if (c < 4) {
+        const int key = k0 + 4 * g + c;
+        if (key < n) a.score[b * a.s_sb + kh * a.s_sh + key] = c == 0 ? sum[0] : c == 1 ? sum[1] : c == 2 ? sum[2] : sum[3];
+    }
+}
+
+}  // namespace
+}  // namespace st3
+
+extern "C" size_t st3_packed_workspace_bytes(const st3_gqa_shape* shape, int32_t total) {
+    if (st3::check_gqa_shape(shape) != ST3_OK || total < 0) return 0;
+    return st3::align_up((size_t)total * shape->heads * sizeof(float2), 256);
+}
+
+extern "C" st3_status st3_packed_attention(const st3_gqa_shape* shape, const st3_rows* q, const st3_rows* k, const st3_rows* v,
+                                           const int32_t* cu_len, int32_t total, int32_t max_len, const st3_rows* out, int32_t window,
+                                           float* score, int64_t score_stride_b, int64_t score_stride_h, void* workspace,
+                                           size_t workspace_bytes, void* stream) {
+    using namespace st3;
+    st3_status s = check_gqa_shape(shape);
+    if (s != ST3_OK) return s;
+    const int H = shape->heads, Hk = shape->kv_heads, D = shape->head_dim, eb = elem_bytes(shape->dtype), G = H / Hk;
+    if (!cu_len || total < 0 || max_len < 0 || max_len > total || window < 0) return ST3_ERR_INVALID_ARG;
+    for (auto [r, h] : {std::pair{q, H}, {k, Hk}, {v, Hk}, {out, H}})
+        if ((s = check_rows(r, h, D, eb)) != ST3_OK) return s;
+    if ((int64_t)max_len * G > 0x3fffffff || k->stride_t * eb * 32 >= (int64_t)1 << 31 || v->stride_t * eb * 32 >= (int64_t)1 << 31) return ST3_ERR_UNSUPPORTED;
+    if (total == 0 || max_len == 0) return ST3_OK;
+    if (packed_rows_meet(q, H, out, H, total, D, eb) || packed_rows_meet(k, Hk, out, H, total, D, eb) || packed_rows_meet(v, Hk, out, H, total, D, eb))
+        return ST3_ERR_INVALID_ARG;
+    if (score) {
+        if (window < 1 || score_stride_h < max_len || (shape->batch > 1 && score_stride_b < max_len)) return ST3_ERR_INVALID_ARG;
+        if (!workspace || !aligned16(workspace)) return ST3_ERR_INVALID_ARG;
+        if (workspace_bytes < st3_packed_workspace_bytes(shape, total)) return ST3_ERR_WORKSPACE_TOO_SMALL;
+    }
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    PackedArgs a{q->data, k->data, v->data, out->data, q->stride_t, q->stride_h, k->stride_t, k->stride_h, v->stride_t, v->stride_h, out->stride_t,
+                 out->stride_h, cu_len, shape->batch, total, max_len, H, Hk, G, 0, gqa_scale_log2(shape), score, score_stride_b, score_stride_h,
+                 score ? reinterpret_cast<float2*>(workspace) : nullptr, window};
+    const int rows = shape->dtype == ST3_BF16 ? 128 : 64;
+    a.levels = (int)(((int64_t)max_len * G + rows - 1) / rows);
+    // no more tiles than this, whatever the lengths are: each sequence has one that is not full
+    const int64_t tiles = std::min((int64_t)total * G / rows + std::min(shape->batch, total), (int64_t)a.levels * shape->batch);
+    if (tiles * Hk > 0x7fffffff) return ST3_ERR_UNSUPPORTED;
+    const unsigned grid = (unsigned)(tiles * Hk);
+    if (shape->dtype == ST3_BF16) {
+        if (D == 128) packed_kernel<128, 2><<<grid, 256, 0, st>>>(a);
+        else packed_kernel<64, 2><<<grid, 256, 0, st>>>(a);
+    } else {
+        if (D == 128) packed_f32_kernel<128><<<grid, 256, 0, st>>>(a);
+        else packed_f32_kernel<64><<<grid, 256, 0, st>>>(a);
+    }
+    if (score) {
+        const dim3 sg(Hk, (max_len + 63) / 64, shape->batch);
+        if (sg.y > 65535) return ST3_ERR_UNSUPPORTED;
+        if (shape->dtype == ST3_BF16) {
+            if (D == 128) packed_score_kernel<bf16_t, 128><<<sg, 256, 0, st>>>(a);
+            else packed_score_kernel<bf16_t, 64><<<sg, 256, 0, st>>>(a);
+        } else {
+            if (D == 128) packed_score_kernel<float, 128><<<sg, 256, 0, st>>>(a);
+            else packed_score_kernel<float, 64><<<sg, 256, 0, st>>>(a);
+        }
+    }
+    return check_launch();
+}
