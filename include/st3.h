@@ -530,8 +530,8 @@ ST3_EXPORT st3_status st3_packed_attention(const st3_gqa_shape* shape, const st3
                                            void* workspace, size_t workspace_bytes, void* stream);
 
 /* How a block's 8-bit codes stand for values: value = code * scale, one scale for the 64 rows of a block and key head.
- * ST3_BLOCK_INT8: two's complement in [-127, 127], scale = max|x| / 127.  ST3_BLOCK_E4M3: OCP FP8 E4M3 (see
- * st3_kv_format), scale = max|x| / 448.  Codes are x / scale in float32 (one correctly rounded division), rounded to nearest, ties
+ * ST3_BLOCK_INT8: two's complement in [-127, 127], scale = max|x| * (1/127), both in float32.  ST3_BLOCK_E4M3: OCP FP8 E4M3 (see
+ * st3_kv_format), scale = max|x| * (1/448).  Codes are x / scale in float32 (one correctly rounded division), rounded to nearest, ties
  * to even, saturated; a block of zeros has scale 0 and codes 0.  The maximum is over finite entries; an infinity saturates,
  * a NaN becomes code 0 (INT8) or the format's NaN (E4M3). */
 typedef enum { ST3_BLOCK_INT8 = 0, ST3_BLOCK_E4M3 = 1 } st3_block_code;

@@ -43,7 +43,7 @@ def quantize_block(x: np.ndarray, code: str):
     x = np.asarray(x, np.float32)
     top = np.float32(127.0 if code == "int8" else 448.0)
     finite = np.where(np.isfinite(x), np.abs(x), np.float32(0))
-    scale = np.float32(finite.max()) / top
+    scale = np.float32(finite.max()) * (np.float32(1) / top)
     if scale > 0:
         with np.errstate(invalid="ignore", over="ignore"):
             y = x / scale

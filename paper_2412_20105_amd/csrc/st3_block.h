@@ -87,7 +87,7 @@ __device__ __forceinline__ int page_of(const BlockPages& c, int b, int j) {
 
 template <int CODE> struct BlockCode;
 template <> struct BlockCode<ST3_BLOCK_INT8> {
-    static constexpr float kTop = 127.0f;
+    static constexpr float kTop = 127.0f, kUnit = 1.0f / 127.0f;
     // x / scale as the format defines it
     __device__ static __forceinline__ uint32_t code(float x, float scale) {
         const float y = scale > 0.f ? __fdiv_rn(x, scale) : 0.f;
@@ -103,7 +103,7 @@ template <> struct BlockCode<ST3_BLOCK_INT8> {
     }
 };
 template <> struct BlockCode<ST3_BLOCK_E4M3> {
-    static constexpr float kTop = 448.0f;
+    static constexpr float kTop = 448.0f, kUnit = 1.0f / 448.0f;
     __device__ static __forceinline__ uint32_t code(float x, float scale) {
         return f32_to_e4m3(scale > 0.f ? __fdiv_rn(x, scale) : x == x ? 0.f : x);
     }

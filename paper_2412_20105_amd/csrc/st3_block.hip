@@ -30,7 +30,7 @@ __device__ __forceinline__ void write_block(const float (&x)[D / 4], uint8_t* co
     float mx = 0.f;
 #pragma unroll
     for (int e = 0; e < D / 4; ++e) mx = fmaxf(mx, finite_abs(x[e]));
-    const float scale = __fdiv_rn(block_max(mx, sm, tid), F::kTop);
+    const float scale = block_max(mx, sm, tid) * F::kUnit;
     if (tid == 0) *scale_out = scale;
     if constexpr (COLUMNS) {
 #pragma unroll

@@ -267,7 +267,7 @@ __global__ __launch_bounds__(256) void block_finish_kernel(BlockDecodeArgs a) {
             __syncthreads();
             if ((tid & 63) == 0) sm[tid >> 6] = mx;
             __syncthreads();
-            const float scale = __fdiv_rn(fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])), F::kTop);
+            const float scale = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])) * F::kUnit;
             for (int e = tid; e < kBlk * D; e += 256) dst[e] = (uint8_t)F::code(__uint_as_float((uint32_t)src[e] << 16), scale);
             if (tid == 0) (which ? a.c.v_scale : a.c.k_scale)[at] = scale;
         }

@@ -93,6 +93,7 @@ struct Rows {
 };
 
 // 32 keys for one wave: S^T = K Q^T, one online-softmax update, O^T += V^T P^T.  MASKED: some row does not see some of the keys.
+// (The scheduling barriers keep the compiler from holding more fragments than there are registers for.)
 template <int D, int QC, bool MASKED>
 __device__ __forceinline__ void packed_step(uint32_t Kt, uint32_t Vt, const Frag (&qf)[QC][D / 32], Rows<D, QC>& st, float scale_l2, int g, int k0) {
     constexpr int KS = D / 32, DT = D / 16;
@@ -107,12 +108,14 @@ __device__ __forceinline__ void packed_step(uint32_t Kt, uint32_t Vt, const Frag
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         if (half == 0) load_k(1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int qc = 0; qc < QC; ++qc) {
             f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < KS; ++i) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[half][i].v, qf[qc][i].v, x, 0, 0, 0);
             s[half][qc] = x;
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     constexpr int VB = DT < 4 ? DT : 4;
@@ -124,6 +127,7 @@ __device__ __forceinline__ void packed_step(uint32_t Kt, uint32_t Vt, const Frag
     };
 #pragma unroll
     for (int i = 0; i < VB; ++i) load_v(i);
+    __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(0);
     if (MASKED) {
 #pragma unroll
@@ -156,8 +160,8 @@ __device__ __forceinline__ void packed_step(uint32_t Kt, uint32_t Vt, const Frag
             for (int dt = 0; dt < DT; ++dt) st.o[dt][qc] *= alpha;
         }
     }
-    // P is rounded to bf16 once, to nearest: an error of 2^-9 of a probability at most and without bias, beside the output's own rounding by as much;
-    // the sum is of the unrounded ones
+    // P is rounded to bf16 once, to nearest: an error of 2^-8 of a probability at most and without bias, beside the output's own rounding by as
+    // much; the sum is of the unrounded ones
     Frag pb[QC];
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc)
@@ -171,34 +175,49 @@ __device__ __forceinline__ void packed_step(uint32_t Kt, uint32_t Vt, const Frag
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
         if (dt > 0 && dt + VB - 1 < DT) load_v(dt + VB - 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int qc = 0; qc < QC; ++qc) st.o[dt][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[dt % VB].v, pb[qc].v, st.o[dt][qc], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-// Starts the direct loads of the tile of 32 keys at k0 (rows past the last are clamped: no row sees them).
+// Starts the direct loads of the tile of 32 keys at k0 (rows past the last are clamped: no row sees them).  k_lane, v_lane: byte offset of
+// this lane's 16 bytes in a tile's first 1 KB; the 1 KB pieces of a tile lie RPI * 4 rows apart.
 template <int D>
-__device__ __forceinline__ void load_tile(uint32_t lds, const uint16_t* K, const uint16_t* V, int64_t k_st, int64_t v_st, int k0, int n, int lane, int wave,
-                                          int wave_s) {
+__device__ __forceinline__ void load_tile(uint32_t lds, const uint16_t* K, const uint16_t* V, int64_t k_st, int64_t v_st, int k0, int n, uint32_t k_lane,
+                                          uint32_t v_lane, int row0, int wave_s) {
     using L = TileLayout<D, 32>;
-    const int row0 = wave * L::RPI + lane / L::UPR, u = lane % L::UPR;
-    const uint32_t ku = 16 * (u ^ L::k_swz(row0)), vu = 16 * (u ^ L::v_swz(row0));
-    const uint16_t* kp = uniform_ptr(K + k0 * k_st);
-    const uint16_t* vp = uniform_ptr(V + k0 * v_st);
+    if (k0 + 32 <= n) {
 #pragma unroll
-    for (int i = 0; i < L::NI; ++i) {
-        const uint32_t dst = lds + (4 * i + wave_s) * 1024;
-        const uint32_t row = (uint32_t)min(row0 + 4 * i * L::RPI, n - 1 - k0);
-        direct_load16(kp, ku + row * (uint32_t)(2 * k_st), dst);
-        direct_load16(vp, vu + row * (uint32_t)(2 * v_st), dst + 2 * L::TILE);
+        for (int i = 0; i < L::NI; ++i) {
+            const uint32_t dst = lds + (4 * i + wave_s) * 1024;
+            direct_load16(uniform_ptr(K + (k0 + 4 * i * L::RPI) * k_st), k_lane, dst);
+            direct_load16(uniform_ptr(V + (k0 + 4 * i * L::RPI) * v_st), v_lane, dst + 2 * L::TILE);
+        }
+    } else {
+        const uint16_t* kp = uniform_ptr(K + k0 * k_st);
+        const uint16_t* vp = uniform_ptr(V + k0 * v_st);
+#pragma unroll
+        for (int i = 0; i < L::NI; ++i) {
+            const uint32_t dst = lds + (4 * i + wave_s) * 1024;
+            const int back = min(row0 + 4 * i * L::RPI, n - 1 - k0) - row0;          // rows from where k_lane points
+            direct_load16(kp, k_lane + (uint32_t)(back * (int)(2 * k_st)), dst);
+            direct_load16(vp, v_lane + (uint32_t)(back * (int)(2 * v_st)), dst + 2 * L::TILE);
+        }
     }
 }
 
+#ifndef ST3_PACKED_COLS
+#define ST3_PACKED_COLS 2
+#define ST3_PACKED_WAVES 3
+#endif
 template <int D, int QC>
-__global__ __launch_bounds__(256, 3) void packed_kernel(PackedArgs a) {
+__global__ __launch_bounds__(256, ST3_PACKED_WAVES) void packed_kernel(PackedArgs a) {
     using L = TileLayout<D, 32>;
-    constexpr int kRows = 64 * QC, KS = D / 32, DT = D / 16, kRing = 3;
-    __shared__ __attribute__((aligned(1024))) uint16_t buf[kRing * 2 * L::TILE];
+    constexpr int kRows = 64 * QC, KS = D / 32, DT = D / 16, kRing = 3, OSTR = D + 8;
+    constexpr int kTiles = kRing * 2 * L::TILE, kOut = 4 * 16 * QC * OSTR;
+    __shared__ __attribute__((aligned(1024))) uint16_t buf[kTiles > kOut ? kTiles : kOut];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wave_s = __builtin_amdgcn_readfirstlane(wave);
     const int g = lane >> 4, c = lane & 15;
     int b, kh, tile;
@@ -214,7 +233,10 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(PackedArgs a) {
     constexpr int kBuf = 4 * L::TILE;
     const int last = min(rows, (tile + 1) * kRows - shift) - 1;      // the workgroup's last row
     const int nt = last / a.G / 32 + 1;
-    auto issue = [&](int t, int slot) { load_tile<D>(lds0 + slot * kBuf, K, V, a.k_st, a.v_st, t * 32, n, lane, wave, wave_s); };
+    const int row0 = wave * L::RPI + lane / L::UPR;
+    const uint32_t k_lane = (uint32_t)(2 * (row0 * (int)a.k_st + (lane % L::UPR ^ L::k_swz(row0)) * 8));
+    const uint32_t v_lane = (uint32_t)(2 * (row0 * (int)a.v_st + (lane % L::UPR ^ L::v_swz(row0)) * 8));
+    auto issue = [&](int t, int slot) { load_tile<D>(lds0 + slot * kBuf, K, V, a.k_st, a.v_st, t * 32, n, k_lane, v_lane, row0, wave_s); };
     issue(0, 0);
     Rows<D, QC> st;
     st.init();
@@ -227,8 +249,7 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(PackedArgs a) {
 #pragma unroll
         for (int s = 0; s < KS; ++s) qf[qc][s].u4 = *reinterpret_cast<const u32x4*>(row + 32 * s + 8 * g);
     }
-    const bool live = r0 >= 0 && r0 < rows;
-    const int p_first = __builtin_amdgcn_readfirstlane(max(r0, 0) / a.G), p_last = __builtin_amdgcn_readfirstlane(min(r0 + 16 * QC, rows) - 1) / a.G;
+    const int p_last = __builtin_amdgcn_readfirstlane(min(r0 + 16 * QC, rows) - 1) / a.G;        // (a wave without rows has none or works on its neighbour's)
     uint32_t k_at, v_at;                                             // this lane's operands in a tile (as in the prefill's kernel)
     {
         k_at = (uint32_t)(2 * (c * D + (g ^ L::k_swz(c)) * 8));
@@ -238,23 +259,28 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(PackedArgs a) {
     if (nt > 1) { issue(1, 1); wait_direct_loads_but<2 * L::NI>(); }
     else wait_direct_loads();
     __syncthreads();
-    int slot = 0, next = 2;
-    for (int t = 0; t < nt; ++t) {
-        const int k0 = 32 * t;
-        const uint32_t at = lds0 + slot * kBuf;
-        if (live && k0 <= p_last) {
-            if (k0 + 31 <= p_first) packed_step<D, QC, false>(at + k_at, at + v_at, qf, st, a.scale_l2, g, k0);
-            else packed_step<D, QC, true>(at + k_at, at + v_at, qf, st, a.scale_l2, g, k0);
-        }
+    // Tiles that every row of the workgroup sees whole come first, in a loop without conditions (with both kinds in one loop the accumulators were moved
+    // between the two forms' registers, and spilled); the few at the edge follow.
+    int t = 0, slot = 0, next = 2;
+    auto advance = [&]() {
         if (t + 2 < nt) { issue(t + 2, next); wait_direct_loads_but<2 * L::NI>(); }
         else wait_direct_loads();
         __syncthreads();
         slot = slot == kRing - 1 ? 0 : slot + 1;
         next = next == kRing - 1 ? 0 : next + 1;
+    };
+    for (const int whole = (max(tile * kRows - shift, 0) / a.G + 1) / 32; t < whole; ++t) {
+        const uint32_t at = lds0 + slot * kBuf;
+        packed_step<D, QC, false>(at + k_at, at + v_at, qf, st, a.scale_l2, g, 32 * t);
+        advance();
+    }
+    for (; t < nt; ++t) {
+        const uint32_t at = lds0 + slot * kBuf;
+        if (32 * t <= p_last) packed_step<D, QC, true>(at + k_at, at + v_at, qf, st, a.scale_l2, g, 32 * t);
+        advance();
     }
     // ---- normalise; the block of outputs goes through LDS and leaves as whole rows ----------------------------------------------
-    constexpr int OSTR = D + 8, VPR = D / 8, RPI = 64 / VPR;
-    static_assert(4 * 16 * QC * OSTR <= kRing * 2 * L::TILE, "the waves' output blocks fit the tile buffers");
+    constexpr int VPR = D / 8, RPI = 64 / VPR;
     uint16_t* ob = buf + wave * 16 * QC * OSTR;
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc) {
@@ -436,15 +462,15 @@ extern "C" st3_status st3_packed_attention(const st3_gqa_shape* shape, const st3
     PackedArgs a{q->data, k->data, v->data, out->data, q->stride_t, q->stride_h, k->stride_t, k->stride_h, v->stride_t, v->stride_h, out->stride_t,
                  out->stride_h, cu_len, shape->batch, total, max_len, H, Hk, G, 0, gqa_scale_log2(shape), score, score_stride_b, score_stride_h,
                  score ? reinterpret_cast<float2*>(workspace) : nullptr, window};
-    const int rows = shape->dtype == ST3_BF16 ? 128 : 64;
+    const int rows = shape->dtype == ST3_BF16 ? 64 * ST3_PACKED_COLS : 64;
     a.levels = (int)(((int64_t)max_len * G + rows - 1) / rows);
     // no more tiles than this, whatever the lengths are: each sequence has one that is not full
     const int64_t tiles = std::min((int64_t)total * G / rows + std::min(shape->batch, total), (int64_t)a.levels * shape->batch);
     if (tiles * Hk > 0x7fffffff) return ST3_ERR_UNSUPPORTED;
     const unsigned grid = (unsigned)(tiles * Hk);
     if (shape->dtype == ST3_BF16) {
-        if (D == 128) packed_kernel<128, 2><<<grid, 256, 0, st>>>(a);
-        else packed_kernel<64, 2><<<grid, 256, 0, st>>>(a);
+        if (D == 128) packed_kernel<128, ST3_PACKED_COLS><<<grid, 256, 0, st>>>(a);
+        else packed_kernel<64, ST3_PACKED_COLS><<<grid, 256, 0, st>>>(a);
     } else {
         if (D == 128) packed_f32_kernel<128><<<grid, 256, 0, st>>>(a);
         else packed_f32_kernel<64><<<grid, 256, 0, st>>>(a);

@@ -153,7 +153,7 @@ def test_oracle_quantizer():
     x = rng.standard_normal((64, 8)).astype(np.float32)
     for code, top, step in (("int8", 127, 0.5), ("e4m3", 448, 16)):
         c, s = bo.quantize_block(x, code)
-        assert np.abs(c).max() == top and s == np.float32(np.abs(x).max()) / np.float32(top)
+        assert np.abs(c).max() == top and s == np.float32(np.abs(x).max()) * (np.float32(1) / np.float32(top))
         assert np.all(np.abs(c * s - x) <= step * s * (1 + 1e-6))
         z, s = bo.quantize_block(np.zeros((64, 8)), code)
         assert s == 0 and not z.any()
