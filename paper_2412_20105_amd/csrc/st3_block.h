@@ -97,6 +97,7 @@ template <> struct BlockCode<ST3_BLOCK_INT8> {
     __device__ static __forceinline__ float value(uint32_t byte) { return (float)(int8_t)byte; }
     // four codes as four bf16 (exact: at most seven bits)
     __device__ static __forceinline__ uint2 to_bf16(uint32_t w) {
+        asm("" : "+v"(w));              // (opaque: else the bytes are taken apart where the word is loaded, and wait in four registers for one)
         const float f0 = (float)(int8_t)w, f1 = (float)(int8_t)(w >> 8), f2 = (float)(int8_t)(w >> 16), f3 = (float)(int8_t)(w >> 24);
         return make_uint2(__builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u),
                           __builtin_amdgcn_perm(__float_as_uint(f3), __float_as_uint(f2), 0x07060302u));

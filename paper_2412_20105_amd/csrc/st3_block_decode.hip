@@ -16,8 +16,8 @@
 namespace st3 {
 namespace {
 
-constexpr int kMaxChunks = 64;
 constexpr int kCols = 16;               // query heads of a workgroup
+constexpr int kStream = 2;              // cache policy of a load: read once, "nt"
 
 struct BlockDecodeArgs {
     BlockPages c;
@@ -37,21 +37,84 @@ struct BlockDecodeArgs {
 // Blocks that hold rows to attend (the last one may be the tail).
 __device__ __forceinline__ int units_of(int n, bool fresh) { return n / kBlk + (n % kBlk + (fresh ? 1 : 0) > 0 ? 1 : 0); }
 
-template <int D, int CODE>
-__global__ __launch_bounds__(256, 2) void block_attend_kernel(BlockDecodeArgs a) {
+// A block's K lies in a wave's own LDS, rows of D bytes, the 16-byte units of a row permuted: unit u of row r is at u ^ swz(r), so that the 16 rows
+// that a fragment's lanes read (16 (c / 4) + c % 4 + 4 t) lie in 16 different units of the banks.
+template <int D> struct KeyTile {
+    static constexpr int UPR = D / 16, RPI = 1024 / D, NI = kBlk / RPI;     // units of a row; rows of a wave-wide load; loads of a block
+    __device__ static __forceinline__ int swz(int row) { return D == 128 ? ((row >> 4 & 3) << 1 | (row >> 1 & 1)) : row >> 4 & 3; }
+};
+
+// Dynamic LDS: the waves' K blocks, and where those were the waves' outputs [waves][columns][D + 4], their maxima and sums [2][waves][16], the heads' [2][16], and in a launch of whole strips the
+// logits [columns][rows].
+template <int D>
+inline size_t attend_lds(int waves, int cols, int64_t staged_rows) {
+    const size_t keys = (size_t)waves * kBlk * D, parts = sizeof(float) * waves * cols * (D + 4);
+    return std::max(keys, parts) + sizeof(float) * (2 * waves * kCols + 2 * kCols + (size_t)cols * staged_rows);
+}
+
+// WHOLE: a workgroup takes the whole strip, writes the output itself and, from logits that it kept in LDS, the weights.  Else it takes a chunk, and
+// leaves a part of the output and the logits of its keys for the launch behind.
+template <int D, int CODE, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(WAVES * 64, 3) void block_attend_kernel(BlockDecodeArgs a) {
     using F = BlockCode<CODE>;
     constexpr int KS = D / 32, DT = D / 16, KH = D / 64;    // contraction steps of S, row tiles of O, 16-byte pieces of a K row per lane
-    __shared__ float sm_o[4][kCols][D + 4];
-    __shared__ float sm_m[4][kCols], sm_l[4][kCols];
+    constexpr int kThr = WAVES * 64, OS = D + 4;
+    extern __shared__ __attribute__((aligned(16))) float lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
     const int kh = blockIdx.x / a.QG, q0 = (blockIdx.x % a.QG) * kCols, b = blockIdx.z, ch = blockIdx.y;
-    const int nq = min(kCols, a.G - q0);                    // query heads of this workgroup
-    const bool fresh = a.k_new != nullptr;
-    const int n = min(a.c.len[b], a.max_len);
-    const int units = n < 0 ? 0 : units_of(n, fresh), blocks = n / kBlk;
-    if (ch > 0 && ch * a.chunk >= units) return;
-    const int h0 = kh * a.G + q0, u_end = min(units, (ch + 1) * a.chunk);
+    const int nq = min(kCols, a.G - q0), cols = min(kCols, a.G);     // query heads of this workgroup, of the fullest
+    float* sm_o = lds;
+    constexpr int kKeys = WAVES * kBlk * D / 4;             // floats
+    float* sm_m = lds + max(kKeys, WAVES * cols * OS);
+    float* sm_l = sm_m + WAVES * kCols;
+    float* sm_h = sm_l + WAVES * kCols;                     // a head's maximum, and one over its sum
+    float* staged = sm_h + 2 * kCols;                       // [cols][stage_rows]
+    const bool fresh = a.k_new != nullptr, scored = a.score != nullptr;
+    const int n = __builtin_amdgcn_readfirstlane(min(a.c.len[b], a.max_len));
+    const int units = n < 0 ? 0 : units_of(n, fresh), blocks = max(n, 0) / kBlk;
+    if (!WHOLE && ch > 0 && ch * a.chunk >= units) return;
+    const int h0 = kh * a.G + q0, u_begin = WHOLE ? 0 : ch * a.chunk, u_end = WHOLE ? units : min(units, (ch + 1) * a.chunk);
     const int hq = h0 + min(c, nq - 1);                     // this lane's query head (columns past the last repeat it)
+
+    using L = KeyTile<D>;
+    const int krow = 16 * (c >> 2) + (c & 3);               // + 4 t: the key of row c of product t
+    const uint32_t v_lane = (uint32_t)(c * kBlk + 16 * g);
+    uint8_t* keys = reinterpret_cast<uint8_t*>(lds) + wave * (kBlk * D);
+    u32x4 vr[DT];
+    // Direct loads (st3_mfma.h): 1 KB of consecutive rows each, in which a lane chooses the unit that belongs where its 16 bytes land.
+    const uint32_t k_lane = (uint32_t)(lane / L::UPR * D + 16 * ((lane % L::UPR) ^ L::swz(lane / L::UPR)));
+    const uint32_t keys_at = __builtin_amdgcn_readfirstlane(lds_addr(keys));
+    auto load_k = [&](int page) {
+        const uint8_t* p = a.c.k_codes + ((int64_t)page * a.Hk + kh) * (kBlk * D);
+#pragma unroll
+        for (int i = 0; i < L::NI; ++i)                     // (what the first row adds to the permutation of a lane's row comes on top of it)
+            direct_load16_stream(p + 1024 * i, k_lane ^ (16 * L::swz(i * L::RPI)), keys_at + 1024 * i);
+    };
+    // (buffer loads: one base for the block in scalar registers, 32 bits of offset a lane; read once, so past the caches)
+    auto load_v = [&](int page) {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(a.c.v_codes + ((int64_t)page * a.Hk + kh) * (kBlk * D), 0, kBlk * D, 0x00020000);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vr[dt] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, v_lane, 16 * dt * kBlk, kStream);
+    };
+    // A wave's work is at the positions wave, wave + WAVES, ...: first the halves of the tail, where it belongs to the chunk, then the chunk's blocks in order.  Lane i has
+    // the page and the scales of the block at the wave's i-th position (a chunk has no more than 64 of them; fetched one by one they had to be waited for, and with them every load in
+    // flight).  A block without a page is passed over: whatever lies elsewhere is not read.
+    const int u_most = WHOLE ? a.max_len / kBlk : min((ch + 1) * a.chunk, a.max_len / kBlk);       // (known before the length has arrived)
+    const int u_stop = min(u_end, blocks);
+    const bool with_tail = units > blocks && blocks >= u_begin && blocks < u_end;
+    const int tail_rows = n % kBlk + (fresh ? 1 : 0), halves = !with_tail ? 0 : tail_rows > 32 ? 2 : 1;
+    auto unit_at = [&](int i) { return u_begin + wave + WAVES * i - halves; };      // (less than u_begin: a half of the tail)
+    int page_l = -1;
+    float ks_l = 0.f, vs_l = 0.f;
+    {
+        const int unit = unit_at(lane);
+        page_l = unit >= u_begin && unit < u_most ? page_of(a.c, b, unit) : -1;
+        if (page_l >= 0) {
+            const int64_t at = (int64_t)page_l * a.Hk + kh;
+            ks_l = a.c.k_scale[at];
+            vs_l = a.c.v_scale[at];
+        }
+    }
     Frag qf[KS];
     {
         const uint16_t* row = a.q + (int64_t)b * a.q_st + (int64_t)hq * a.q_sh;
@@ -62,14 +125,18 @@ __global__ __launch_bounds__(256, 2) void block_attend_kernel(BlockDecodeArgs a)
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -3.402823466e38f, l = 0.f;
-    float* logit = a.score != nullptr && c < nq ? a.logits + ((int64_t)b * a.H + hq) * a.logit_stride : nullptr;
+    // (a chunk's logits wait in LDS too, and leave as whole lines: from the registers they would go 16 bytes a head at a time)
+    const int stage_rows = (WHOLE ? a.max_len / kBlk + 1 : a.chunk) * kBlk;
+    float* logit = scored && c < nq ? staged + c * stage_rows : nullptr;
 
     // softmax of 64 keys (s[t][i]: key 16 g + 4 t + i, in the log2 domain) and the weights of V, times vs, as two bf16 terms
-    auto weigh = [&](f32x4 (&s)[4], float vs, int u, Frag (&hi)[2], Frag (&lo)[2]) {
+    auto keep_logits = [&](const f32x4 (&s)[4], int unit) {
         if (logit != nullptr) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(logit + u * kBlk + 16 * g + 4 * t) = s[t];
+            for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(logit + (unit - u_begin) * kBlk + 16 * g + 4 * t) = s[t];
         }
+    };
+    auto follow = [&](const f32x4 (&s)[4]) {                // the reference point of the exponents
         float mx = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 4; ++t) mx = fmaxf(mx, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
@@ -83,237 +150,374 @@ __global__ __launch_bounds__(256, 2) void block_attend_kernel(BlockDecodeArgs a)
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
         }
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float p0 = exp2_fast(s[t][2 * j] - m), p1 = exp2_fast(s[t][2 * j + 1] - m);
-                l += p0 + p1;
-                const float w0 = p0 * vs, w1 = p1 * vs;
-                const uint32_t b0 = __float_as_uint(w0), b1 = __float_as_uint(w1);
-                hi[t / 2].w[2 * (t & 1) + j] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
-                const f32x2 rest = {w0 - __uint_as_float(b0 & 0xffff0000u), w1 - __uint_as_float(b1 & 0xffff0000u)};
-                lo[t / 2].w[2 * (t & 1) + j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
-            }
     };
-    const int krow = 16 * (c >> 2) + (c & 3);               // + 4 t: the key of row c of product t
-    for (int u = ch * a.chunk + wave; u < min(u_end, blocks); u += 4) {
-        const int page = page_of(a.c, b, u);
-        if (page < 0) {                                     // (whatever lies elsewhere is not read)
-            if (logit != nullptr) {
+    auto weigh = [&](const f32x4 &s0, const f32x4 &s1, float scale, Frag& hi, Frag& lo) {
 #pragma unroll
-                for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4*>(logit + u * kBlk + 16 * g + 4 * t) = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            }
-            continue;
+        for (int j = 0; j < 4; ++j) {
+            const float p0 = exp2_fast((j < 2 ? s0 : s1)[2 * (j & 1)] - m), p1 = exp2_fast((j < 2 ? s0 : s1)[2 * (j & 1) + 1] - m);
+            l += p0 + p1;
+            const float w0 = p0 * scale, w1 = p1 * scale;
+            const uint32_t b0 = __float_as_uint(w0), b1 = __float_as_uint(w1);
+            hi.w[j] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+            const f32x2 rest = {w0 - __uint_as_float(b0 & 0xffff0000u), w1 - __uint_as_float(b1 & 0xffff0000u)};
+            lo.w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
         }
-        const int64_t at = (int64_t)page * a.Hk + kh;
-        const uint8_t* kp = a.c.k_codes + at * kBlk * D;
-        const uint8_t* vp = a.c.v_codes + at * kBlk * D;
-        const float ks = a.c.k_scale[at] * a.scale_l2, vs = a.c.v_scale[at];
-        uint4 kr[4][KH], vr[DT];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int x = 0; x < KH; ++x) kr[t][x] = *reinterpret_cast<const uint4*>(kp + (krow + 4 * t) * D + 64 * x + 16 * g);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) vr[dt] = *reinterpret_cast<const uint4*>(vp + (16 * dt + c) * kBlk + 16 * g);
-        f32x4 s[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int x = 0; x < KH; ++x) {
-                const uint2 w0 = F::to_bf16(kr[t][x].x), w1 = F::to_bf16(kr[t][x].y), w2 = F::to_bf16(kr[t][x].z), w3 = F::to_bf16(kr[t][x].w);
-                Frag f0, f1;
-                f0.u4 = u32x4{w0.x, w0.y, w1.x, w1.y};
-                f1.u4 = u32x4{w2.x, w2.y, w3.x, w3.y};
-                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0.v, qf[2 * x].v, s[t], 0, 0, 0);
-                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f1.v, qf[2 * x + 1].v, s[t], 0, 0, 0);
-            }
-            s[t] *= ks;
-        }
-        Frag hi[2], lo[2];
-        weigh(s, vs, u, hi, lo);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-            const uint2 w0 = F::to_bf16(vr[dt].x), w1 = F::to_bf16(vr[dt].y), w2 = F::to_bf16(vr[dt].z), w3 = F::to_bf16(vr[dt].w);
-            Frag f[2];
-            f[0].u4 = u32x4{w0.x, w0.y, w1.x, w1.y};
-            f[1].u4 = u32x4{w2.x, w2.y, w3.x, w3.y};
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[x].v, hi[x].v, o[dt], 0, 0, 0);
-                o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[x].v, lo[x].v, o[dt], 0, 0, 0);
-            }
-        }
-    }
-    // ---- the rows in 16 bits, and the new one ------------------------------------------------------------------------------------
-    if (units > blocks && blocks >= ch * a.chunk && blocks < u_end && (blocks - ch * a.chunk) % 4 == wave) {
-        const int r = n % kBlk;                             // rows in the tail; the new row's place
+    };
+    // The rows in 16 bits, and the new one, 32 at a time (product t of two: row 4g'+i of A is key 8 g' + 4 t + i), by the first waves while the others have begun
+    // with the blocks.
+    if (wave < halves) {
+        const int r = n % kBlk, first = 32 * wave;          // rows in the tail, the new row's place; the half's first row
         const int64_t at = ((int64_t)b * a.Hk + kh) * kBlk * D;
         const uint16_t* kt = a.c.k_tail + at;
         const uint16_t* vt = a.c.v_tail + at;
-        const uint16_t* kn = fresh ? a.k_new + (int64_t)b * a.k_st + (int64_t)kh * a.k_sh : nullptr;
-        const uint16_t* vn = fresh ? a.v_new + (int64_t)b * a.v_st + (int64_t)kh * a.v_sh : nullptr;
-        f32x4 s[4];
+        // (without a new row: any row that exists; what it says is masked)
+        const uint16_t* kn = fresh ? a.k_new + (int64_t)b * a.k_st + (int64_t)kh * a.k_sh : kt;
+        const uint16_t* vn = fresh ? a.v_new + (int64_t)b * a.v_st + (int64_t)kh * a.v_sh : vt;
+        Frag tk[2][KS], tv[DT];
+        uint32_t fresh_v[DT];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int key = krow + 4 * t;
-            const uint16_t* row = fresh && key == r ? kn : kt + key * D;
-            s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < 2; ++t) {
+            const int key = first + 8 * (c >> 2) + (c & 3) + 4 * t;
+            const uint16_t* row = key >= r ? kn : kt + key * D;
 #pragma unroll
-            for (int i = 0; i < KS; ++i) {
-                Frag f;
-                f.u4 = *reinterpret_cast<const u32x4*>(row + 64 * (i / 2) + 16 * g + 8 * (i & 1));
-                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[i].v, s[t], 0, 0, 0);
-            }
-            s[t] *= a.scale_l2;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key_c = 16 * g + 4 * t + i;
-                if (key_c > r || (key_c == r && !fresh)) s[t][i] = -INFINITY;       // whatever lies there
-            }
+            for (int i = 0; i < KS; ++i) tk[t][i].u4 = *reinterpret_cast<const u32x4*>(row + 64 * (i / 2) + 16 * g + 8 * (i & 1));
         }
-        Frag hi[2], lo[2];
-        weigh(s, 1.0f, blocks, hi, lo);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
-            const uint32_t fresh_v = fresh ? vn[16 * dt + c] : 0u;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                Frag f;
-                f.u4 = *reinterpret_cast<const u32x4*>(vt + (16 * dt + c) * kBlk + 16 * g + 8 * x);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {               // rows that hold nothing weigh nothing, whatever their bits are
-                    const int key = 16 * g + 8 * x + i;
-                    const uint32_t keep = i & 1 ? 0x0000ffffu : 0xffff0000u;
-                    if (key >= r) f.w[i / 2] = (f.w[i / 2] & keep) | (key == r ? fresh_v << (16 * (i & 1)) : 0u);
-                }
-                o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, hi[x].v, o[dt], 0, 0, 0);
-                o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, lo[x].v, o[dt], 0, 0, 0);
-            }
+            fresh_v[dt] = vn[16 * dt + c];
+            tv[dt].u4 = *reinterpret_cast<const u32x4*>(vt + (16 * dt + c) * kBlk + first + 8 * g);
         }
-        if (fresh && q0 == 0) {
+        __builtin_amdgcn_sched_barrier(0);                  // (all of that is on its way)
+        f32x4 s[4];
+        s[2] = s[3] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tk[t][i].v, qf[i].v, s[t], 0, 0, 0);
+            s[t] *= a.scale_l2;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (first + 8 * g + 4 * t + i >= tail_rows) s[t][i] = -INFINITY;    // whatever lies there
+            if (logit != nullptr) *reinterpret_cast<f32x4*>(logit + (blocks - u_begin) * kBlk + first + 8 * g + 4 * t) = s[t];
+        }
+        follow(s);
+        Frag hi, lo;
+        weigh(s[0], s[1], 1.0f, hi, lo);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            Frag f = tv[dt];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {                   // rows that hold nothing weigh nothing, whatever their bits are
+                const int key = first + 8 * g + i;
+                const uint32_t keep = i & 1 ? 0x0000ffffu : 0xffff0000u;
+                if (key >= r) f.w[i / 2] = (f.w[i / 2] & keep) | (key < tail_rows ? fresh_v[dt] << (16 * (i & 1)) : 0u);
+            }
+            o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, hi.v, o[dt], 0, 0, 0);
+            o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, lo.v, o[dt], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (fresh && q0 == 0 && r / 32 == wave) {
             for (int e = lane; e < D; e += kWave) {
                 a.c.k_tail[at + r * D + e] = kn[e];
                 a.c.v_tail[at + e * kBlk + r] = vn[e];
             }
         }
     }
-    // ---- the four waves' parts ----------------------------------------------------------------------------------------------------
+    auto lane_value = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
+    const int unit_l = unit_at(lane);
+    uint64_t left = __ballot(page_l >= 0 && unit_l < u_stop);
+    for (uint64_t gone = __ballot(page_l < 0 && unit_l >= u_begin && unit_l < u_stop); gone != 0; gone &= gone - 1) {
+        const f32x4 none = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, s[4] = {none, none, none, none};
+        keep_logits(s, unit_at(__ffsll((unsigned long long)gone) - 1));
+    }
+    if (left != 0) {
+        int i = __ffsll((unsigned long long)left) - 1;
+        load_k(__builtin_amdgcn_readlane(page_l, i));
+        load_v(__builtin_amdgcn_readlane(page_l, i));
+        while (true) {
+            left &= left - 1;
+            const int next = left != 0 ? __ffsll((unsigned long long)left) - 1 : -1;
+            wait_direct_loads_but<DT>();                    // K is there: all of the wave's loads but V's, which came behind
+            asm volatile("" ::: "memory");
+            f32x4 s[4];
+            u32x4 kr[2][4];
+            auto fetch = [&](int x) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    kr[x & 1][t] = *reinterpret_cast<const u32x4*>(keys + (krow + 4 * t) * D + 16 * ((4 * x + g) ^ L::swz(krow)));
+            };
+            fetch(0);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < KH; ++x) {
+                if (x + 1 < KH) fetch(x + 1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const u32x4 w = kr[x & 1][t];
+                    const uint2 w0 = F::to_bf16(w.x), w1 = F::to_bf16(w.y), w2 = F::to_bf16(w.z), w3 = F::to_bf16(w.w);
+                    Frag f0, f1;
+                    f0.u4 = u32x4{w0.x, w0.y, w1.x, w1.y};
+                    f1.u4 = u32x4{w2.x, w2.y, w3.x, w3.y};
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0.v, qf[2 * x].v, s[t], 0, 0, 0);
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f1.v, qf[2 * x + 1].v, s[t], 0, 0, 0);
+                    if (t & 1) __builtin_amdgcn_sched_barrier(0);   // (else all codes are converted ahead, into more registers than there are)
+                }
+            }
+            const float ks = lane_value(ks_l, i) * a.scale_l2, vs = lane_value(vs_l, i);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) s[t] *= ks;
+            keep_logits(s, unit_at(i));
+            follow(s);
+            // V is there.  Only now may the next K follow it: the compiler does not see direct loads, and would wait for them where it waits for V.
+            wait_direct_loads();
+            __builtin_amdgcn_sched_barrier(0);
+            if (next >= 0) load_k(__builtin_amdgcn_readlane(page_l, next));
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                Frag hi, lo;
+                weigh(s[2 * x], s[2 * x + 1], vs, hi, lo);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int d2 = 0; d2 < DT; d2 += 2) {        // two chains of products at a time
+                    Frag f[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const uint2 w0 = F::to_bf16(vr[d2 + y][2 * x]), w1 = F::to_bf16(vr[d2 + y][2 * x + 1]);
+                        f[y].u4 = u32x4{w0.x, w0.y, w1.x, w1.y};
+                    }
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) o[d2 + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[y].v, hi.v, o[d2 + y], 0, 0, 0);
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) o[d2 + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[y].v, lo.v, o[d2 + y], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if (next < 0) break;
+            load_v(__builtin_amdgcn_readlane(page_l, next));
+            __builtin_amdgcn_sched_barrier(0);
+            i = next;
+        }
+    }
+    // what the first rows have received so far, on its way while the waves' parts are joined
+    constexpr int kAhead = 4;
+    float old[kAhead];
+    if constexpr (WHOLE) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) old[j] = scored && tid + j * kThr < n ? a.score[b * a.s_sb + kh * a.s_sh + tid + j * kThr] : 0.f;
+    }
+    // ---- the waves' parts ---------------------------------------------------------------------------------------------------------
     l = wave_sum_from<16>(l);
-    if (g == 0) { sm_m[wave][c] = m; sm_l[wave][c] = l; }
+    __syncthreads();                                        // (no wave reads its keys any more)
+    if (g == 0) { sm_m[wave * kCols + c] = m; sm_l[wave * kCols + c] = l; }
+    if (c < nq) {
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(&sm_o[wave][c][16 * dt + 4 * g]) = o[dt];
+        for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(sm_o + (wave * cols + c) * OS + 16 * dt + 4 * g) = o[dt];
+    }
     __syncthreads();
-    for (int e = tid; e < nq * D; e += 256) {
+    for (int e = tid; e < nq * D; e += kThr) {
         const int col = e / D, dim = e % D;
-        float top = sm_m[0][col];
+        float top = sm_m[col];
 #pragma unroll
-        for (int w = 1; w < 4; ++w) top = fmaxf(top, sm_m[w][col]);
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sm_m[w * kCols + col]);
         float sum = 0.f, x = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = exp2_fast(sm_m[w][col] - top);
-            sum = fmaf(sm_l[w][col], f, sum);
-            x = fmaf(sm_o[w][col][dim], f, x);
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = exp2_fast(sm_m[w * kCols + col] - top);
+            sum = fmaf(sm_l[w * kCols + col], f, sum);
+            x = fmaf(sm_o[(w * cols + col) * OS + dim], f, x);
         }
-        const int64_t part = ((int64_t)b * a.H + h0 + col) * a.nsplit + ch;
-        a.part_o[part * D + dim] = x;
-        if (dim == 0) { a.part_ml[2 * part] = top; a.part_ml[2 * part + 1] = sum; }
+        if constexpr (WHOLE) {
+            const float rl = sum > 0.f ? 1.0f / sum : 0.f;
+            a.out[(int64_t)b * a.o_st + (int64_t)(h0 + col) * a.o_sh + dim] = (uint16_t)f32_to_bf16_bits(x * rl);
+            if (dim == 0) { sm_h[col] = top; sm_h[kCols + col] = rl; }
+        } else {
+            const int64_t part = ((int64_t)b * a.H + h0 + col) * a.nsplit + ch;
+            a.part_o[part * D + dim] = x;
+            if (dim == 0) { a.part_ml[2 * part] = top; a.part_ml[2 * part + 1] = sum; }
+        }
+    }
+    if constexpr (!WHOLE) {
+        if (scored) {
+            const int quads = (u_end - u_begin) * (kBlk / 4);
+            for (int e = tid; e < nq * quads; e += kThr) {
+                const int col = e / quads, at = e - col * quads;
+                __builtin_nontemporal_store(reinterpret_cast<const f32x4*>(staged + col * stage_rows)[at],
+                                            reinterpret_cast<f32x4*>(a.logits + ((int64_t)b * a.H + h0 + col) * a.logit_stride + u_begin * kBlk) + at);
+            }
+        }
+    }
+    if constexpr (WHOLE) {
+        if (scored && n >= 0) {                             // (one workgroup holds all heads of the group: the launcher sees to it)
+            __syncthreads();
+            float* score = a.score + b * a.s_sb + kh * a.s_sh;
+            auto weight = [&](int key) {
+                float w = 0.f;
+                for (int col = 0; col < nq; ++col) w = fmaf(exp2_fast(staged[col * stage_rows + key] - sm_h[col]), sm_h[kCols + col], w);
+                return w;
+            };
+            const int rows = n + (fresh ? 1 : 0);
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int key = tid + j * kThr;
+                if (key < rows) score[key] = old[j] + weight(key);
+            }
+            for (int key = tid + kAhead * kThr; key < rows; key += kThr) score[key] = (key < n ? score[key] : 0.f) + weight(key);
+        }
+    }
+    // ---- a block that is whole now -------------------------------------------------------------------------------------------------
+    if (with_tail && fresh && q0 == 0 && n % kBlk == kBlk - 1) {
+        const int to = page_of(a.c, b, n / kBlk);
+        __syncthreads();                                    // (the new row is written, sm_m is free)
+        if (to < 0) return;
+        const int64_t at = (int64_t)to * a.Hk + kh, tail = ((int64_t)b * a.Hk + kh) * kBlk * D;
+        for (int which = 0; which < 2; ++which) {
+            const uint16_t* src = (which ? a.c.v_tail : a.c.k_tail) + tail;     // (codes lie in the tails' own order)
+            uint8_t* dst = (which ? a.c.v_codes : a.c.k_codes) + at * (kBlk * D);
+            float mx = 0.f;
+            for (int e = tid; e < kBlk * D; e += kThr) mx = fmaxf(mx, finite_abs(__uint_as_float((uint32_t)src[e] << 16)));
+            mx = wave_max_from<1>(mx);
+            if (lane == 0) sm_m[which * WAVES + wave] = mx;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, sm_m[which * WAVES + w]);
+            const float scale = mx * F::kUnit;
+            for (int e = tid; e < kBlk * D; e += kThr) dst[e] = (uint8_t)F::code(__uint_as_float((uint32_t)src[e] << 16), scale);
+            if (tid == 0) (which ? a.c.v_scale : a.c.k_scale)[at] = scale;
+        }
     }
 }
 
-// Maximum and sum of a head over its chunks.
-__device__ __forceinline__ float2 head_sum(const BlockDecodeArgs& a, int64_t part, int chunks) {
-    float top = a.part_ml[2 * part], sum = 0.f;
-    for (int i = 1; i < chunks; ++i) top = fmaxf(top, a.part_ml[2 * (part + i)]);
-    for (int i = 0; i < chunks; ++i) sum = fmaf(a.part_ml[2 * (part + i) + 1], exp2_fast(a.part_ml[2 * (part + i)] - top), sum);
-    return make_float2(top, sum > 0.f ? 1.0f / sum : 0.f);
+// Maximum, and one over the sum, of a head over its chunks.
+__device__ __forceinline__ float2 head_sum(const BlockDecodeArgs& a, int64_t part, int chunks, int lane) {
+    float top = -3.402823466e38f, sum = 0.f;
+    for (int i = lane; i < chunks; i += kWave) {
+        const float2 ml = reinterpret_cast<const float2*>(a.part_ml)[part + i];
+        const float m = fmaxf(top, ml.x);
+        sum = sum * exp2_fast(top - m) + ml.y * exp2_fast(ml.x - m);
+        top = m;
+    }
+    const float m = wave_max_from<1>(top);
+    sum = wave_sum_from<1>(sum * exp2_fast(top - m));
+    return make_float2(m, sum > 0.f ? 1.0f / sum : 0.f);
 }
 
-// Behind the attention: workgroups [0, H) merge a head's chunks, the next Hk code a block that is whole now, the rest add 256 keys' weights.
-template <int D, int CODE>
-__global__ __launch_bounds__(256) void block_finish_kernel(BlockDecodeArgs a) {
-    using F = BlockCode<CODE>;
-    const int tid = threadIdx.x, b = blockIdx.y;
+constexpr int kFinishThreads = 256, kScoreKeys = 4 * kFinishThreads;
+
+// Behind the chunks: workgroups [0, H) merge a head's parts, the rest add the weights of 1024 keys of a key head.
+template <int D>
+__global__ __launch_bounds__(kFinishThreads) void block_finish_kernel(BlockDecodeArgs a) {
+    constexpr int kGroups = kFinishThreads / D;             // chunks are dealt to groups of D threads
+    __shared__ float sm[kFinishThreads + 2 * 1024];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.y;
     const bool fresh = a.k_new != nullptr;
     const int n = min(a.c.len[b], a.max_len);
     const int units = n < 0 ? 0 : units_of(n, fresh), chunks = max(1, (units + a.chunk - 1) / a.chunk);
     int x = blockIdx.x;
     if (x < a.H) {
         const int64_t part = ((int64_t)b * a.H + x) * a.nsplit;
-        const float2 hs = head_sum(a, part, chunks);
-        for (int e = tid; e < D; e += 256) {
-            float v = 0.f;
-            for (int i = 0; i < chunks; ++i) v = fmaf(a.part_o[(part + i) * D + e], exp2_fast(a.part_ml[2 * (part + i)] - hs.x), v);
-            a.out[(int64_t)b * a.o_st + (int64_t)x * a.o_sh + e] = (uint16_t)f32_to_bf16_bits(v * hs.y);
+        const float2 hs = head_sum(a, part, chunks, lane);
+        const int dim = tid % D, grp = tid / D;
+        float v = 0.f;
+#pragma unroll 4
+        for (int i = grp; i < chunks; i += kGroups) v = fmaf(a.part_o[(part + i) * D + dim], exp2_fast(a.part_ml[2 * (part + i)] - hs.x), v);
+        sm[tid] = v;
+        __syncthreads();
+        if (grp == 0) {
+#pragma unroll
+            for (int i = 1; i < kGroups; ++i) v += sm[i * D + dim];
+            a.out[(int64_t)b * a.o_st + (int64_t)x * a.o_sh + dim] = (uint16_t)f32_to_bf16_bits(v * hs.y);
         }
         return;
     }
     x -= a.H;
-    if (x < a.Hk) {
-        if (!fresh || n < 0 || n % kBlk != kBlk - 1) return;
-        const int page = page_of(a.c, b, n / kBlk);
-        if (page < 0) return;
-        __shared__ float sm[4];
-        const int64_t at = (int64_t)page * a.Hk + x, tail = ((int64_t)b * a.Hk + x) * kBlk * D;
-        for (int which = 0; which < 2; ++which) {
-            const uint16_t* src = (which ? a.c.v_tail : a.c.k_tail) + tail;     // (codes lie in the tails' own order)
-            uint8_t* dst = (which ? a.c.v_codes : a.c.k_codes) + at * kBlk * D;
-            float mx = 0.f;
-            for (int e = tid; e < kBlk * D; e += 256) mx = fmaxf(mx, finite_abs(__uint_as_float((uint32_t)src[e] << 16)));
-            mx = wave_max_from<1>(mx);
-            __syncthreads();
-            if ((tid & 63) == 0) sm[tid >> 6] = mx;
-            __syncthreads();
-            const float scale = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])) * F::kUnit;
-            for (int e = tid; e < kBlk * D; e += 256) dst[e] = (uint8_t)F::code(__uint_as_float((uint32_t)src[e] << 16), scale);
-            if (tid == 0) (which ? a.c.v_scale : a.c.k_scale)[at] = scale;
-        }
-        return;
+    const int kh = x % a.Hk, first = x / a.Hk * kScoreKeys, rows = n + (fresh ? 1 : 0);
+    if (n < 0 || first >= rows) return;
+    float2* heads = reinterpret_cast<float2*>(sm);
+    for (int i = wave; i < a.G; i += kFinishThreads / kWave) {
+        const float2 hs = head_sum(a, ((int64_t)b * a.H + kh * a.G + i) * a.nsplit, chunks, lane);
+        if (lane == 0) heads[i] = hs;
     }
-    x -= a.Hk;
-    if (a.score == nullptr || n < 0) return;
-    const int kh = x % a.Hk, key = x / a.Hk * 256 + tid, rows = n + (fresh ? 1 : 0);
-    if (x / a.Hk * 256 >= rows) return;
-    float w = 0.f;
-    for (int h = kh * a.G; h < (kh + 1) * a.G; ++h) {
-        const float2 hs = head_sum(a, ((int64_t)b * a.H + h) * a.nsplit, chunks);
-        if (key < rows) w = fmaf(exp2_fast(a.logits[((int64_t)b * a.H + h) * a.logit_stride + key] - hs.x), hs.y, w);
+    __syncthreads();
+    const int key = first + 4 * tid;
+    if (key >= rows) return;
+    const float* logit = a.logits + ((int64_t)b * a.H + kh * a.G) * a.logit_stride + key;
+    f32x4 w = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < a.G; ++i) {
+        const f32x4 s = *reinterpret_cast<const f32x4*>(logit + i * a.logit_stride);
+        const float2 hs = heads[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = fmaf(exp2_fast(s[j] - hs.x), hs.y, w[j]);
     }
-    if (key < rows) {
-        float* s = a.score + b * a.s_sb + kh * a.s_sh + key;
-        *s = key < n ? *s + w : w;
-    }
+    float* score = a.score + b * a.s_sb + kh * a.s_sh + key;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (key + j < rows) score[j] = key + j < n ? score[j] + w[j] : w[j];
 }
 
-struct BlockWs { size_t part_o, part_ml, logits, total; int64_t logit_stride; int chunk, nsplit; };
+// How a call is cut: waves of a workgroup, blocks of a chunk (0: whole strips, one launch).
+//   Whole strips while there are enough to fill the card, or while they are so short that the second launch of a cut costs more than it brings: us a call,
+//   whole / cut, 64 strips of 32 blocks 19.0 / 14.6, 8 strips of 12 blocks 10.2 / 13.4, 256 strips of 10 to 49 blocks 30.3 / 38.8 (with their logits in LDS, up to what
+//   there is of it).
+//   Workgroups of 12 waves, one on a compute unit, where strips are no more than compute units: 256 strips 30.3 us, with 4 waves 34; else of 4 waves, three on a unit:
+//   320 strips of 11 to 20 blocks 20.6 us, with 12 waves 24.2.
+//   Chunks for about three workgroups on a unit; where logits are kept, no longer than leaves room for three in LDS: 16 strips of 1100 to 2049 blocks, 20 blocks (20 KB) 107 us,
+//   10 blocks 116, 40 blocks 109; 512 / 768 / 1536 workgroups without logits 79.4 / 81.2 / 89.0.
+struct Cut { int waves, chunk; };
+constexpr int kWholeStrips = 192, kShortUnits = 20, kManyStrips = 256, kStageBytes = 20 << 10, kChunkWgs = 768;
 
-// Chunks: enough workgroups to fill the card, no more than kMaxChunks a sequence.
-inline BlockWs block_ws(const st3_gqa_shape* s, int max_len) {
-    const int G = s->heads / s->kv_heads, QG = (G + kCols - 1) / kCols;
-    const int64_t units = max_len / kBlk + 1, strips = (int64_t)s->batch * s->kv_heads * QG;
-    int64_t chunk = std::max<int64_t>(4, (units * strips + 511) / 512);
-    chunk = std::max(chunk, (units + kMaxChunks - 1) / kMaxChunks);
+template <int D>
+inline Cut cut_of(int B, int Hk, int G, int max_len, bool scored) {
+    constexpr size_t kLds = 160 << 10;
+    const int QG = (G + kCols - 1) / kCols, cols = std::min(G, kCols);
+    const int64_t units = max_len / kBlk + 1, strips = (int64_t)B * Hk * QG;
+    const int waves = strips > kManyStrips ? 4 : 12;
+    const bool fits = units + 2 <= waves * kWave && (!scored || (QG == 1 && attend_lds<D>(waves, cols, units * kBlk) <= kLds));
+    if (fits && (strips >= kWholeStrips || units <= kShortUnits)) return Cut{waves, 0};
+    int64_t chunk = std::max<int64_t>(4, (units * strips + kChunkWgs - 1) / kChunkWgs);
+    if (scored) chunk = std::min<int64_t>(chunk, std::max<int64_t>(8, kStageBytes / (cols * kBlk * (int)sizeof(float))));
+    return Cut{4, (int)std::min<int64_t>({chunk, units, 4 * kWave - 2})};
+}
+inline Cut cut_of(const st3_gqa_shape* s, int max_len, bool scored) {
+    const int G = s->heads / s->kv_heads;
+    return s->head_dim == 128 ? cut_of<128>(s->batch, s->kv_heads, G, max_len, scored) : cut_of<64>(s->batch, s->kv_heads, G, max_len, scored);
+}
+
+struct BlockWs { size_t part_o, part_ml, logits, total; int64_t logit_stride; int nsplit; };
+
+inline BlockWs block_ws(const st3_gqa_shape* s, int max_len, bool scored) {
+    const Cut cut = cut_of(s, max_len, scored);
+    const int64_t units = max_len / kBlk + 1;
     BlockWs w{};
-    w.chunk = (int)chunk;
-    w.nsplit = (int)((units + chunk - 1) / chunk);
+    if (cut.chunk == 0) return w;
+    w.nsplit = (int)((units + cut.chunk - 1) / cut.chunk);
     w.logit_stride = units * kBlk;
     const size_t BH = (size_t)s->batch * s->heads;
     size_t off = 0;
     w.part_o = off;  off = align_up(off + BH * w.nsplit * s->head_dim * sizeof(float), 256);
     w.part_ml = off; off = align_up(off + BH * w.nsplit * 2 * sizeof(float), 256);
-    w.logits = off;  off = align_up(off + BH * w.logit_stride * sizeof(float), 256);
+    w.logits = off;  if (scored) off = align_up(off + BH * w.logit_stride * sizeof(float), 256);
     w.total = off;
     return w;
 }
 
 template <int D, int CODE>
-void launch_decode(const BlockDecodeArgs& a, int B, hipStream_t st) {
-    block_attend_kernel<D, CODE><<<dim3(a.Hk * a.QG, a.nsplit, B), 256, 0, st>>>(a);
-    const int tiles = a.score ? (a.max_len + 1 + 255) / 256 : 0;
-    block_finish_kernel<D, CODE><<<dim3(a.H + a.Hk + a.Hk * tiles, B), 256, 0, st>>>(a);
+void launch_decode(const BlockDecodeArgs& a, int B, int waves, hipStream_t st) {
+    const int cols = std::min(kCols, a.G);
+    if (a.chunk == 0) {
+        const size_t lds = attend_lds<D>(waves, cols, a.score ? (a.max_len / kBlk + 1) * kBlk : 0);
+        const dim3 grid(a.Hk * a.QG, 1, B);
+        if (waves == 12) block_attend_kernel<D, CODE, 12, true><<<grid, 768, lds, st>>>(a);
+        else block_attend_kernel<D, CODE, 4, true><<<grid, 256, lds, st>>>(a);
+        return;
+    }
+    block_attend_kernel<D, CODE, 4, false><<<dim3(a.Hk * a.QG, a.nsplit, B), 256, attend_lds<D>(4, cols, a.score ? a.chunk * kBlk : 0), st>>>(a);
+    const int tiles = a.score ? (a.max_len + 1 + kScoreKeys - 1) / kScoreKeys : 0;
+    block_finish_kernel<D><<<dim3(a.H + a.Hk * tiles, B), kFinishThreads, 0, st>>>(a);
 }
 
 }  // namespace
@@ -321,7 +525,7 @@ void launch_decode(const BlockDecodeArgs& a, int B, hipStream_t st) {
 
 extern "C" size_t st3_block_workspace_bytes(const st3_gqa_shape* shape, int32_t max_len) {
     if (st3::check_gqa_shape(shape) != ST3_OK || max_len < 0) return 0;
-    return st3::block_ws(shape, max_len).total;
+    return std::max<size_t>(256, std::max(st3::block_ws(shape, max_len, true).total, st3::block_ws(shape, max_len, false).total));
 }
 
 extern "C" st3_status st3_block_decode(const st3_gqa_shape* shape, const st3_rows* q, const st3_rows* k_new, const st3_rows* v_new,
@@ -340,8 +544,9 @@ extern "C" st3_status st3_block_decode(const st3_gqa_shape* shape, const st3_row
     if (cache->table_blocks < (max_len + (k_new ? 1 : 0)) / kBlk) return ST3_ERR_INVALID_ARG;
     if (score && (score_stride_h < (int64_t)max_len + 1 || (B > 1 && score_stride_b < (int64_t)max_len + 1))) return ST3_ERR_INVALID_ARG;
     if (!workspace || !aligned16(workspace)) return ST3_ERR_INVALID_ARG;
-    const BlockWs wl = block_ws(shape, max_len);
-    if (workspace_bytes < wl.total) return ST3_ERR_WORKSPACE_TOO_SMALL;
+    const Cut cut = cut_of(shape, max_len, score != nullptr);
+    const BlockWs wl = block_ws(shape, max_len, score != nullptr);
+    if (workspace_bytes < st3_block_workspace_bytes(shape, max_len)) return ST3_ERR_WORKSPACE_TOO_SMALL;
     char* ws = reinterpret_cast<char*>(workspace);
     auto bits = [](const st3_rows* r) { return r ? reinterpret_cast<uint16_t*>(r->data) : nullptr; };
     BlockDecodeArgs a{};
@@ -350,7 +555,7 @@ extern "C" st3_status st3_block_decode(const st3_gqa_shape* shape, const st3_row
     a.q_st = q->stride_t; a.q_sh = q->stride_h; a.o_st = out->stride_t; a.o_sh = out->stride_h;
     if (k_new) { a.k_st = k_new->stride_t; a.k_sh = k_new->stride_h; a.v_st = v_new->stride_t; a.v_sh = v_new->stride_h; }
     a.max_len = max_len; a.H = H; a.Hk = Hk; a.G = G; a.QG = (G + kCols - 1) / kCols;
-    a.chunk = wl.chunk; a.nsplit = wl.nsplit;
+    a.chunk = cut.chunk; a.nsplit = wl.nsplit;
     a.scale_l2 = gqa_scale_log2(shape);
     a.score = score; a.s_sb = score_stride_b; a.s_sh = score_stride_h;
     a.part_o = reinterpret_cast<float*>(ws + wl.part_o);
@@ -359,11 +564,11 @@ extern "C" st3_status st3_block_decode(const st3_gqa_shape* shape, const st3_row
     a.logit_stride = wl.logit_stride;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     if (cache->code == ST3_BLOCK_INT8) {
-        if (D == 128) launch_decode<128, ST3_BLOCK_INT8>(a, B, st);
-        else launch_decode<64, ST3_BLOCK_INT8>(a, B, st);
+        if (D == 128) launch_decode<128, ST3_BLOCK_INT8>(a, B, cut.waves, st);
+        else launch_decode<64, ST3_BLOCK_INT8>(a, B, cut.waves, st);
     } else {
-        if (D == 128) launch_decode<128, ST3_BLOCK_E4M3>(a, B, st);
-        else launch_decode<64, ST3_BLOCK_E4M3>(a, B, st);
+        if (D == 128) launch_decode<128, ST3_BLOCK_E4M3>(a, B, cut.waves, st);
+        else launch_decode<64, ST3_BLOCK_E4M3>(a, B, cut.waves, st);
     }
     return check_launch();
 }

@@ -54,6 +54,14 @@ __device__ __forceinline__ void direct_load16(const uint16_t* base, uint32_t lan
                  : "memory", "m0");
 }
 
+// The same for data that is read once and should not displace what the caches hold.
+__device__ __forceinline__ void direct_load16_stream(const uint8_t* base, uint32_t lane_byte_off, uint32_t lds_byte_addr) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
+                 :
+                 : "s"(lds_byte_addr), "v"(lane_byte_off), "s"(base)
+                 : "memory", "m0");
+}
+
 // A value that is the same in every lane, moved to scalar registers.
 __device__ __forceinline__ const uint16_t* uniform_ptr(const uint16_t* p) {
     const uint64_t v = reinterpret_cast<uint64_t>(p);
