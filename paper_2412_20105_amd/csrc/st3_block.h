@@ -85,14 +85,35 @@ __device__ __forceinline__ int page_of(const BlockPages& c, int b, int j) {
     return p >= 0 && p < c.n_pages ? p : -1;
 }
 
+// x / scale, correctly rounded, for many x and one scale: two corrections of x * (1 / scale) by the remainder, which a fused multiply-add gives exactly (Markstein).
+// That holds while nothing on the way leaves the normal range; a scale near its ends is divided by.
+struct Divider {
+    float scale, inv, top;          // top: the largest magnitude; an infinity counts as that
+    bool plain;
+    __device__ __forceinline__ Divider(float s, float largest) : scale(s), top(largest) {
+        plain = !(s > 0x1p-60f && s < 0x1p60f);
+        inv = plain ? 0.f : __fdiv_rn(1.0f, s);
+    }
+    __device__ __forceinline__ float operator()(float x) const {
+        x = __builtin_amdgcn_fmed3f(x, -top, top);
+        if (plain) return scale > 0.f ? __fdiv_rn(x, scale) : 0.f;
+        float q = x * inv;
+        q = fmaf(fmaf(-q, scale, x), inv, q);
+        return fmaf(fmaf(-q, scale, x), inv, q);
+    }
+};
+
+// The two formats.  code4: four quotients (of x[0..3], no larger than the top by more than a rounding) as four bytes.
 template <int CODE> struct BlockCode;
 template <> struct BlockCode<ST3_BLOCK_INT8> {
     static constexpr float kTop = 127.0f, kUnit = 1.0f / 127.0f;
-    // x / scale as the format defines it
-    __device__ static __forceinline__ uint32_t code(float x, float scale) {
-        const float y = scale > 0.f ? __fdiv_rn(x, scale) : 0.f;
-        if (!(y == y)) return 0;
-        return (uint32_t)(int)rintf(fminf(fmaxf(y, -kTop), kTop)) & 0xffu;
+    __device__ static __forceinline__ uint32_t code4(const float* x, const Divider& d) {
+        uint32_t u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)                     // the sum's last bits are the integer nearest, ties to even
+            u[i] = __float_as_uint(x[i] == x[i] ? d(x[i]) + 12582912.0f : 12582912.0f);
+        const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(u[3], u[2], 0x04000c0cu);
+        return lo | hi;
     }
     __device__ static __forceinline__ float value(uint32_t byte) { return (float)(int8_t)byte; }
     // four codes as four bf16 (exact: at most seven bits)
@@ -105,8 +126,13 @@ template <> struct BlockCode<ST3_BLOCK_INT8> {
 };
 template <> struct BlockCode<ST3_BLOCK_E4M3> {
     static constexpr float kTop = 448.0f, kUnit = 1.0f / 448.0f;
-    __device__ static __forceinline__ uint32_t code(float x, float scale) {
-        return f32_to_e4m3(scale > 0.f ? __fdiv_rn(x, scale) : x == x ? 0.f : x);
+    __device__ static __forceinline__ uint32_t code4(const float* x, const Divider& d) {
+        float q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = x[i] == x[i] ? copysignf(d(x[i]), x[i]) : x[i];       // (zeros keep their sign)
+        uint32_t w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
+        return w;
     }
     __device__ static __forceinline__ float value(uint32_t byte) { return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0); }
     __device__ static __forceinline__ uint2 to_bf16(uint32_t w) {

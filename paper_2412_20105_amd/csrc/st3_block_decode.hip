@@ -385,7 +385,12 @@ __global__ __launch_bounds__(WAVES * 64, 3) void block_attend_kernel(BlockDecode
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, sm_m[which * WAVES + w]);
             const float scale = mx * F::kUnit;
-            for (int e = tid; e < kBlk * D; e += kThr) dst[e] = (uint8_t)F::code(__uint_as_float((uint32_t)src[e] << 16), scale);
+            const Divider divide(scale, mx);
+            for (int e = 4 * tid; e < kBlk * D; e += 4 * kThr) {
+                const uint2 raw = *reinterpret_cast<const uint2*>(src + e);
+                const float x[4] = {bf16_lo(raw.x), bf16_hi(raw.x), bf16_lo(raw.y), bf16_hi(raw.y)};
+                *reinterpret_cast<uint32_t*>(dst + e) = F::code4(x, divide);
+            }
             if (tid == 0) (which ? a.c.v_scale : a.c.k_scale)[at] = scale;
         }
     }
