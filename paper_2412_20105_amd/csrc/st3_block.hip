@@ -1,9 +1,10 @@
 // The cache of 8-bit blocks: packed prompts into pages, and eviction by accumulated weight into other pages.
 //
-// A workgroup of 256 threads makes one block of one key head, K and V.  Thread (group y = tid / 16, x = tid % 16) holds rows 4 y .. + 3 of it and columns
-// w x .. + w - 1, w = d / 16: 16 threads read and write whole rows of K; V's codes, whose rows lie in memory as columns, are packed four rows to a word and
-// change places through LDS, so that they too leave as 16 bytes a thread.  Bound by memory: both read and write what they must once, but for the lines
-// of a page's V of which an eviction keeps a part.
+// A workgroup of 256 threads makes K or V of one block of one key head.  A thread holds four rows that follow each other and d / 16 columns that do
+// (Place): for K 16 threads in a row have a row group's columns, so that they read and write whole rows; for V they have a column's rows, so that four codes make a word
+// and 16 words a column of the page, without a trip through LDS.  Bound by memory: both read and write what they must once, but for the lines of a page's V of which
+// an eviction keeps a part.  A workgroup is a chain of a few trips to memory; with K and V in workgroups of their own there are twice as many, of half the
+// registers, beside each other.
 #include <algorithm>
 #include <utility>
 
@@ -15,69 +16,66 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kRankThreads = 1024;
 
-// Largest magnitudes of K's and V's values over the workgroup; every thread gets both.
-__device__ __forceinline__ float2 block_max(float k, float v, float2* sm, int tid) {
-    k = wave_max_from<1>(k);
-    v = wave_max_from<1>(v);
-    if ((tid & 63) == 0) sm[tid >> 6] = make_float2(k, v);
+// Largest magnitude over the workgroup; every thread gets it.
+__device__ __forceinline__ float block_max(float x, float* sm, int tid) {
+    x = wave_max_from<1>(x);
+    if ((tid & 63) == 0) sm[tid >> 6] = x;
     __syncthreads();
-    return make_float2(fmaxf(fmaxf(sm[0].x, sm[1].x), fmaxf(sm[2].x, sm[3].x)), fmaxf(fmaxf(sm[0].y, sm[1].y), fmaxf(sm[2].y, sm[3].y)));
+    return fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
 }
 
-// LDS words of V's codes: [d][64 / 4], a row of 16 words followed by 4 of padding.
-constexpr int kWordRow = kBlk / 4 + 4;
+// A thread's part of a block: rows row .. + 3, columns col .. + d / 16 - 1.
+template <int D, bool COLUMNS>
+struct Place {
+    int row, col;
+    __device__ __forceinline__ explicit Place(int tid) {
+        const int fast = tid & 15, slow = tid >> 4;
+        row = 4 * (COLUMNS ? fast : slow);
+        col = D / 16 * (COLUMNS ? slow : fast);
+    }
+};
 
-// Codes a block from the threads' values (k, v [row][column] as above) into a page.
-template <int D, int CODE>
-__device__ __forceinline__ void write_block(const float (&k)[4][D / 16], const float (&v)[4][D / 16], const BlockPages& c, int64_t at, uint32_t* words,
-                                            float2* sm, int tid) {
+// Codes a block of K (COLUMNS: of V) from the threads' values v [row][column] into a page.
+template <int D, int CODE, bool COLUMNS>
+__device__ __forceinline__ void write_block(const float (&v)[4][D / 16], const BlockPages& c, int64_t at, float* sm, int tid) {
     using F = BlockCode<CODE>;
     constexpr int W = D / 16;
-    const int x = tid & 15, y = tid >> 4;
-    float mk = 0.f, mv = 0.f;
+    const Place<D, COLUMNS> my(tid);
+    float mx = 0.f;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int e = 0; e < W; ++e) { mk = fmaxf(mk, finite_abs(k[r][e])); mv = fmaxf(mv, finite_abs(v[r][e])); }
-    const float2 top = block_max(mk, mv, sm, tid);
-    const Divider dk(top.x * F::kUnit, top.x), dv(top.y * F::kUnit, top.y);
-    if (tid == 0) { c.k_scale[at] = dk.scale; c.v_scale[at] = dv.scale; }
-    uint8_t* kc = c.k_codes + at * (kBlk * D);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        uint32_t w[W / 4];
-#pragma unroll
-        for (int j = 0; j < W / 4; ++j) w[j] = F::code4(k[r] + 4 * j, dk);
-        uint32_t* to = reinterpret_cast<uint32_t*>(kc + (4 * y + r) * D + W * x);
-        if constexpr (W == 8) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
-        else *to = w[0];
-    }
-#pragma unroll
-    for (int e = 0; e < W; ++e) {
-        const float col[4] = {v[0][e], v[1][e], v[2][e], v[3][e]};
-        words[(W * x + e) * kWordRow + y] = F::code4(col, dv);
-    }
-    __syncthreads();
-    uint4* vc = reinterpret_cast<uint4*>(c.v_codes + at * (kBlk * D));
-#pragma unroll
-    for (int i = tid; i < D * 4; i += kThreads) vc[i] = *reinterpret_cast<const uint4*>(words + (i >> 2) * kWordRow + 4 * (i & 3));
-}
-
-// The rows [0, rows) of a partial block into the tails, `put(r, e, k, v)` being the bits of row r's column e.
-template <int D, typename Bits>
-__device__ __forceinline__ void write_tail(const Bits& bits, const BlockPages& c, int64_t strip, int rows, int tid) {
-    constexpr int W = D / 16;
-    const int x = tid & 15, y = tid >> 4;
-    uint16_t* kt = c.k_tail + strip * (kBlk * D);
-    uint16_t* vt = c.v_tail + strip * (kBlk * D);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        if (4 * y + r >= rows) continue;
+        for (int e = 0; e < W; ++e) mx = fmaxf(mx, finite_abs(v[r][e]));
+    const float top = block_max(mx, sm, tid);
+    const Divider divide(top * F::kUnit, top);
+    if (tid == 0) (COLUMNS ? c.v_scale : c.k_scale)[at] = divide.scale;
+    uint8_t* codes = (COLUMNS ? c.v_codes : c.k_codes) + at * (kBlk * D);
+    if constexpr (COLUMNS) {
 #pragma unroll
         for (int e = 0; e < W; ++e) {
-            kt[(4 * y + r) * D + W * x + e] = bits(0, r, e);
-            vt[(W * x + e) * kBlk + 4 * y + r] = bits(1, r, e);
+            const float x[4] = {v[0][e], v[1][e], v[2][e], v[3][e]};
+            *reinterpret_cast<uint32_t*>(codes + (my.col + e) * kBlk + my.row) = F::code4(x, divide);
         }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            uint32_t* to = reinterpret_cast<uint32_t*>(codes + (my.row + r) * D + my.col);
+            if constexpr (W == 8) *reinterpret_cast<uint2*>(to) = make_uint2(F::code4(v[r], divide), F::code4(v[r] + 4, divide));
+            else *to = F::code4(v[r], divide);
+        }
+    }
+}
+
+// The rows [0, rows) of a partial block into a tail; bits(r, e): the thread's row r, column e.
+template <int D, bool COLUMNS, typename Bits>
+__device__ __forceinline__ void write_tail(const Bits& bits, const BlockPages& c, int64_t strip, int rows, int tid) {
+    const Place<D, COLUMNS> my(tid);
+    uint16_t* tail = (COLUMNS ? c.v_tail : c.k_tail) + strip * (kBlk * D);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        if (my.row + r >= rows) continue;
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) tail[COLUMNS ? (my.col + e) * kBlk + my.row + r : (my.row + r) * D + my.col + e] = bits(r, e);
     }
 }
 
@@ -104,39 +102,38 @@ struct StoreArgs {
     int32_t total, max_len, Hk;
 };
 
-template <int D, int CODE>
-__global__ __launch_bounds__(kThreads) void block_store_kernel(StoreArgs a) {
+template <int D, int CODE, bool COLUMNS>
+__device__ __forceinline__ void store_block(const StoreArgs& a, int kh, int j, int b, float* sm) {
     constexpr int W = D / 16;
-    __shared__ __attribute__((aligned(16))) uint32_t words[D * kWordRow];
-    __shared__ float2 sm[4];
-    const int tid = threadIdx.x, x = tid & 15, y = tid >> 4;
-    const int kh = blockIdx.x, j = blockIdx.y, b = blockIdx.z;
+    const int tid = threadIdx.x;
+    const Place<D, COLUMNS> my(tid);
+    const int page = page_of(a.c, b, j);                    // (on its way beside the lengths)
     const int start = max(0, min(a.cu[b], a.total)), n = min(max(start, min(a.cu[b + 1], a.total)) - start, a.max_len);
     if (j * kBlk >= n) return;
-    const bool whole = (j + 1) * kBlk <= n;
-    uint32_t kr[4][W / 2], vr[4][W / 2];
+    const uint16_t* src = (COLUMNS ? a.v + kh * a.v_sh : a.k + kh * a.k_sh) + my.col;
+    const int64_t stride = COLUMNS ? a.v_st : a.k_st;
+    uint32_t raw[4][W / 2];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int64_t row = start + min(j * kBlk + 4 * y + r, n - 1);
-        load_bf16<W>(a.k + kh * a.k_sh + row * a.k_st + W * x, kr[r]);
-        load_bf16<W>(a.v + kh * a.v_sh + row * a.v_st + W * x, vr[r]);
-    }
-    if (!whole) {
-        write_tail<D>([&](int which, int r, int e) { return (uint16_t)((which ? vr[r][e / 2] : kr[r][e / 2]) >> (16 * (e & 1))); }, a.c,
-                      (int64_t)b * a.Hk + kh, n - j * kBlk, tid);
+    for (int r = 0; r < 4; ++r) load_bf16<W>(src + (start + min(j * kBlk + my.row + r, n - 1)) * stride, raw[r]);
+    if ((j + 1) * kBlk > n) {
+        write_tail<D, COLUMNS>([&](int r, int e) { return (uint16_t)(raw[r][e / 2] >> (16 * (e & 1))); }, a.c, (int64_t)b * a.Hk + kh, n - j * kBlk, tid);
         return;
     }
-    const int page = page_of(a.c, b, j);
     if (page < 0) return;
-    float k[4][W], v[4][W];
+    float v[4][W];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int e = 0; e < W; e += 2) {
-            k[r][e] = bf16_lo(kr[r][e / 2]); k[r][e + 1] = bf16_hi(kr[r][e / 2]);
-            v[r][e] = bf16_lo(vr[r][e / 2]); v[r][e + 1] = bf16_hi(vr[r][e / 2]);
-        }
-    write_block<D, CODE>(k, v, a.c, (int64_t)page * a.Hk + kh, words, sm, tid);
+        for (int e = 0; e < W; e += 2) { v[r][e] = bf16_lo(raw[r][e / 2]); v[r][e + 1] = bf16_hi(raw[r][e / 2]); }
+    write_block<D, CODE, COLUMNS>(v, a.c, (int64_t)page * a.Hk + kh, sm, tid);
+}
+
+template <int D, int CODE>
+__global__ __launch_bounds__(kThreads) void block_store_kernel(StoreArgs a) {
+    __shared__ float sm[4];
+    const int kh = blockIdx.x % a.Hk;
+    if ((int)blockIdx.x < a.Hk) store_block<D, CODE, false>(a, kh, blockIdx.y, blockIdx.z, sm);
+    else store_block<D, CODE, true>(a, kh, blockIdx.y, blockIdx.z, sm);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
@@ -266,94 +263,91 @@ __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs
     for (int i = min(n, a.keep) + tid; i < a.keep; i += kRankThreads) kept[i] = -1;
 }
 
-// Workgroup (key head, new block, sequence).  K's rows are fetched one by one; any row of a page's V lies in all of its lines, so V comes as whole pages, one
-// after the other (a block's rows ascend: a few pages that follow each other), and is picked from LDS.
-template <int D, int CODE>
-__global__ __launch_bounds__(kThreads) void block_move_kernel(EvictBlockArgs a) {
+// Workgroup (K or V of a key head, new block, sequence).  V is picked byte by byte: a block's rows ascend, so that a wave's picks of a column lie in a few
+// lines, and any kept row of a page lies in all lines of its V.
+template <int D, int CODE, bool COLUMNS>
+__device__ __forceinline__ void move_block(const EvictBlockArgs& a, int kh, int j, int b, float* sm) {
     using F = BlockCode<CODE>;
-    constexpr int W = D / 16, kPiece = D * kBlk / 16 / kThreads;       // 16-byte pieces of a page a thread fetches
-    __shared__ __attribute__((aligned(16))) uint32_t words[D * kWordRow];
-    __shared__ __attribute__((aligned(16))) uint8_t page_v[D * kBlk];
-    __shared__ float2 sm[4];
-    const int tid = threadIdx.x, lane = tid & 63, x = tid & 15, y = tid >> 4;
-    const int kh = blockIdx.x, j = blockIdx.y, b = blockIdx.z;
+    constexpr int W = D / 16, kPage = D * kBlk;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const Place<D, COLUMNS> my(tid);
+    // lane i looks up row i (every wave all of them): its old block, and that block's page (what stands there for rows that are not kept is not used)
+    const int32_t* kept = a.kept + b * a.i_sb + kh * a.i_sh;
+    const int first = j * kBlk, raw_l = kept[min(first + lane, a.keep - 1)];
+    const int to_page_any = page_of(a.to, b, j);
+    int row_l = max(0, min(raw_l, a.max_len - 1));
+    int page_l = page_of(a.from, b, row_l / kBlk);
     const int n = min(a.from.len[b], a.max_len), count = min(n, a.keep);
-    if (j * kBlk >= count) return;
-    const int32_t* kept = a.kept + b * a.i_sb + kh * a.i_sh + j * kBlk;
-    const bool whole = (j + 1) * kBlk <= count;
-    const int to_page = whole ? page_of(a.to, b, j) : 0;
+    if (first >= count) return;
+    const bool whole = first + kBlk <= count;
+    const int to_page = whole ? to_page_any : 0;
     if (to_page < 0) return;
-    const int64_t strip = (int64_t)b * a.Hk + kh, to_at = (int64_t)to_page * a.Hk + kh;
-    // lane i looks up row i (every wave all of them): its old block, -1 where it is in the tail, and that block's page
-    const int row_l = kept[min(lane, count - 1 - j * kBlk)], blk_l = row_l < n / kBlk * kBlk ? row_l / kBlk : -1;
-    const int page_l = blk_l >= 0 ? page_of(a.from, b, blk_l) : -1;
-    const int64_t at_l = (int64_t)max(page_l, 0) * a.Hk + kh;
-    const float ks_l = page_l >= 0 ? a.from.k_scale[at_l] : 0.f, vs_l = page_l >= 0 ? a.from.v_scale[at_l] : 0.f;
-    const uint64_t in_place = __ballot(page_l >= 0 && row_l % kBlk == lane);
-    if (whole && in_place == ~0ull && __ballot(blk_l == __builtin_amdgcn_readfirstlane(blk_l)) == ~0ull) {     // one whole old block
-        for (int i = tid; i < D * kBlk / 16; i += kThreads) {
-            reinterpret_cast<uint4*>(a.to.k_codes + to_at * (kBlk * D))[i] = reinterpret_cast<const uint4*>(a.from.k_codes + at_l * (kBlk * D))[i];
-            reinterpret_cast<uint4*>(a.to.v_codes + to_at * (kBlk * D))[i] = reinterpret_cast<const uint4*>(a.from.v_codes + at_l * (kBlk * D))[i];
-        }
-        if (tid == 0) { a.to.k_scale[to_at] = ks_l; a.to.v_scale[to_at] = vs_l; }
+    const int last = count - 1 - first;                     // (lanes past the last row repeat it)
+    const int row_last = __shfl(row_l, min(last, 63)), page_last = __shfl(page_l, min(last, 63));
+    if (lane > last) { row_l = row_last; page_l = page_last; }
+    const int blk_l = row_l < n / kBlk * kBlk ? row_l / kBlk : -1;      // -1: in the tail
+    if (blk_l < 0) page_l = -1;
+    const float* scales = COLUMNS ? a.from.v_scale : a.from.k_scale;
+    const uint8_t* codes = COLUMNS ? a.from.v_codes : a.from.k_codes;
+    const int64_t strip = (int64_t)b * a.Hk + kh, to_at = (int64_t)to_page * a.Hk + kh, at_l = (int64_t)max(page_l, 0) * a.Hk + kh;
+    const float scale_l = page_l >= 0 ? scales[at_l] : 0.f;
+    if (whole && __ballot(page_l >= 0 && row_l % kBlk == lane && blk_l == __builtin_amdgcn_readfirstlane(blk_l)) == ~0ull) {     // one whole old block
+        uint8_t* to = (COLUMNS ? a.to.v_codes : a.to.k_codes) + to_at * kPage;
+        for (int i = tid; i < kPage / 16; i += kThreads) reinterpret_cast<uint4*>(to)[i] = reinterpret_cast<const uint4*>(codes + at_l * kPage)[i];
+        if (tid == 0) (COLUMNS ? a.to.v_scale : a.to.k_scale)[to_at] = scale_l;
         return;
     }
-    // the pages that the rows lie in, from the first to the last (in every wave alike)
-    uint64_t left = __ballot(page_l >= 0);
-    uint4 piece[kPiece];
-    auto fetch = [&](int first) {
-        const int64_t at = (int64_t)__builtin_amdgcn_readlane(page_l, first) * a.Hk + kh;
-        const uint4* src = reinterpret_cast<const uint4*>(a.from.v_codes + at * (kBlk * D));
-#pragma unroll
-        for (int i = 0; i < kPiece; ++i) piece[i] = src[tid + i * kThreads];
-    };
-    if (left != 0) fetch(__ffsll((unsigned long long)left) - 1);
-    // this thread's rows: K as it is, V's rows of the tail
-    float k[4][W], v[4][W];
-    int row[4], blk[4];
+    // this thread's rows: their codes, or the tail's 16 bits
+    constexpr int kWords = COLUMNS ? W : W / 2;             // V: a word for each column
+    uint32_t raw[4][kWords];
+    float scale[4];
+    bool coded[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        row[r] = __shfl(row_l, 4 * y + r) % kBlk;
-        blk[r] = __shfl(blk_l, 4 * y + r);
-        const int page = __shfl(page_l, 4 * y + r);
-        const float ks = __shfl(ks_l, 4 * y + r);
-        const int64_t at = (int64_t)max(page, 0) * a.Hk + kh;
-        if (blk[r] >= 0) {
-            uint32_t w[W / 4];
-            const uint8_t* p = a.from.k_codes + at * (kBlk * D) + row[r] * D + W * x;
+        const int row = __shfl(row_l, my.row + r) % kBlk, page = __shfl(page_l, my.row + r);
+        coded[r] = __shfl(blk_l, my.row + r) >= 0;
+        scale[r] = __shfl(scale_l, my.row + r);
+        const uint8_t* block = codes + ((int64_t)max(page, 0) * a.Hk + kh) * kPage;
 #pragma unroll
-            for (int i = 0; i < W / 4; ++i) w[i] = page >= 0 ? reinterpret_cast<const uint32_t*>(p)[i] : 0u;
+        for (int i = 0; i < kWords; ++i) raw[r][i] = 0;     // (a row whose page does not exist)
+        if constexpr (COLUMNS) {
+            const uint16_t* tail = a.from.v_tail + strip * kPage + my.col * kBlk + row;
+            if (page >= 0) {
 #pragma unroll
-            for (int e = 0; e < W; ++e) { k[r][e] = F::value(w[e / 4] >> (8 * (e & 3)) & 0xffu) * ks; v[r][e] = 0.f; }
+                for (int e = 0; e < W; ++e) raw[r][e] = block[(my.col + e) * kBlk + row];
+            } else if (!coded[r]) {
+#pragma unroll
+                for (int e = 0; e < W; ++e) raw[r][e] = tail[e * kBlk];
+            }
         } else {
-            const uint16_t* kt = a.from.k_tail + strip * (kBlk * D) + row[r] * D + W * x;
-            const uint16_t* vt = a.from.v_tail + strip * (kBlk * D) + row[r];
+            if (page >= 0) {
+                const uint32_t* p = reinterpret_cast<const uint32_t*>(block + row * D + my.col);
 #pragma unroll
-            for (int e = 0; e < W; ++e) {
-                k[r][e] = __uint_as_float((uint32_t)kt[e] << 16);
-                v[r][e] = __uint_as_float((uint32_t)vt[(W * x + e) * kBlk] << 16);
+                for (int i = 0; i < W / 4; ++i) raw[r][i] = p[i];
+            } else if (!coded[r]) {
+                load_bf16<W>(a.from.k_tail + strip * kPage + row * D + my.col, raw[r]);
             }
         }
     }
-    while (left != 0) {
-        const int now = __builtin_amdgcn_readlane(blk_l, __ffsll((unsigned long long)left) - 1);
-        __syncthreads();                                    // (the page before is not read any more)
+    float v[4][W];
 #pragma unroll
-        for (int i = 0; i < kPiece; ++i) reinterpret_cast<uint4*>(page_v)[tid + i * kThreads] = piece[i];
-        left &= ~__ballot(blk_l == now);
-        if (left != 0) fetch(__ffsll((unsigned long long)left) - 1);
-        __syncthreads();
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float vs = __shfl(vs_l, 4 * y + r);
-            if (blk[r] == now) {
-#pragma unroll
-                for (int e = 0; e < W; ++e) v[r][e] = F::value(page_v[(W * x + e) * kBlk + row[r]]) * vs;
-            }
+        for (int e = 0; e < W; ++e) {
+            const uint32_t byte = COLUMNS ? raw[r][e] : raw[r][e / 4] >> (8 * (e & 3));
+            const uint32_t half = COLUMNS ? raw[r][e] : raw[r][e / 2] >> (16 * (e & 1));
+            v[r][e] = coded[r] ? F::value(byte & 0xffu) * scale[r] : __uint_as_float(half << 16);
         }
-    }
-    if (whole) write_block<D, CODE>(k, v, a.to, to_at, words, sm, tid);
-    else write_tail<D>([&](int which, int r, int e) { return (uint16_t)f32_to_bf16_bits(which ? v[r][e] : k[r][e]); }, a.to, strip, count - j * kBlk, tid);
+    if (whole) write_block<D, CODE, COLUMNS>(v, a.to, to_at, sm, tid);
+    else write_tail<D, COLUMNS>([&](int r, int e) { return (uint16_t)f32_to_bf16_bits(v[r][e]); }, a.to, strip, count - first, tid);
+}
+
+template <int D, int CODE>
+__global__ __launch_bounds__(kThreads) void block_move_kernel(EvictBlockArgs a) {
+    __shared__ float sm[4];
+    const int kh = blockIdx.x % a.Hk;
+    if ((int)blockIdx.x < a.Hk) move_block<D, CODE, false>(a, kh, blockIdx.y, blockIdx.z, sm);
+    else move_block<D, CODE, true>(a, kh, blockIdx.y, blockIdx.z, sm);
 }
 
 }  // namespace
@@ -374,7 +368,7 @@ extern "C" st3_status st3_block_store(const st3_gqa_shape* shape, const st3_rows
     if (cache->table_blocks < max_len / kBlk) return ST3_ERR_INVALID_ARG;
     const StoreArgs a{block_pages(cache), reinterpret_cast<const uint16_t*>(k->data), reinterpret_cast<const uint16_t*>(v->data), k->stride_t, k->stride_h,
                       v->stride_t, v->stride_h, cu_len, total, max_len, Hk};
-    const dim3 grid(Hk, blocks, shape->batch);
+    const dim3 grid(2 * Hk, blocks, shape->batch);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     if (cache->code == ST3_BLOCK_INT8) {
         if (D == 128) block_store_kernel<128, ST3_BLOCK_INT8><<<grid, kThreads, 0, st>>>(a);
@@ -415,7 +409,7 @@ extern "C" st3_status st3_block_evict(const st3_gqa_shape* shape, const st3_bloc
     else if (max_len <= 16 * kRankThreads) block_rank_kernel<16><<<dim3(Hk, B), kRankThreads, 0, st>>>(a);
     else block_rank_kernel<0><<<dim3(Hk, B), kRankThreads, 0, st>>>(a);
     if (blocks == 0) return check_launch();
-    const dim3 grid(Hk, blocks, B);
+    const dim3 grid(2 * Hk, blocks, B);
     if (from->code == ST3_BLOCK_INT8) {
         if (D == 128) block_move_kernel<128, ST3_BLOCK_INT8><<<grid, kThreads, 0, st>>>(a);
         else block_move_kernel<64, ST3_BLOCK_INT8><<<grid, kThreads, 0, st>>>(a);
