@@ -86,32 +86,52 @@ __device__ __forceinline__ int page_of(const BlockPages& c, int b, int j) {
 }
 
 // x / scale, correctly rounded, for many x and one scale: two corrections of x * (1 / scale) by the remainder, which a fused multiply-add gives exactly (Markstein).
-// That holds while nothing on the way leaves the normal range; a scale near its ends is divided by.
+// That holds while nothing on the way leaves the normal range.  Else, and where a block holds what is not finite, x is divided with care first (`care`: the caller puts
+// careful(x) in x's place): an infinity counts as the largest finite magnitude, and the quotients are then "divided" by one.
 struct Divider {
-    float scale, inv, top;          // top: the largest magnitude; an infinity counts as that
-    bool plain;
-    __device__ __forceinline__ Divider(float s, float largest) : scale(s), top(largest) {
-        plain = !(s > 0x1p-60f && s < 0x1p60f);
-        inv = plain ? 0.f : __fdiv_rn(1.0f, s);
+    float by, inv, scale, top;
+    bool care;
+    __device__ __forceinline__ Divider(float s, float largest, bool all_finite) : scale(s), top(largest) {
+        care = !(all_finite && s > 0x1p-60f && s < 0x1p60f);
+        by = care ? 1.0f : s;
+        inv = __fdiv_rn(1.0f, by);
+    }
+    __device__ __forceinline__ float careful(float x, float if_nan) const {
+        return !(x == x) ? if_nan : scale > 0.f ? __fdiv_rn(fminf(fmaxf(x, -top), top), scale) : copysignf(0.f, x);
     }
     __device__ __forceinline__ float operator()(float x) const {
-        x = __builtin_amdgcn_fmed3f(x, -top, top);
-        if (plain) return scale > 0.f ? __fdiv_rn(x, scale) : 0.f;
         float q = x * inv;
-        q = fmaf(fmaf(-q, scale, x), inv, q);
-        return fmaf(fmaf(-q, scale, x), inv, q);
+        q = fmaf(fmaf(-q, by, x), inv, q);
+        return fmaf(fmaf(-q, by, x), inv, q);
     }
 };
+
+// Magnitudes compare as integers: what is not finite is above all that is.
+constexpr uint32_t kInfinity = 0x7f800000u;
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// The largest magnitude of a workgroup's values (`mine` of a thread's), as its bits; all threads call it and get it.  sm: a word for each wave.
+template <int WAVES>
+__device__ __forceinline__ uint32_t largest_of(uint32_t mine, uint32_t* sm, int tid) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) mine = max(mine, (uint32_t)__shfl_xor((int)mine, off));
+    if ((tid & 63) == 0) sm[tid >> 6] = mine;
+    __syncthreads();
+    uint32_t all = sm[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) all = max(all, sm[w]);
+    return all;
+}
 
 // The two formats.  code4: four quotients (of x[0..3], no larger than the top by more than a rounding) as four bytes.
 template <int CODE> struct BlockCode;
 template <> struct BlockCode<ST3_BLOCK_INT8> {
-    static constexpr float kTop = 127.0f, kUnit = 1.0f / 127.0f;
+    static constexpr float kUnit = 1.0f / 127.0f;
+    __device__ static __forceinline__ float nan_code() { return 0.f; }
     __device__ static __forceinline__ uint32_t code4(const float* x, const Divider& d) {
         uint32_t u[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)                     // the sum's last bits are the integer nearest, ties to even
-            u[i] = __float_as_uint(x[i] == x[i] ? d(x[i]) + 12582912.0f : 12582912.0f);
+        for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(d(x[i]) + 12582912.0f);      // the sum's last bits are the integer nearest, ties to even
         const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(u[3], u[2], 0x04000c0cu);
         return lo | hi;
     }
@@ -125,11 +145,12 @@ template <> struct BlockCode<ST3_BLOCK_INT8> {
     }
 };
 template <> struct BlockCode<ST3_BLOCK_E4M3> {
-    static constexpr float kTop = 448.0f, kUnit = 1.0f / 448.0f;
+    static constexpr float kUnit = 1.0f / 448.0f;
+    __device__ static __forceinline__ float nan_code() { return __uint_as_float(0x7fc00000u); }
     __device__ static __forceinline__ uint32_t code4(const float* x, const Divider& d) {
         float q[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = x[i] == x[i] ? copysignf(d(x[i]), x[i]) : x[i];       // (zeros keep their sign)
+        for (int i = 0; i < 4; ++i) q[i] = copysignf(d(x[i]), x[i]);        // (zeros keep their sign)
         uint32_t w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
         w = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
         return w;
@@ -140,11 +161,6 @@ template <> struct BlockCode<ST3_BLOCK_E4M3> {
         return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
     }
 };
-
-__device__ __forceinline__ float finite_abs(float x) {
-    const float a = fabsf(x);
-    return a <= 3.402823466e38f ? a : 0.f;
-}
 
 #endif  // __HIPCC__
 

@@ -14,15 +14,7 @@ namespace st3 {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRankThreads = 1024;
-
-// Largest magnitude over the workgroup; every thread gets it.
-__device__ __forceinline__ float block_max(float x, float* sm, int tid) {
-    x = wave_max_from<1>(x);
-    if ((tid & 63) == 0) sm[tid >> 6] = x;
-    __syncthreads();
-    return fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-}
+constexpr int kRankThreads = 1024;         // (512 take as long, 256 take 12.9 us where 1024 take 9.7: 8 strips of 1200 rows)
 
 // A thread's part of a block: rows row .. + 3, columns col .. + d / 16 - 1.
 template <int D, bool COLUMNS>
@@ -35,33 +27,52 @@ struct Place {
     }
 };
 
-// Codes a block of K (COLUMNS: of V) from the threads' values v [row][column] into a page.
+// Codes a block of K (COLUMNS: of V) from the threads' values v [row][column] into a page (past the caches: 16 prompts into pages 20.3 -> 18.7 us).
 template <int D, int CODE, bool COLUMNS>
-__device__ __forceinline__ void write_block(const float (&v)[4][D / 16], const BlockPages& c, int64_t at, float* sm, int tid) {
+__device__ __forceinline__ void write_block(float (&v)[4][D / 16], const BlockPages& c, int64_t at, uint32_t* sm, int tid) {
     using F = BlockCode<CODE>;
     constexpr int W = D / 16;
     const Place<D, COLUMNS> my(tid);
-    float mx = 0.f;
+    uint32_t mx = 0;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int e = 0; e < W; ++e) mx = fmaxf(mx, finite_abs(v[r][e]));
-    const float top = block_max(mx, sm, tid);
-    const Divider divide(top * F::kUnit, top);
+        for (int e = 0; e < W; ++e) mx = max(mx, magnitude(v[r][e]));
+    uint32_t top = largest_of<kThreads / 64>(mx, sm, tid);
+    const bool all_finite = top < kInfinity;
+    if (!all_finite) {                                      // (rare: without the magnitudes from above, which would wait in registers)
+        float f = 0.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < W; ++e) f = fmaxf(f, fabsf(v[r][e]) <= 3.402823466e38f ? fabsf(v[r][e]) : 0.f);
+        top = largest_of<kThreads / 64>(__float_as_uint(f), sm + kThreads / 64, tid);
+    }
+    const Divider divide(__uint_as_float(top) * F::kUnit, __uint_as_float(top), all_finite);
     if (tid == 0) (COLUMNS ? c.v_scale : c.k_scale)[at] = divide.scale;
+    if (divide.care) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < W; ++e) v[r][e] = divide.careful(v[r][e], F::nan_code());
+    }
     uint8_t* codes = (COLUMNS ? c.v_codes : c.k_codes) + at * (kBlk * D);
     if constexpr (COLUMNS) {
 #pragma unroll
         for (int e = 0; e < W; ++e) {
             const float x[4] = {v[0][e], v[1][e], v[2][e], v[3][e]};
-            *reinterpret_cast<uint32_t*>(codes + (my.col + e) * kBlk + my.row) = F::code4(x, divide);
+            __builtin_nontemporal_store(F::code4(x, divide), reinterpret_cast<uint32_t*>(codes + (my.col + e) * kBlk + my.row));
         }
     } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            uint32_t* to = reinterpret_cast<uint32_t*>(codes + (my.row + r) * D + my.col);
-            if constexpr (W == 8) *reinterpret_cast<uint2*>(to) = make_uint2(F::code4(v[r], divide), F::code4(v[r] + 4, divide));
-            else *to = F::code4(v[r], divide);
+            uint8_t* to = codes + (my.row + r) * D + my.col;
+            if constexpr (W == 8) {
+                const u32x2 w = {F::code4(v[r], divide), F::code4(v[r] + 4, divide)};
+                __builtin_nontemporal_store(w, reinterpret_cast<u32x2*>(to));
+            } else {
+                __builtin_nontemporal_store(F::code4(v[r], divide), reinterpret_cast<uint32_t*>(to));
+            }
         }
     }
 }
@@ -103,7 +114,7 @@ struct StoreArgs {
 };
 
 template <int D, int CODE, bool COLUMNS>
-__device__ __forceinline__ void store_block(const StoreArgs& a, int kh, int j, int b, float* sm) {
+__device__ __forceinline__ void store_block(const StoreArgs& a, int kh, int j, int b, uint32_t* sm) {
     constexpr int W = D / 16;
     const int tid = threadIdx.x;
     const Place<D, COLUMNS> my(tid);
@@ -129,8 +140,8 @@ __device__ __forceinline__ void store_block(const StoreArgs& a, int kh, int j, i
 }
 
 template <int D, int CODE>
-__global__ __launch_bounds__(kThreads) void block_store_kernel(StoreArgs a) {
-    __shared__ float sm[4];
+__global__ __launch_bounds__(kThreads, 8) void block_store_kernel(StoreArgs a) {
+    __shared__ uint32_t sm[2 * kThreads / 64];
     const int kh = blockIdx.x % a.Hk;
     if ((int)blockIdx.x < a.Hk) store_block<D, CODE, false>(a, kh, blockIdx.y, blockIdx.z, sm);
     else store_block<D, CODE, true>(a, kh, blockIdx.y, blockIdx.z, sm);
@@ -156,12 +167,14 @@ __device__ __forceinline__ uint32_t rank_key(float x) {
 
 // Sum over the workgroup's threads before this one, and over all; waves: one word for each wave, two of them in turn.
 __device__ __forceinline__ uint2 count_before(uint32_t mine, uint32_t* waves, int lane, int wave) {
-    uint32_t incl = mine;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t up = __shfl_up(incl, off);
-        if (lane >= off) incl += up;
-    }
+    // inclusive sum over the wave: within rows of 16 lanes, then the rows before (DPP: row_shr 1, 2, 4, 8, row_bcast 15, 31)
+    int incl = (int)mine;
+    incl += __builtin_amdgcn_update_dpp(0, incl, 0x111, 0xf, 0xf, true);
+    incl += __builtin_amdgcn_update_dpp(0, incl, 0x112, 0xf, 0xf, true);
+    incl += __builtin_amdgcn_update_dpp(0, incl, 0x114, 0xf, 0xf, true);
+    incl += __builtin_amdgcn_update_dpp(0, incl, 0x118, 0xf, 0xf, true);
+    incl += __builtin_amdgcn_update_dpp(0, incl, 0x142, 0xa, 0xf, true);
+    incl += __builtin_amdgcn_update_dpp(0, incl, 0x143, 0xc, 0xf, true);
     if (lane == 63) waves[wave] = incl;
     __syncthreads();
     const uint32_t other = lane < kRankThreads / 64 ? waves[lane] : 0;
@@ -180,28 +193,29 @@ __device__ __forceinline__ uint2 count_before(uint32_t mine, uint32_t* waves, in
 // 0: rows of any length, read again in every pass.  Bound by its chain of passes: evictions of 8 strips of 1200 rows 8.5 us with PER = 0.
 template <int PER>
 __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs a) {
+    constexpr int kBins = 2048 / kRankThreads;
     __shared__ uint32_t hist[2048];
     __shared__ uint32_t waves[2][kRankThreads / 64];
     __shared__ uint32_t found[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kh = blockIdx.x, b = blockIdx.y;
+    const float* score = a.score + b * a.s_sb + kh * a.s_sh;
+    float x[PER > 0 ? PER : 1];
+    if constexpr (PER > 0) {                                // (on their way beside the length)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) x[i] = tid * PER + i < a.max_len ? score[tid * PER + i] : 0.f;
+    }
     const int n = min(a.from.len[b], a.max_len);
     if (n < 0) return;
-    const float* score = a.score + b * a.s_sb + kh * a.s_sh;
     float* to = a.to_score + b * a.t_sb + kh * a.t_sh;
     int32_t* kept = a.kept + b * a.i_sb + kh * a.i_sh;
     const int lo = a.n_sink, hi = n - a.n_recent;
     const bool all = n <= a.keep;
-    float x[PER > 0 ? PER : 1];
-    if constexpr (PER > 0) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) x[i] = tid * PER + i < n ? score[tid * PER + i] : 0.f;
-    }
     uint32_t want = all ? 0 : a.keep - a.n_sink - a.n_recent;   // candidates wanted, at last of those with the last key
     uint32_t key = want > 0 ? 0 : 0xffffffffu, mask = 0;        // (no row has the key of all ones)
     for (int pass = 0; pass < 3 && want > 0; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        hist[tid] = 0;
-        hist[tid + kRankThreads] = 0;
+#pragma unroll
+        for (int i = 0; i < kBins; ++i) hist[tid + i * kRankThreads] = 0;
         __syncthreads();
         auto note = [&](int i, float s) {
             const uint32_t u = rank_key(s);
@@ -214,11 +228,16 @@ __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs
             for (int i = lo + tid; i < hi; i += kRankThreads) note(i, score[i]);
         }
         __syncthreads();
-        // bins from the top: thread t owns bins 2047 - 2 t and 2046 - 2 t
-        const uint32_t h0 = hist[2047 - 2 * tid], h1 = hist[2046 - 2 * tid];
-        const uint32_t before = count_before(h0 + h1, waves[0], lane, wave).x;
-        if (before < want && before + h0 >= want) { found[0] = 2047 - 2 * tid; found[1] = want - before; }
-        else if (before + h0 < want && before + h0 + h1 >= want) { found[0] = 2046 - 2 * tid; found[1] = want - before - h0; }
+        // bins from the top: thread t owns kBins of them
+        uint32_t h[kBins], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kBins; ++i) { h[i] = hist[2047 - kBins * tid - i]; sum += h[i]; }
+        uint32_t before = count_before(sum, waves[0], lane, wave).x;
+#pragma unroll
+        for (int i = 0; i < kBins; ++i) {
+            if (before < want && before + h[i] >= want) { found[0] = 2047 - kBins * tid - i; found[1] = want - before; }
+            before += h[i];
+        }
         __syncthreads();
         key |= found[0] << shift;
         mask |= ((1u << bits) - 1) << shift;
@@ -263,12 +282,14 @@ __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs
     for (int i = min(n, a.keep) + tid; i < a.keep; i += kRankThreads) kept[i] = -1;
 }
 
-// Workgroup (K or V of a key head, new block, sequence).  V is picked byte by byte: a block's rows ascend, so that a wave's picks of a column lie in a few
-// lines, and any kept row of a page lies in all lines of its V.
+// Workgroup (K or V of a key head, new block, sequence).  K's rows are fetched one by one; any row of a page lies in all lines of its V, so V comes as whole pages,
+// two at a time (a block's rows ascend: a few pages that follow each other), and is picked from LDS.  (Picked byte by byte from memory it kept the address units busy: 32
+// caches 84 us.)
+constexpr int kPageRow = kBlk + 8;          // bytes: the 4 columns that a wave picks at a time, 8 apart, are 16 banks apart
 template <int D, int CODE, bool COLUMNS>
-__device__ __forceinline__ void move_block(const EvictBlockArgs& a, int kh, int j, int b, float* sm) {
+__device__ __forceinline__ void move_block(const EvictBlockArgs& a, int kh, int j, int b, uint8_t* pages, uint32_t* sm) {
     using F = BlockCode<CODE>;
-    constexpr int W = D / 16, kPage = D * kBlk;
+    constexpr int W = D / 16, kPage = D * kBlk, kPiece = kPage / 16 / kThreads;       // 16-byte pieces of a page a thread fetches
     const int tid = threadIdx.x, lane = tid & 63;
     const Place<D, COLUMNS> my(tid);
     // lane i looks up row i (every wave all of them): its old block, and that block's page (what stands there for rows that are not kept is not used)
@@ -297,57 +318,99 @@ __device__ __forceinline__ void move_block(const EvictBlockArgs& a, int kh, int 
         if (tid == 0) (COLUMNS ? a.to.v_scale : a.to.k_scale)[to_at] = scale_l;
         return;
     }
-    // this thread's rows: their codes, or the tail's 16 bits
-    constexpr int kWords = COLUMNS ? W : W / 2;             // V: a word for each column
-    uint32_t raw[4][kWords];
-    float scale[4];
-    bool coded[4];
+    float v[4][W], scale[4];
+    int row[4], blk[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const int row = __shfl(row_l, my.row + r) % kBlk, page = __shfl(page_l, my.row + r);
-        coded[r] = __shfl(blk_l, my.row + r) >= 0;
+        row[r] = __shfl(row_l, my.row + r) % kBlk;
+        blk[r] = __shfl(blk_l, my.row + r);
         scale[r] = __shfl(scale_l, my.row + r);
-        const uint8_t* block = codes + ((int64_t)max(page, 0) * a.Hk + kh) * kPage;
+    }
+    if constexpr (COLUMNS) {
+        uint64_t left = __ballot(page_l >= 0);              // rows whose pages are still to come (in every wave alike)
+        u32x4 piece[2][kPiece];
+        int now[2];
+        auto fetch = [&]() {
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) raw[r][i] = 0;     // (a row whose page does not exist)
-        if constexpr (COLUMNS) {
-            const uint16_t* tail = a.from.v_tail + strip * kPage + my.col * kBlk + row;
-            if (page >= 0) {
+            for (int p = 0; p < 2; ++p) {
+                const int lead = left != 0 ? __ffsll((unsigned long long)left) - 1 : 0;
+                now[p] = left != 0 ? __builtin_amdgcn_readlane(blk_l, lead) : -2;
+                const int64_t at = (int64_t)max(__builtin_amdgcn_readlane(page_l, lead), 0) * a.Hk + kh;
+                const u32x4* src = reinterpret_cast<const u32x4*>(codes + at * kPage);
+                if (now[p] >= 0) {
 #pragma unroll
-                for (int e = 0; e < W; ++e) raw[r][e] = block[(my.col + e) * kBlk + row];
-            } else if (!coded[r]) {
-#pragma unroll
-                for (int e = 0; e < W; ++e) raw[r][e] = tail[e * kBlk];
+                    for (int i = 0; i < kPiece; ++i) piece[p][i] = src[tid + i * kThreads];
+                }
+                left &= ~__ballot(blk_l == now[p]);
             }
-        } else {
+        };
+        fetch();
+        const uint16_t* tail = a.from.v_tail + strip * kPage + my.col * kBlk;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+#pragma unroll
+            for (int e = 0; e < W; ++e) v[r][e] = 0.f;      // (a row whose page does not exist)
+            if (blk[r] < 0) {
+#pragma unroll
+                for (int e = 0; e < W; ++e) v[r][e] = __uint_as_float((uint32_t)tail[e * kBlk + row[r]] << 16);
+            }
+        }
+        while (now[0] >= 0) {
+            __syncthreads();                                // (the pages before are not read any more)
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) {
+                    if (now[p] < 0) continue;
+                    const int unit = tid + i * kThreads;
+                    u32x2* to = reinterpret_cast<u32x2*>(pages + (p * D + (unit >> 2)) * kPageRow + 16 * (unit & 3));
+                    to[0] = u32x2{piece[p][i].x, piece[p][i].y};
+                    to[1] = u32x2{piece[p][i].z, piece[p][i].w};
+                }
+            const int here0 = now[0], here1 = now[1];
+            fetch();
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (blk[r] != here0 && blk[r] != here1) continue;
+                const uint8_t* at = pages + ((blk[r] == here0 ? 0 : D) + my.col) * kPageRow + row[r];
+#pragma unroll
+                for (int e = 0; e < W; ++e) v[r][e] = F::value(at[e * kPageRow]) * scale[r];
+            }
+        }
+    } else {
+        uint32_t raw[4][W / 2];                             // (codes, or the tail's 16 bits)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int page = __shfl(page_l, my.row + r);
+#pragma unroll
+            for (int i = 0; i < W / 2; ++i) raw[r][i] = 0;
             if (page >= 0) {
-                const uint32_t* p = reinterpret_cast<const uint32_t*>(block + row * D + my.col);
+                const uint32_t* p = reinterpret_cast<const uint32_t*>(codes + ((int64_t)page * a.Hk + kh) * kPage + row[r] * D + my.col);
 #pragma unroll
                 for (int i = 0; i < W / 4; ++i) raw[r][i] = p[i];
-            } else if (!coded[r]) {
-                load_bf16<W>(a.from.k_tail + strip * kPage + row * D + my.col, raw[r]);
+            } else if (blk[r] < 0) {
+                load_bf16<W>(a.from.k_tail + strip * kPage + row[r] * D + my.col, raw[r]);
             }
         }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+                v[r][e] = blk[r] >= 0 ? F::value(raw[r][e / 4] >> (8 * (e & 3)) & 0xffu) * scale[r]
+                                      : __uint_as_float((raw[r][e / 2] >> (16 * (e & 1))) << 16);
     }
-    float v[4][W];
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-            const uint32_t byte = COLUMNS ? raw[r][e] : raw[r][e / 4] >> (8 * (e & 3));
-            const uint32_t half = COLUMNS ? raw[r][e] : raw[r][e / 2] >> (16 * (e & 1));
-            v[r][e] = coded[r] ? F::value(byte & 0xffu) * scale[r] : __uint_as_float(half << 16);
-        }
     if (whole) write_block<D, CODE, COLUMNS>(v, a.to, to_at, sm, tid);
     else write_tail<D, COLUMNS>([&](int r, int e) { return (uint16_t)f32_to_bf16_bits(v[r][e]); }, a.to, strip, count - first, tid);
 }
 
 template <int D, int CODE>
-__global__ __launch_bounds__(kThreads) void block_move_kernel(EvictBlockArgs a) {
-    __shared__ float sm[4];
+__global__ __launch_bounds__(kThreads, 6) void block_move_kernel(EvictBlockArgs a) {
+    __shared__ __attribute__((aligned(16))) uint8_t pages[2 * D * kPageRow];
+    __shared__ uint32_t sm[2 * kThreads / 64];
     const int kh = blockIdx.x % a.Hk;
-    if ((int)blockIdx.x < a.Hk) move_block<D, CODE, false>(a, kh, blockIdx.y, blockIdx.z, sm);
-    else move_block<D, CODE, true>(a, kh, blockIdx.y, blockIdx.z, sm);
+    if ((int)blockIdx.x < a.Hk) move_block<D, CODE, false>(a, kh, blockIdx.y, blockIdx.z, pages, sm);
+    else move_block<D, CODE, true>(a, kh, blockIdx.y, blockIdx.z, pages, sm);
 }
 
 }  // namespace
@@ -405,8 +468,8 @@ extern "C" st3_status st3_block_evict(const st3_gqa_shape* shape, const st3_bloc
     const EvictBlockArgs a{block_pages(from), block_pages(to), max_len, keep, n_sink, n_recent, Hk, score, score_stride_b, score_stride_h, to_score,
                            to_score_stride_b, to_score_stride_h, kept, kept_stride_b, kept_stride_h};
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    if (max_len <= 4 * kRankThreads) block_rank_kernel<4><<<dim3(Hk, B), kRankThreads, 0, st>>>(a);
-    else if (max_len <= 16 * kRankThreads) block_rank_kernel<16><<<dim3(Hk, B), kRankThreads, 0, st>>>(a);
+    if (max_len <= 4096) block_rank_kernel<4096 / kRankThreads><<<dim3(Hk, B), kRankThreads, 0, st>>>(a);
+    else if (max_len <= 16384) block_rank_kernel<16384 / kRankThreads><<<dim3(Hk, B), kRankThreads, 0, st>>>(a);
     else block_rank_kernel<0><<<dim3(Hk, B), kRankThreads, 0, st>>>(a);
     if (blocks == 0) return check_launch();
     const dim3 grid(2 * Hk, blocks, B);

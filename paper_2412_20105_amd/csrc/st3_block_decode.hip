@@ -377,18 +377,27 @@ __global__ __launch_bounds__(WAVES * 64, 3) void block_attend_kernel(BlockDecode
         for (int which = 0; which < 2; ++which) {
             const uint16_t* src = (which ? a.c.v_tail : a.c.k_tail) + tail;     // (codes lie in the tails' own order)
             uint8_t* dst = (which ? a.c.v_codes : a.c.k_codes) + at * (kBlk * D);
-            float mx = 0.f;
-            for (int e = tid; e < kBlk * D; e += kThr) mx = fmaxf(mx, finite_abs(__uint_as_float((uint32_t)src[e] << 16)));
-            mx = wave_max_from<1>(mx);
-            if (lane == 0) sm_m[which * WAVES + wave] = mx;
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, sm_m[which * WAVES + w]);
-            const float scale = mx * F::kUnit;
-            const Divider divide(scale, mx);
+            auto largest = [&](uint32_t below, uint32_t* words) {
+                uint32_t mx = 0;
+                for (int e = tid; e < kBlk * D; e += kThr) {
+                    const uint32_t m = magnitude(__uint_as_float((uint32_t)src[e] << 16));
+                    mx = max(mx, m < below ? m : 0u);
+                }
+                return largest_of<WAVES>(mx, words, tid);
+            };
+            uint32_t* words = reinterpret_cast<uint32_t*>(sm_m) + 2 * which * WAVES;
+            uint32_t top = largest(0xffffffffu, words);
+            const bool all_finite = top < kInfinity;
+            if (!all_finite) top = largest(kInfinity, words + WAVES);
+            const float scale = __uint_as_float(top) * F::kUnit;
+            const Divider divide(scale, __uint_as_float(top), all_finite);
             for (int e = 4 * tid; e < kBlk * D; e += 4 * kThr) {
                 const uint2 raw = *reinterpret_cast<const uint2*>(src + e);
-                const float x[4] = {bf16_lo(raw.x), bf16_hi(raw.x), bf16_lo(raw.y), bf16_hi(raw.y)};
+                float x[4] = {bf16_lo(raw.x), bf16_hi(raw.x), bf16_lo(raw.y), bf16_hi(raw.y)};
+                if (divide.care) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = divide.careful(x[i], F::nan_code());
+                }
                 *reinterpret_cast<uint32_t*>(dst + e) = F::code4(x, divide);
             }
             if (tid == 0) (which ? a.c.v_scale : a.c.k_scale)[at] = scale;
