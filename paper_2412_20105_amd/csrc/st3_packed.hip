@@ -29,6 +29,17 @@ __device__ __forceinline__ Seq sequence(const PackedArgs& a, int b) {
     return Seq{s, min(e - s, a.max_len)};
 }
 
+// Sum over the wave, the same in every lane (DPP: row_shr 1, 2, 4, 8, row_bcast 15, 31; the last lane has it).
+__device__ __forceinline__ int wave_total(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
 // Workgroup -> (sequence, key head, row tile).  A tile costs in proportion to its index, and lengths differ: tiles are dealt in
 // descending order of their index over all sequences, so the launch ends with its shortest workgroups.  Lengths are known to the device
 // only: every wave finds its place with a search over S(t), the number of tiles (of all sequences) with index t or more.  Key heads run fastest:
@@ -42,9 +53,7 @@ __device__ __forceinline__ bool place(const PackedArgs& a, int lane, int& b, int
     auto from = [&](int t) {            // S(t)
         int s = max(0, mine - t);
         for (int i = lane + kWave; i < a.B; i += kWave) s += max(0, tiles_of(i) - t);
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
-        return __builtin_amdgcn_readfirstlane(s);
+        return wave_total(s);
     };
     int lo = 0, hi = a.levels;          // S(lo) > x >= S(hi)
     if (from(0) <= x) return false;
@@ -344,34 +353,48 @@ template <int D> struct RowFrag<float, D> {
 };
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// float32: the same rows on v_mfma_f32_16x16x4f32 (A: lane (c, g) holds A[c][g]), 16 rows a wave, 64 a workgroup, operands straight from memory.
+// float32: the same rows on v_mfma_f32_16x16x4f32 (A: lane (c, g) holds A[c][g]).  A workgroup has 16 rows; its four waves take the key tiles of 16 in turn,
+// operands straight from memory, a wave's next tile on its way, and join their parts through LDS.  Bound by the latency of a tile's loads (600 rows of 300 keys, one
+// wave for 16 rows and all their keys, 22 us).
 // ---------------------------------------------------------------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void packed_f32_kernel(PackedArgs a) {
-    constexpr int DT = D / 16, kRows = 64;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c = lane & 15;
+    constexpr int DT = D / 16, kRows = 16;
+    __shared__ __attribute__((aligned(16))) float sm_o[4][16][D + 4];
+    __shared__ float sm_m[4][16], sm_l[4][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
     int b, kh, tile;
     Seq sq;
     if (!place<kRows>(a, lane, b, kh, tile, sq)) return;
-    const int n = sq.n, rows = n * a.G, r0 = tile * kRows + wave * 16;
-    if (r0 >= rows) return;
+    const int n = sq.n, rows = n * a.G, r0 = tile * kRows;
     const float* K = reinterpret_cast<const float*>(a.k) + (int64_t)sq.start * a.k_st + kh * a.k_sh;
     const float* V = reinterpret_cast<const float*>(a.v) + (int64_t)sq.start * a.v_st + kh * a.v_sh;
     const int r = min(r0 + c, rows - 1), pos = r / a.G, head = kh * a.G + r - pos * a.G;
-    RowFrag<float, D> qf;
+    const int tiles = (min(r0 + 15, rows - 1) / a.G) / 16 + 1;
+    RowFrag<float, D> kf, qf;
+    float vf[DT][4];                                        // contraction slot g of product i is key 4 g + i, the one whose weight this lane holds
+    auto load_k = [&](int t) { kf.load(K + (int64_t)min(16 * t + c, n - 1) * a.k_st, g); };
+    auto load_v = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float* row = V + (int64_t)min(16 * t + 4 * g + i, n - 1) * a.v_st + c;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) vf[dt][i] = row[16 * dt];
+        }
+    };
+    int t = wave;
+    if (t < tiles) { load_k(t); load_v(t); }
     qf.load(reinterpret_cast<const float*>(a.q) + (int64_t)(sq.start + pos) * a.q_st + (int64_t)head * a.q_sh, g);
     f32x4 o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -3.402823466e38f, l = 0.f;
-    const int p_last = min(r0 + 15, rows - 1) / a.G;
-    for (int k0 = 0; k0 <= p_last; k0 += 16) {
-        RowFrag<float, D> kf;
-        kf.load(K + (int64_t)min(k0 + c, n - 1) * a.k_st, g);
+    for (; t < tiles; t += 4) {
         f32x4 s = kf.dot(qf) * a.scale_l2;
+        if (t + 4 < tiles) load_k(t + 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (k0 + 4 * g + i > pos) s[i] = -INFINITY;
+            if (16 * t + 4 * g + i > pos) s[i] = -INFINITY;
         const float mx = fmaxf(m, wave_max_from<16>(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
         const float alpha = exp2_fast(m - mx);
         m = mx;
@@ -383,51 +406,93 @@ __global__ __launch_bounds__(256) void packed_f32_kernel(PackedArgs a) {
         for (int dt = 0; dt < DT; ++dt) {
             o[dt] *= alpha;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)         // contraction slot g of product i is key 4 g + i, the one whose weight this lane holds
-                o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(V[(int64_t)min(k0 + 4 * g + i, n - 1) * a.v_st + 16 * dt + c], p[i], o[dt], 0, 0, 0);
+            for (int i = 0; i < 4; ++i) o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[dt][i], p[i], o[dt], 0, 0, 0);
         }
+        if (t + 4 < tiles) load_v(t + 4);
     }
-    const float rl = 1.0f / wave_sum_from<16>(l);
-    if (r0 + c >= rows) return;
-    float* out = reinterpret_cast<float*>(a.out) + (int64_t)(sq.start + pos) * a.o_st + (int64_t)head * a.o_sh;
+    // ---- join the waves' parts (one without tiles has sum 0 at the lowest float) -------------------------------------------------
+    l = wave_sum_from<16>(l);
+    if (g == 0) { sm_m[wave][c] = m; sm_l[wave][c] = l; }
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(out + 16 * dt + 4 * g) = o[dt] * rl;
-    if (a.ml != nullptr && g == 0 && pos >= n - a.window) a.ml[(int64_t)(sq.start + pos) * a.H + head] = make_float2(m, rl);
+    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(&sm_o[wave][c][16 * dt + 4 * g]) = o[dt];
+    __syncthreads();
+    for (int e = tid; e < 16 * (D / 4); e += 256) {
+        const int x = e / (D / 4), col = e % (D / 4) * 4;
+        if (r0 + x >= rows) continue;
+        float top = fmaxf(fmaxf(sm_m[0][x], sm_m[1][x]), fmaxf(sm_m[2][x], sm_m[3][x])), sum = 0.f;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = exp2_fast(sm_m[w][x] - top);
+            sum = fmaf(sm_l[w][x], f, sum);
+            v += *reinterpret_cast<const f32x4*>(&sm_o[w][x][col]) * f;
+        }
+        const float rl = 1.0f / sum;
+        const int p = (r0 + x) / a.G, hd = kh * a.G + r0 + x - p * a.G;
+        *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + (int64_t)(sq.start + p) * a.o_st + (int64_t)hd * a.o_sh + col) = v * rl;
+        if (a.ml != nullptr && col == 0 && p >= n - a.window) a.ml[(int64_t)(sq.start + p) * a.H + hd] = make_float2(top, rl);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// score[b,kh,j] = sum over the rows of the window of exp2(logit - maximum) / sum: the logits are formed again, 16 keys a wave against 16 rows at a
-// time, and a lane adds up what its four keys get.
+// score[b,kh,j] = sum over the rows of the window of exp2(logit - maximum) / sum.  The logits are formed again: a workgroup has 64 keys, every wave all of them in
+// registers, and its four waves take the window's rows in turn, 16 at a time; a lane adds up what its 16 keys get.  (With 16 keys a wave, which read all rows each: 64 rows
+// of 4 heads over 21000 tokens 100 us.)
 // ---------------------------------------------------------------------------------------------------------------------------------
 template <typename T, int D>
 __global__ __launch_bounds__(256) void packed_score_kernel(PackedArgs a) {
+    __shared__ float part[4][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c = lane & 15;
     const int kh = blockIdx.x, b = blockIdx.z;
     const Seq sq = sequence(a, b);
-    const int n = sq.n, k0 = blockIdx.y * 64 + wave * 16;
+    const int n = sq.n, k0 = blockIdx.y * 64;
     if (k0 >= n) return;
-    RowFrag<T, D> kf;
-    kf.load(reinterpret_cast<const T*>(a.k) + (int64_t)(sq.start + min(k0 + c, n - 1)) * a.k_st + kh * a.k_sh, g);
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    const int first = max(max(0, n - a.window), k0) * a.G, rows = n * a.G;
-    for (int r0 = first; r0 < rows; r0 += 16) {
-        const int r = min(r0 + c, rows - 1), pos = r / a.G, head = kh * a.G + r - pos * a.G;
-        RowFrag<T, D> qf;
-        qf.load(reinterpret_cast<const T*>(a.q) + (int64_t)(sq.start + pos) * a.q_st + (int64_t)head * a.q_sh, g);
-        const float2 ml = a.ml[(int64_t)(sq.start + pos) * a.H + head];
-        const f32x4 s = kf.dot(qf);
+    RowFrag<T, D> kf[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float p = exp2_fast(fmaf(s[i], a.scale_l2, -ml.x)) * ml.y;
-            sum[i] += r0 + c < rows && k0 + 4 * g + i <= pos ? p : 0.f;
+    for (int x = 0; x < 4; ++x) kf[x].load(reinterpret_cast<const T*>(a.k) + (int64_t)(sq.start + min(k0 + 16 * x + c, n - 1)) * a.k_st + kh * a.k_sh, g);
+    f32x4 sum[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) sum[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int from = max(max(0, n - a.window), k0), rows = n * a.G;     // (rows in front of the first key see none of them)
+    const bool masked = from < k0 + 63;
+    RowFrag<T, D> qf, next;
+    float2 ml, ml_next;
+    int pos, pos_next;
+    auto fetch = [&](int r0) {
+        const int r = min(r0 + c, rows - 1);
+        pos_next = r / a.G;
+        const int head = kh * a.G + r - pos_next * a.G;
+        next.load(reinterpret_cast<const T*>(a.q) + (int64_t)(sq.start + pos_next) * a.q_st + (int64_t)head * a.q_sh, g);
+        ml_next = a.ml[(int64_t)(sq.start + pos_next) * a.H + head];
+        if (r0 + c >= rows) pos_next = -1;                             // (a row that does not exist)
+    };
+    int r0 = from * a.G + 16 * wave;
+    if (r0 < rows) fetch(r0);
+    for (; r0 < rows; r0 += 64) {
+        qf = next; pos = pos_next;
+        ml = make_float2(ml_next.x, pos < 0 ? 0.f : ml_next.y);
+        if (r0 + 64 < rows) fetch(r0 + 64);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const f32x4 s = kf[x].dot(qf);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = exp2_fast(fmaf(s[i], a.scale_l2, -ml.x)) * ml.y;
+                sum[x][i] += masked && k0 + 16 * x + 4 * g + i > pos ? 0.f : p;
+            }
         }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] = group_sum<16>(sum[i]);
-    if (c < 4) {
-        const int key = k0 + 4 * g + c;
-        if (key < n) a.score[b * a.s_sb + kh * a.s_sh + key] = c == 0 ? sum[0] : c == 1 ? sum[1] : c == 2 ? sum[2] : sum[3];
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[x][i] = group_sum<16>(sum[x][i]);
+    if (c == 0) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4*>(&part[wave][16 * x + 4 * g]) = sum[x];
     }
+    __syncthreads();
+    if (tid < 64 && k0 + tid < n)
+        a.score[b * a.s_sb + kh * a.s_sh + k0 + tid] = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
 }
 
 }  // namespace
@@ -462,7 +527,7 @@ extern "C" st3_status st3_packed_attention(const st3_gqa_shape* shape, const st3
     PackedArgs a{q->data, k->data, v->data, out->data, q->stride_t, q->stride_h, k->stride_t, k->stride_h, v->stride_t, v->stride_h, out->stride_t,
                  out->stride_h, cu_len, shape->batch, total, max_len, H, Hk, G, 0, gqa_scale_log2(shape), score, score_stride_b, score_stride_h,
                  score ? reinterpret_cast<float2*>(workspace) : nullptr, window};
-    const int rows = shape->dtype == ST3_BF16 ? 64 * ST3_PACKED_COLS : 64;
+    const int rows = shape->dtype == ST3_BF16 ? 64 * ST3_PACKED_COLS : 16;
     a.levels = (int)(((int64_t)max_len * G + rows - 1) / rows);
     // no more tiles than this, whatever the lengths are: each sequence has one that is not full
     const int64_t tiles = std::min((int64_t)total * G / rows + std::min(shape->batch, total), (int64_t)a.levels * shape->batch);
