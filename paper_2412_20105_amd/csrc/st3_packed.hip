@@ -435,18 +435,18 @@ __global__ __launch_bounds__(256) void packed_f32_kernel(PackedArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// score[b,kh,j] = sum over the rows of the window of exp2(logit - maximum) / sum.  The logits are formed again: a workgroup has 64 keys, every wave all of them in
-// registers, and its four waves take the window's rows in turn, 16 at a time; a lane adds up what its 16 keys get.  (With 16 keys a wave, which read all rows each: 64 rows
-// of 4 heads over 21000 tokens 100 us.)
+// score[b,kh,j] = sum over the rows of the window of exp2(logit - maximum) / sum.  The logits are formed again: a wave has 64 keys in registers and takes rows 16 at a time, the
+// next ones on their way; a lane adds up what its 16 keys get.  DEAL: the workgroup's four waves have the same keys and take the rows in turn, which is the shorter way where
+// workgroups are few; else they have 256 keys and all take all rows, which come from memory once for the four (64 rows of 4 heads, 21000 tokens: 48 us dealt).
 // ---------------------------------------------------------------------------------------------------------------------------------
-template <typename T, int D>
+template <typename T, int D, bool DEAL>
 __global__ __launch_bounds__(256) void packed_score_kernel(PackedArgs a) {
     __shared__ float part[4][64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c = lane & 15;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
     const int kh = blockIdx.x, b = blockIdx.z;
     const Seq sq = sequence(a, b);
-    const int n = sq.n, k0 = blockIdx.y * 64;
-    if (k0 >= n) return;
+    const int n = sq.n, k0 = DEAL ? blockIdx.y * 64 : (blockIdx.y * 4 + wave) * 64;
+    if (k0 >= n) return;                                    // (no barrier below unless DEAL, where all waves have the same keys)
     RowFrag<T, D> kf[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) kf[x].load(reinterpret_cast<const T*>(a.k) + (int64_t)(sq.start + min(k0 + 16 * x + c, n - 1)) * a.k_st + kh * a.k_sh, g);
@@ -466,12 +466,13 @@ __global__ __launch_bounds__(256) void packed_score_kernel(PackedArgs a) {
         ml_next = a.ml[(int64_t)(sq.start + pos_next) * a.H + head];
         if (r0 + c >= rows) pos_next = -1;                             // (a row that does not exist)
     };
-    int r0 = from * a.G + 16 * wave;
+    constexpr int kStep = DEAL ? 64 : 16;
+    int r0 = from * a.G + (DEAL ? 16 * wave : 0);
     if (r0 < rows) fetch(r0);
-    for (; r0 < rows; r0 += 64) {
+    for (; r0 < rows; r0 += kStep) {
         qf = next; pos = pos_next;
         ml = make_float2(ml_next.x, pos < 0 ? 0.f : ml_next.y);
-        if (r0 + 64 < rows) fetch(r0 + 64);
+        if (r0 + kStep < rows) fetch(r0 + kStep);
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const f32x4 s = kf[x].dot(qf);
@@ -490,9 +491,24 @@ __global__ __launch_bounds__(256) void packed_score_kernel(PackedArgs a) {
 #pragma unroll
         for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4*>(&part[wave][16 * x + 4 * g]) = sum[x];
     }
-    __syncthreads();
-    if (tid < 64 && k0 + tid < n)
-        a.score[b * a.s_sb + kh * a.s_sh + k0 + tid] = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
+    float* score = a.score + b * a.s_sb + kh * a.s_sh + k0;
+    if constexpr (DEAL) {
+        __syncthreads();
+        if (tid < 64 && k0 + tid < n) score[tid] = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
+    } else {
+        if (k0 + lane < n) score[lane] = part[wave][lane];  // (written by this wave)
+    }
+}
+
+#ifndef DT_
+#define DT_ 1024
+#endif
+constexpr int kDealTiles = DT_;
+template <typename T, int D>
+void launch_score(const PackedArgs& a, hipStream_t st) {
+    const int64_t strips = (int64_t)a.Hk * a.B, tiles = (a.max_len + 63) / 64;
+    if (tiles * strips <= kDealTiles) packed_score_kernel<T, D, true><<<dim3(a.Hk, (unsigned)tiles, a.B), 256, 0, st>>>(a);
+    else packed_score_kernel<T, D, false><<<dim3(a.Hk, (unsigned)((tiles + 3) / 4), a.B), 256, 0, st>>>(a);
 }
 
 }  // namespace
@@ -532,6 +548,7 @@ extern "C" st3_status st3_packed_attention(const st3_gqa_shape* shape, const st3
     // no more tiles than this, whatever the lengths are: each sequence has one that is not full
     const int64_t tiles = std::min((int64_t)total * G / rows + std::min(shape->batch, total), (int64_t)a.levels * shape->batch);
     if (tiles * Hk > 0x7fffffff) return ST3_ERR_UNSUPPORTED;
+    if (score && (max_len + 63) / 64 > 65535) return ST3_ERR_UNSUPPORTED;
     const unsigned grid = (unsigned)(tiles * Hk);
     if (shape->dtype == ST3_BF16) {
         if (D == 128) packed_kernel<128, ST3_PACKED_COLS><<<grid, 256, 0, st>>>(a);
@@ -541,14 +558,12 @@ extern "C" st3_status st3_packed_attention(const st3_gqa_shape* shape, const st3
         else packed_f32_kernel<64><<<grid, 256, 0, st>>>(a);
     }
     if (score) {
-        const dim3 sg(Hk, (max_len + 63) / 64, shape->batch);
-        if (sg.y > 65535) return ST3_ERR_UNSUPPORTED;
         if (shape->dtype == ST3_BF16) {
-            if (D == 128) packed_score_kernel<bf16_t, 128><<<sg, 256, 0, st>>>(a);
-            else packed_score_kernel<bf16_t, 64><<<sg, 256, 0, st>>>(a);
+            if (D == 128) launch_score<bf16_t, 128>(a, st);
+            else launch_score<bf16_t, 64>(a, st);
         } else {
-            if (D == 128) packed_score_kernel<float, 128><<<sg, 256, 0, st>>>(a);
-            else packed_score_kernel<float, 64><<<sg, 256, 0, st>>>(a);
+            if (D == 128) launch_score<float, 128>(a, st);
+            else launch_score<float, 64>(a, st);
         }
     }
     return check_launch();
