@@ -17,6 +17,7 @@ struct PackedArgs {
     const int32_t* cu;
     int32_t B, total, max_len, H, Hk, G;
     int32_t levels;                 // row tiles of the longest prompt that may come
+    int32_t spread;                 // row tiles dealt together at the end of the launch
     float scale_l2;
     float* score; int64_t s_sb, s_sh;
     float2* ml;                     // [total][H] maximum and sum of the rows whose weights count; null: no score
@@ -29,55 +30,79 @@ __device__ __forceinline__ Seq sequence(const PackedArgs& a, int b) {
     return Seq{s, min(e - s, a.max_len)};
 }
 
-// Sum over the wave, the same in every lane (DPP: row_shr 1, 2, 4, 8, row_bcast 15, 31; the last lane has it).
-__device__ __forceinline__ int wave_total(int x) {
+// Inclusive sum over the wave's lanes (DPP: row_shr 1, 2, 4, 8, row_bcast 15, 31); the sum, and the largest of values that are not negative, the same in every lane.
+__device__ __forceinline__ int wave_prefix(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
     x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
     x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
     x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
     x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);
+    return x;
+}
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_prefix(x), 63); }
+__device__ __forceinline__ int wave_most(int x) {
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true));
     return __builtin_amdgcn_readlane(x, 63);
 }
 
-// Workgroup -> (sequence, key head, row tile).  A tile costs in proportion to its index, and lengths differ: tiles are dealt in
-// descending order of their index over all sequences, so the launch ends with its shortest workgroups.  Lengths are known to the device
-// only: every wave finds its place with a search over S(t), the number of tiles (of all sequences) with index t or more.  Key heads run fastest:
-// workgroups go round-robin to the 8 XCDs, so with a multiple of 8 key heads a pair's K and V stay in one XCD's L2.
+// Workgroup -> (sequence, key head, row tile).  Key heads run fastest: workgroups go round-robin to the 8 XCDs, so with a multiple of 8 key heads a pair's K and V stay in
+// one XCD's L2, and a sequence's tiles follow each other, heaviest (last) first, longest sequences first, so that they are there when the next tile wants them.  A
+// tile costs in proportion to its index: the last sequences' tiles (a.spread of them, or so) are dealt together, heaviest first over all of them, so that the launch ends with its
+// shortest workgroups.  Lengths are known to the device only: every wave finds its place, a lane for each of up to 64 sequences; more keep their own order.
 template <int ROWS>
 __device__ __forceinline__ bool place(const PackedArgs& a, int lane, int& b, int& kh, int& tile, Seq& sq) {
     kh = blockIdx.x % a.Hk;
-    const int x = blockIdx.x / a.Hk;
+    int x = blockIdx.x / a.Hk;
     auto tiles_of = [&](int i) { return i < a.B ? (int)(((int64_t)sequence(a, i).n * a.G + ROWS - 1) / ROWS) : 0; };
-    const int mine = tiles_of(lane);
-    auto from = [&](int t) {            // S(t)
-        int s = max(0, mine - t);
-        for (int i = lane + kWave; i < a.B; i += kWave) s += max(0, tiles_of(i) - t);
-        return wave_total(s);
+    auto found = [&](int seq, int t) {
+        b = __builtin_amdgcn_readfirstlane(seq);
+        tile = __builtin_amdgcn_readfirstlane(t);
+        sq = sequence(a, b);
+        return true;
     };
-    int lo = 0, hi = a.levels;          // S(lo) > x >= S(hi)
-    if (from(0) <= x) return false;
-    int above = 0;
+    if (a.B > kWave) {
+        for (int i0 = 0; i0 < a.B; i0 += kWave) {
+            const int mine = tiles_of(i0 + lane), upto = wave_prefix(mine), all = __builtin_amdgcn_readlane(upto, 63);
+            if (x < all) {
+                const int at = __ffsll((unsigned long long)__ballot(x < upto)) - 1;
+                return found(i0 + at, __builtin_amdgcn_readlane(upto, at) - 1 - x);
+            }
+            x -= all;
+        }
+        return false;
+    }
+    const int mine = tiles_of(lane);
+    int before = 0;                     // tiles of the sequences in front of this one, longest first
+    for (int i = 0; i < a.B; ++i) {
+        const int other = __builtin_amdgcn_readlane(mine, i);
+        before += other > mine || (other == mine && i < lane) ? other : 0;
+    }
+    const int total = wave_total(mine);
+    if (x >= total) return false;
+    // the sequences in front of `apart` have their tiles to themselves
+    const int end = before + mine, apart = wave_most(mine > 0 && end <= total - a.spread ? end : 0);
+    if (x < apart) {
+        const int at = __ffsll((unsigned long long)__ballot(mine > 0 && before <= x && x < end)) - 1;
+        return found(at, __builtin_amdgcn_readlane(end, at) - 1 - x);
+    }
+    x -= apart;
+    const int dealt = before >= apart ? mine : 0;
+    auto from = [&](int t) { return wave_total(max(0, dealt - t)); };      // tiles of index t or more
+    int lo = 0, hi = a.levels, above = 0;                                  // from(lo) > x >= from(hi)
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2, s = from(mid);
         if (s > x) lo = mid;
         else { hi = mid; above = s; }
     }
-    tile = lo;
-    int rank = x - above;               // among the sequences with more than `tile` tiles
-    for (int i0 = 0; i0 < a.B; i0 += kWave) {
-        const bool has = (i0 == 0 ? mine : tiles_of(i0 + lane)) > tile;
-        const uint64_t who = __ballot(has);
-        const int cnt = __popcll(who);
-        if (rank < cnt) {
-            const uint64_t me = __ballot(has && __popcll(who & ((1ull << lane) - 1)) == rank);
-            b = __builtin_amdgcn_readfirstlane(i0 + __ffsll((unsigned long long)me) - 1);
-            sq = sequence(a, b);
-            return true;
-        }
-        rank -= cnt;
-    }
-    return false;
+    const uint64_t who = __ballot(dealt > lo);
+    const uint64_t me = __ballot(dealt > lo && __popcll(who & ((1ull << lane) - 1)) == x - above);
+    return found(__ffsll((unsigned long long)me) - 1, lo);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
@@ -102,8 +127,9 @@ struct Rows {
 };
 
 // 32 keys for one wave: S^T = K Q^T, one online-softmax update, O^T += V^T P^T.  MASKED: some row does not see some of the keys.
+// CAREFUL: V may hold infinities or NaN, and a weight of 0 does not silence those; row by row, V's keys that the row does not see count as 0.
 // (The scheduling barriers keep the compiler from holding more fragments than there are registers for.)
-template <int D, int QC, bool MASKED>
+template <int D, int QC, bool MASKED, bool CAREFUL = false>
 __device__ __forceinline__ void packed_step(uint32_t Kt, uint32_t Vt, const Frag (&qf)[QC][D / 32], Rows<D, QC>& st, float scale_l2, int g, int k0) {
     constexpr int KS = D / 32, DT = D / 16;
     f32x4 s[2][QC];
@@ -181,6 +207,29 @@ __device__ __forceinline__ void packed_step(uint32_t Kt, uint32_t Vt, const Frag
             st.l[qc] += p.x + p.y;
             pb[qc].w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
         }
+    if constexpr (CAREFUL) {
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc)
+            for (int x = 0; x < 16; ++x) {
+                const int pos = __builtin_amdgcn_readlane(st.pos[qc], x), c = threadIdx.x & 15;
+                Frag seen;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int key = k0 + 16 * (j / 2) + 4 * g + 2 * (j & 1);
+                    seen.w[j] = (key <= pos ? 0xffffu : 0u) | (key < pos ? 0xffff0000u : 0u);
+                }
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    load_v(dt);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) va[dt % VB].w[j] &= seen.w[j];
+                    const f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[dt % VB].v, pb[qc].v, st.o[dt][qc], 0, 0, 0);
+                    st.o[dt][qc] = c == x ? o : st.o[dt][qc];
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        return;
+    }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
         if (dt > 0 && dt + VB - 1 < DT) load_v(dt + VB - 1);
@@ -217,28 +266,31 @@ __device__ __forceinline__ void load_tile(uint32_t lds, const uint16_t* K, const
     }
 }
 
-#ifndef ST3_PACKED_COLS
-#define ST3_PACKED_COLS 2
-#define ST3_PACKED_WAVES 3
-#endif
-template <int D, int QC>
-__global__ __launch_bounds__(256, ST3_PACKED_WAVES) void packed_kernel(PackedArgs a) {
+// A workgroup's four waves have 16 QC rows each and share the K and V tiles, which go straight from memory to LDS, two tiles ahead.  Bound by the matrix
+// instructions' power at long prompts: 21000 tokens of 32 heads over 8 of 128 in 1.66 ms, 1150 TF/s of the 1366 that a large product reaches, at
+// 1.7 GHz.  Two columns of rows leave registers for 3 waves a SIMD; three columns with 2 waves: 1.61 ms there, but 40 and 54 us for 36 and 50 at prompts of 700.
+// SPLIT: as many groups of four waves take the same rows and every SPLIT-th tile, and join their sums in LDS at the end.
+template <int D, int QC, int SPLIT>
+__global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 3 : SPLIT) void packed_kernel(PackedArgs a) {
     using L = TileLayout<D, 32>;
     constexpr int kRows = 64 * QC, KS = D / 32, DT = D / 16, kRing = 3, OSTR = D + 8;
     constexpr int kTiles = kRing * 2 * L::TILE, kOut = 4 * 16 * QC * OSTR;
-    __shared__ __attribute__((aligned(1024))) uint16_t buf[kTiles > kOut ? kTiles : kOut];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wave_s = __builtin_amdgcn_readfirstlane(wave);
+    __shared__ __attribute__((aligned(1024))) uint16_t buf[SPLIT * kTiles > kOut ? SPLIT * kTiles : kOut];
+    __shared__ int redo;
+    const int lane = threadIdx.x & 63, wave_s = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 3), wave = wave_s;
+    const int part = SPLIT == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
     const int g = lane >> 4, c = lane & 15;
     int b, kh, tile;
     Seq sq;
     if (!place<kRows>(a, lane, b, kh, tile, sq)) return;
+    if (threadIdx.x == 0) redo = 0;
     const int n = sq.n, rows = n * a.G;
     // row tiles are cut from the end, in whole columns: a prompt's first tile, the cheapest, is the one that is not full
     const int tiles = (rows + kRows - 1) / kRows, shift = (tiles * kRows - rows) / (16 * QC) * (16 * QC);
     const int r0 = tile * kRows - shift + wave * 16 * QC;            // the wave's first row; < 0 or >= rows: it has none
     const uint16_t* K = reinterpret_cast<const uint16_t*>(a.k) + (int64_t)sq.start * a.k_st + kh * a.k_sh;
     const uint16_t* V = reinterpret_cast<const uint16_t*>(a.v) + (int64_t)sq.start * a.v_st + kh * a.v_sh;
-    const uint32_t lds0 = lds_addr(buf);
+    const uint32_t lds0 = lds_addr(buf) + part * (2 * kTiles);
     constexpr int kBuf = 4 * L::TILE;
     const int last = min(rows, (tile + 1) * kRows - shift) - 1;      // the workgroup's last row
     const int nt = last / a.G / 32 + 1;
@@ -246,7 +298,7 @@ __global__ __launch_bounds__(256, ST3_PACKED_WAVES) void packed_kernel(PackedArg
     const uint32_t k_lane = (uint32_t)(2 * (row0 * (int)a.k_st + (lane % L::UPR ^ L::k_swz(row0)) * 8));
     const uint32_t v_lane = (uint32_t)(2 * (row0 * (int)a.v_st + (lane % L::UPR ^ L::v_swz(row0)) * 8));
     auto issue = [&](int t, int slot) { load_tile<D>(lds0 + slot * kBuf, K, V, a.k_st, a.v_st, t * 32, n, k_lane, v_lane, row0, wave_s); };
-    issue(0, 0);
+    if (SPLIT == 1 || part < nt) issue(part, 0);
     Rows<D, QC> st;
     st.init();
     Frag qf[QC][KS];
@@ -265,32 +317,84 @@ __global__ __launch_bounds__(256, ST3_PACKED_WAVES) void packed_kernel(PackedArg
         const int row = 4 * g + (c >> 2);
         v_at = (uint32_t)(2 * (row * D + (((c & 3) >> 1) ^ L::v_swz(row)) * 8 + 4 * (c & 1))) + 2 * L::TILE;
     }
-    if (nt > 1) { issue(1, 1); wait_direct_loads_but<2 * L::NI>(); }
+    if (part + SPLIT < nt) { issue(part + SPLIT, 1); wait_direct_loads_but<2 * L::NI>(); }
     else wait_direct_loads();
     __syncthreads();
     // Tiles that every row of the workgroup sees whole come first, in a loop without conditions (with both kinds in one loop the accumulators were moved
     // between the two forms' registers, and spilled); the few at the edge follow.
-    int t = 0, slot = 0, next = 2;
+    int t = part, slot = 0, next = 2;
     auto advance = [&]() {
-        if (t + 2 < nt) { issue(t + 2, next); wait_direct_loads_but<2 * L::NI>(); }
+        if (t + 2 * SPLIT < nt) { issue(t + 2 * SPLIT, next); wait_direct_loads_but<2 * L::NI>(); }
         else wait_direct_loads();
         __syncthreads();
         slot = slot == kRing - 1 ? 0 : slot + 1;
         next = next == kRing - 1 ? 0 : next + 1;
+        t += SPLIT;
     };
-    for (const int whole = (max(tile * kRows - shift, 0) / a.G + 1) / 32; t < whole; ++t) {
+    for (int whole = (max(tile * kRows - shift, 0) / a.G + 1) / 32 / SPLIT; whole > 0; --whole) {
         const uint32_t at = lds0 + slot * kBuf;
         packed_step<D, QC, false>(at + k_at, at + v_at, qf, st, a.scale_l2, g, 32 * t);
         advance();
     }
-    for (; t < nt; ++t) {
+    while (t - part < nt) {
         const uint32_t at = lds0 + slot * kBuf;
         if (32 * t <= p_last) packed_step<D, QC, true>(at + k_at, at + v_at, qf, st, a.scale_l2, g, 32 * t);
         advance();
     }
+    // Anything but finite: it may be from V of keys that a row does not see (0 times infinity).  Once more, such V left out.
+    float odd = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) odd = fmaf(st.o[dt][qc][i], 0.f, odd);
+    if (odd != 0.f) redo = 1;
+    __syncthreads();
+    if (redo) {
+        st.init();
+        for (t = part; t - part < nt; t += SPLIT) {
+            if (t < nt) issue(t, 0);
+            wait_direct_loads();
+            __syncthreads();
+            if (32 * t <= p_last) packed_step<D, QC, true, true>(lds0 + k_at, lds0 + v_at, qf, st, a.scale_l2, g, 32 * t);
+            __syncthreads();
+        }
+    }
+    uint16_t* ob = buf + wave * 16 * QC * OSTR;
+    if constexpr (SPLIT > 1) {                                       // join the parts' sums: lane for lane the same rows and columns
+        constexpr int kLane = DT * QC * 256;                         // floats of a wave's accumulators
+        static_assert((SPLIT - 1) * 4 * (4 * kLane + 512 * QC) <= (int)sizeof(buf), "parts in LDS");
+        float* acc = reinterpret_cast<float*>(buf) + wave * (kLane + 128 * QC);
+        constexpr int kPart = 4 * (kLane + 128 * QC);
+        if (part > 0) {
+            float* to = acc + (part - 1) * kPart;
+#pragma unroll
+            for (int qc = 0; qc < QC; ++qc) {
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(to + (qc * DT + dt) * 256 + 4 * lane) = st.o[dt][qc];
+                to[kLane + 128 * qc + lane] = st.m[qc];
+                to[kLane + 128 * qc + 64 + lane] = st.l[qc];
+            }
+        }
+        __syncthreads();
+        if (part > 0) return;
+#pragma unroll
+        for (int x = 0; x < SPLIT - 1; ++x) {
+            const float* from = acc + x * kPart;
+#pragma unroll
+            for (int qc = 0; qc < QC; ++qc) {
+                const float m = from[kLane + 128 * qc + lane], top = fmaxf(m, st.m[qc]), f = exp2_fast(m - top), mine = exp2_fast(st.m[qc] - top);
+                st.m[qc] = top;
+                st.l[qc] = st.l[qc] * mine + from[kLane + 128 * qc + 64 + lane] * f;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) st.o[dt][qc] = st.o[dt][qc] * mine + *reinterpret_cast<const f32x4*>(from + (qc * DT + dt) * 256 + 4 * lane) * f;
+            }
+        }
+        ob = reinterpret_cast<uint16_t*>(acc);                       // (read by this wave only)
+    }
     // ---- normalise; the block of outputs goes through LDS and leaves as whole rows ----------------------------------------------
     constexpr int VPR = D / 8, RPI = 64 / VPR;
-    uint16_t* ob = buf + wave * 16 * QC * OSTR;
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc) {
         const float l = wave_sum_from<16>(st.l[qc]), rl = 1.0f / l;
@@ -303,9 +407,11 @@ __global__ __launch_bounds__(256, ST3_PACKED_WAVES) void packed_kernel(PackedArg
             pk.y = __builtin_bit_cast(uint32_t, __builtin_convertvector(o23, bf16x2));
             *reinterpret_cast<uint2*>(ob + (16 * qc + c) * OSTR + 16 * dt + 4 * g) = pk;
         }
-        const int r = r0 + 16 * qc + c;
-        if (a.ml != nullptr && g == 0 && r >= 0 && r < rows && st.pos[qc] >= n - a.window)
-            a.ml[(int64_t)(sq.start + st.pos[qc]) * a.H + kh * a.G + r - st.pos[qc] * a.G] = make_float2(st.m[qc], rl);
+        int col = c;
+        asm volatile("" : "+v"(col));                                // (formed again: kept from the start, rows and addresses were spilled)
+        const int r = r0 + 16 * qc + col, p = r / a.G;
+        if (a.ml != nullptr && g == 0 && r >= 0 && r < rows && p >= n - a.window)
+            a.ml[(int64_t)(sq.start + p) * a.H + kh * a.G + r - p * a.G] = make_float2(st.m[qc], rl);
     }
     uint16_t* O = reinterpret_cast<uint16_t*>(a.out);
 #pragma unroll
@@ -402,9 +508,28 @@ __global__ __launch_bounds__(256) void packed_f32_kernel(PackedArgs a) {
         float p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) { p[i] = exp2_fast(s[i] - m); l += p[i]; }
+        // at the edge: infinities and NaN in V of keys that a row does not see stay out of it, row by row (a weight of 0 does not silence them)
+        float odd = 0.f;
+        if (16 * t + 15 > r0 / a.G) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) odd = fmaf(vf[dt][i], 0.f, odd);
+        }
+        const bool careful = __any(odd != 0.f);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
             o[dt] *= alpha;
+            if (careful) {
+                for (int x = 0; x < 16; ++x) {
+                    const int seen = __builtin_amdgcn_readlane(pos, x) - 16 * t - 4 * g;
+                    f32x4 y = o[dt];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y = __builtin_amdgcn_mfma_f32_16x16x4f32(i <= seen ? vf[dt][i] : 0.f, p[i], y, 0, 0, 0);
+                    o[dt] = c == x ? y : o[dt];
+                }
+                continue;
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[dt][i], p[i], o[dt], 0, 0, 0);
         }
@@ -500,15 +625,26 @@ __global__ __launch_bounds__(256) void packed_score_kernel(PackedArgs a) {
     }
 }
 
-#ifndef DT_
-#define DT_ 1024
-#endif
-constexpr int kDealTiles = DT_;
+// Dealt or not, in us, by workgroups of 64 keys: 40 4.4 / 6.4, 128 5.6 / 8.9, 352 8.7 / 9.6; 1920 8.4 / 7.4, 3072 49 / 35, 6272 23 / 21.
+constexpr int kDealTiles = 1024;
 template <typename T, int D>
 void launch_score(const PackedArgs& a, hipStream_t st) {
     const int64_t strips = (int64_t)a.Hk * a.B, tiles = (a.max_len + 63) / 64;
     if (tiles * strips <= kDealTiles) packed_score_kernel<T, D, true><<<dim3(a.Hk, (unsigned)tiles, a.B), 256, 0, st>>>(a);
     else packed_score_kernel<T, D, false><<<dim3(a.Hk, (unsigned)((tiles + 3) / 4), a.B), 256, 0, st>>>(a);
+}
+
+// Few workgroups with long walks leave most of the chip's waves idle: then two groups of waves share a walk.  In us, one group / two: 1 x 500 tokens of 8 key heads
+// (128 workgroups) 24 / 22, 1 x 1000 (256) 38 / 31, 2 x 700 (360) 31 / 29.5, 1 x 2000 (504) 64 / 55; 1 x 200 17.0 / 17.6, 3 x 400 (320) 24 / 26, 4 x 700
+// (704) 37 / 49.  (Three groups: within 1 us of two, but 1 x 300 20 for 18.)
+constexpr int kCols = 2, kFewWorkgroups = 512, kLongWalk = 448;
+// Row tiles dealt over the prompts at a launch's end, as workgroups: all the tiles of 32 x 739 tokens, 40 key heads, in order of their length 499 us, no dealing 368, 768 to 3000 364 to
+// 380; 4 x 700 42 without, 36 with; 8 x 3136, 32 key heads, 809 / 722 / 710 at 1536.
+constexpr int kSpread = 1536;
+template <int D>
+void launch_packed(const PackedArgs& a, unsigned grid, hipStream_t st) {
+    if (grid <= kFewWorkgroups && a.max_len > kLongWalk) packed_kernel<D, kCols, 2><<<grid, 512, 0, st>>>(a);
+    else packed_kernel<D, kCols, 1><<<grid, 256, 0, st>>>(a);
 }
 
 }  // namespace
@@ -541,18 +677,19 @@ extern "C" st3_status st3_packed_attention(const st3_gqa_shape* shape, const st3
     }
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     PackedArgs a{q->data, k->data, v->data, out->data, q->stride_t, q->stride_h, k->stride_t, k->stride_h, v->stride_t, v->stride_h, out->stride_t,
-                 out->stride_h, cu_len, shape->batch, total, max_len, H, Hk, G, 0, gqa_scale_log2(shape), score, score_stride_b, score_stride_h,
+                 out->stride_h, cu_len, shape->batch, total, max_len, H, Hk, G, 0, 0, gqa_scale_log2(shape), score, score_stride_b, score_stride_h,
                  score ? reinterpret_cast<float2*>(workspace) : nullptr, window};
-    const int rows = shape->dtype == ST3_BF16 ? 64 * ST3_PACKED_COLS : 16;
+    const int rows = shape->dtype == ST3_BF16 ? 64 * kCols : 16;
     a.levels = (int)(((int64_t)max_len * G + rows - 1) / rows);
+    a.spread = (kSpread + Hk - 1) / Hk;
     // no more tiles than this, whatever the lengths are: each sequence has one that is not full
     const int64_t tiles = std::min((int64_t)total * G / rows + std::min(shape->batch, total), (int64_t)a.levels * shape->batch);
     if (tiles * Hk > 0x7fffffff) return ST3_ERR_UNSUPPORTED;
     if (score && (max_len + 63) / 64 > 65535) return ST3_ERR_UNSUPPORTED;
     const unsigned grid = (unsigned)(tiles * Hk);
     if (shape->dtype == ST3_BF16) {
-        if (D == 128) packed_kernel<128, ST3_PACKED_COLS><<<grid, 256, 0, st>>>(a);
-        else packed_kernel<64, ST3_PACKED_COLS><<<grid, 256, 0, st>>>(a);
+        if (D == 128) launch_packed<128>(a, grid, st);
+        else launch_packed<64>(a, grid, st);
     } else {
         if (D == 128) packed_f32_kernel<128><<<grid, 256, 0, st>>>(a);
         else packed_f32_kernel<64><<<grid, 256, 0, st>>>(a);

@@ -159,6 +159,36 @@ def test_later_keys_do_not_leak():
         assert torch.equal(a[:min(clean, at)], b[:min(clean, at)])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens, H, Hk, d", [([40], 4, 1, 128), ([5, 300, 33], 8, 8, 64), ([100, 31, 700], 12, 4, 128), ([300] * 9, 32, 32, 64)])
+def test_values_that_are_not_finite_reach_the_rows_that_see_them(lens, H, Hk, d, dtype):
+    """Infinities and NaN in single elements of V, in a row's own tile of keys and in earlier ones: 0 times them is no part of any sum."""
+    rng = np.random.default_rng(sum(lens))
+    T, dt = sum(lens), TORCH_DTYPE[dtype]
+    q, k, v = (torch.from_numpy(rand_values(rng, (T, h, d), dtype, 1.0)).to(DEV).to(dt) for h in (H, Hk, Hk))
+    bad = []
+    for j in rng.choice(T, 5, replace=False):
+        at = (int(j), int(rng.integers(Hk)), int(rng.integers(d)))
+        bad.append(at)
+        v[at] = float(rng.choice([np.inf, -np.inf, np.nan]))
+    shape = st3.gqa_shape(len(lens), H, Hk, d, st3.ST3_F32 if dtype == "f32" else st3.ST3_BF16)
+    cu = torch.tensor([0, *np.cumsum(lens)], dtype=torch.int32, device=DEV)
+    out = torch.empty((T, H, d), dtype=dt, device=DEV)
+    st3.st3_packed_attention(shape, q, k, v, cu, max(lens), out)
+    clean = torch.where(torch.isfinite(v), v, torch.zeros_like(v))
+    want, spread, _, worst = reference(q, k, clean, lens, 1.0 / np.sqrt(d), 0)
+    for j, kh, col in bad:
+        end = next(int(e) for e in cu[1:].tolist() if j < e)
+        for h in range(kh * (H // Hk), (kh + 1) * (H // Hk)):
+            want[j:end, h, col] += float(v[j, kh, col])     # (every weight of these logits is above 0)
+    got, odd = out.double(), ~torch.isfinite(want)
+    assert bool(odd.any()) and torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(got[odd].nan_to_num(nan=0.0), want[odd].nan_to_num(nan=0.0))
+    slack = fp32_slack(worst, d, max(lens))
+    room = spread * (slack + (2 * HALF if dtype == "bf16" else 0)) + want.abs() * (HALF if dtype == "bf16" else 0) + 1e-30
+    assert bool(((got - want).abs() <= room)[~odd].all())
+
+
 def test_lengths_that_lie_are_cut():
     """cu_len past the rows that exist, or a sequence longer than the bound: what exists is attended, nothing else is touched."""
     rng = np.random.default_rng(13)
