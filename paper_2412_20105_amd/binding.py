@@ -269,15 +269,15 @@ _DTYPE_OF_CODE = {ST3_F32: torch.float32, ST3_BF16: torch.bfloat16}
 
 def _rows(shape: GqaShape, t: torch.Tensor, heads: int, total: int) -> Rows:
     """t [total, heads, d] of the shape's element type, as the library takes it (the caller keeps t alive)."""
-    if tuple(t.shape) != (total, heads, shape.head_dim):
-        raise ValueError(f"rows {tuple(t.shape)}: ({total}, {heads}, {shape.head_dim}) expected")
+    d = shape.head_dim
+    if t.shape != (total, heads, d):
+        raise ValueError(f"rows {tuple(t.shape)}: ({total}, {heads}, {d}) expected")
     if t.dtype != _DTYPE_OF_CODE.get(shape.dtype) or not t.is_cuda:
         raise TypeError(f"rows of {t.dtype} on {t.device}: the shape says {_DTYPE_OF_CODE.get(shape.dtype)}, on the device")
     st, sh, sc = t.stride()
     if sc != 1 and t.numel():
         raise ValueError("the elements of a row follow each other")
     # (a dimension of one element has any stride)
-    d = shape.head_dim
     if heads == 1:
         sh = d
     if total <= 1:
@@ -297,10 +297,11 @@ def _scores(shape: GqaShape, t: Optional[torch.Tensor], what: str, width: int, d
         return None, 0, 0
     if t.dtype != dtype or not t.is_cuda:
         raise TypeError(f"{what}: {dtype} on the device expected, {t.dtype} on {t.device} given")
-    if t.dim() != 3 or t.shape[0] != shape.batch or t.shape[1] != shape.kv_heads or t.shape[2] < width or (t.stride(2) != 1 and t.shape[2] > 1):
-        raise ValueError(f"{what}: [{shape.batch}, {shape.kv_heads}, {width} or more] expected, entries side by side; {tuple(t.shape)} given")
-    sb, sh = t.stride(0), t.stride(1)
-    if shape.kv_heads == 1:
+    size, steps, hk = t.shape, t.stride(), shape.kv_heads
+    if len(size) != 3 or size[0] != shape.batch or size[1] != hk or size[2] < width or (steps[2] != 1 and size[2] > 1):
+        raise ValueError(f"{what}: [{shape.batch}, {hk}, {width} or more] expected, entries side by side; {tuple(size)} given")
+    sb, sh, _ = steps
+    if hk == 1:
         sh = max(sh, width)
     return t.data_ptr(), sb, sh
 
