@@ -1,14 +1,15 @@
 // Attention of single tokens over a cache of 8-bit blocks, with grouped heads, appended rows and accumulated weights.
 //
-// A workgroup of four waves takes a chunk of the blocks of one (sequence, key head); a wave takes a block of 64 keys at a time, with
-// v_mfma_f32_16x16x32_bf16 (A: lane (c, g) holds A[c][8g..8g+7], B: B[8g..8g+7][c], C: C[4g..4g+3][c]); the group's query heads are the columns
-// (up to 16; a larger group is several workgroups).  8-bit codes are at most 8 significant bits: exact in bf16, so the products are exact and the block's
-// scale multiplies the finished sums.
-//   S^T = K Q^T    product t of four: row 4g'+i of A is key 16 g' + 4 t + i, so that lane (c, g) of C ends with keys 16 g .. 16 g + 15 of query c.  A lane
-//                  reads 16 codes of its row at once: columns 64 x + 16 g .. + 15, contraction steps 2 x and 2 x + 1.
-//   O^T = V^T P^T  the lane's 16 keys are the contraction slots 8g..8g+7 of two steps: P^T is where S^T left it, and V^T, whose rows lie in memory, is
-//                  read 16 codes at a time too.
-// No value crosses lanes but the maximum.  Bound by memory: 256 bytes a key and key head at d = 128 against some 25 cycles of a SIMD.
+// A workgroup of four or twelve waves takes a chunk of the blocks of one (sequence, key head), or the whole strip; a wave takes a block of 64 keys at a time, with
+// v_mfma_f32_16x16x32_bf16 (A: lane (c, g) holds A[c][8g..8g+7], B: B[8g..8g+7][c], C: C[4g..4g+3][c]); the group's query heads are the
+// columns (up to 16; a larger group is several workgroups).  8-bit codes have at most 8 significant bits: exact in bf16, so the products are exact,
+// and the block's scale multiplies the finished sums.
+//   S^T = K Q^T    product t of four: row 4g'+i of A is key 16 g' + 4 t + i, so that lane (c, g) of C ends with keys 16 g .. 16 g + 15 of query c.
+//                  A lane reads 16 codes of its row at once: columns 64 x + 16 g .. + 15, contraction steps 2 x and 2 x + 1.
+//   O^T = V^T P^T  the lane's 16 keys are the contraction slots 8g..8g+7 of two steps: P^T is where S^T left it, and V^T, whose rows lie in
+//                  memory, is read 16 codes at a time too.  P is two bf16 terms (16 significant bits: what is left out is 2^-17 of a weight at most).
+// No value crosses lanes but the maximum.  Bound by memory: K goes straight to LDS, a block ahead, V into registers.  2 sequences of 70000 and
+// 131072 rows, 32 heads over 8 of 128: 489 MB in 107 us, 4.6 TB/s (a large copy: 5.0); 32 of 611 to 3136 rows, 114 MB in 30 us.
 #include <algorithm>
 
 #include "st3_block.h"
@@ -32,7 +33,6 @@ struct BlockDecodeArgs {
     float* logits;                      // [B][H][logit_stride], in the log2 domain
     int64_t logit_stride;
 };
-
 
 // Blocks that hold rows to attend (the last one may be the tail).
 __device__ __forceinline__ int units_of(int n, bool fresh) { return n / kBlk + (n % kBlk + (fresh ? 1 : 0) > 0 ? 1 : 0); }
@@ -481,7 +481,7 @@ __global__ __launch_bounds__(kFinishThreads) void block_finish_kernel(BlockDecod
 //   320 strips of 11 to 20 blocks 20.6 us, with 12 waves 24.2.
 //   Chunks for about three workgroups on a unit; where logits are kept, no longer than leaves room for three in LDS: 16 strips of 1100 to 2049 blocks, 20 blocks (20 KB) 107 us,
 //   10 blocks 116, 40 blocks 109; 512 / 768 / 1536 workgroups without logits 79.4 / 81.2 / 89.0.
-struct Cut { int waves, chunk; };
+struct Cut { int waves, chunk, most; };      // most: chunks of a strip, at any length up to this one
 constexpr int kWholeStrips = 192, kShortUnits = 20, kManyStrips = 256, kStageBytes = 20 << 10, kChunkWgs = 768;
 
 template <int D>
@@ -491,10 +491,13 @@ inline Cut cut_of(int B, int Hk, int G, int max_len, bool scored) {
     const int64_t units = max_len / kBlk + 1, strips = (int64_t)B * Hk * QG;
     const int waves = strips > kManyStrips ? 4 : 12;
     const bool fits = units + 2 <= waves * kWave && (!scored || (QG == 1 && attend_lds<D>(waves, cols, units * kBlk) <= kLds));
-    if (fits && (strips >= kWholeStrips || units <= kShortUnits)) return Cut{waves, 0};
-    int64_t chunk = std::max<int64_t>(4, (units * strips + kChunkWgs - 1) / kChunkWgs);
-    if (scored) chunk = std::min<int64_t>(chunk, std::max<int64_t>(8, kStageBytes / (cols * kBlk * (int)sizeof(float))));
-    return Cut{4, (int)std::min<int64_t>({chunk, units, 4 * kWave - 2})};
+    if (fits && (strips >= kWholeStrips || units <= kShortUnits)) return Cut{waves, 0, 0};
+    constexpr int kLeast = 4;
+    int64_t top = 4 * kWave - 2;
+    if (scored) top = std::min<int64_t>(top, std::max<int64_t>(8, kStageBytes / (cols * kBlk * (int)sizeof(float))));
+    const int64_t chunk = std::min<int64_t>({std::max<int64_t>(kLeast, (units * strips + kChunkWgs - 1) / kChunkWgs), top, units});
+    const int64_t most = std::max<int64_t>(std::min<int64_t>((units + kLeast - 1) / kLeast, (kChunkWgs + strips - 1) / strips), (units + top - 1) / top);
+    return Cut{4, (int)chunk, (int)most};
 }
 inline Cut cut_of(const st3_gqa_shape* s, int max_len, bool scored) {
     const int G = s->heads / s->kv_heads;
@@ -511,9 +514,9 @@ inline BlockWs block_ws(const st3_gqa_shape* s, int max_len, bool scored) {
     w.nsplit = (int)((units + cut.chunk - 1) / cut.chunk);
     w.logit_stride = units * kBlk;
     const size_t BH = (size_t)s->batch * s->heads;
-    size_t off = 0;
-    w.part_o = off;  off = align_up(off + BH * w.nsplit * s->head_dim * sizeof(float), 256);
-    w.part_ml = off; off = align_up(off + BH * w.nsplit * 2 * sizeof(float), 256);
+    size_t off = 0;                     // (room for cut.most chunks: shorter lengths may be cut into more, and what is enough here is enough for them)
+    w.part_o = off;  off = align_up(off + BH * cut.most * s->head_dim * sizeof(float), 256);
+    w.part_ml = off; off = align_up(off + BH * cut.most * 2 * sizeof(float), 256);
     w.logits = off;  if (scored) off = align_up(off + BH * w.logit_stride * sizeof(float), 256);
     w.total = off;
     return w;

@@ -201,3 +201,11 @@ def test_binding_refuses_what_the_library_cannot_see():
     with pytest.raises(ValueError):
         st3.block_cache(*(torch.zeros(1, 2, 32, 64, dtype=torch.int8) for _ in range(2)), *(torch.zeros(1, 2) for _ in range(2)),
                         *(torch.zeros(2, 2, 64, 64) for _ in range(2)), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("batch,heads,kv_heads,dim", [(1, 32, 8, 128), (4, 32, 8, 128), (2, 40, 40, 128), (8, 16, 1, 64), (32, 32, 8, 128), (3, 48, 2, 64)])
+def test_workspace_for_the_longest_is_enough_for_every_shorter_cache(batch, heads, kv_heads, dim):
+    shape = st3.gqa_shape(batch, heads, kv_heads, dim)
+    sizes = [st3.st3_block_workspace_bytes(shape, n) for n in [*range(0, 70000, 37), *range(63, 20000, 64)]]
+    by_length = [s for _, s in sorted(zip([*range(0, 70000, 37), *range(63, 20000, 64)], sizes))]
+    assert by_length == sorted(by_length)
