@@ -209,3 +209,12 @@ def test_workspace_for_the_longest_is_enough_for_every_shorter_cache(batch, head
     sizes = [st3.st3_block_workspace_bytes(shape, n) for n in [*range(0, 70000, 37), *range(63, 20000, 64)]]
     by_length = [s for _, s in sorted(zip([*range(0, 70000, 37), *range(63, 20000, 64)], sizes))]
     assert by_length == sorted(by_length)
+
+
+@pytest.mark.parametrize("change", [dict(layers=0), dict(budget=0), dict(budget=256), dict(n_sink=-1), dict(n_sink=100, n_recent=29), dict(window=0), dict(code=7)])
+def test_generation_refuses_before_it_allocates(change):
+    from paper_2412_20105_amd.block_pipeline import BlockGeneration
+
+    good = dict(layers=2, heads=8, kv_heads=2, head_dim=128, batch=2, capacity=256, budget=128, n_sink=4, n_recent=64, window=32)
+    with pytest.raises(ValueError):
+        BlockGeneration(**{**good, **change})
