@@ -100,9 +100,9 @@ struct Divider {
         return !(x == x) ? if_nan : scale > 0.f ? __fdiv_rn(fminf(fmaxf(x, -top), top), scale) : copysignf(0.f, x);
     }
     __device__ __forceinline__ float operator()(float x) const {
-        float q = x * inv;
-        q = fmaf(fmaf(-q, by, x), inv, q);
-        return fmaf(fmaf(-q, by, x), inv, q);
+        float q = x * inv;                                  // (with the remainder's sign this way round zeros keep theirs)
+        q = fmaf(-fmaf(q, by, -x), inv, q);
+        return fmaf(-fmaf(q, by, -x), inv, q);
     }
 };
 
@@ -136,6 +136,9 @@ template <> struct BlockCode<ST3_BLOCK_INT8> {
         return lo | hi;
     }
     __device__ static __forceinline__ float value(uint32_t byte) { return (float)(int8_t)byte; }
+    __device__ static __forceinline__ f32x4 value4(uint32_t w) {
+        return f32x4{(float)(int8_t)w, (float)(int8_t)(w >> 8), (float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24)};
+    }
     // four codes as four bf16 (exact: at most seven bits)
     __device__ static __forceinline__ uint2 to_bf16(uint32_t w) {
         asm("" : "+v"(w));              // (opaque: else the bytes are taken apart where the word is loaded, and wait in four registers for one)
@@ -148,14 +151,15 @@ template <> struct BlockCode<ST3_BLOCK_E4M3> {
     static constexpr float kUnit = 1.0f / 448.0f;
     __device__ static __forceinline__ float nan_code() { return __uint_as_float(0x7fc00000u); }
     __device__ static __forceinline__ uint32_t code4(const float* x, const Divider& d) {
-        float q[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = copysignf(d(x[i]), x[i]);        // (zeros keep their sign)
-        uint32_t w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
+        uint32_t w = __builtin_amdgcn_cvt_pk_fp8_f32(d(x[0]), d(x[1]), 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(d(x[2]), d(x[3]), w, true);
         return w;
     }
     __device__ static __forceinline__ float value(uint32_t byte) { return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0); }
+    __device__ static __forceinline__ f32x4 value4(uint32_t w) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+        return f32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
     __device__ static __forceinline__ uint2 to_bf16(uint32_t w) {
         const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
         return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));

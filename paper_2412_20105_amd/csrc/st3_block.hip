@@ -393,12 +393,19 @@ __device__ __forceinline__ void move_block(const EvictBlockArgs& a, int kh, int 
                 load_bf16<W>(a.from.k_tail + strip * kPage + row[r] * D + my.col, raw[r]);
             }
         }
+        if (__ballot(blk_l < 0) == 0) {                     // (in all waves alike; nearly every block)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int e = 0; e < W; ++e)
-                v[r][e] = blk[r] >= 0 ? F::value(raw[r][e / 4] >> (8 * (e & 3)) & 0xffu) * scale[r]
-                                      : __uint_as_float((raw[r][e / 2] >> (16 * (e & 1))) << 16);
+                for (int e = 0; e < W; ++e) v[r][e] = F::value4(raw[r][e / 4])[e & 3] * scale[r];
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < W; ++e)
+                    v[r][e] = blk[r] >= 0 ? F::value(raw[r][e / 4] >> (8 * (e & 3)) & 0xffu) * scale[r]
+                                          : __uint_as_float((raw[r][e / 2] >> (16 * (e & 1))) << 16);
+        }
     }
     if (whole) write_block<D, CODE, COLUMNS>(v, a.to, to_at, sm, tid);
     else write_tail<D, COLUMNS>([&](int r, int e) { return (uint16_t)f32_to_bf16_bits(v[r][e]); }, a.to, strip, count - first, tid);
