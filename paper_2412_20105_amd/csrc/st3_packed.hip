@@ -634,17 +634,35 @@ void launch_score(const PackedArgs& a, hipStream_t st) {
     else packed_score_kernel<T, D, false><<<dim3(a.Hk, (unsigned)((tiles + 3) / 4), a.B), 256, 0, st>>>(a);
 }
 
-// Few workgroups with long walks leave most of the chip's waves idle: then two groups of waves share a walk.  In us, one group / two: 1 x 500 tokens of 8 key heads
-// (128 workgroups) 24 / 22, 1 x 1000 (256) 38 / 31, 2 x 700 (360) 31 / 29.5, 1 x 2000 (504) 64 / 55; 1 x 200 17.0 / 17.6, 3 x 400 (320) 24 / 26, 4 x 700
-// (704) 37 / 49.  (Three groups: within 1 us of two, but 1 x 300 20 for 18.)
-constexpr int kCols = 2, kFewWorkgroups = 512, kLongWalk = 448;
+// How a launch is cut, by the number of row tiles of 64 over all key heads and by the longest prompt.  Few tiles: one column of rows a wave, twice the workgroups, each with the shorter step; and
+// where the walk over the keys is long, two groups of waves share it.  us with 1 / 1 shared / 2 / 2 shared columns:
+//   tiles  104   1 x 200   14.1  14.2  17.0  17.5          704   2 x 700   26.7  34.7  31.1  29.7
+//          152   1 x 300   15.0  14.3  18.4  17.9          752   1 x 1500  43.2  50.3  50.6  39.5
+//          256   1 x 500   20.1  17.6  24.3  22.1         1000   1 x 2000  57.7  72.5  63.9  55.6
+//          504   1 x 1000  31.6  29.4  38.0  31.0         1408   4 x 700   39.9  62.6  36.9  49.6
+//          512   8 x 120   14.5  20.1  16.5  17.5         1568   1 x 3136   109   151   104   114
+//          600   3 x 400   20.9  28.6  23.8  26.2         1920   4 x 739   59.5  89.1  50.7  70.3
+//   (32 heads over 8 of 128, the last 40 over 40.  Three groups: within 1 us of two.)
+struct PackedCut { int cols, split; };
+inline PackedCut packed_cut(int64_t tiles64, int max_len) {
+    if (tiles64 <= 512) return PackedCut{1, max_len > 256 ? 2 : 1};
+    if (tiles64 <= 1024) return max_len > 1024 ? PackedCut{2, 2} : PackedCut{1, 1};
+    return PackedCut{2, 1};
+}
+// No more row tiles than this, whatever the lengths are: each sequence has one that is not full.
+inline int64_t packed_tiles(const st3_gqa_shape* s, int total, int max_len, int rows) {
+    const int G = s->heads / s->kv_heads;
+    return std::min((int64_t)total * G / rows + std::min(s->batch, total), ((int64_t)max_len * G + rows - 1) / rows * s->batch);
+}
 // Row tiles dealt over the prompts at a launch's end, as workgroups: all the tiles of 32 x 739 tokens, 40 key heads, in order of their length 499 us, no dealing 368, 768 to 3000 364 to
 // 380; 4 x 700 42 without, 36 with; 8 x 3136, 32 key heads, 809 / 722 / 710 at 1536.
 constexpr int kSpread = 1536;
 template <int D>
-void launch_packed(const PackedArgs& a, unsigned grid, hipStream_t st) {
-    if (grid <= kFewWorkgroups && a.max_len > kLongWalk) packed_kernel<D, kCols, 2><<<grid, 512, 0, st>>>(a);
-    else packed_kernel<D, kCols, 1><<<grid, 256, 0, st>>>(a);
+void launch_packed(const PackedArgs& a, PackedCut cut, unsigned grid, hipStream_t st) {
+    if (cut.cols == 1 && cut.split == 1) packed_kernel<D, 1, 1><<<grid, 256, 0, st>>>(a);
+    else if (cut.cols == 1) packed_kernel<D, 1, 2><<<grid, 512, 0, st>>>(a);
+    else if (cut.split == 2) packed_kernel<D, 2, 2><<<grid, 512, 0, st>>>(a);
+    else packed_kernel<D, 2, 1><<<grid, 256, 0, st>>>(a);
 }
 
 }  // namespace
@@ -679,17 +697,17 @@ extern "C" st3_status st3_packed_attention(const st3_gqa_shape* shape, const st3
     PackedArgs a{q->data, k->data, v->data, out->data, q->stride_t, q->stride_h, k->stride_t, k->stride_h, v->stride_t, v->stride_h, out->stride_t,
                  out->stride_h, cu_len, shape->batch, total, max_len, H, Hk, G, 0, 0, gqa_scale_log2(shape), score, score_stride_b, score_stride_h,
                  score ? reinterpret_cast<float2*>(workspace) : nullptr, window};
-    const int rows = shape->dtype == ST3_BF16 ? 64 * kCols : 16;
+    const PackedCut cut = packed_cut(packed_tiles(shape, total, max_len, 64) * Hk, max_len);
+    const int rows = shape->dtype == ST3_BF16 ? 64 * cut.cols : 16;
     a.levels = (int)(((int64_t)max_len * G + rows - 1) / rows);
     a.spread = (kSpread + Hk - 1) / Hk;
-    // no more tiles than this, whatever the lengths are: each sequence has one that is not full
-    const int64_t tiles = std::min((int64_t)total * G / rows + std::min(shape->batch, total), (int64_t)a.levels * shape->batch);
+    const int64_t tiles = packed_tiles(shape, total, max_len, rows);
     if (tiles * Hk > 0x7fffffff) return ST3_ERR_UNSUPPORTED;
     if (score && (max_len + 63) / 64 > 65535) return ST3_ERR_UNSUPPORTED;
     const unsigned grid = (unsigned)(tiles * Hk);
     if (shape->dtype == ST3_BF16) {
-        if (D == 128) launch_packed<128>(a, grid, st);
-        else launch_packed<64>(a, grid, st);
+        if (D == 128) launch_packed<128>(a, cut, grid, st);
+        else launch_packed<64>(a, cut, grid, st);
     } else {
         if (D == 128) packed_f32_kernel<128><<<grid, 256, 0, st>>>(a);
         else packed_f32_kernel<64><<<grid, 256, 0, st>>>(a);

@@ -109,6 +109,13 @@ def test_long(lens, H, Hk):
     run(np.random.default_rng(sum(lens)), lens, H, Hk, 128, "bf16", 33)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[130, 17], [300], [257, 255], [1100], [1025, 3], [400] * 3, [600] * 4], ids=lambda x: "-".join(map(str, x)))
+def test_few_and_many_row_tiles(lens, d):
+    """Short and long walks over the keys with few row tiles, more, and many: however a launch is cut."""
+    run(np.random.default_rng(sum(lens) + d), lens, 32, 8, d, "bf16", 21)
+
+
 @pytest.mark.parametrize("seed", range(24))
 def test_random_batches(seed):
     rng = np.random.default_rng(1000 + seed)
