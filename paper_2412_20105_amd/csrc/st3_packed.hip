@@ -4,6 +4,7 @@
 // so a group's queries meet a K and V tile together, any G fills the MFMA's columns, and a tile of rows spans few positions (the
 // causal edge wastes little).  A workgroup takes kRows such rows of a pair and walks the key tiles up to its last position.
 #include <algorithm>
+#include <type_traits>
 #include <utility>
 
 #include "st3_block.h"
@@ -78,21 +79,24 @@ __device__ __forceinline__ bool place(const PackedArgs& a, int lane, int& b, int
         return false;
     }
     const int mine = tiles_of(lane);
-    int before = 0;                     // tiles of the sequences in front of this one, longest first
-    for (int i = 0; i < a.B; ++i) {
-        const int other = __builtin_amdgcn_readlane(mine, i);
-        before += other > mine || (other == mine && i < lane) ? other : 0;
-    }
     const int total = wave_total(mine);
     if (x >= total) return false;
-    // the sequences in front of `apart` have their tiles to themselves
-    const int end = before + mine, apart = wave_most(mine > 0 && end <= total - a.spread ? end : 0);
-    if (x < apart) {
-        const int at = __ffsll((unsigned long long)__ballot(mine > 0 && before <= x && x < end)) - 1;
-        return found(at, __builtin_amdgcn_readlane(end, at) - 1 - x);
+    int dealt = mine;
+    if (total > a.spread) {
+        int before = 0;                 // tiles of the sequences in front of this one, longest first
+        for (int i = 0; i < a.B; ++i) {
+            const int other = __builtin_amdgcn_readlane(mine, i);
+            before += other > mine || (other == mine && i < lane) ? other : 0;
+        }
+        // the sequences in front of `apart` have their tiles to themselves
+        const int end = before + mine, apart = wave_most(mine > 0 && end <= total - a.spread ? end : 0);
+        if (x < apart) {
+            const int at = __ffsll((unsigned long long)__ballot(mine > 0 && before <= x && x < end)) - 1;
+            return found(at, __builtin_amdgcn_readlane(end, at) - 1 - x);
+        }
+        x -= apart;
+        dealt = before >= apart ? mine : 0;
     }
-    x -= apart;
-    const int dealt = before >= apart ? mine : 0;
     auto from = [&](int t) { return wave_total(max(0, dealt - t)); };      // tiles of index t or more
     int lo = 0, hi = a.levels, above = 0;                                  // from(lo) > x >= from(hi)
     while (hi - lo > 1) {
@@ -488,52 +492,57 @@ __global__ __launch_bounds__(256) void packed_f32_kernel(PackedArgs a) {
             for (int dt = 0; dt < DT; ++dt) vf[dt][i] = row[16 * dt];
         }
     };
-    int t = wave;
-    if (t < tiles) { load_k(t); load_v(t); }
+    if (wave < tiles) { load_k(wave); load_v(wave); }
     qf.load(reinterpret_cast<const float*>(a.q) + (int64_t)(sq.start + pos) * a.q_st + (int64_t)head * a.q_sh, g);
     f32x4 o[DT];
+    float m, l;
+    // (CAREFUL as in packed_step)
+    auto walk = [&](auto careful) {
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -3.402823466e38f, l = 0.f;
-    for (; t < tiles; t += 4) {
-        f32x4 s = kf.dot(qf) * a.scale_l2;
-        if (t + 4 < tiles) load_k(t + 4);
+        for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m = -3.402823466e38f; l = 0.f;
+        for (int t = wave; t < tiles; t += 4) {
+            f32x4 s = kf.dot(qf) * a.scale_l2;
+            if (t + 4 < tiles) load_k(t + 4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (16 * t + 4 * g + i > pos) s[i] = -INFINITY;
-        const float mx = fmaxf(m, wave_max_from<16>(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
-        const float alpha = exp2_fast(m - mx);
-        m = mx;
-        l *= alpha;
-        float p[4];
+            for (int i = 0; i < 4; ++i)
+                if (16 * t + 4 * g + i > pos) s[i] = -INFINITY;
+            const float mx = fmaxf(m, wave_max_from<16>(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
+            const float alpha = exp2_fast(m - mx);
+            m = mx;
+            l *= alpha;
+            float p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { p[i] = exp2_fast(s[i] - m); l += p[i]; }
-        // at the edge: infinities and NaN in V of keys that a row does not see stay out of it, row by row (a weight of 0 does not silence them)
-        float odd = 0.f;
-        if (16 * t + 15 > r0 / a.G) {
+            for (int i = 0; i < 4; ++i) { p[i] = exp2_fast(s[i] - m); l += p[i]; }
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
+            for (int dt = 0; dt < DT; ++dt) {
+                o[dt] *= alpha;
+                if constexpr (decltype(careful)::value) {
+                    for (int x = 0; x < 16; ++x) {
+                        const int seen = __builtin_amdgcn_readlane(pos, x) - 16 * t - 4 * g;
+                        f32x4 y = o[dt];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) odd = fmaf(vf[dt][i], 0.f, odd);
-        }
-        const bool careful = __any(odd != 0.f);
+                        for (int i = 0; i < 4; ++i) y = __builtin_amdgcn_mfma_f32_16x16x4f32(i <= seen ? vf[dt][i] : 0.f, p[i], y, 0, 0, 0);
+                        o[dt] = c == x ? y : o[dt];
+                    }
+                } else {
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-            o[dt] *= alpha;
-            if (careful) {
-                for (int x = 0; x < 16; ++x) {
-                    const int seen = __builtin_amdgcn_readlane(pos, x) - 16 * t - 4 * g;
-                    f32x4 y = o[dt];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) y = __builtin_amdgcn_mfma_f32_16x16x4f32(i <= seen ? vf[dt][i] : 0.f, p[i], y, 0, 0, 0);
-                    o[dt] = c == x ? y : o[dt];
+                    for (int i = 0; i < 4; ++i) o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[dt][i], p[i], o[dt], 0, 0, 0);
                 }
-                continue;
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[dt][i], p[i], o[dt], 0, 0, 0);
+            if (t + 4 < tiles) load_v(t + 4);
         }
-        if (t + 4 < tiles) load_v(t + 4);
+    };
+    walk(std::false_type{});
+    float odd = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) odd = fmaf(o[dt][i], 0.f, odd);
+    if (__any(odd != 0.f)) {                                // not finite: V of keys that a row does not see?
+        load_k(wave);
+        load_v(wave);
+        walk(std::true_type{});
     }
     // ---- join the waves' parts (one without tiles has sum 0 at the lowest float) -------------------------------------------------
     l = wave_sum_from<16>(l);
