@@ -163,6 +163,10 @@ __global__ __launch_bounds__(WAVES * 64, 3) void block_attend_kernel(BlockDecode
             lo.w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
         }
     };
+    const int unit_l = unit_at(lane);
+    uint64_t left = __ballot(page_l >= 0 && unit_l < u_stop);          // the wave's positions whose blocks are to come
+    if (left != 0) load_k(__builtin_amdgcn_readlane(page_l, __ffsll((unsigned long long)left) - 1));     // (on its way beside the tail)
+    __builtin_amdgcn_sched_barrier(0);
     // The rows in 16 bits, and the new one, 32 at a time (product t of two: row 4g'+i of A is key 8 g' + 4 t + i), by the first waves while the others have begun
     // with the blocks.
     if (wave < halves) {
@@ -225,15 +229,12 @@ __global__ __launch_bounds__(WAVES * 64, 3) void block_attend_kernel(BlockDecode
         }
     }
     auto lane_value = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
-    const int unit_l = unit_at(lane);
-    uint64_t left = __ballot(page_l >= 0 && unit_l < u_stop);
     for (uint64_t gone = __ballot(page_l < 0 && unit_l >= u_begin && unit_l < u_stop); gone != 0; gone &= gone - 1) {
         const f32x4 none = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, s[4] = {none, none, none, none};
         keep_logits(s, unit_at(__ffsll((unsigned long long)gone) - 1));
     }
     if (left != 0) {
         int i = __ffsll((unsigned long long)left) - 1;
-        load_k(__builtin_amdgcn_readlane(page_l, i));
         load_v(__builtin_amdgcn_readlane(page_l, i));
         while (true) {
             left &= left - 1;
