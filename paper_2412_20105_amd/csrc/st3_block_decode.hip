@@ -305,10 +305,13 @@ __global__ __launch_bounds__(WAVES * 64, 3) void block_attend_kernel(BlockDecode
     }
     // what the first rows have received so far, on its way while the waves' parts are joined
     constexpr int kAhead = 4;
-    float old[kAhead];
+    float old[kAhead] = {};
     if constexpr (WHOLE) {
+        if (scored && n > 0) {
+            const float* score = a.score + b * a.s_sb + kh * a.s_sh;
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) old[j] = scored && tid + j * kThr < n ? a.score[b * a.s_sb + kh * a.s_sh + tid + j * kThr] : 0.f;
+            for (int j = 0; j < kAhead; ++j) old[j] = score[min(tid + j * kThr, n - 1)];
+        }
     }
     // ---- the waves' parts ---------------------------------------------------------------------------------------------------------
     l = wave_sum_from<16>(l);
@@ -364,7 +367,7 @@ __global__ __launch_bounds__(WAVES * 64, 3) void block_attend_kernel(BlockDecode
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 const int key = tid + j * kThr;
-                if (key < rows) score[key] = old[j] + weight(key);
+                if (key < rows) score[key] = (key < n ? old[j] : 0.f) + weight(key);
             }
             for (int key = tid + kAhead * kThr; key < rows; key += kThr) score[key] = (key < n ? score[key] : 0.f) + weight(key);
         }
