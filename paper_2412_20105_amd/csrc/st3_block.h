@@ -85,9 +85,10 @@ __device__ __forceinline__ int page_of(const BlockPages& c, int b, int j) {
     return p >= 0 && p < c.n_pages ? p : -1;
 }
 
-// x / scale, correctly rounded, for many x and one scale: two corrections of x * (1 / scale) by the remainder, which a fused multiply-add gives exactly (Markstein).
-// That holds while nothing on the way leaves the normal range.  Else, and where a block holds what is not finite, x is divided with care first (`care`: the caller puts
-// careful(x) in x's place): an infinity counts as the largest finite magnitude, and the quotients are then "divided" by one.
+// x / scale, correctly rounded, for many x and one scale: two corrections of x * (1 / scale) by the remainder, which a fused multiply-add gives
+// exactly (Markstein). That holds while nothing on the way leaves the normal range.  Else, and where a block holds what is not finite, x is divided
+// with care first (`care`: the caller puts careful(x) in x's place): an infinity counts as the largest finite magnitude, and the quotients are then
+// "divided" by one.
 struct Divider {
     float by, inv, scale, top;
     bool care;

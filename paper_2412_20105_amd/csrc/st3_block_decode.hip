@@ -1,7 +1,7 @@
 // Attention of single tokens over a cache of 8-bit blocks, with grouped heads, appended rows and accumulated weights.
 //
-// A workgroup of four or twelve waves takes a chunk of the blocks of one (sequence, key head), or the whole strip; a wave takes a block of 64 keys at a time, with
-// v_mfma_f32_16x16x32_bf16 (A: lane (c, g) holds A[c][8g..8g+7], B: B[8g..8g+7][c], C: C[4g..4g+3][c]); the group's query heads are the
+// A workgroup of four or twelve waves takes a chunk of the blocks of one (sequence, key head), or the whole strip; a wave takes a block of 64 keys at
+// a time, with v_mfma_f32_16x16x32_bf16 (A: lane (c, g) holds A[c][8g..8g+7], B: B[8g..8g+7][c], C: C[4g..4g+3][c]); the group's query heads are the
 // columns (up to 16; a larger group is several workgroups).  8-bit codes have at most 8 significant bits: exact in bf16, so the products are exact,
 // and the block's scale multiplies the finished sums.
 //   S^T = K Q^T    product t of four: row 4g'+i of A is key 16 g' + 4 t + i, so that lane (c, g) of C ends with keys 16 g .. 16 g + 15 of query c.
@@ -9,7 +9,7 @@
 //   O^T = V^T P^T  the lane's 16 keys are the contraction slots 8g..8g+7 of two steps: P^T is where S^T left it, and V^T, whose rows lie in
 //                  memory, is read 16 codes at a time too.  P is two bf16 terms (16 significant bits: what is left out is 2^-17 of a weight at most).
 // No value crosses lanes but the maximum.  Bound by memory: K goes straight to LDS, a block ahead, V into registers.  2 sequences of 70000 and
-// 131072 rows, 32 heads over 8 of 128: 489 MB in 107 us, 4.6 TB/s (a large copy: 5.0); 32 of 611 to 3136 rows, 114 MB in 30 us.
+// 131072 rows, 32 heads over 8 of 128: 489 MB in 107 us, 4.6 TB/s (a large copy: 5.0); 32 of 611 to 3136 rows, 114 MB in 28.5 us.
 #include <algorithm>
 
 #include "st3_block.h"
@@ -44,8 +44,8 @@ template <int D> struct KeyTile {
     __device__ static __forceinline__ int swz(int row) { return D == 128 ? ((row >> 4 & 3) << 1 | (row >> 1 & 1)) : row >> 4 & 3; }
 };
 
-// Dynamic LDS: the waves' K blocks, and where those were the waves' outputs [waves][columns][D + 4], their maxima and sums [2][waves][16], the heads' [2][16], and in a launch of whole strips the
-// logits [columns][rows].
+// Dynamic LDS: the waves' K blocks, and where those were the waves' outputs [waves][columns][D + 4], their maxima and sums [2][waves][16], the heads'
+// [2][16], and in a launch of whole strips the logits [columns][rows].
 template <int D>
 inline size_t attend_lds(int waves, int cols, int64_t staged_rows) {
     const size_t keys = (size_t)waves * kBlk * D, parts = sizeof(float) * waves * cols * (D + 4);
@@ -96,9 +96,9 @@ __global__ __launch_bounds__(WAVES * 64, 3) void block_attend_kernel(BlockDecode
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) vr[dt] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, v_lane, 16 * dt * kBlk, kStream);
     };
-    // A wave's work is at the positions wave, wave + WAVES, ...: first the halves of the tail, where it belongs to the chunk, then the chunk's blocks in order.  Lane i has
-    // the page and the scales of the block at the wave's i-th position (a chunk has no more than 64 of them; fetched one by one they had to be waited for, and with them every load in
-    // flight).  A block without a page is passed over: whatever lies elsewhere is not read.
+    // A wave's work is at the positions wave, wave + WAVES, ...: first the halves of the tail, where it belongs to the chunk, then the chunk's blocks
+    // in order.  Lane i has the page and the scales of the block at the wave's i-th position (a chunk has no more than 64 of them; fetched one by one
+    // they had to be waited for, and with them every load in flight).  A block without a page is passed over: whatever lies elsewhere is not read.
     const int u_most = WHOLE ? a.max_len / kBlk : min((ch + 1) * a.chunk, a.max_len / kBlk);       // (known before the length has arrived)
     const int u_stop = min(u_end, blocks);
     const bool with_tail = units > blocks && blocks >= u_begin && blocks < u_end;
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(WAVES * 64, 3) void block_attend_kernel(BlockDecode
     uint64_t left = __ballot(page_l >= 0 && unit_l < u_stop);          // the wave's positions whose blocks are to come
     if (left != 0) load_k(__builtin_amdgcn_readlane(page_l, __ffsll((unsigned long long)left) - 1));     // (on its way beside the tail)
     __builtin_amdgcn_sched_barrier(0);
-    // The rows in 16 bits, and the new one, 32 at a time (product t of two: row 4g'+i of A is key 8 g' + 4 t + i), by the first waves while the others have begun
-    // with the blocks.
+    // The rows in 16 bits, and the new one, 32 at a time (product t of two: row 4g'+i of A is key 8 g' + 4 t + i), by the first waves while the
+    // others have begun with the blocks.
     if (wave < halves) {
         const int r = n % kBlk, first = 32 * wave;          // rows in the tail, the new row's place; the half's first row
         const int64_t at = ((int64_t)b * a.Hk + kh) * kBlk * D;
@@ -478,13 +478,13 @@ __global__ __launch_bounds__(kFinishThreads) void block_finish_kernel(BlockDecod
 }
 
 // How a call is cut: waves of a workgroup, blocks of a chunk (0: whole strips, one launch).
-//   Whole strips while there are enough to fill the card, or while they are so short that the second launch of a cut costs more than it brings: us a call,
-//   whole / cut, 64 strips of 32 blocks 19.0 / 14.6, 8 strips of 12 blocks 10.2 / 13.4, 256 strips of 10 to 49 blocks 30.3 / 38.8 (with their logits in LDS, up to what
-//   there is of it).
-//   Workgroups of 12 waves, one on a compute unit, where strips are no more than compute units: 256 strips 30.3 us, with 4 waves 34; else of 4 waves, three on a unit:
-//   320 strips of 11 to 20 blocks 20.6 us, with 12 waves 24.2.
-//   Chunks for about three workgroups on a unit; where logits are kept, no longer than leaves room for three in LDS: 16 strips of 1100 to 2049 blocks, 20 blocks (20 KB) 107 us,
-//   10 blocks 116, 40 blocks 109; 512 / 768 / 1536 workgroups without logits 79.4 / 81.2 / 89.0.
+//   Whole strips while there are enough to fill the card, or while they are so short that the second launch of a cut costs more than it
+//   brings (with their logits in LDS, up to what there is of it).  us a call, whole / cut: 64 strips of 32 blocks 18.3 / 14.2, 8 strips of 12 blocks
+//   10.0 / 12.6, 256 strips of 10 to 49 blocks 28.5 / 36.9.
+//   Workgroups of 12 waves, one on a compute unit, where strips are no more than compute units, else of 4 waves, three on a unit.  12 / 4: 256 strips
+//   28.5 / 31.7, 320 strips of 11 to 20 blocks 22.6 / 19.2.
+//   Chunks for about three workgroups on a unit; where logits are kept, no longer than leaves room for three in LDS.  16 strips of 1100 to 2049 blocks: 20
+//   blocks (20 KB) 107, 10 blocks 115, 40 blocks 109; 512 / 768 / 1536 workgroups without logits 79.9 / 81.4 / 89.1.
 struct Cut { int waves, chunk, most; };      // most: chunks of a strip, at any length up to this one
 constexpr int kWholeStrips = 192, kShortUnits = 20, kManyStrips = 256, kStageBytes = 20 << 10, kChunkWgs = 768;
 

@@ -31,7 +31,8 @@ __device__ __forceinline__ Seq sequence(const PackedArgs& a, int b) {
     return Seq{s, min(e - s, a.max_len)};
 }
 
-// Inclusive sum over the wave's lanes (DPP: row_shr 1, 2, 4, 8, row_bcast 15, 31); the sum, and the largest of values that are not negative, the same in every lane.
+// Inclusive sum over the wave's lanes (DPP: row_shr 1, 2, 4, 8, row_bcast 15, 31); the sum, and the largest of values that are not negative, the same
+// in every lane.
 __device__ __forceinline__ int wave_prefix(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
     x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
@@ -52,10 +53,11 @@ __device__ __forceinline__ int wave_most(int x) {
     return __builtin_amdgcn_readlane(x, 63);
 }
 
-// Workgroup -> (sequence, key head, row tile).  Key heads run fastest: workgroups go round-robin to the 8 XCDs, so with a multiple of 8 key heads a pair's K and V stay in
-// one XCD's L2, and a sequence's tiles follow each other, heaviest (last) first, longest sequences first, so that they are there when the next tile wants them.  A
-// tile costs in proportion to its index: the last sequences' tiles (a.spread of them, or so) are dealt together, heaviest first over all of them, so that the launch ends with its
-// shortest workgroups.  Lengths are known to the device only: every wave finds its place, a lane for each of up to 64 sequences; more keep their own order.
+// Workgroup -> (sequence, key head, row tile).  Key heads run fastest: workgroups go round-robin to the 8 XCDs, so with a multiple of 8 key heads a
+// pair's K and V stay in one XCD's L2, and a sequence's tiles follow each other, heaviest (last) first, longest sequences first, so that they are
+// there when the next tile wants them.  A tile costs in proportion to its index: the last sequences' tiles (a.spread of them, or so) are dealt
+// together, heaviest first over all of them, so that the launch ends with its shortest workgroups.  Lengths are known to the device only: every wave
+// finds its place, a lane for each of up to 64 sequences; more keep their own order.
 template <int ROWS>
 __device__ __forceinline__ bool place(const PackedArgs& a, int lane, int& b, int& kh, int& tile, Seq& sq) {
     kh = blockIdx.x % a.Hk;
@@ -270,10 +272,12 @@ __device__ __forceinline__ void load_tile(uint32_t lds, const uint16_t* K, const
     }
 }
 
-// A workgroup's four waves have 16 QC rows each and share the K and V tiles, which go straight from memory to LDS, two tiles ahead.  Bound by the matrix
-// instructions' power at long prompts: 21000 tokens of 32 heads over 8 of 128 in 1.66 ms, 1150 TF/s of the 1366 that a large product reaches, at
-// 1.7 GHz.  Two columns of rows leave registers for 3 waves a SIMD; three columns with 2 waves: 1.61 ms there, but 40 and 54 us for 36 and 50 at prompts of 700.
+// A workgroup's four waves have 16 QC rows each and share the K and V tiles, which go straight from memory to LDS, two tiles ahead.
 // SPLIT: as many groups of four waves take the same rows and every SPLIT-th tile, and join their sums in LDS at the end.
+// Bound by the matrix instructions' power at long prompts (clock 1.7 GHz): 21000 tokens of 32 heads over 8 of 128 in 1.67 ms, 1150 TF/s of the 1366
+// that a large product reaches; by a step's chain of products, maximum, exponentials and products at short ones: 1 us for 32 keys and 128 rows alone
+// on a unit. Two columns of rows leave registers for 3 waves a SIMD; three columns with 2 waves take 1.66 ms there, but 395 us for 368 at 32 x 739
+// tokens of 40 key heads.
 template <int D, int QC, int SPLIT>
 __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 3 : SPLIT) void packed_kernel(PackedArgs a) {
     using L = TileLayout<D, 32>;
@@ -324,8 +328,8 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 3 : SPLIT) void packed_ke
     if (part + SPLIT < nt) { issue(part + SPLIT, 1); wait_direct_loads_but<2 * L::NI>(); }
     else wait_direct_loads();
     __syncthreads();
-    // Tiles that every row of the workgroup sees whole come first, in a loop without conditions (with both kinds in one loop the accumulators were moved
-    // between the two forms' registers, and spilled); the few at the edge follow.
+    // Tiles that every row of the workgroup sees whole come first, in a loop without conditions (with both kinds in one loop the accumulators were
+    // moved between the two forms' registers, and spilled); the few at the edge follow.
     int t = part, slot = 0, next = 2;
     auto advance = [&]() {
         if (t + 2 * SPLIT < nt) { issue(t + 2 * SPLIT, next); wait_direct_loads_but<2 * L::NI>(); }
@@ -463,9 +467,9 @@ template <int D> struct RowFrag<float, D> {
 };
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// float32: the same rows on v_mfma_f32_16x16x4f32 (A: lane (c, g) holds A[c][g]).  A workgroup has 16 rows; its four waves take the key tiles of 16 in turn,
-// operands straight from memory, a wave's next tile on its way, and join their parts through LDS.  Bound by the latency of a tile's loads (600 rows of 300 keys, one
-// wave for 16 rows and all their keys, 22 us).
+// float32: the same rows on v_mfma_f32_16x16x4f32 (A: lane (c, g) holds A[c][g]).  A workgroup has 16 rows; its four waves take the key tiles of 16
+// in turn, operands straight from memory, a wave's next tile on its way, and join their parts through LDS.  Bound by the latency of a tile's loads
+// (600 rows of 300 keys, one wave for 16 rows and all their keys, 22 us).
 // ---------------------------------------------------------------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void packed_f32_kernel(PackedArgs a) {
@@ -569,9 +573,10 @@ __global__ __launch_bounds__(256) void packed_f32_kernel(PackedArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// score[b,kh,j] = sum over the rows of the window of exp2(logit - maximum) / sum.  The logits are formed again: a wave has 64 keys in registers and takes rows 16 at a time, the
-// next ones on their way; a lane adds up what its 16 keys get.  DEAL: the workgroup's four waves have the same keys and take the rows in turn, which is the shorter way where
-// workgroups are few; else they have 256 keys and all take all rows, which come from memory once for the four (64 rows of 4 heads, 21000 tokens: 48 us dealt).
+// score[b,kh,j] = sum over the rows of the window of exp2(logit - maximum) / sum.  The logits are formed again: a wave has 64 keys in registers and
+// takes rows 16 at a time, the next ones on their way; a lane adds up what its 16 keys get.  DEAL: the workgroup's four waves have the same keys and
+// take the rows in turn, which is the shorter way where workgroups are few; else they have 256 keys and all take all rows, which come from memory
+// once for the four (64 rows of 4 heads, 21000 tokens: 48 us dealt).
 // ---------------------------------------------------------------------------------------------------------------------------------
 template <typename T, int D, bool DEAL>
 __global__ __launch_bounds__(256) void packed_score_kernel(PackedArgs a) {
@@ -643,15 +648,16 @@ void launch_score(const PackedArgs& a, hipStream_t st) {
     else packed_score_kernel<T, D, false><<<dim3(a.Hk, (unsigned)((tiles + 3) / 4), a.B), 256, 0, st>>>(a);
 }
 
-// How a launch is cut, by the number of row tiles of 64 over all key heads and by the longest prompt.  Few tiles: one column of rows a wave, twice the workgroups, each with the shorter step; and
-// where the walk over the keys is long, two groups of waves share it.  us with 1 / 1 shared / 2 / 2 shared columns:
+// How a launch is cut, by the number of row tiles of 64 over all key heads and by the longest prompt.  Few tiles: one column of rows a wave, twice
+// the workgroups, each with the shorter step; and where the walk over the keys is long, two groups of waves share it.  us with 1 / 1 shared / 2 / 2
+// shared columns:
 //   tiles  104   1 x 200   14.1  14.2  17.0  17.5          704   2 x 700   26.7  34.7  31.1  29.7
 //          152   1 x 300   15.0  14.3  18.4  17.9          752   1 x 1500  43.2  50.3  50.6  39.5
 //          256   1 x 500   20.1  17.6  24.3  22.1         1000   1 x 2000  57.7  72.5  63.9  55.6
 //          504   1 x 1000  31.6  29.4  38.0  31.0         1408   4 x 700   39.9  62.6  36.9  49.6
 //          512   8 x 120   14.5  20.1  16.5  17.5         1568   1 x 3136   109   151   104   114
 //          600   3 x 400   20.9  28.6  23.8  26.2         1920   4 x 739   59.5  89.1  50.7  70.3
-//   (32 heads over 8 of 128, the last 40 over 40.  Three groups: within 1 us of two.)
+//   (32 heads over 8 of 128, the last row 40 over 40.  Three groups: within 1 us of two.)
 struct PackedCut { int cols, split; };
 inline PackedCut packed_cut(int64_t tiles64, int max_len) {
     if (tiles64 <= 512) return PackedCut{1, max_len > 256 ? 2 : 1};
@@ -663,8 +669,8 @@ inline int64_t packed_tiles(const st3_gqa_shape* s, int total, int max_len, int 
     const int G = s->heads / s->kv_heads;
     return std::min((int64_t)total * G / rows + std::min(s->batch, total), ((int64_t)max_len * G + rows - 1) / rows * s->batch);
 }
-// Row tiles dealt over the prompts at a launch's end, as workgroups: all the tiles of 32 x 739 tokens, 40 key heads, in order of their length 499 us, no dealing 368, 768 to 3000 364 to
-// 380; 4 x 700 42 without, 36 with; 8 x 3136, 32 key heads, 809 / 722 / 710 at 1536.
+// Row tiles dealt over the prompts at a launch's end, as workgroups: all the tiles of 32 x 739 tokens, 40 key heads, in order of their length 499 us,
+// no dealing 368, 768 to 3000 364 to 380; 4 x 700 42 without, 36 with; 8 x 3136, 32 key heads, 809 / 722 / 710 at 1536.
 constexpr int kSpread = 1536;
 template <int D>
 void launch_packed(const PackedArgs& a, PackedCut cut, unsigned grid, hipStream_t st) {
