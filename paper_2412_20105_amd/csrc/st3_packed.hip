@@ -439,6 +439,7 @@ __global__ __launch_bounds__(256 * SPLIT, SPLIT == 1 ? 3 : SPLIT) void packed_ke
 template <typename T, int D> struct RowFrag;
 template <int D> struct RowFrag<bf16_t, D> {
     Frag f[D / 32];
+    __device__ __forceinline__ void set(int s, u32x4 unit) { f[s].u4 = unit; }      // the 16 bytes 4 s + g of the row
     __device__ __forceinline__ void load(const bf16_t* row, int g) {
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) f[s].u4 = *reinterpret_cast<const u32x4*>(row + 32 * s + 8 * g);
@@ -452,6 +453,7 @@ template <int D> struct RowFrag<bf16_t, D> {
 };
 template <int D> struct RowFrag<float, D> {
     f32x4 f[D / 16];
+    __device__ __forceinline__ void set(int s, u32x4 unit) { f[s] = __builtin_bit_cast(f32x4, unit); }
     __device__ __forceinline__ void load(const float* row, int g) {
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) f[s] = *reinterpret_cast<const f32x4*>(row + 16 * s + 4 * g);
@@ -574,26 +576,57 @@ __global__ __launch_bounds__(256) void packed_f32_kernel(PackedArgs a) {
 
 // ---------------------------------------------------------------------------------------------------------------------------------
 // score[b,kh,j] = sum over the rows of the window of exp2(logit - maximum) / sum.  The logits are formed again: a wave has 64 keys in registers and
-// takes rows 16 at a time, the next ones on their way; a lane adds up what its 16 keys get.  DEAL: the workgroup's four waves have the same keys and
-// take the rows in turn, which is the shorter way where workgroups are few; else they have 256 keys and all take all rows, which come from memory
-// once for the four (64 rows of 4 heads, 21000 tokens: 48 us dealt).
+// meets the rows 16 at a time; a lane adds up what its 16 keys get.
 // ---------------------------------------------------------------------------------------------------------------------------------
-template <typename T, int D, bool DEAL>
-__global__ __launch_bounds__(256) void packed_score_kernel(PackedArgs a) {
+template <typename T, int D>
+struct ScoreKeys {
+    RowFrag<T, D> k[4];
+    f32x4 sum[4];
+    __device__ __forceinline__ void load(const PackedArgs& a, const Seq& sq, int kh, int k0, int g, int c) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            k[x].load(reinterpret_cast<const T*>(a.k) + (int64_t)(sq.start + min(k0 + 16 * x + c, sq.n - 1)) * a.k_st + kh * a.k_sh, g);
+            sum[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    // 16 rows, this lane's at position pos (ml: maximum, one over the sum); MASKED: some may not see all of the keys k0 ..
+    template <bool MASKED>
+    __device__ __forceinline__ void add(const RowFrag<T, D>& q, float2 ml, int pos, float scale_l2, int k0, int g) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const f32x4 s = k[x].dot(q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = exp2_fast(fmaf(s[i], scale_l2, -ml.x)) * ml.y;
+                sum[x][i] += MASKED && k0 + 16 * x + 4 * g + i > pos ? 0.f : p;
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(float* part, int g, int c) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[x][i] = group_sum<16>(sum[x][i]);
+        if (c == 0) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4*>(part + 16 * x + 4 * g) = sum[x];
+        }
+    }
+};
+
+// The workgroup's four waves have the same keys and take the rows in turn, straight from memory, the next ones on their way: the shorter way where
+// workgroups are few.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void packed_score_deal_kernel(PackedArgs a) {
     __shared__ float part[4][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-    const int kh = blockIdx.x, b = blockIdx.z;
+    const int kh = blockIdx.x, b = blockIdx.z, k0 = blockIdx.y * 64;
     const Seq sq = sequence(a, b);
-    const int n = sq.n, k0 = DEAL ? blockIdx.y * 64 : (blockIdx.y * 4 + wave) * 64;
-    if (k0 >= n) return;                                    // (no barrier below unless DEAL, where all waves have the same keys)
-    RowFrag<T, D> kf[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) kf[x].load(reinterpret_cast<const T*>(a.k) + (int64_t)(sq.start + min(k0 + 16 * x + c, n - 1)) * a.k_st + kh * a.k_sh, g);
-    f32x4 sum[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) sum[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int n = sq.n;
+    if (k0 >= n) return;
+    ScoreKeys<T, D> keys;
+    keys.load(a, sq, kh, k0, g, c);
     const int from = max(max(0, n - a.window), k0), rows = n * a.G;     // (rows in front of the first key see none of them)
-    const bool masked = from < k0 + 63;
     RowFrag<T, D> qf, next;
     float2 ml, ml_next;
     int pos, pos_next;
@@ -605,47 +638,93 @@ __global__ __launch_bounds__(256) void packed_score_kernel(PackedArgs a) {
         ml_next = a.ml[(int64_t)(sq.start + pos_next) * a.H + head];
         if (r0 + c >= rows) pos_next = -1;                             // (a row that does not exist)
     };
-    constexpr int kStep = DEAL ? 64 : 16;
-    int r0 = from * a.G + (DEAL ? 16 * wave : 0);
+    int r0 = from * a.G + 16 * wave;
     if (r0 < rows) fetch(r0);
-    for (; r0 < rows; r0 += kStep) {
-        qf = next; pos = pos_next;
-        ml = make_float2(ml_next.x, pos < 0 ? 0.f : ml_next.y);
-        if (r0 + kStep < rows) fetch(r0 + kStep);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const f32x4 s = kf[x].dot(qf);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float p = exp2_fast(fmaf(s[i], a.scale_l2, -ml.x)) * ml.y;
-                sum[x][i] += masked && k0 + 16 * x + 4 * g + i > pos ? 0.f : p;
-            }
-        }
+    for (; r0 < rows; r0 += 64) {
+        qf = next; pos = pos_next; ml = ml_next;
+        if (r0 + 64 < rows) fetch(r0 + 64);
+        keys.template add<true>(qf, ml, pos, a.scale_l2, k0, g);
     }
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[x][i] = group_sum<16>(sum[x][i]);
-    if (c == 0) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4*>(&part[wave][16 * x + 4 * g]) = sum[x];
-    }
-    float* score = a.score + b * a.s_sb + kh * a.s_sh + k0;
-    if constexpr (DEAL) {
-        __syncthreads();
-        if (tid < 64 && k0 + tid < n) score[tid] = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
-    } else {
-        if (k0 + lane < n) score[lane] = part[wave][lane];  // (written by this wave)
-    }
+    keys.finish(part[wave], g, c);
+    __syncthreads();
+    if (tid < 64 && k0 + tid < n)
+        a.score[b * a.s_sb + kh * a.s_sh + k0 + tid] = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
 }
 
-// Dealt or not, in us, by workgroups of 64 keys: 40 4.4 / 6.4, 128 5.6 / 8.9, 352 8.7 / 9.6; 1920 8.4 / 7.4, 3072 49 / 35, 6272 23 / 21.
-constexpr int kDealTiles = 1024;
+// The workgroup has 256 keys; all of its waves take all rows, which come through LDS, 16 KB of them at a time, the next ones on their way in registers.
+// Bound by the exponentials and products of as many waves as the fullest SIMD has, and by the start.  16 prompts of 35 to 3136 tokens, windows of 32, 4
+// heads of 128 a key head: 15.0 us; 2 of 6000 and 12288, windows of 64: 26.2.  (Each wave fetching rows for itself, 16 at a time: 21.8 and 33.9; 32 KB at
+// a time: 17.5 and 32.5, more registers and fewer waves.)
+template <typename T, int D>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 1) void packed_score_kernel(PackedArgs a) {
+    constexpr int UPR = D * (int)sizeof(T) / 16, PER = 4, kRows = 256 * PER / UPR;       // 16-byte units of a row; rows in LDS; units a thread fetches
+    __shared__ u32x4 sm_q[256 * PER];
+    __shared__ float2 sm_ml[kRows];
+    __shared__ float part[4][64];
+    // unit u of row r lies at u ^ swz(r): the 16 rows that a fragment's lanes read lie in 16 different units of the banks
+    auto swz = [](int row) { return UPR == 8 ? row >> 1 & 7 : row & 15; };
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
+    const int kh = blockIdx.x, b = blockIdx.z, k_first = blockIdx.y * 256, k0 = k_first + wave * 64;
+    const Seq sq = sequence(a, b);
+    const int n = sq.n;
+    if (k_first >= n) return;
+    const int rows = n * a.G;
+    int r0 = max(max(0, n - a.window), k_first) * a.G;                  // (rows in front of the first key see none of them)
+    u32x4 raw[PER];
+    float2 ml_raw;
+    auto fetch = [&]() {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = tid + i * 256, r = min(r0 + e / UPR, rows - 1), p = r / a.G;
+            const T* row = reinterpret_cast<const T*>(a.q) + (int64_t)(sq.start + p) * a.q_st + (int64_t)(kh * a.G + r - p * a.G) * a.q_sh;
+            raw[i] = reinterpret_cast<const u32x4*>(row)[e % UPR];
+        }
+        if (tid < kRows) {
+            const int r = min(r0 + tid, rows - 1), p = r / a.G;
+            ml_raw = a.ml[(int64_t)(sq.start + p) * a.H + kh * a.G + r - p * a.G];
+        }
+    };
+    fetch();
+    ScoreKeys<T, D> keys;
+    keys.load(a, sq, kh, k0, g, c);
+    while (true) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = tid + i * 256, row = e / UPR;
+            sm_q[row * UPR + (e % UPR ^ swz(row))] = raw[i];
+        }
+        if (tid < kRows) sm_ml[tid] = ml_raw;
+        __syncthreads();
+        const int first = r0, here = min(kRows, rows - r0);
+        r0 += kRows;
+        if (r0 < rows) fetch();
+#pragma unroll 1
+        for (int x = 0; x < here; x += 16) {
+            const int row = x + c;
+            RowFrag<T, D> q;
+#pragma unroll
+            for (int s = 0; s < D * (int)sizeof(T) / 64; ++s) q.set(s, sm_q[row * UPR + ((4 * s + g) ^ swz(row))]);
+            if (x + 16 > here || first + x < (k0 + 63) * a.G)
+                keys.template add<true>(q, sm_ml[row], row < here ? (first + row) / a.G : -1, a.scale_l2, k0, g);
+            else
+                keys.template add<false>(q, sm_ml[row], 0, a.scale_l2, k0, g);
+        }
+        if (r0 >= rows) break;
+        __syncthreads();
+    }
+    keys.finish(part[wave], g, c);
+    if (k0 + lane < n) a.score[b * a.s_sb + kh * a.s_sh + k0 + lane] = part[wave][lane];     // (written by this wave)
+}
+
+// Dealt or not, in us, by blocks of 64 keys over all prompts.  128 rows: 40 5.0 / 7.4, 160 5.4 / 7.6, 352 8.4 / 8.8, 512 8.6 / 8.6, 704 11.1 / 8.5,
+// 1024 14.3 / 9.6; 700 rows, whose steps weigh more than the start: 1024 25 / 31; 1600 rows: 96 17 / 53.
+constexpr int kDealTiles = 512, kDealTilesOfManyRows = 1024, kManyRows = 256;
 template <typename T, int D>
 void launch_score(const PackedArgs& a, hipStream_t st) {
     const int64_t strips = (int64_t)a.Hk * a.B, tiles = (a.max_len + 63) / 64;
-    if (tiles * strips <= kDealTiles) packed_score_kernel<T, D, true><<<dim3(a.Hk, (unsigned)tiles, a.B), 256, 0, st>>>(a);
-    else packed_score_kernel<T, D, false><<<dim3(a.Hk, (unsigned)((tiles + 3) / 4), a.B), 256, 0, st>>>(a);
+    const int deal = (int64_t)a.window * a.G > kManyRows ? kDealTilesOfManyRows : kDealTiles;
+    if (tiles * strips <= deal) packed_score_deal_kernel<T, D><<<dim3(a.Hk, (unsigned)tiles, a.B), 256, 0, st>>>(a);
+    else packed_score_kernel<T, D><<<dim3(a.Hk, (unsigned)((tiles + 3) / 4), a.B), 256, 0, st>>>(a);
 }
 
 // How a launch is cut, by the number of row tiles of 64 over all key heads and by the longest prompt.  Few tiles: one column of rows a wave, twice
