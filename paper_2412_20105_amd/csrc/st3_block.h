@@ -78,6 +78,28 @@ inline BlockPages block_pages(const st3_block_cache* c) {
 
 #if defined(__HIPCC__)
 
+// Inclusive sum over the wave's lanes (DPP: row_shr 1, 2, 4, 8, row_bcast 15, 31); the sum, and the largest of values that are not negative, the same
+// in every lane.
+__device__ __forceinline__ int wave_prefix(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);
+    return x;
+}
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_prefix(x), 63); }
+__device__ __forceinline__ int wave_most(int x) {
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true));
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
 // Page of block j of sequence b; -1: there is none.
 __device__ __forceinline__ int page_of(const BlockPages& c, int b, int j) {
     if (j >= c.table_blocks) return -1;
@@ -114,8 +136,7 @@ __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(
 // The largest magnitude of a workgroup's values (`mine` of a thread's), as its bits; all threads call it and get it.  sm: a word for each wave.
 template <int WAVES>
 __device__ __forceinline__ uint32_t largest_of(uint32_t mine, uint32_t* sm, int tid) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) mine = max(mine, (uint32_t)__shfl_xor((int)mine, off));
+    mine = (uint32_t)wave_most((int)mine);
     if ((tid & 63) == 0) sm[tid >> 6] = mine;
     __syncthreads();
     uint32_t all = sm[0];

@@ -168,38 +168,29 @@ __device__ __forceinline__ uint32_t rank_key(float x) {
 
 // Sum over the workgroup's threads before this one, and over all; waves: one word for each wave, two of them in turn.
 __device__ __forceinline__ uint2 count_before(uint32_t mine, uint32_t* waves, int lane, int wave) {
-    // inclusive sum over the wave: within rows of 16 lanes, then the rows before (DPP: row_shr 1, 2, 4, 8, row_bcast 15, 31)
-    int incl = (int)mine;
-    incl += __builtin_amdgcn_update_dpp(0, incl, 0x111, 0xf, 0xf, true);
-    incl += __builtin_amdgcn_update_dpp(0, incl, 0x112, 0xf, 0xf, true);
-    incl += __builtin_amdgcn_update_dpp(0, incl, 0x114, 0xf, 0xf, true);
-    incl += __builtin_amdgcn_update_dpp(0, incl, 0x118, 0xf, 0xf, true);
-    incl += __builtin_amdgcn_update_dpp(0, incl, 0x142, 0xa, 0xf, true);
-    incl += __builtin_amdgcn_update_dpp(0, incl, 0x143, 0xc, 0xf, true);
+    constexpr int kWaves = kRankThreads / 64;
+    const int incl = wave_prefix((int)mine);
     if (lane == 63) waves[wave] = incl;
     __syncthreads();
-    const uint32_t other = lane < kRankThreads / 64 ? waves[lane] : 0;
-    uint32_t before = incl - mine, all = 0;
-#pragma unroll
-    for (int w = 0; w < kRankThreads / 64; ++w) {
-        const uint32_t x = __builtin_amdgcn_readlane(other, w);
-        before += w < wave ? x : 0;
-        all += x;
-    }
-    return make_uint2(before, all);
+    const int upto = wave_prefix(lane < kWaves ? (int)waves[lane] : 0);     // (each wave for itself; picked one by one they took 0.5 us)
+    const int before = wave > 0 ? __builtin_amdgcn_readlane(upto, wave - 1) : 0;
+    return make_uint2(before + incl - (int)mine, __builtin_amdgcn_readlane(upto, kWaves - 1));
 }
 
-// Workgroup (key head, sequence): the key of the last row kept by a radix search (11 + 11 + 10 bits), then the rows kept, their scores, and, of the
-// rows with that last key, as many of the first as are wanted.  PER > 0: a thread holds PER rows that follow each other in registers (rows of up to
-// 1024 PER); 0: rows of any length, read again in every pass.  Bound by its chain of passes: 8 strips of 1200 rows 7.9 us, with
-// PER = 0 8.5; 256 strips of up to 3136 rows 9.5.
+// Workgroup (key head, sequence): the key of the last row kept by a radix search (12 + 10 + 10 bits; as soon as a bin holds kFew rows or less, their
+// places among each other are counted instead), then the rows kept, their scores, and, of the rows with that last key, as many of the first as
+// are wanted.  PER > 0: a thread holds PER rows that follow each other in registers (rows of up to 1024 PER); 0: rows of any length, read again in
+// every pass.  Bound by its chain of passes and barriers: 8 strips of 1200 rows 6.3 us (7.9 by the radix alone, 11 + 11 + 10 bits), 256 strips of up to 3136
+// rows 8.3 (9.5).
+constexpr int kFew = 128;
 template <int PER>
 __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs a) {
-    constexpr int kBins = 2048 / kRankThreads;
-    __shared__ uint32_t hist[2048];
+    constexpr int kTop = 4096, kBins = kTop / kRankThreads;
+    __shared__ uint32_t hist[kTop];
     __shared__ uint32_t waves[2][kRankThreads / 64];
-    __shared__ uint32_t found[2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kh = blockIdx.x, b = blockIdx.y;
+    __shared__ uint32_t found[3];
+    __shared__ uint32_t few[kFew], n_few;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kh = blockIdx.x, b = blockIdx.y;
     const float* score = a.score + b * a.s_sb + kh * a.s_sh;
     float x[PER > 0 ? PER : 1];
     if constexpr (PER > 0) {                                // (on their way beside the length)
@@ -214,37 +205,62 @@ __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs
     const bool all = n <= a.keep;
     uint32_t want = all ? 0 : a.keep - a.n_sink - a.n_recent;   // candidates wanted, at last of those with the last key
     uint32_t key = want > 0 ? 0 : 0xffffffffu, mask = 0;        // (no row has the key of all ones)
-    for (int pass = 0; pass < 3 && want > 0; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-#pragma unroll
-        for (int i = 0; i < kBins; ++i) hist[tid + i * kRankThreads] = 0;
-        __syncthreads();
-        auto note = [&](int i, float s) {
-            const uint32_t u = rank_key(s);
-            if (i >= lo && i < hi && (u & mask) == key) atomicAdd(&hist[(u >> shift) & ((1u << bits) - 1)], 1u);
-        };
+    auto each = [&](auto f) {                                   // the candidates
         if constexpr (PER > 0) {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) note(tid * PER + i, x[i]);
+            for (int i = 0; i < PER; ++i)
+                if (tid * PER + i >= lo && tid * PER + i < hi) f(rank_key(x[i]));
         } else {
-            for (int i = lo + tid; i < hi; i += kRankThreads) note(i, score[i]);
+            for (int i = lo + tid; i < hi; i += kRankThreads) f(rank_key(score[i]));
         }
+    };
+    for (int pass = 0; pass < 3 && want > 0; ++pass) {
+        const int shift = pass == 0 ? 20 : pass == 1 ? 10 : 0;
+        const uint32_t low = pass == 0 ? 0xfff : 0x3ff;
+#pragma unroll
+        for (int i = 0; i < kBins; ++i) hist[tid + i * kRankThreads] = 0;
+        if (tid == 0) n_few = 0;
+        __syncthreads();
+        each([&](uint32_t u) {
+            if ((u & mask) == key) atomicAdd(&hist[(u >> shift) & low], 1u);
+        });
         __syncthreads();
         // bins from the top: thread t owns kBins of them
         uint32_t h[kBins], sum = 0;
 #pragma unroll
-        for (int i = 0; i < kBins; ++i) { h[i] = hist[2047 - kBins * tid - i]; sum += h[i]; }
+        for (int i = 0; i < kBins; ++i) { h[i] = hist[kTop - 1 - kBins * tid - i]; sum += h[i]; }
         uint32_t before = count_before(sum, waves[0], lane, wave).x;
 #pragma unroll
         for (int i = 0; i < kBins; ++i) {
-            if (before < want && before + h[i] >= want) { found[0] = 2047 - kBins * tid - i; found[1] = want - before; }
+            if (before < want && before + h[i] >= want) { found[0] = kTop - 1 - kBins * tid - i; found[1] = want - before; found[2] = h[i]; }
             before += h[i];
         }
         __syncthreads();
         key |= found[0] << shift;
-        mask |= ((1u << bits) - 1) << shift;
+        mask |= low << shift;
         want = found[1];
+        const uint32_t here = found[2];
         __syncthreads();
+        if (here <= kFew && pass < 2) {
+            each([&](uint32_t u) {
+                if ((u & mask) == key) few[atomicAdd(&n_few, 1u)] = u;      // (in any order: only values are compared)
+            });
+            __syncthreads();
+            constexpr int kTeam = kRankThreads / kFew;          // threads that count for one of them
+            const uint32_t one = tid / kTeam;
+            if (one < here) {
+                const uint32_t u = few[one];
+                uint32_t more = 0, same = 0;
+                for (uint32_t i = tid % kTeam; i < here; i += kTeam) { more += few[i] > u ? 1 : 0; same += few[i] == u ? 1 : 0; }
+#pragma unroll
+                for (int off = 1; off < kTeam; off <<= 1) { more += __shfl_xor(more, off); same += __shfl_xor(same, off); }
+                if (more < want && more + same >= want) { found[0] = u; found[1] = want - more; }       // (equal ones write the same)
+            }
+            __syncthreads();
+            key = found[0];
+            want = found[1];
+            break;
+        }
     }
     auto safe = [&](int i) { return all || i < lo || i >= hi; };
     if constexpr (PER > 0) {
@@ -286,7 +302,7 @@ __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs
 
 // Workgroup (K or V of a key head, new block, sequence).  K's rows are fetched one by one; any row of a page lies in all lines of its V, so V comes
 // as whole pages, two at a time (a block's rows ascend: a few pages that follow each other), and is picked from LDS.  (Picked byte by byte from
-// memory it kept the address units busy: 32 caches 84 us.)  32 caches of 611 to 3136 rows to 1500 rows: 190 MB in 53 us, 3.6 TB/s, the vector units
+// memory it kept the address units busy: 32 caches 84 us.)  32 caches of 611 to 3136 rows to 1500 rows: 190 MB in 51 us, 3.7 TB/s, the vector units
 // busy for 58 % of it with codes, values and quotients; with registers for 5 waves a SIMD instead of 6 it takes 59.
 constexpr int kPageRow = kBlk + 8;          // bytes: the 4 columns that a wave picks at a time, 8 apart, are 16 banks apart
 template <int D, int CODE, bool COLUMNS>

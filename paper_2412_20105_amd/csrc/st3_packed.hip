@@ -31,28 +31,6 @@ __device__ __forceinline__ Seq sequence(const PackedArgs& a, int b) {
     return Seq{s, min(e - s, a.max_len)};
 }
 
-// Inclusive sum over the wave's lanes (DPP: row_shr 1, 2, 4, 8, row_bcast 15, 31); the sum, and the largest of values that are not negative, the same
-// in every lane.
-__device__ __forceinline__ int wave_prefix(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);
-    return x;
-}
-__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_prefix(x), 63); }
-__device__ __forceinline__ int wave_most(int x) {
-    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));
-    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
-    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
-    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
-    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true));
-    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true));
-    return __builtin_amdgcn_readlane(x, 63);
-}
-
 // Workgroup -> (sequence, key head, row tile).  Key heads run fastest: workgroups go round-robin to the 8 XCDs, so with a multiple of 8 key heads a
 // pair's K and V stay in one XCD's L2, and a sequence's tiles follow each other, heaviest (last) first, longest sequences first, so that they are
 // there when the next tile wants them.  A tile costs in proportion to its index: the last sequences' tiles (a.spread of them, or so) are dealt
