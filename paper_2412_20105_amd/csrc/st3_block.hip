@@ -159,44 +159,48 @@ struct EvictBlockArgs {
     int32_t* kept; int64_t i_sb, i_sh;
 };
 
-// Greater means better; NaN below everything, -0 as +0.
+// Greater means better; NaN below everything, -0 as +0.  0 is left for rows that do not exist, what is above kRankTop for rows kept whatever their score.
+constexpr uint32_t kRankTop = 0xff800000u;      // (an infinity)
 __device__ __forceinline__ uint32_t rank_key(float x) {
-    if (!(x == x)) return 0;
+    if (!(x == x)) return 1;
     const uint32_t u = __float_as_uint(x == 0.f ? 0.f : x);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Sum over the workgroup's threads before this one, and over all; waves: one word for each wave, two of them in turn.
-__device__ __forceinline__ uint2 count_before(uint32_t mine, uint32_t* waves, int lane, int wave) {
+// Sums over the workgroup's waves before this one, and over all, of a value that is the same in a wave's lanes; waves: a word for each wave.
+__device__ __forceinline__ uint2 waves_before(uint32_t mine, uint32_t* waves, int lane, int wave) {
     constexpr int kWaves = kRankThreads / 64;
-    const int incl = wave_prefix((int)mine);
-    if (lane == 63) waves[wave] = incl;
+    if (lane == 0) waves[wave] = mine;
     __syncthreads();
     const int upto = wave_prefix(lane < kWaves ? (int)waves[lane] : 0);     // (each wave for itself; picked one by one they took 0.5 us)
-    const int before = wave > 0 ? __builtin_amdgcn_readlane(upto, wave - 1) : 0;
-    return make_uint2(before + incl - (int)mine, __builtin_amdgcn_readlane(upto, kWaves - 1));
+    return make_uint2(wave > 0 ? __builtin_amdgcn_readlane(upto, wave - 1) : 0, __builtin_amdgcn_readlane(upto, kWaves - 1));
 }
 
 // Workgroup (key head, sequence): the key of the last row kept by a radix search (12 + 10 + 10 bits; as soon as a bin holds kFew rows or less, their
 // places among each other are counted instead), then the rows kept, their scores, and, of the rows with that last key, as many of the first as
-// are wanted.  PER > 0: a thread holds PER rows that follow each other in registers (rows of up to 1024 PER); 0: rows of any length, read again in
-// every pass.  Bound by its chain of passes and barriers: 8 strips of 1200 rows 6.3 us (7.9 by the radix alone, 11 + 11 + 10 bits), 256 strips of up to 3136
-// rows 8.3 (9.5).
+// are wanted.  A wave holds 64 PER rows that follow each other, lane by lane, so that loads and stores are whole lines and places are counts of
+// ballots; LONG: any number of rows, 1024 PER at a time, read again in every pass.  Bound by its chain of passes and barriers: 8 strips
+// of 1200 rows 5.8 us (7.9 by the radix alone, 11 + 11 + 10 bits, with threads that hold rows in a row), 256 of up to 3136 6.9 (9.5), 40 of 12596 12.7
+// (20.1), 40 of up to 18347 20.3 (LONG 30.3).
 constexpr int kFew = 128;
-template <int PER>
+template <int PER, bool LONG>
 __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs a) {
-    constexpr int kTop = 4096, kBins = kTop / kRankThreads;
+    constexpr int kTop = 4096, kBins = kTop / kRankThreads, kRows = PER * kRankThreads;
+    static_assert(kRows <= 32768, "counts of a chunk's rows in 16 bits");
     __shared__ uint32_t hist[kTop];
     __shared__ uint32_t waves[2][kRankThreads / 64];
     __shared__ uint32_t found[3];
     __shared__ uint32_t few[kFew], n_few;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kh = blockIdx.x, b = blockIdx.y;
     const float* score = a.score + b * a.s_sb + kh * a.s_sh;
-    float x[PER > 0 ? PER : 1];
-    if constexpr (PER > 0) {                                // (on their way beside the length)
+    const int mine = wave * (64 * PER) + lane;              // + 64 i: this thread's rows of a chunk
+    float x[PER];
+    uint32_t u[PER];
+    auto load = [&](int base) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) x[i] = tid * PER + i < a.max_len ? score[tid * PER + i] : 0.f;
-    }
+        for (int i = 0; i < PER; ++i) x[i] = base + mine + 64 * i < a.max_len ? score[base + mine + 64 * i] : 0.f;
+    };
+    if constexpr (!LONG) load(0);                           // (on their way beside the length)
     const int n = min(a.from.len[b], a.max_len);
     if (n < 0) return;
     float* to = a.to_score + b * a.t_sb + kh * a.t_sh;
@@ -204,14 +208,21 @@ __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs
     const int lo = a.n_sink, hi = n - a.n_recent;
     const bool all = n <= a.keep;
     uint32_t want = all ? 0 : a.keep - a.n_sink - a.n_recent;   // candidates wanted, at last of those with the last key
-    uint32_t key = want > 0 ? 0 : 0xffffffffu, mask = 0;        // (no row has the key of all ones)
-    auto each = [&](auto f) {                                   // the candidates
-        if constexpr (PER > 0) {
+    uint32_t key = want > 0 ? 0 : kRankTop, mask = 0;
+    auto rank = [&](int base) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int r = base + mine + 64 * i;
+            u[i] = r >= n ? 0 : all || r < lo || r >= hi ? 0xffffffffu : rank_key(x[i]);
+        }
+    };
+    if constexpr (!LONG) rank(0);
+    auto each = [&](auto f) {                                   // the candidates that share the key's leading bits
+        for (int base = 0; base < (LONG ? n : 1); base += kRows) {
+            if constexpr (LONG) { load(base); rank(base); }
 #pragma unroll
             for (int i = 0; i < PER; ++i)
-                if (tid * PER + i >= lo && tid * PER + i < hi) f(rank_key(x[i]));
-        } else {
-            for (int i = lo + tid; i < hi; i += kRankThreads) f(rank_key(score[i]));
+                if (u[i] - 1 < kRankTop && (u[i] & mask) == key) f(u[i]);
         }
     };
     for (int pass = 0; pass < 3 && want > 0; ++pass) {
@@ -222,14 +233,15 @@ __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs
         if (tid == 0) n_few = 0;
         __syncthreads();
         each([&](uint32_t u) {
-            if ((u & mask) == key) atomicAdd(&hist[(u >> shift) & low], 1u);
+            atomicAdd(&hist[(u >> shift) & low], 1u);
         });
         __syncthreads();
         // bins from the top: thread t owns kBins of them
         uint32_t h[kBins], sum = 0;
 #pragma unroll
         for (int i = 0; i < kBins; ++i) { h[i] = hist[kTop - 1 - kBins * tid - i]; sum += h[i]; }
-        uint32_t before = count_before(sum, waves[0], lane, wave).x;
+        const uint32_t incl = wave_prefix((int)sum);
+        uint32_t before = incl - sum + waves_before(__builtin_amdgcn_readlane(incl, 63), waves[0], lane, wave).x;
 #pragma unroll
         for (int i = 0; i < kBins; ++i) {
             if (before < want && before + h[i] >= want) { found[0] = kTop - 1 - kBins * tid - i; found[1] = want - before; found[2] = h[i]; }
@@ -243,7 +255,7 @@ __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs
         __syncthreads();
         if (here <= kFew && pass < 2) {
             each([&](uint32_t u) {
-                if ((u & mask) == key) few[atomicAdd(&n_few, 1u)] = u;      // (in any order: only values are compared)
+                few[atomicAdd(&n_few, 1u)] = u;             // (in any order: only values are compared)
             });
             __syncthreads();
             constexpr int kTeam = kRankThreads / kFew;          // threads that count for one of them
@@ -262,40 +274,33 @@ __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs
             break;
         }
     }
-    auto safe = [&](int i) { return all || i < lo || i >= hi; };
-    if constexpr (PER > 0) {
-        uint32_t ties = 0, mine = 0;
+    // Rows written and rows with the last key met, by the chunks before.  (A chunk's scores are read before any of its rows is written, and a row moves
+    // to the front if at all: to_score may be score.)
+    uint32_t out = 0, ties = 0;
+    for (int base = 0, turn = 0; base < (LONG ? n : 1); base += kRows, turn ^= 1) {
+        if constexpr (LONG) { load(base); rank(base); }
+        uint32_t count = 0;                                 // the wave's rows above the key, and from bit 16 on those with it
 #pragma unroll
-        for (int i = 0; i < PER; ++i) { const int r = tid * PER + i; ties += r < n && !safe(r) && rank_key(x[i]) == key ? 1 : 0; }
-        uint32_t tie = count_before(ties, waves[0], lane, wave).x;
-        bool keep[PER];
+        for (int i = 0; i < PER; ++i) count += __popcll(__ballot(u[i] > key)) + (__popcll(__ballot(want > 0 && u[i] == key)) << 16);
+        const uint2 sums = waves_before(count, waves[turn], lane, wave);
+        uint32_t at = out + (sums.x & 0xffff), met = ties + (sums.x >> 16);     // of ties, the first `want` of all are kept
+        at += min(met, want) - min(ties, want);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int r = tid * PER + i;
-            const uint32_t u = rank_key(x[i]);
-            const bool is_tie = r < n && !safe(r) && u == key;
-            keep[i] = r < n && (safe(r) || u > key || (is_tie && tie < want));
-            tie += is_tie ? 1 : 0;
-            mine += keep[i] ? 1 : 0;
+            const uint64_t tied = __ballot(want > 0 && u[i] == key), below = (1ull << lane) - 1;
+            const bool keep = u[i] > key || (want > 0 && u[i] == key && met + __popcll(tied & below) < want);
+            const uint64_t all_kept = __ballot(keep);
+            if (keep) {
+                const uint32_t place = at + __popcll(all_kept & below);
+                kept[place] = base + mine + 64 * i;
+                to[place] = x[i];
+            }
+            at += __popcll(all_kept);
+            met += __popcll(tied);
         }
-        uint32_t at = count_before(mine, waves[1], lane, wave).x;      // (every thread has read its scores: to_score may be score)
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (keep[i]) { kept[at] = tid * PER + i; to[at] = x[i]; ++at; }
-    } else {
-        uint32_t out = 0, ties = 0;             // rows written, rows with the last key met
-        for (int i0 = 0; i0 < n; i0 += kRankThreads) {
-            const int i = i0 + tid;
-            const float s = i < n ? score[i] : 0.f;
-            const uint32_t u = rank_key(s);
-            const bool tie = i < n && !safe(i) && u == key;
-            const uint2 t = count_before(tie ? 1 : 0, waves[0], lane, wave);
-            const bool keep = i < n && (safe(i) || u > key || (tie && ties + t.x < want));
-            const uint2 at = count_before(keep ? 1 : 0, waves[1], lane, wave);      // (the chunk's scores are read: to_score may be score)
-            if (keep) { kept[out + at.x] = i; to[out + at.x] = s; }
-            out += at.y;
-            ties += t.y;
-        }
+        const uint32_t ties_now = ties + (sums.y >> 16);
+        out += (sums.y & 0xffff) + min(ties_now, want) - min(ties, want);
+        ties = ties_now;
     }
     for (int i = min(n, a.keep) + tid; i < a.keep; i += kRankThreads) kept[i] = -1;
 }
@@ -494,9 +499,12 @@ extern "C" st3_status st3_block_evict(const st3_gqa_shape* shape, const st3_bloc
     const EvictBlockArgs a{block_pages(from), block_pages(to), max_len, keep, n_sink, n_recent, Hk, score, score_stride_b, score_stride_h, to_score,
                            to_score_stride_b, to_score_stride_h, kept, kept_stride_b, kept_stride_h};
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    if (max_len <= 4096) block_rank_kernel<4096 / kRankThreads><<<dim3(Hk, B), kRankThreads, 0, st>>>(a);
-    else if (max_len <= 16384) block_rank_kernel<16384 / kRankThreads><<<dim3(Hk, B), kRankThreads, 0, st>>>(a);
-    else block_rank_kernel<0><<<dim3(Hk, B), kRankThreads, 0, st>>>(a);
+    const dim3 strips(Hk, B);
+    if (max_len <= 4 * kRankThreads) block_rank_kernel<4, false><<<strips, kRankThreads, 0, st>>>(a);
+    else if (max_len <= 8 * kRankThreads) block_rank_kernel<8, false><<<strips, kRankThreads, 0, st>>>(a);
+    else if (max_len <= 16 * kRankThreads) block_rank_kernel<16, false><<<strips, kRankThreads, 0, st>>>(a);
+    else if (max_len <= 32 * kRankThreads) block_rank_kernel<32, false><<<strips, kRankThreads, 0, st>>>(a);
+    else block_rank_kernel<16, true><<<strips, kRankThreads, 0, st>>>(a);
     if (blocks == 0) return check_launch();
     const dim3 grid(2 * Hk, blocks, B);
     if (from->code == ST3_BLOCK_INT8) {

@@ -36,7 +36,7 @@ def check(rng, lens, score, keep, n_sink=0, n_recent=0):
             np.testing.assert_array_equal(t[b, h].cpu().numpy(), score[b, h, want].astype(np.float32))
 
 
-@pytest.mark.parametrize("n", [700, 1200, 4096, 5000, 16384, 17000])
+@pytest.mark.parametrize("n", [700, 1200, 4096, 4097, 8192, 9000, 16384, 17000, 32768])
 @pytest.mark.parametrize("many", [1, 127, 128, 129, 500])
 def test_scores_that_share_their_leading_bits(n, many):
     """`many` scores in [1, 1 + 2^-10), all others above or below; keep so many that the last row kept is among them."""
@@ -59,3 +59,27 @@ def test_scores_of_every_kind(n):
                       np.where(rng.random(n) < 0.3, np.inf, -np.inf), np.where(rng.random(n) < 0.3, np.nan, rng.normal(size=n))])[None]
     for keep, first, last in ((n // 3, 4, 20), (n - 1, 0, 0), (150, 75, 75), (1, 0, 0)):
         check(rng, [n], score, keep, first, last)
+
+
+@pytest.mark.parametrize("n,keep", [(16385, 16000), (30000, 20000), (33000, 16500), (40000, 300), (40000, 39990)])
+def test_long_sequences_in_place(n, keep):
+    """More rows than a workgroup holds at a time, scores written over those that are read; ties everywhere."""
+    rng = np.random.default_rng(n + keep)
+    score = rng.integers(0, 50, size=(2, 2, n)) / 8.0
+    score[1, 1] = 1.0
+    lens = [n, n - 700]
+    dev, _ = filled(rng, [BLOCK] * 2, 2, 64, "int8", n // BLOCK + 1, pages=2 * (n // BLOCK + keep // BLOCK + 3))
+    dev.set_len(lens)
+    to = DeviceCache(rng, 2, 2, 64, "int8", keep // BLOCK, pool=dev)
+    dev.table[:, 1:] = dev.table[:, :1]
+    s = torch.from_numpy(score.astype(np.float32)).to(DEV)
+    kept = torch.full((2, 2, keep), 77, dtype=torch.int32, device=DEV)
+    st3.st3_block_evict(st3.gqa_shape(2, 2, 2, 64), dev.c, to.c, n, keep, 5, 60, s, s, kept)
+    torch.cuda.synchronize()
+    for b, m in enumerate(lens):
+        for h in range(2):
+            want = np.arange(m) if m <= keep else kept_rows(score[b, h].astype(np.float32), m, keep, 5, 60)
+            got = kept[b, h].cpu().numpy()
+            np.testing.assert_array_equal(got[:len(want)], want, err_msg=f"{b} {h}")
+            assert (got[len(want):] == -1).all()
+            np.testing.assert_array_equal(s[b, h, :len(want)].cpu().numpy(), score[b, h, want].astype(np.float32))
