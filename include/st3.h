@@ -578,6 +578,7 @@ ST3_EXPORT size_t st3_block_workspace_bytes(const st3_gqa_shape* shape, int32_t 
  *   score[b,kh,j] += sum_{h in group kh} p_h[j]  for j < r,   score[b,kh,r] = that sum at r
  * q, out: [batch, H, d] rows, k_new, v_new: [batch, Hk, d].  k_new and v_new NULL: rows 0 .. r - 1 are attended and nothing is appended
  * (no rows: out = 0).  score may be NULL; its rows hold max_len + 1 entries at least.
+ * out shares no memory with k_new or v_new.
  * The cache's `len` still says r behind the call.
  * ------------------------------------------------------------------------------------------- */
 ST3_EXPORT st3_status st3_block_decode(const st3_gqa_shape* shape, const st3_rows* q, const st3_rows* k_new, const st3_rows* v_new,
@@ -590,7 +591,7 @@ ST3_EXPORT st3_status st3_block_decode(const st3_gqa_shape* shape, const st3_row
  * n_recent and the best of the rest by score (order of st3_select_topk, ties by the lower row; a NaN ranks last), `keep` in all, in
  * ascending order; a sequence with fewer keeps them all.  With kept[b,kh,0..k_b) the rows kept, k_b = min(len[b], keep):
  *   row i of `to`     = row kept[i] of `from`        to_score[b,kh,i] = score[b,kh,kept[i]]
- * to_score may be score itself.  kept (DEVICE int32) is padded with -1 up to keep entries.  A block of `to` that is one whole block of
+ * to_score may be score itself, rows on rows, and else shares no memory with it.  kept (DEVICE int32) is padded with -1 up to keep entries.  A block of `to` that is one whole block of
  * `from` keeps its codes and scale; others are coded anew from the values that their rows stand for (rounded to bf16 in
  * the tail), so a value moves by half a step of its new block's scale at most.
  * `to` shares codes' format with `from` and may share its pools; its table names pages that `from` does not use and its tails are other

@@ -496,6 +496,9 @@ extern "C" st3_status st3_block_evict(const st3_gqa_shape* shape, const st3_bloc
     }
     const int blocks = (most + kBlk - 1) / kBlk;
     if (blocks > 65535) return ST3_ERR_UNSUPPORTED;
+    const bool in_place = score == to_score && (B == 1 || score_stride_b == to_score_stride_b) && (Hk == 1 || score_stride_h == to_score_stride_h);
+    const st3_rows old_scores{const_cast<float*>(score), score_stride_b, score_stride_h}, new_scores{to_score, to_score_stride_b, to_score_stride_h};
+    if (most > 0 && !in_place && packed_rows_meet(&old_scores, Hk, &new_scores, Hk, B, max_len, 4, most)) return ST3_ERR_INVALID_ARG;
     const EvictBlockArgs a{block_pages(from), block_pages(to), max_len, keep, n_sink, n_recent, Hk, score, score_stride_b, score_stride_h, to_score,
                            to_score_stride_b, to_score_stride_h, kept, kept_stride_b, kept_stride_h};
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);

@@ -83,3 +83,24 @@ def test_long_sequences_in_place(n, keep):
             np.testing.assert_array_equal(got[:len(want)], want, err_msg=f"{b} {h}")
             assert (got[len(want):] == -1).all()
             np.testing.assert_array_equal(s[b, h, :len(want)].cpu().numpy(), score[b, h, want].astype(np.float32))
+
+
+def test_scores_beside_each_other_in_one_buffer():
+    rng = np.random.default_rng(8)
+    n, keep, B, Hk = 300, 130, 2, 3
+    dev, _ = filled(rng, [BLOCK] * B, Hk, 64, "int8", n // BLOCK + 1, pages=B * (n // BLOCK + keep // BLOCK + 3))
+    dev.set_len([n] * B)
+    to = DeviceCache(rng, B, Hk, 64, "int8", keep // BLOCK, pool=dev)
+    dev.table[:, 1:] = dev.table[:, :1]
+    score = rng.exponential(size=(B, Hk, n))
+    both = torch.full((B, Hk, n + keep), -5.0, device=DEV)
+    both[..., :n] = torch.from_numpy(score.astype(np.float32)).to(DEV)
+    kept = torch.full((B, Hk, keep), 77, dtype=torch.int32, device=DEV)
+    st3.st3_block_evict(st3.gqa_shape(B, Hk, Hk, 64), dev.c, to.c, n, keep, 4, 10, both[..., :n], both[..., n:], kept)
+    torch.cuda.synchronize()
+    for b in range(B):
+        for h in range(Hk):
+            want = kept_rows(score[b, h].astype(np.float32), n, keep, 4, 10)
+            np.testing.assert_array_equal(kept[b, h].cpu().numpy(), want)
+            np.testing.assert_array_equal(both[b, h, n:].cpu().numpy(), score[b, h, want].astype(np.float32))
+            np.testing.assert_array_equal(both[b, h, :n].cpu().numpy(), score[b, h].astype(np.float32))
