@@ -593,7 +593,8 @@ ST3_EXPORT st3_status st3_block_decode(const st3_gqa_shape* shape, const st3_row
  *   row i of `to`     = row kept[i] of `from`        to_score[b,kh,i] = score[b,kh,kept[i]]
  * to_score may be score itself, rows on rows, and else shares no memory with it.  kept (DEVICE int32) is padded with -1 up to keep entries.  A block of `to` that is one whole block of
  * `from` keeps its codes and scale; others are coded anew from the values that their rows stand for (rounded to bf16 in
- * the tail), so a value moves by half a step of its new block's scale at most.
+ * the tail), so a value moves by half a step of its new block's scale at most (by more where that scale is subnormal: it is rounded
+ * itself, and the largest codes saturate).
  * `to` shares codes' format with `from` and may share its pools; its table names pages that `from` does not use and its tails are other
  * buffers, so nothing that is read is written, and `from` stays as it is (but for score).  len of `from` is read, that of `to` is not:
  * the caller sets lengths to min(len, keep).  0 <= n_sink, n_recent; n_sink + n_recent <= keep; keep >= 1.

@@ -119,8 +119,9 @@ struct Divider {
         by = care ? 1.0f : s;
         inv = __fdiv_rn(1.0f, by);
     }
-    __device__ __forceinline__ float careful(float x, float if_nan) const {
-        return !(x == x) ? if_nan : scale > 0.f ? __fdiv_rn(fminf(fmaxf(x, -top), top), scale) : copysignf(0.f, x);
+    // most: the largest code.  A scale of a few of the smallest float32 is rounded by so much that a quotient can pass it.
+    __device__ __forceinline__ float careful(float x, float if_nan, float most) const {
+        return !(x == x) ? if_nan : scale > 0.f ? fminf(fmaxf(__fdiv_rn(fminf(fmaxf(x, -top), top), scale), -most), most) : copysignf(0.f, x);
     }
     __device__ __forceinline__ float operator()(float x) const {
         float q = x * inv;                                  // (with the remainder's sign this way round zeros keep theirs)
@@ -145,10 +146,11 @@ __device__ __forceinline__ uint32_t largest_of(uint32_t mine, uint32_t* sm, int 
     return all;
 }
 
-// The two formats.  code4: four quotients (of x[0..3], no larger than the top by more than a rounding) as four bytes.
+// The two formats.  code4: four quotients (of x[0..3], no larger than kMost by more than a rounding that its code takes back) as four
+// bytes.
 template <int CODE> struct BlockCode;
 template <> struct BlockCode<ST3_BLOCK_INT8> {
-    static constexpr float kUnit = 1.0f / 127.0f;
+    static constexpr float kMost = 127.0f, kUnit = 1.0f / kMost;
     __device__ static __forceinline__ float nan_code() { return 0.f; }
     __device__ static __forceinline__ uint32_t code4(const float* x, const Divider& d) {
         uint32_t u[4];
@@ -170,7 +172,7 @@ template <> struct BlockCode<ST3_BLOCK_INT8> {
     }
 };
 template <> struct BlockCode<ST3_BLOCK_E4M3> {
-    static constexpr float kUnit = 1.0f / 448.0f;
+    static constexpr float kMost = 448.0f, kUnit = 1.0f / kMost;
     __device__ static __forceinline__ float nan_code() { return __uint_as_float(0x7fc00000u); }
     __device__ static __forceinline__ uint32_t code4(const float* x, const Divider& d) {
         uint32_t w = __builtin_amdgcn_cvt_pk_fp8_f32(d(x[0]), d(x[1]), 0, false);

@@ -54,7 +54,7 @@ __device__ __forceinline__ void write_block(float (&v)[4][D / 16], const BlockPa
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int e = 0; e < W; ++e) v[r][e] = divide.careful(v[r][e], F::nan_code());
+            for (int e = 0; e < W; ++e) v[r][e] = divide.careful(v[r][e], F::nan_code(), F::kMost);
     }
     uint8_t* codes = (COLUMNS ? c.v_codes : c.k_codes) + at * (kBlk * D);
     if constexpr (COLUMNS) {

@@ -400,7 +400,7 @@ __global__ __launch_bounds__(WAVES * 64, 3) void block_attend_kernel(BlockDecode
                 float x[4] = {bf16_lo(raw.x), bf16_hi(raw.x), bf16_lo(raw.y), bf16_hi(raw.y)};
                 if (divide.care) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = divide.careful(x[i], F::nan_code());
+                    for (int i = 0; i < 4; ++i) x[i] = divide.careful(x[i], F::nan_code(), F::kMost);
                 }
                 *reinterpret_cast<uint32_t*>(dst + e) = F::code4(x, divide);
             }
