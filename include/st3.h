@@ -578,6 +578,8 @@ ST3_EXPORT size_t st3_block_workspace_bytes(const st3_gqa_shape* shape, int32_t 
  *   score[b,kh,j] += sum_{h in group kh} p_h[j]  for j < r,   score[b,kh,r] = that sum at r
  * q, out: [batch, H, d] rows, k_new, v_new: [batch, Hk, d].  k_new and v_new NULL: rows 0 .. r - 1 are attended and nothing is appended
  * (no rows: out = 0).  score may be NULL; its rows hold max_len + 1 entries at least.
+ * A logit that is NaN or +infinity makes its head's output and all of that head's weights NaN, and so the key head's scores of the rows up
+ * to r; one of -infinity weighs nothing, and where all are, out = 0 and so are the weights.
  * out shares no memory with k_new or v_new.
  * The cache's `len` still says r behind the call.
  * ------------------------------------------------------------------------------------------- */

@@ -335,7 +335,7 @@ __global__ __launch_bounds__(WAVES * 64, 3) void block_attend_kernel(BlockDecode
             x = fmaf(sm_o[(w * cols + col) * OS + dim], f, x);
         }
         if constexpr (WHOLE) {
-            const float rl = sum > 0.f ? 1.0f / sum : 0.f;
+            const float rl = sum == 0.f ? 0.f : 1.0f / sum;      // (a sum of NaN stays one)
             a.out[(int64_t)b * a.o_st + (int64_t)(h0 + col) * a.o_sh + dim] = (uint16_t)f32_to_bf16_bits(x * rl);
             if (dim == 0) { sm_h[col] = top; sm_h[kCols + col] = rl; }
         } else {
@@ -420,7 +420,7 @@ __device__ __forceinline__ float2 head_sum(const BlockDecodeArgs& a, int64_t par
     }
     const float m = wave_max_from<1>(top);
     sum = wave_sum_from<1>(sum * exp2_fast(top - m));
-    return make_float2(m, sum > 0.f ? 1.0f / sum : 0.f);
+    return make_float2(m, sum == 0.f ? 0.f : 1.0f / sum);
 }
 
 constexpr int kFinishThreads = 256, kScoreKeys = 4 * kFinishThreads;
