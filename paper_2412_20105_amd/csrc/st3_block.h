@@ -35,16 +35,17 @@ inline st3_status check_rows(const st3_rows* r, int heads, int D, int eb) {
 }
 
 // Whether a row of x (D elements) meets a row of y (Dy of them, or as many).  Of tensors with equal strides it is told exactly (slices of one buffer may
-// alternate); of others, all that lies between the first byte and the last counts.
+// alternate); of others, all that lies between the first byte and the last counts.  Where there are several rows, strides of rows are a row long at least.
 inline bool packed_rows_meet(const st3_rows* x, int hx, const st3_rows* y, int hy, int64_t T, int D, int eb, int Dy = -1) {
     const int64_t row = (int64_t)D * eb, row_y = Dy < 0 ? row : (int64_t)Dy * eb, d = (int64_t)(reinterpret_cast<intptr_t>(y->data) - reinterpret_cast<intptr_t>(x->data));
     auto extent = [&](const st3_rows* t, int h, int64_t last) { return ((h - 1) * t->stride_h + (T - 1) * t->stride_t) * eb + last; };
     if (d >= extent(x, hx, row) || -d >= extent(y, hy, row_y)) return false;
-    if (x->stride_t != y->stride_t || x->stride_h != y->stride_h) return true;
+    // (one row of each, or one head: that stride says nothing, and may be 0)
+    if ((T > 1 && x->stride_t != y->stride_t) || ((hx > 1 || hy > 1) && x->stride_h != y->stride_h)) return true;
     const int64_t sh = x->stride_h * eb, st = x->stride_t * eb;
     for (int64_t h = 1 - hx; h < hy; ++h) {
         // rows i of x and j of y begin gap + (j - i) * st apart; the two nearest values of j - i on either side of -gap / st
-        const int64_t gap = d + h * sh, near = -gap / st;
+        const int64_t gap = d + h * sh, near = T > 1 ? -gap / st : 0;
         for (int64_t k = near - 1; k <= near + 1; ++k)
             if (k > -T && k < T && gap + k * st < row && -(gap + k * st) < row_y) return true;
     }
