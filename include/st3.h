@@ -580,7 +580,8 @@ ST3_EXPORT size_t st3_block_workspace_bytes(const st3_gqa_shape* shape, int32_t 
  * (no rows: out = 0).  score may be NULL; its rows hold max_len + 1 entries at least.
  * A logit that is NaN or +infinity makes its head's output and all of that head's weights NaN, and so the key head's scores of the rows up
  * to r; one of -infinity weighs nothing, and where all are, out = 0 and so are the weights.
- * out shares no memory with k_new or v_new.
+ * out shares no memory with k_new or v_new; it may be q itself, row for row, and else shares none with q either (rows of one buffer may
+ * alternate where the strides are equal).
  * The cache's `len` still says r behind the call.
  * ------------------------------------------------------------------------------------------- */
 ST3_EXPORT st3_status st3_block_decode(const st3_gqa_shape* shape, const st3_rows* q, const st3_rows* k_new, const st3_rows* v_new,

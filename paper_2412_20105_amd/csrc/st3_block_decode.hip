@@ -568,8 +568,10 @@ extern "C" st3_status st3_block_decode(const st3_gqa_shape* shape, const st3_row
     const Cut cut = cut_of(shape, max_len, score != nullptr);
     const BlockWs wl = block_ws(shape, max_len, score != nullptr);
     if (workspace_bytes < st3_block_workspace_bytes(shape, max_len)) return ST3_ERR_WORKSPACE_TOO_SMALL;
-    // (a workgroup's output may be written before another has read the new row)
+    // (a workgroup's output may be written before another has read the new row, or queries that are not the first one's own)
     if (k_new && (packed_rows_meet(k_new, Hk, out, H, B, D, 2) || packed_rows_meet(v_new, Hk, out, H, B, D, 2))) return ST3_ERR_INVALID_ARG;
+    const bool in_place = q->data == out->data && (B == 1 || q->stride_t == out->stride_t) && (H == 1 || q->stride_h == out->stride_h);
+    if (!in_place && packed_rows_meet(q, H, out, H, B, D, 2)) return ST3_ERR_INVALID_ARG;
     char* ws = reinterpret_cast<char*>(workspace);
     auto bits = [](const st3_rows* r) { return r ? reinterpret_cast<uint16_t*>(r->data) : nullptr; };
     BlockDecodeArgs a{};
