@@ -96,7 +96,10 @@ class BlockGeneration:
         return max(0, max(self.lens))
 
     def prefill_layer(self, l: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Packed prompts (slices of a fused projection's output are fine) of layer l: attended, and stored."""
+        """Packed prompts (slices of a fused projection's output are fine) of layer l: attended, and stored.  As many rows
+        as the lengths that begin() was told have together."""
+        if not q.shape[0] == k.shape[0] == v.shape[0] == self.total:
+            raise ValueError(f"{q.shape[0]}, {k.shape[0]} and {v.shape[0]} rows of q, k and v: {self.total} expected, the lengths' sum")
         if out is None:
             out = torch.empty((q.shape[0], self.H, self.d), dtype=q.dtype, device=q.device)
         if self.total == 0:
