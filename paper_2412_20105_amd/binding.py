@@ -327,6 +327,8 @@ def block_cache(k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Ten
         raise TypeError("scales are float32, tails bfloat16")
     if table.shape[1] > 1 and table.stride(1) != 1:
         raise ValueError("the blocks of a sequence follow each other in the table")
+    if batch > 1 and table.stride(0) < table.shape[1]:
+        raise ValueError("the table's rows lie one behind the other")
     if kv_len.dim() != 1 or not (kv_len.is_contiguous()):
         raise ValueError("kv_len: [batch], contiguous, expected")
     c = BlockCache(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_tail.data_ptr(), v_tail.data_ptr(),
