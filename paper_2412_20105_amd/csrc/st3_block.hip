@@ -454,8 +454,9 @@ extern "C" st3_status st3_block_store(const st3_gqa_shape* shape, const st3_rows
     if (s != ST3_OK) return s;
     if ((s = check_block_cache(shape, cache)) != ST3_OK) return s;
     const int Hk = shape->kv_heads, D = shape->head_dim;
-    if ((s = check_rows(k, Hk, D, 2)) != ST3_OK || (s = check_rows(v, Hk, D, 2)) != ST3_OK) return s;
     if (!cu_len || total < 0 || max_len < 0 || max_len > total) return ST3_ERR_INVALID_ARG;
+    if (total == 0) return ST3_OK;          // (an empty tensor may have no address)
+    if ((s = check_rows(k, Hk, D, 2)) != ST3_OK || (s = check_rows(v, Hk, D, 2)) != ST3_OK) return s;
     const int blocks = (max_len + kBlk - 1) / kBlk;
     if (blocks == 0) return ST3_OK;
     if (blocks > 65535) return ST3_ERR_UNSUPPORTED;
