@@ -6,6 +6,10 @@
 namespace st3 {
 
 constexpr int kBlk = ST3_BLOCK_TOKENS;      // rows of a block
+constexpr int kMostRows = 0x3fffffff;       // rows of a sequence: what is added to them on the way stays below 2^31
+
+// The limits of a grid: y, and x in threads.
+inline bool grid_fits(int64_t x, int threads, int64_t y) { return x * threads < (int64_t)1 << 32 && y <= 65535; }
 
 inline st3_status check_gqa_shape(const st3_gqa_shape* s) {
     if (!s) return ST3_ERR_INVALID_ARG;

@@ -457,8 +457,8 @@ extern "C" st3_status st3_block_store(const st3_gqa_shape* shape, const st3_rows
     if (!cu_len || total < 0 || max_len < 0 || max_len > total) return ST3_ERR_INVALID_ARG;
     if (total == 0) return ST3_OK;          // (an empty tensor may have no address)
     if ((s = check_rows(k, Hk, D, 2)) != ST3_OK || (s = check_rows(v, Hk, D, 2)) != ST3_OK) return s;
-    const int blocks = (max_len + kBlk - 1) / kBlk;
-    if (blocks == 0) return ST3_OK;
+    if (max_len == 0) return ST3_OK;
+    const int blocks = (max_len - 1) / kBlk + 1;
     if (blocks > 65535) return ST3_ERR_UNSUPPORTED;
     if (cache->table_blocks < max_len / kBlk) return ST3_ERR_INVALID_ARG;
     const StoreArgs a{block_pages(cache), reinterpret_cast<const uint16_t*>(k->data), reinterpret_cast<const uint16_t*>(v->data), k->stride_t, k->stride_h,
@@ -495,6 +495,7 @@ extern "C" st3_status st3_block_evict(const st3_gqa_shape* shape, const st3_bloc
         const int64_t d = reinterpret_cast<intptr_t>(x) - reinterpret_cast<intptr_t>(y);
         if (d < tail && -d < tail) return ST3_ERR_INVALID_ARG;
     }
+    if (max_len > kMostRows) return ST3_ERR_UNSUPPORTED;
     const int blocks = (most + kBlk - 1) / kBlk;
     if (blocks > 65535) return ST3_ERR_UNSUPPORTED;
     const bool in_place = score == to_score && (B == 1 || score_stride_b == to_score_stride_b) && (Hk == 1 || score_stride_h == to_score_stride_h);

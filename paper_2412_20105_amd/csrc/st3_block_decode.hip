@@ -526,6 +526,9 @@ inline BlockWs block_ws(const st3_gqa_shape* s, int max_len, bool scored) {
     return w;
 }
 
+// Workgroups of the launch behind the chunks, for a sequence.
+inline int64_t finish_groups(int H, int Hk, int max_len, bool scored) { return H + (scored ? (int64_t)Hk * ((max_len + kScoreKeys) / kScoreKeys) : 0); }
+
 template <int D, int CODE>
 void launch_decode(const BlockDecodeArgs& a, int B, int waves, hipStream_t st) {
     const int cols = std::min(kCols, a.G);
@@ -537,8 +540,7 @@ void launch_decode(const BlockDecodeArgs& a, int B, int waves, hipStream_t st) {
         return;
     }
     block_attend_kernel<D, CODE, 4, false><<<dim3(a.Hk * a.QG, a.nsplit, B), 256, attend_lds<D>(4, cols, a.score ? a.chunk * kBlk : 0), st>>>(a);
-    const int tiles = a.score ? (a.max_len + 1 + kScoreKeys - 1) / kScoreKeys : 0;
-    block_finish_kernel<D><<<dim3(a.H + a.Hk * tiles, B), kFinishThreads, 0, st>>>(a);
+    block_finish_kernel<D><<<dim3((unsigned)finish_groups(a.H, a.Hk, a.max_len, a.score != nullptr), B), kFinishThreads, 0, st>>>(a);
 }
 
 }  // namespace
@@ -560,13 +562,15 @@ extern "C" st3_status st3_block_decode(const st3_gqa_shape* shape, const st3_row
     if ((s = check_rows(q, H, D, 2)) != ST3_OK || (s = check_rows(out, H, D, 2)) != ST3_OK) return s;
     if (!k_new != !v_new) return ST3_ERR_INVALID_ARG;
     if (k_new && ((s = check_rows(k_new, Hk, D, 2)) != ST3_OK || (s = check_rows(v_new, Hk, D, 2)) != ST3_OK)) return s;
-    if (max_len < 0 || max_len > 0x3fffffff) return ST3_ERR_INVALID_ARG;
+    if (max_len < 0 || max_len > kMostRows) return ST3_ERR_INVALID_ARG;
     // (a row that fills its block needs that block's page)
     if (cache->table_blocks < (max_len + (k_new ? 1 : 0)) / kBlk) return ST3_ERR_INVALID_ARG;
     if (score && (score_stride_h < (int64_t)max_len + 1 || (B > 1 && score_stride_b < (int64_t)max_len + 1))) return ST3_ERR_INVALID_ARG;
     if (!workspace || !aligned16(workspace)) return ST3_ERR_INVALID_ARG;
     const Cut cut = cut_of(shape, max_len, score != nullptr);
     const BlockWs wl = block_ws(shape, max_len, score != nullptr);
+    if (cut.chunk > 0 && !(grid_fits(1, 1, wl.nsplit) && grid_fits(finish_groups(H, Hk, max_len, score != nullptr), kFinishThreads, B)))
+        return ST3_ERR_UNSUPPORTED;
     if (workspace_bytes < st3_block_workspace_bytes(shape, max_len)) return ST3_ERR_WORKSPACE_TOO_SMALL;
     // (a workgroup's output may be written before another has read the new row, or queries that are not the first one's own)
     if (k_new && (packed_rows_meet(k_new, Hk, out, H, B, D, 2) || packed_rows_meet(v_new, Hk, out, H, B, D, 2))) return ST3_ERR_INVALID_ARG;

@@ -762,7 +762,7 @@ extern "C" st3_status st3_packed_attention(const st3_gqa_shape* shape, const st3
     if (total == 0) return ST3_OK;          // (an empty tensor may have no address)
     for (auto [r, h] : {std::pair{q, H}, {k, Hk}, {v, Hk}, {out, H}})
         if ((s = check_rows(r, h, D, eb)) != ST3_OK) return s;
-    if ((int64_t)max_len * G > 0x3fffffff || k->stride_t * eb * 32 >= (int64_t)1 << 31 || v->stride_t * eb * 32 >= (int64_t)1 << 31) return ST3_ERR_UNSUPPORTED;
+    if ((int64_t)max_len * G > kMostRows || k->stride_t * eb * 32 >= (int64_t)1 << 31 || v->stride_t * eb * 32 >= (int64_t)1 << 31) return ST3_ERR_UNSUPPORTED;
     if (max_len == 0) return ST3_OK;
     if (packed_rows_meet(q, H, out, H, total, D, eb) || packed_rows_meet(k, Hk, out, H, total, D, eb) || packed_rows_meet(v, Hk, out, H, total, D, eb))
         return ST3_ERR_INVALID_ARG;
@@ -780,7 +780,7 @@ extern "C" st3_status st3_packed_attention(const st3_gqa_shape* shape, const st3
     a.levels = (int)(((int64_t)max_len * G + rows - 1) / rows);
     a.spread = (kSpread + Hk - 1) / Hk;
     const int64_t tiles = packed_tiles(shape, total, max_len, rows);
-    if (tiles * Hk > 0x7fffffff) return ST3_ERR_UNSUPPORTED;
+    if (!grid_fits(tiles * Hk, shape->dtype == ST3_BF16 ? 256 * cut.split : 256, 1)) return ST3_ERR_UNSUPPORTED;
     if (score && (max_len + 63) / 64 > 65535) return ST3_ERR_UNSUPPORTED;
     const unsigned grid = (unsigned)(tiles * Hk);
     if (shape->dtype == ST3_BF16) {
