@@ -502,7 +502,7 @@ typedef struct {
 } st3_gqa_shape;
 
 /* Rows [T, heads, d] on the DEVICE: element (t,h,c) at data + t*stride_t + h*stride_h + c (strides in elements).
- * Rows are 16-byte aligned; a slice of a fused projection's output is one. */
+ * Rows are 16-byte aligned, strides d at least; a slice of a fused projection's output is one.  Those of an output do not lie on each other. */
 typedef struct {
     void*   data;
     int64_t stride_t, stride_h;

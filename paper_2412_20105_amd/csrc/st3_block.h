@@ -27,14 +27,24 @@ inline float gqa_scale_log2(const st3_gqa_shape* s) {
     return sc * kLog2e;
 }
 
-// Rows of eb-byte elements: 16-byte aligned, heads and rows far enough apart not to overlap themselves.
-inline st3_status check_rows(const st3_rows* r, int heads, int D, int eb) {
+// Rows of eb-byte elements: 16-byte aligned, no stride below a row (heads may lie outside rows: [H, T, d] seen as [T, H, d]).
+inline st3_status check_rows(const st3_rows* r, int D, int eb) {
     if (!r || !r->data) return ST3_ERR_INVALID_ARG;
-    if (r->stride_h < D || r->stride_t < (heads - 1) * r->stride_h + D) {
-        // (heads outside rows: [H, T, d] seen as [T, H, d])
-        if (r->stride_t < D || r->stride_h < D) return ST3_ERR_INVALID_ARG;
-    }
+    if (r->stride_t < D || r->stride_h < D) return ST3_ERR_INVALID_ARG;
     if (!aligned16(r->data) || r->stride_t * eb % 16 != 0 || r->stride_h * eb % 16 != 0) return ST3_ERR_INVALID_ARG;
+    return ST3_OK;
+}
+
+// Rows that are written, T of them: none lies on another.
+inline st3_status check_output(const st3_rows* r, int heads, int64_t T, int D, int eb) {
+    const st3_status s = check_rows(r, D, eb);
+    if (s != ST3_OK) return s;
+    if (T <= 1 || r->stride_t >= (heads - 1) * r->stride_h + D || r->stride_h >= (T - 1) * r->stride_t + D) return ST3_OK;
+    for (int64_t h = 1; h < heads; ++h) {           // head h of a row and head 0 of one of the two nearest to it
+        const int64_t at = h * r->stride_h, near = at / r->stride_t;
+        if (near < T && at - near * r->stride_t < D) return ST3_ERR_INVALID_ARG;
+        if (near + 1 < T && (near + 1) * r->stride_t - at < D) return ST3_ERR_INVALID_ARG;
+    }
     return ST3_OK;
 }
 

@@ -456,7 +456,7 @@ extern "C" st3_status st3_block_store(const st3_gqa_shape* shape, const st3_rows
     const int Hk = shape->kv_heads, D = shape->head_dim;
     if (!cu_len || total < 0 || max_len < 0 || max_len > total) return ST3_ERR_INVALID_ARG;
     if (total == 0) return ST3_OK;          // (an empty tensor may have no address)
-    if ((s = check_rows(k, Hk, D, 2)) != ST3_OK || (s = check_rows(v, Hk, D, 2)) != ST3_OK) return s;
+    if ((s = check_rows(k, D, 2)) != ST3_OK || (s = check_rows(v, D, 2)) != ST3_OK) return s;
     if (max_len == 0) return ST3_OK;
     const int blocks = (max_len - 1) / kBlk + 1;
     if (blocks > 65535) return ST3_ERR_UNSUPPORTED;

@@ -559,9 +559,9 @@ extern "C" st3_status st3_block_decode(const st3_gqa_shape* shape, const st3_row
     if (s != ST3_OK) return s;
     if ((s = check_block_cache(shape, cache)) != ST3_OK) return s;
     const int B = shape->batch, H = shape->heads, Hk = shape->kv_heads, D = shape->head_dim, G = H / Hk;
-    if ((s = check_rows(q, H, D, 2)) != ST3_OK || (s = check_rows(out, H, D, 2)) != ST3_OK) return s;
+    if ((s = check_rows(q, D, 2)) != ST3_OK || (s = check_output(out, H, B, D, 2)) != ST3_OK) return s;
     if (!k_new != !v_new) return ST3_ERR_INVALID_ARG;
-    if (k_new && ((s = check_rows(k_new, Hk, D, 2)) != ST3_OK || (s = check_rows(v_new, Hk, D, 2)) != ST3_OK)) return s;
+    if (k_new && ((s = check_rows(k_new, D, 2)) != ST3_OK || (s = check_rows(v_new, D, 2)) != ST3_OK)) return s;
     if (max_len < 0 || max_len > kMostRows) return ST3_ERR_INVALID_ARG;
     // (a row that fills its block needs that block's page)
     if (cache->table_blocks < (max_len + (k_new ? 1 : 0)) / kBlk) return ST3_ERR_INVALID_ARG;

@@ -5,7 +5,6 @@
 // causal edge wastes little).  A workgroup takes kRows such rows of a pair and walks the key tiles up to its last position.
 #include <algorithm>
 #include <type_traits>
-#include <utility>
 
 #include "st3_block.h"
 
@@ -760,8 +759,9 @@ extern "C" st3_status st3_packed_attention(const st3_gqa_shape* shape, const st3
     const int H = shape->heads, Hk = shape->kv_heads, D = shape->head_dim, eb = elem_bytes(shape->dtype), G = H / Hk;
     if (!cu_len || total < 0 || max_len < 0 || max_len > total || window < 0) return ST3_ERR_INVALID_ARG;
     if (total == 0) return ST3_OK;          // (an empty tensor may have no address)
-    for (auto [r, h] : {std::pair{q, H}, {k, Hk}, {v, Hk}, {out, H}})
-        if ((s = check_rows(r, h, D, eb)) != ST3_OK) return s;
+    for (const st3_rows* r : {q, k, v})
+        if ((s = check_rows(r, D, eb)) != ST3_OK) return s;
+    if ((s = check_output(out, H, total, D, eb)) != ST3_OK) return s;
     if ((int64_t)max_len * G > kMostRows || k->stride_t * eb * 32 >= (int64_t)1 << 31 || v->stride_t * eb * 32 >= (int64_t)1 << 31) return ST3_ERR_UNSUPPORTED;
     if (max_len == 0) return ST3_OK;
     if (packed_rows_meet(q, H, out, H, total, D, eb) || packed_rows_meet(k, Hk, out, H, total, D, eb) || packed_rows_meet(v, Hk, out, H, total, D, eb))
