@@ -24,7 +24,7 @@
  *     returns a non-zero st3_status and enqueues nothing.  A failed HIP launch returns
  *     ST3_ERR_HIP and st3_last_hip_error() gives the hipError_t (thread-local).
  *   - Element types: ST3_F32 (4 bytes) or ST3_BF16 (2 bytes, upper half of an IEEE float32).
- *     Arithmetic is float32 throughout; outputs are rounded to the element type (nearest even).
+ *     Arithmetic is float32 unless a call names what it rounds further; outputs are rounded to the element type (nearest even).
  *   - head_dim must be 64 or 128.  Rows of head_dim elements are contiguous and 16-byte aligned;
  *     strides are given in ELEMENTS unless a parameter says bytes.
  *   - Counts of kept tokens are integers chosen by the caller (see the schedule helpers below);
@@ -518,6 +518,8 @@ ST3_EXPORT size_t st3_packed_workspace_bytes(const st3_gqa_shape* shape, int32_t
  *   A_h[i,:]     = softmax over j <= i of (q_h[i] . k_{h/G}[j]) * scale,   G = heads / kv_heads
  *   out[i,h,:]   = sum_j A_h[i,j] v_{h/G}[j]
  *   score[b,kh,j] = sum_{h in group kh} sum_{i in last `window` rows, i >= j} A_h[i,j],  j in [0, n_b)
+ * Logits, maxima, sums and scores are float32.  ST3_BF16: in the product with v each exp(logit - maximum) is rounded to bf16 once, to
+ * nearest (off by 2^-8 of itself at most, without bias), beside the output's own rounding; its sum is that of the unrounded ones.
  * total: rows that q, k, v and out have.  max_len: HOST upper bound of n_b; rows of a sequence past it
  * are not attended.  score: DEVICE float32, row (b,kh) at score + b*score_stride_b + kh*score_stride_h,
  * or NULL; entries from n_b on are left untouched; the caller's rows hold max_len entries at least.  window >= 1 when a
@@ -578,6 +580,8 @@ ST3_EXPORT size_t st3_block_workspace_bytes(const st3_gqa_shape* shape, int32_t 
  *   score[b,kh,j] += sum_{h in group kh} p_h[j]  for j < r,   score[b,kh,r] = that sum at r
  * q, out: [batch, H, d] rows, k_new, v_new: [batch, Hk, d].  k_new and v_new NULL: rows 0 .. r - 1 are attended and nothing is appended
  * (no rows: out = 0).  score may be NULL; its rows hold max_len + 1 entries at least.
+ * Logits, maxima, sums and scores are float32; in the product with v a weight, times v's scale, is held as two bf16 terms (off by 2^-16 of
+ * itself at most), so that an infinity in v gives an infinity or NaN.
  * A logit that is NaN or +infinity makes its head's output and all of that head's weights NaN, and so the key head's scores of the rows up
  * to r; one of -infinity weighs nothing, and where all are, out = 0 and so are the weights.
  * out shares no memory with k_new or v_new; it may be q itself, row for row, and else shares none with q either (rows of one buffer may

@@ -519,7 +519,8 @@ def st3_packed_workspace_bytes(shape: GqaShape, total: int) -> int:
 
 
 def st3_packed_attention(shape: GqaShape, q, k, v, cu_len, max_len: int, out, window: int = 0, score=None, workspace=None, stream=None) -> None:
-    """q, out [T, H, d]; k, v [T, Hk, d]; cu_len int32 [batch + 1]; score float32 [batch, Hk, >= max_len] or None."""
+    """q, out [T, H, d]; k, v [T, Hk, d]; cu_len int32 [batch + 1]; score float32 [batch, Hk, >= max_len] or None.
+    bf16: weights are rounded to bf16 once in the product with v; everything else is float32."""
     total = q.shape[0]
     H, Hk = shape.heads, shape.kv_heads
     if cu_len.shape != (shape.batch + 1,) or not cu_len.is_contiguous():

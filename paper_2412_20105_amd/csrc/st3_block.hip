@@ -307,8 +307,8 @@ __global__ __launch_bounds__(kRankThreads) void block_rank_kernel(EvictBlockArgs
 
 // Workgroup (K or V of a key head, new block, sequence).  K's rows are fetched one by one; any row of a page lies in all lines of its V, so V comes
 // as whole pages, two at a time (a block's rows ascend: a few pages that follow each other), and is picked from LDS.  (Picked byte by byte from
-// memory it kept the address units busy: 32 caches 84 us.)  32 caches of 611 to 3136 rows to 1500 rows: 190 MB in 51 us, 3.7 TB/s, the vector units
-// busy for 58 % of it with codes, values and quotients; with registers for 5 waves a SIMD instead of 6 it takes 59.
+// memory it kept the address units busy: 32 caches 84 us.)  32 caches of 611 to 3136 rows to 1500 rows: 189 MB in 52 us, 3.6 TB/s, the vector units
+// busy for 51 % of the cycles with codes, values and quotients; with registers for 5 waves a SIMD instead of 6 it takes 59.
 constexpr int kPageRow = kBlk + 8;          // bytes: the 4 columns that a wave picks at a time, 8 apart, are 16 banks apart
 template <int D, int CODE, bool COLUMNS>
 __device__ __forceinline__ void move_block(const EvictBlockArgs& a, int kh, int j, int b, uint8_t* pages, uint32_t* sm) {

@@ -7,9 +7,9 @@
 //   S^T = K Q^T    product t of four: row 4g'+i of A is key 16 g' + 4 t + i, so that lane (c, g) of C ends with keys 16 g .. 16 g + 15 of query c.
 //                  A lane reads 16 codes of its row at once: columns 64 x + 16 g .. + 15, contraction steps 2 x and 2 x + 1.
 //   O^T = V^T P^T  the lane's 16 keys are the contraction slots 8g..8g+7 of two steps: P^T is where S^T left it, and V^T, whose rows lie in
-//                  memory, is read 16 codes at a time too.  P is two bf16 terms (16 significant bits: what is left out is 2^-17 of a weight at most).
+//                  memory, is read 16 codes at a time too.  P is two bf16 terms (16 significant bits: what is left out is 2^-16 of a weight at most).
 // No value crosses lanes but the maximum.  Bound by memory: K goes straight to LDS, a block ahead, V into registers.  2 sequences of 70000 and
-// 131072 rows, 32 heads over 8 of 128: 489 MB in 107 us, 4.6 TB/s (a large copy: 5.0); 32 of 611 to 3136 rows, 114 MB in 28.5 us.
+// 131072 rows, 32 heads over 8 of 128: 489 MB in 107 us, 4.6 TB/s (a large copy: 4.8); 32 of 611 to 3136 rows, 114 MB in 28.5 us.
 #include <algorithm>
 
 #include "st3_block.h"
@@ -480,7 +480,10 @@ __global__ __launch_bounds__(kFinishThreads) void block_finish_kernel(BlockDecod
 // How a call is cut: waves of a workgroup, blocks of a chunk (0: whole strips, one launch).
 //   Whole strips while there are enough to fill the card, or while they are so short that the second launch of a cut costs more than it
 //   brings (with their logits in LDS, up to what there is of it).  us a call, whole / cut: 64 strips of 32 blocks 18.3 / 14.2, 8 strips of 12 blocks
-//   10.0 / 12.6, 256 strips of 10 to 49 blocks 28.5 / 36.9.
+//   10.0 / 12.6, 256 strips of 10 to 49 blocks 28.5 / 36.9.  Lengths are known to the device only, so the rule goes by the longest that may come and
+//   takes strips for equal: that holds at 256 of 49 blocks (38.8 / 42.5, with scores 42.5 / 52.3) and of 188 (136 / 140), not where one sequence is far
+//   longer than the others, whose strips are then walked by one unit each.  248 strips of 11 blocks and 8 of 63: 29.5 / 23.7, of 125 48.9 / 31.3, of
+//   250 87.5 / 47.1, of 625 204 / 96; 280 of 11 and 40 of 49, with scores, 35.7 / 30.3, 40 of 250 127 / 58.
 //   Workgroups of 12 waves, one on a compute unit, where strips are no more than compute units, else of 4 waves, three on a unit.  12 / 4: 256 strips
 //   28.5 / 31.7, 320 strips of 11 to 20 blocks 22.6 / 19.2.
 //   Chunks for about three workgroups on a unit; where logits are kept, no longer than leaves room for three in LDS.  16 strips of 1100 to 2049 blocks: 20
