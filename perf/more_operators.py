@@ -204,7 +204,7 @@ def prepare(c, seed):
     s["v_tail"] = _randn(g, (B, Hk, d, BLOCK), sigma, torch.bfloat16)
     s["len"] = torch.tensor(old, dtype=torch.int32, device=DEV)
     s["cu"] = torch.tensor([0] + new, device=DEV).cumsum(0).to(torch.int32)
-    s["old_top"], s["new_top"], s["top"], s["scale"] = max(old), max(new), max(both), 1.0 / math.sqrt(d)
+    s["new_top"], s["top"], s["scale"] = max(new), max(both), 1.0 / math.sqrt(d)
     # one matrix product gives a token's queries, keys and values: rows of one tensor
     qkv = _randn(g, (M, H + 2 * Hk, d), sigma, torch.bfloat16)
     if c["op"] == "append":
@@ -246,7 +246,7 @@ def _handle(s):
         h["shape"] = st3.gqa_shape(c["batch"], c["heads"], c["kv_heads"], c["dim"])
         h["cache"] = st3.block_cache(s["k_codes"], s["v_codes"], s["k_scale"], s["v_scale"], s["k_tail"], s["v_tail"], s["table"], s["len"])
     if c["op"] == "attend":
-        need = st3.st3_block_attend_workspace_bytes(h["shape"], s["q"].shape[0], s["new_top"], s["old_top"])
+        need = st3.st3_block_attend_workspace_bytes(h["shape"], s["q"].shape[0], s["new_top"], s["top"])
         h["ws"] = torch.empty(need, dtype=torch.uint8, device=DEV)
     return h
 
@@ -263,12 +263,12 @@ def _own_rotate(s):
 
 def _own_append(s):
     h = s.get("handle") or _handle(s)
-    h["st3"].st3_block_append(h["shape"], s["k"], s["v"], s["cu"], s["new_top"], h["cache"], s["old_top"], h["rotary"])
+    h["st3"].st3_block_append(h["shape"], s["k"], s["v"], s["cu"], s["new_top"], h["cache"], s["top"], h["rotary"])
 
 
 def _own_attend(s):
     h = s.get("handle") or _handle(s)
-    h["st3"].st3_block_attend(h["shape"], s["q"], s["cu"], s["new_top"], h["cache"], s["old_top"], s["out"], s["case"]["window"], s["score"], h["ws"])
+    h["st3"].st3_block_attend(h["shape"], s["q"], s["cu"], s["new_top"], h["cache"], s["top"], s["out"], s["case"]["window"], s["score"], h["ws"])
 
 
 # -- plain forms --------------------------------------------------------------------------------------------------------------------
