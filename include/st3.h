@@ -613,6 +613,69 @@ ST3_EXPORT st3_status st3_block_evict(const st3_gqa_shape* shape, const st3_bloc
                                       int64_t kept_stride_b, int64_t kept_stride_h, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * The next turn: several new tokens for sequences that have a cache (the next question of a dialogue, a piece of a long prompt, tokens that
+ * were drafted and are to be checked).  Once a step the tokens' positions become a table of cosines and sines
+ * (st3_rotary_table), for all layers; in each layer queries are rotated by it (st3_rotate_rows), keys, on the way, and values are appended to the
+ * cache (st3_block_append), and the new tokens attend to everything up to themselves (st3_block_attend).
+ * ------------------------------------------------------------------------------------------- */
+
+/* table[t][c] = (cos, sin) of positions[axis[c]][t] * inv_freq[c]: the angle by which pair c of token t's columns turns.
+ * positions: DEVICE int32, [axes][total], a token's components (time, height, width ...) in rows position_stride entries apart; 1 to 4 axes.
+ * axis: HOST [pairs], each below axes, or NULL where all are 0.  inv_freq: DEVICE float32 [pairs].  pairs: 8 to 64, a multiple of 8.
+ * table: DEVICE float32, row t at table + t*table_stride (at least 2*pairs, a multiple of 4; 16-byte aligned): cosine, sine, pair by pair.
+ * Angles are formed and reduced in 64 bits, so a far position costs nothing: cosine and sine are off by 2^-23 at most, up to
+ * angles of 2^40 either way.  An inv_freq that is not finite gives NaN. */
+ST3_EXPORT st3_status st3_rotary_table(int32_t axes, int32_t pairs, const uint8_t* axis, const float* inv_freq, const int32_t* positions,
+                                       int64_t position_stride, int32_t total, float* table, int64_t table_stride, void* stream);
+
+/* Which columns make pair c: c and c + pairs, or 2c and 2c + 1.  Columns from 2*pairs on do not turn. */
+typedef enum { ST3_ROTARY_HALVES = 0, ST3_ROTARY_ADJACENT = 1 } st3_rotary_layout;
+
+/* A rotation of packed rows: row t of the table (as st3_rotary_table leaves it, or any other cosines and sines) turns row t. */
+typedef struct {
+    const float* table;     /* DEVICE float32, 16-byte aligned */
+    int64_t stride_t;       /* floats; at least 2*pairs, a multiple of 4 */
+    int32_t pairs;          /* 8 .. head_dim/2, a multiple of 8 */
+    int32_t layout;         /* st3_rotary_layout */
+} st3_rotary;
+
+/* out[t,h] = x[t,h] with each pair (a, b) of its columns turned: (a cos - b sin, b cos + a sin); inverse: the other way, which is also what a gradient
+ * with respect to out becomes as one with respect to x.  x, out: [total, heads, head_dim] rows of `dtype`.  Each product, and their sum, is
+ * rounded to float32, then to the element type.  out may be x itself, row for row, and else shares no memory with it; it shares none with the table. */
+ST3_EXPORT st3_status st3_rotate_rows(const st3_rows* x, const st3_rows* out, int32_t heads, int32_t total, int32_t head_dim, int32_t dtype,
+                                      const st3_rotary* rotary, int32_t inverse, void* stream);
+
+/* Rows behind those that sequences have.  With n = len[b] and m = cu_len[b+1] - cu_len[b], packed as for st3_packed_attention; max_new and max_len: HOST
+ * bounds of m and of n + m (rows past either are left out):
+ *   rows n .. n + m - 1 of sequence b <- rows cu_len[b] .. of k, turned by rotary where it is not NULL and rounded to bf16, and of v.
+ * Blocks that are whole then are coded into their pages from rows of 16 bits, those in the tail among them, the rest goes into the tail: the
+ * cache is the same, bit for bit, however the rows are cut into calls (st3_block_store, st3_block_decode and this one).
+ * len still says n behind the call.  A place with a negative length stays as it is. */
+ST3_EXPORT st3_status st3_block_append(const st3_gqa_shape* shape, const st3_rows* k, const st3_rows* v, const int32_t* cu_len, int32_t total,
+                                       int32_t max_new, const st3_block_cache* cache, int32_t max_len, const st3_rotary* rotary, void* stream);
+
+/* Bytes of DEVICE workspace that st3_block_attend needs for `total` packed rows, max_new of a sequence at most, in caches of at most max_len rows then.
+ * What is enough for these is enough for less. */
+ST3_EXPORT size_t st3_block_attend_workspace_bytes(const st3_gqa_shape* shape, int32_t total, int32_t max_new, int32_t max_len);
+
+/* Causal attention of new tokens over a cache that holds them already (st3_block_append; len still says n, the rows in front of them).
+ * Row t of a sequence's m packed rows sees its rows 0 .. n + t:
+ *   p_h[t] = softmax over those of (q_h[t] . k_{h/G}) * scale,   out[t,h,:] = sum_j p_h[t][j] v_{h/G}[j]
+ *   score[b,kh,j] += sum_{h in group kh} sum_{t in the last `window` of the m rows, n + t >= j} p_h[t][j]  for j < n; = that sum for n <= j < n + m
+ * q, out: [total, H, d] rows; the other arguments are those of st3_block_append and st3_packed_attention.  score may be NULL; its rows hold
+ * max_len entries at least, a sequence without new rows keeps its own.  window >= 1 when a score is wanted.
+ * Logits, maxima, sums and scores are float32; in the product with v a weight, times v's scale, is rounded to bf16 once, to nearest (off by 2^-8 of itself
+ * at most, without bias), beside the output's own rounding; sums of n + m such products, weights of up to 2^8, stay in float32 as long as no |v| is above
+ * 2^119 / (n + m).
+ * Rows whose table entry names no page are not attended, whatever lies there; a token that attends none gets out = 0, as do all of
+ * a place with a negative length.  A logit that is NaN or +infinity makes the token's output of that head NaN, and the key head's scores of the
+ * rows that the token sees, if it counts; one of -infinity weighs nothing, and where all are, out = 0.
+ * out shares no memory with q (rows of one buffer may alternate where the strides are equal). */
+ST3_EXPORT st3_status st3_block_attend(const st3_gqa_shape* shape, const st3_rows* q, const int32_t* cu_len, int32_t total, int32_t max_new,
+                                       const st3_block_cache* cache, int32_t max_len, const st3_rows* out, int32_t window, float* score,
+                                       int64_t score_stride_b, int64_t score_stride_h, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Diagnostic block.  Compiled into every build, inert by default: unless the environment held
  * ST3_DEBUG=1 when the library was loaded, every call below returns ST3_ERR_UNSUPPORTED and
  * changes nothing (st3_debug_enabled tells which).  The switches are process-wide and meant for

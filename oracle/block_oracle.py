@@ -1,4 +1,4 @@
-"""CPU oracle (float64 NumPy) of the calls for grouped heads: packed prompts, caches of 8-bit blocks, eviction by accumulated weight.
+"""CPU oracle (float64 NumPy) of the calls for grouped heads: packed prompts, caches of 8-bit blocks, further turns, eviction by accumulated weight.
 
 Written from the definitions in include/st3.h, row by row and head by head, sharing no code with the library.  A cache is
 kept as a list of rows for each (sequence, key head): whole blocks hold codes and a scale, the rows behind them plain values.
@@ -133,3 +133,42 @@ def evict(cache: BlockCache, b: int, score, keep: int, n_sink: int, n_recent: in
         state.append((blocks, [round_row(k[rest]), round_row(v[rest])]))
         rows.append(idx)
     return state, rows
+
+
+def rotary_table(positions, inv_freq, axis):
+    """[T, pairs, 2] cosines and sines (80-bit arithmetic: a position of 31 bits times a float32 has 55) of positions [axes, T]."""
+    angle = np.asarray(positions)[list(axis)].T.astype(np.longdouble) * np.asarray(inv_freq, np.float32).astype(np.longdouble)
+    two_pi = 8 * np.arctan(np.longdouble(1))
+    angle = angle - np.rint(angle / two_pi) * two_pi
+    return np.stack([np.cos(angle), np.sin(angle)], -1).astype(np.float64)
+
+
+def rotate(x, table, adjacent: bool, inverse: bool = False) -> np.ndarray:
+    """Rows x [T, H, d] turned, float32 with every product rounded by itself."""
+    x, table = np.asarray(x, np.float32), np.asarray(table, np.float32)
+    pairs = table.shape[1]
+    c, s = table[:, None, :, 0], table[:, None, :, 1] * np.float32(-1 if inverse else 1)
+    lead = slice(0, 2 * pairs, 2) if adjacent else slice(0, pairs)
+    rear = slice(1, 2 * pairs, 2) if adjacent else slice(pairs, 2 * pairs)
+    y, a, b = x.copy(), x[..., lead], x[..., rear]
+    with np.errstate(invalid="ignore", over="ignore"):
+        y[..., lead], y[..., rear] = a * c - b * s, b * c + a * s
+    return y
+
+
+def extend(cache: BlockCache, b: int, q, k_new, v_new, scale, window=0):
+    """New rows of sequence b (k_new, v_new [m, Hk, d], as the tail holds them): appended, then attended: out [m, H, d], the weights
+    [Hk, n + m] of the last `window` rows, and sums of p |v|."""
+    m, H = q.shape[:2]
+    n, G = cache.length(b), H // cache.Hk
+    out, spread, weights = np.zeros((m, H, cache.d)), np.zeros((m, H, cache.d)), np.zeros((cache.Hk, n + m))
+    for kh in range(cache.Hk):
+        cache.append(b, kh, k_new[:, kh], v_new[:, kh])
+        k, v = cache.values(b, kh)
+        for t in range(m):
+            for h in range(kh * G, (kh + 1) * G):
+                p = softmax_rows(q[t, h] @ k[:n + t + 1].T * scale)
+                out[t, h], spread[t, h] = p @ v[:n + t + 1], p @ np.abs(v[:n + t + 1])
+                if t >= m - window:
+                    weights[kh, :n + t + 1] += p
+    return out, weights, spread

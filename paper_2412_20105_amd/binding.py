@@ -25,6 +25,7 @@ ST3_KV_PLAIN, ST3_KV_E4M3 = 0, 1
 ST3_STABLE, ST3_HOLE_FILL = 0, 1
 ST3_BLOCK_INT8, ST3_BLOCK_E4M3 = 0, 1
 ST3_BLOCK_TOKENS = 64
+ST3_ROTARY_HALVES, ST3_ROTARY_ADJACENT = 0, 1
 ST3_ANNEAL_COS, ST3_ANNEAL_LINEAR, ST3_ANNEAL_EXP, ST3_ANNEAL_DROP, ST3_ANNEAL_NONE = 0, 1, 2, 3, 4
 
 EXPORTED = [
@@ -36,7 +37,8 @@ EXPORTED = [
     "st3_schedule_pvtp", "st3_schedule_linear", "st3_schedule_anneal", "st3_kv_bytes",
     "st3_debug_enabled", "st3_debug_set_prefill_path", "st3_debug_set_attend_tile", "st3_profile_enable", "st3_profile_read", "st3_overlap_topk",
     "st3_cosine_similarity", "st3_packed_workspace_bytes", "st3_packed_attention", "st3_block_store", "st3_block_workspace_bytes",
-    "st3_block_decode", "st3_block_evict",
+    "st3_block_decode", "st3_block_evict", "st3_rotary_table", "st3_rotate_rows", "st3_block_append", "st3_block_attend_workspace_bytes",
+    "st3_block_attend",
 ]
 
 
@@ -90,6 +92,10 @@ class BlockCache(C.Structure):
     _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
                 ("k_tail", C.c_void_p), ("v_tail", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int64),
                 ("len", C.c_void_p), ("table_blocks", C.c_int32), ("n_pages", C.c_int32), ("code", C.c_int32)]
+
+
+class Rotary(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("stride_t", C.c_int64), ("pairs", C.c_int32), ("layout", C.c_int32)]
 
 
 ST3_MAX_GATHER = 4
@@ -198,6 +204,17 @@ def lib() -> C.CDLL:
         L.st3_block_evict.argtypes = [P(GqaShape), P(BlockCache), P(BlockCache), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                       C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]
         L.st3_block_evict.restype = C.c_int
+        L.st3_rotary_table.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+        L.st3_rotary_table.restype = C.c_int
+        L.st3_rotate_rows.argtypes = [P(Rows), P(Rows), C.c_int32, C.c_int32, C.c_int32, C.c_int32, P(Rotary), C.c_int32, C.c_void_p]
+        L.st3_rotate_rows.restype = C.c_int
+        L.st3_block_append.argtypes = [P(GqaShape), P(Rows), P(Rows), C.c_void_p, C.c_int32, C.c_int32, P(BlockCache), C.c_int32, P(Rotary), C.c_void_p]
+        L.st3_block_append.restype = C.c_int
+        L.st3_block_attend_workspace_bytes.restype = C.c_size_t
+        L.st3_block_attend_workspace_bytes.argtypes = [P(GqaShape), C.c_int32, C.c_int32, C.c_int32]
+        L.st3_block_attend.argtypes = [P(GqaShape), P(Rows), C.c_void_p, C.c_int32, C.c_int32, P(BlockCache), C.c_int32, P(Rows), C.c_int32, C.c_void_p,
+                                       C.c_int64, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.st3_block_attend.restype = C.c_int
         L.st3_profile_enable.argtypes = [C.c_int32]
         L.st3_profile_enable.restype = C.c_int
         L.st3_profile_read.argtypes = [P(C.c_double), P(C.c_int64), P(C.c_double), P(C.c_double)]
@@ -274,6 +291,10 @@ def _rows(shape: GqaShape, t: torch.Tensor, heads: int, total: int) -> Rows:
         raise ValueError(f"rows {tuple(t.shape)}: ({total}, {heads}, {d}) expected")
     if t.dtype != _DTYPE_OF_CODE.get(shape.dtype) or not t.is_cuda:
         raise TypeError(f"rows of {t.dtype} on {t.device}: the shape says {_DTYPE_OF_CODE.get(shape.dtype)}, on the device")
+    return _strided(t, heads, total, d)
+
+
+def _strided(t: torch.Tensor, heads: int, total: int, d: int) -> Rows:
     st, sh, sc = t.stride()
     if sc != 1 and t.numel():
         raise ValueError("the elements of a row follow each other")
@@ -336,6 +357,27 @@ def block_cache(k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Ten
     c._refs = (k_codes, v_codes, k_scale, v_scale, k_tail, v_tail, table, kv_len)
     c._dims = (batch, hk, d)
     return c
+
+
+def rotary(table: torch.Tensor, layout: int = ST3_ROTARY_HALVES) -> Rotary:
+    """A rotation of packed rows by table [rows, pairs, 2] (float32: cosine, sine), as st3_rotary_table fills it; its rows may be those of a wider tensor."""
+    if table.dim() != 3 or table.shape[2] != 2 or (table.numel() and (table.stride(2) != 1 or table.stride(1) != 2)):
+        raise ValueError(f"table: [rows, pairs, 2], cosine and sine side by side, expected; {tuple(table.shape)} given")
+    if table.dtype != torch.float32 or not table.is_cuda:
+        raise TypeError(f"table: float32 on the device expected, {table.dtype} on {table.device} given")
+    rows, pairs, _ = table.shape
+    r = Rotary(table.data_ptr(), table.stride(0) if rows > 1 else 2 * pairs, pairs, layout)
+    r._refs = (table,)
+    r._rows = rows
+    return r
+
+
+def _check_rotary(r: Optional[Rotary], total: int):
+    if r is None:
+        return None
+    if r._rows != total:
+        raise ValueError(f"a rotation of {r._rows} rows for {total}")
+    return C.byref(r)
 
 
 def _check_cache(shape: GqaShape, cache: BlockCache) -> None:
@@ -569,6 +611,67 @@ def st3_block_evict(shape: GqaShape, src: BlockCache, dst: BlockCache, max_len: 
     i = _scores(shape, kept, "kept", keep, torch.int32)
     _check(lib().st3_block_evict(C.byref(shape), C.byref(src), C.byref(dst), max_len, keep, n_sink, n_recent, *s, *t, *i, _stream(stream)),
            "st3_block_evict")
+
+
+# -- the next turn: positions, rotation, further rows of a cache, attention over it ---------------
+def st3_rotary_table(positions, inv_freq, axis, table, stream=None) -> None:
+    """table [T, pairs, 2] <- cosines and sines.  positions int32 [axes, T] or [T]; inv_freq float32 [pairs]; axis: the component that turns each
+    pair, a sequence of pairs integers, or None where there is one."""
+    pos = positions if positions.dim() == 2 else positions[None]
+    axes, total = pos.shape
+    t = rotary(table)
+    if t._rows != total or inv_freq.shape != (t.pairs,) or not inv_freq.is_contiguous():
+        raise ValueError(f"{total} positions and {tuple(inv_freq.shape)} frequencies for a table of {tuple(table.shape)}")
+    if inv_freq.dtype != torch.float32 or not inv_freq.is_cuda:
+        raise TypeError(f"inv_freq: float32 on the device expected, {inv_freq.dtype} on {inv_freq.device} given")
+    if total > 1 and pos.stride(1) != 1:
+        raise ValueError("the positions of an axis follow each other")
+    of = None
+    if axis is not None:
+        axis = [int(i) for i in axis]
+        if len(axis) != t.pairs or not all(0 <= i < axes for i in axis):
+            raise ValueError(f"axis: {t.pairs} of 0 .. {axes - 1} expected, {axis} given")
+        of = bytes(axis)
+    _check(lib().st3_rotary_table(axes, t.pairs, of, inv_freq.data_ptr(), _ints(pos, "positions"), max(pos.stride(0), total) if axes > 1 else total, total,
+                                  t.table, t.stride_t, _stream(stream)), "st3_rotary_table")
+
+
+def st3_rotate_rows(x, out, rotary: Rotary, inverse: bool = False, stream=None) -> None:
+    """out [T, heads, d] <- x, turned; out may be x.  inverse: the other way (the gradient's)."""
+    if x.dim() != 3 or out.shape != x.shape or out.dtype != x.dtype or not x.is_cuda or not out.is_cuda:
+        raise ValueError(f"rows [T, heads, d] of one type on the device expected; {tuple(x.shape)} and {tuple(out.shape)} given")
+    total, heads, d = x.shape
+    _check(lib().st3_rotate_rows(C.byref(_strided(x, heads, total, d)), C.byref(_strided(out, heads, total, d)), heads, total, d, _dtype_code(x),
+                                 _check_rotary(rotary, total), int(inverse), _stream(stream)), "st3_rotate_rows")
+
+
+def _check_lengths(shape: GqaShape, cu_len) -> int:
+    if cu_len.shape != (shape.batch + 1,) or not cu_len.is_contiguous():
+        raise ValueError(f"cu_len: [{shape.batch + 1}], contiguous, expected")
+    return _ints(cu_len, "cu_len")
+
+
+def st3_block_append(shape: GqaShape, k, v, cu_len, max_new: int, cache: BlockCache, max_len: int, rotary: Optional[Rotary] = None, stream=None) -> None:
+    """Packed rows [T, Hk, d] behind the rows that the cache's sequences have (max_len at most with them); k turned by `rotary` on the way."""
+    _check_cache(shape, cache)
+    total, hk = k.shape[0], shape.kv_heads
+    _check(lib().st3_block_append(C.byref(shape), C.byref(_rows(shape, k, hk, total)), C.byref(_rows(shape, v, hk, total)), _check_lengths(shape, cu_len), total,
+                                  max_new, C.byref(cache), max_len, _check_rotary(rotary, total), _stream(stream)), "st3_block_append")
+
+
+def st3_block_attend_workspace_bytes(shape: GqaShape, total: int, max_new: int, max_len: int) -> int:
+    return lib().st3_block_attend_workspace_bytes(C.byref(shape), total, max_new, max_len)
+
+
+def st3_block_attend(shape: GqaShape, q, cu_len, max_new: int, cache: BlockCache, max_len: int, out, window: int, score, workspace, stream=None) -> None:
+    """q, out [T, H, d]: new rows that the cache holds already, behind its lengths (max_len at most with them); score float32 [batch, Hk, >= max_len]
+    or None.  Weights are rounded to bf16 once in the product with v; everything else is float32."""
+    _check_cache(shape, cache)
+    total, H = q.shape[0], shape.heads
+    sp, sb, sh = _scores(shape, score, "score", max_len)
+    _check(lib().st3_block_attend(C.byref(shape), C.byref(_rows(shape, q, H, total)), _check_lengths(shape, cu_len), total, max_new, C.byref(cache), max_len,
+                                  C.byref(_rows(shape, out, H, total)), window, sp, sb, sh, workspace.data_ptr(),
+                                  workspace.numel() * workspace.element_size(), _stream(stream)), "st3_block_attend")
 
 
 # -- host-only schedule helpers ---------------------------------------------------------------

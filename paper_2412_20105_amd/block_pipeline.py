@@ -1,4 +1,4 @@
-"""Call sequencing for decoders with grouped heads: packed prompts, caches of 8-bit blocks, eviction by accumulated weight.
+"""Call sequencing for decoders with grouped heads: packed prompts, caches of 8-bit blocks, further turns, eviction by accumulated weight.
 
 Beside `pipeline` (one prompt length, visual segments, Alg. 3), for batches of sequences of different lengths.  This module owns the page
 pool, tails, tables, scores and lengths and issues the library's calls; the only torch operations are allocations and the
@@ -14,7 +14,7 @@ from . import binding as st3
 
 
 class BlockGeneration:
-    """One batch of sequences through prompts, decode steps and evictions.
+    """One batch of sequences through prompts, decode steps, further turns and evictions.
 
         gen = BlockGeneration(layers, heads, kv_heads, head_dim, batch, capacity=4096, budget=2048)
         gen.begin(prompt_lens)
@@ -25,7 +25,13 @@ class BlockGeneration:
             for l in range(layers):
                 out = gen.decode_layer(l, q, k_new, v_new)  # [batch, heads or kv_heads, d]
             gen.finish_step()
+        gen.begin_turn(new_lens)                            # several new tokens at once: the next question, drafted tokens
+        for l in range(layers):
+            out = gen.extend_layer(l, q, k, v, rotary)      # [T, heads or kv_heads, d], packed like prompts
+        gen.finish_turn()
 
+    rotary (binding.rotary, of a table that st3_rotary_table made once for the turn) turns queries and keys on the way; without it they come
+    turned, as those of prefill_layer and decode_layer do.
     capacity: rows that a sequence may hold; when the longest has come to it, begin_step() has every key head of every layer keep
     `budget` rows of each longer sequence: the first n_sink, the last n_recent, and of the others those that have received the most
     attention weight so far, counted from the prompt's last `window` rows on.
@@ -70,6 +76,8 @@ class BlockGeneration:
         self._prompt_ws = torch.empty((0,), dtype=torch.uint8, device=device)
         self._out = torch.empty((layers, batch, heads, head_dim), **half)
         self.lens: List[int] = [-1] * batch     # host copies; negative: an empty place
+        self.new: Optional[List[int]] = None    # rows that the turn adds, while one is open
+        self._turn_ws = torch.empty((0,), dtype=torch.uint8, device=device)
         self.evictions = 0
 
     # ------------------------------------------------------------------------------------
@@ -78,7 +86,7 @@ class BlockGeneration:
         lens = [int(n) for n in prompt_lens]
         if len(lens) != self.B or min(lens) < -1 or max(lens) > self.capacity:
             raise ValueError(f"{self.B} lengths, up to {self.capacity}, expected; {lens} given")
-        self.lens, self.evictions = lens, 0
+        self.lens, self.evictions, self.new = lens, 0, None
         starts = [0]
         for n in lens:
             starts.append(starts[-1] + max(n, 0))
@@ -110,6 +118,8 @@ class BlockGeneration:
 
     def begin_step(self) -> None:
         """Makes room where a sequence has none left for the step's row."""
+        if self.new is not None:
+            raise ValueError("a turn is open: finish_turn() comes first")
         if self.longest >= self.capacity:
             self.evict()
 
@@ -121,6 +131,55 @@ class BlockGeneration:
     def finish_step(self) -> None:
         self.len.add_(self.live)
         self.lens = [n + 1 if n >= 0 else n for n in self.lens]
+
+    # ------------------------------------------------------------------------------------
+    def begin_turn(self, new_lens: Sequence[int]) -> None:
+        """A turn of so many new tokens of each sequence (an empty place has none); makes room where a sequence has too little."""
+        if self.new is not None:
+            raise ValueError("a turn is open: finish_turn() comes first")
+        new = [int(m) for m in new_lens]
+        if len(new) != self.B or min(new) < 0 or any(m and n < 0 for n, m in zip(self.lens, new)):
+            raise ValueError(f"{self.B} numbers of new tokens, none for an empty place, expected; {new} given")
+        if any(min(n, self.budget) + m > self.capacity for n, m in zip(self.lens, new)):
+            raise ValueError(f"{new} new tokens do not fit behind {self.budget} rows into {self.capacity}")
+        if any(n + m > self.capacity for n, m in zip(self.lens, new)):
+            self.evict()
+        starts = [0]
+        for m in new:
+            starts.append(starts[-1] + m)
+        image = torch.tensor(new + starts, dtype=torch.int32).to(self.device)
+        self.new, self.total, self._added, self.cu = new, starts[-1], image[:self.B], image[self.B:]
+        self._top = max(0, max(n + m for n, m in zip(self.lens, new)))
+        need = st3.st3_block_attend_workspace_bytes(self.shape, self.total, max(new), self._top)
+        if need > self._turn_ws.numel():
+            self._turn_ws = torch.empty((need,), dtype=torch.uint8, device=self.device)
+
+    def extend_layer(self, l: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rotary: Optional[st3.Rotary] = None,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The turn's packed rows in layer l: queries and keys turned, keys and values appended, queries attended; the scores go on."""
+        if self.new is None:
+            raise ValueError("no turn is open: begin_turn() comes first")
+        if not q.shape[0] == k.shape[0] == v.shape[0] == self.total:
+            raise ValueError(f"{q.shape[0]}, {k.shape[0]} and {v.shape[0]} rows of q, k and v: {self.total} expected, the new tokens' sum")
+        if out is None:
+            out = torch.empty((q.shape[0], self.H, self.d), dtype=q.dtype, device=q.device)
+        if self.total == 0:
+            return out
+        most, cache = max(self.new), self._sets[self._of[l]]
+        st3.st3_block_append(self.shape, k, v, self.cu, most, cache, self._top, rotary)
+        if rotary is not None:
+            turned = torch.empty((q.shape[0], self.H, self.d), dtype=q.dtype, device=q.device)
+            st3.st3_rotate_rows(q, turned, rotary)
+            q = turned
+        st3.st3_block_attend(self.shape, q, self.cu, most, cache, self._top, out, self.window, self.score[l], self._turn_ws)
+        return out
+
+    def finish_turn(self) -> None:
+        if self.new is None:
+            raise ValueError("no turn is open: begin_turn() comes first")
+        self.len.add_(self._added * self.live)
+        self.lens = [n + m if n >= 0 else n for n, m in zip(self.lens, self.new)]
+        self.new = None
 
     def retire(self, b: int) -> None:
         """Sequence b has ended: its place stays empty until the next begin()."""

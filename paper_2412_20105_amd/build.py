@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libst3.so")
 
 SOURCES = ["st3_api.hip", "st3_decode.hip", "st3_select.hip", "st3_prefill.hip", "st3_prefill_mfma.hip",
-           "st3_noalloc.hip", "st3_packed.hip", "st3_block.hip", "st3_block_decode.hip"]
+           "st3_noalloc.hip", "st3_packed.hip", "st3_block.hip", "st3_block_decode.hip",
+           "st3_block_attend.hip", "st3_rotary.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

@@ -1,4 +1,4 @@
-// The cache of 8-bit blocks: packed prompts into pages, and eviction by accumulated weight into other pages.
+// The cache of 8-bit blocks: packed prompts into pages, further rows behind them, and eviction by accumulated weight into other pages.
 //
 // A workgroup of 256 threads makes K or V of one block of one key head.  A thread holds four rows that follow each other and d / 16 columns that do
 // (Place): for K 16 threads in a row have a row group's columns, so that they read and write whole rows; for V they have a column's rows, so that
@@ -9,6 +9,7 @@
 #include <utility>
 
 #include "st3_block.h"
+#include "st3_rotary.h"
 
 namespace st3 {
 namespace {
@@ -146,6 +147,141 @@ __global__ __launch_bounds__(kThreads, 8) void block_store_kernel(StoreArgs a) {
     const int kh = blockIdx.x % a.Hk;
     if ((int)blockIdx.x < a.Hk) store_block<D, CODE, false>(a, kh, blockIdx.y, blockIdx.z, sm);
     else store_block<D, CODE, true>(a, kh, blockIdx.y, blockIdx.z, sm);
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// further rows: workgroup (K or V of a key head, block from the first that takes new rows on, sequence).  The first one alone reads the tail, and so it
+// also writes what is the tail afterwards.
+// ---------------------------------------------------------------------------------------------------------------------------------
+struct AppendArgs {
+    BlockPages c;
+    const uint16_t* k; const uint16_t* v;
+    int64_t k_st, k_sh, v_st, v_sh;
+    const int32_t* cu;
+    Rotation r;
+    int32_t total, max_new, max_len, Hk;
+};
+
+// Rows row .. + 3 (of those of the sequence) of a thread's columns, 16 bits each, turned on the way; rows outside [0, m) read the nearest.
+enum Turn { kStill, kHalves, kAdjacent };
+template <int D, bool COLUMNS, int TURN>
+__device__ __forceinline__ void new_rows(const AppendArgs& a, int kh, int start, int m, int row, int col, uint32_t (&raw)[4][D / 32]) {
+    constexpr int W = D / 16;
+    const uint16_t* src = COLUMNS ? a.v + kh * a.v_sh : a.k + kh * a.k_sh;
+    const int64_t stride = COLUMNS ? a.v_st : a.k_st;
+    const uint16_t* at[4];
+    int t[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        t[r] = start + max(0, min(row + r, m - 1));
+        at[r] = src + t[r] * stride;
+        load_bf16<W>(at[r] + col, raw[r]);
+    }
+    if constexpr (TURN != kStill && !COLUMNS) {
+        if (col >= 2 * a.r.pairs) return;
+        if constexpr (TURN == kAdjacent) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float4* cs = reinterpret_cast<const float4*>(a.r.table + t[r] * a.r.stride + col);
+#pragma unroll
+                for (int e = 0; e < W; e += 4) {
+                    const float4 x = cs[e / 4];
+                    float p[4] = {bf16_lo(raw[r][e / 2]), bf16_hi(raw[r][e / 2]), bf16_lo(raw[r][e / 2 + 1]), bf16_hi(raw[r][e / 2 + 1])};
+                    turn(p[0], p[1], x.x, x.y);
+                    turn(p[2], p[3], x.z, x.w);
+                    raw[r][e / 2] = bf16_pair(p[0], p[1]);
+                    raw[r][e / 2 + 1] = bf16_pair(p[2], p[3]);
+                }
+            }
+        } else {                                            // the other half's columns are another thread's: read here too
+            const bool upper = col >= a.r.pairs;
+            const int c = upper ? col - a.r.pairs : col;
+            uint32_t other[4][W / 2];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) load_bf16<W>(at[r] + (upper ? c : c + a.r.pairs), other[r]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float4* cs = reinterpret_cast<const float4*>(a.r.table + t[r] * a.r.stride + 2 * c);
+#pragma unroll
+                for (int e = 0; e < W; e += 2) {
+                    const float4 x = cs[e / 2];
+                    float p0 = bf16_lo(raw[r][e / 2]), p1 = bf16_hi(raw[r][e / 2]), q0 = bf16_lo(other[r][e / 2]), q1 = bf16_hi(other[r][e / 2]);
+                    // (b cos + a sin is a cos - b sin with the pair and the sine's sign exchanged)
+                    turn(p0, q0, x.x, upper ? -x.y : x.y);
+                    turn(p1, q1, x.z, upper ? -x.w : x.w);
+                    raw[r][e / 2] = bf16_pair(p0, p1);
+                }
+            }
+        }
+    }
+}
+
+template <int D, int CODE, bool COLUMNS, int TURN>
+__device__ __forceinline__ void append_block(const AppendArgs& a, int kh, int j, int b, uint32_t* sm) {
+    constexpr int W = D / 16;
+    const int tid = threadIdx.x;
+    const Place<D, COLUMNS> my(tid);
+    const int n = a.c.len[b], start = max(0, min(a.cu[b], a.total));
+    const int m = min(min(max(start, min(a.cu[b + 1], a.total)) - start, a.max_new), a.max_len - n);
+    if (n < 0 || n >= a.max_len || m <= 0) return;
+    const int first = n / kBlk, at = (first + j) * kBlk, total = n + m, rest = total % kBlk;
+    const int64_t strip = (int64_t)b * a.Hk + kh;
+    if (at >= total || (j > 0 && at + kBlk > total)) return;        // (the last, partial block is the first workgroup's)
+    uint32_t raw[4][W / 2], behind[4][W / 2];
+    new_rows<D, COLUMNS, TURN>(a, kh, start, m, at + my.row - n, my.col, raw);
+    const bool whole = at + kBlk <= total, more = j == 0 && whole && rest > 0;
+    if (more) new_rows<D, COLUMNS, TURN>(a, kh, start, m, total - rest + my.row - n, my.col, behind);
+    auto bits = [](const uint32_t (&x)[4][W / 2], int r, int e) { return (uint16_t)(x[r][e / 2] >> (16 * (e & 1))); };
+    if (whole) {
+        if (j == 0 && my.row < n % kBlk) {                  // the block's rows that are in the tail
+            const uint16_t* tail = (COLUMNS ? a.c.v_tail : a.c.k_tail) + strip * (kBlk * D);
+            if constexpr (COLUMNS) {
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    const uint2 x = *reinterpret_cast<const uint2*>(tail + (my.col + e) * kBlk + my.row);
+                    const uint32_t half[4] = {x.x & 0xffffu, x.x >> 16, x.y & 0xffffu, x.y >> 16};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (my.row + r < n % kBlk) raw[r][e / 2] = e & 1 ? (raw[r][e / 2] & 0xffffu) | half[r] << 16 : (raw[r][e / 2] & 0xffff0000u) | half[r];
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (my.row + r < n % kBlk) load_bf16<W>(tail + (my.row + r) * D + my.col, raw[r]);
+            }
+        }
+        const int page = page_of(a.c, b, first + j);
+        if (page >= 0) {
+            float v[4][W];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < W; e += 2) { v[r][e] = bf16_lo(raw[r][e / 2]); v[r][e + 1] = bf16_hi(raw[r][e / 2]); }
+            write_block<D, CODE, COLUMNS>(v, a.c, (int64_t)page * a.Hk + kh, sm, tid);
+        }
+        if (more) {
+            __syncthreads();                                // (all have read the tail)
+            write_tail<D, COLUMNS>([&](int r, int e) { return bits(behind, r, e); }, a.c, strip, rest, tid);
+        }
+        return;
+    }
+    const int from = n % kBlk;                              // the new rows stay in the tail, behind those that are there
+    const Place<D, COLUMNS> p(tid);
+    uint16_t* tail = (COLUMNS ? a.c.v_tail : a.c.k_tail) + strip * (kBlk * D);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        if (p.row + r < from || p.row + r >= rest) continue;
+#pragma unroll
+        for (int e = 0; e < W; ++e) tail[COLUMNS ? (p.col + e) * kBlk + p.row + r : (p.row + r) * D + p.col + e] = bits(raw, r, e);
+    }
+}
+
+template <int D, int CODE, int TURN>
+__global__ __launch_bounds__(kThreads) void block_append_kernel(AppendArgs a) {
+    __shared__ uint32_t sm[2 * kThreads / 64];
+    const int kh = blockIdx.x % a.Hk;
+    if ((int)blockIdx.x < a.Hk) append_block<D, CODE, false, TURN>(a, kh, blockIdx.y, blockIdx.z, sm);
+    else append_block<D, CODE, true, TURN>(a, kh, blockIdx.y, blockIdx.z, sm);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
@@ -471,6 +607,42 @@ extern "C" st3_status st3_block_store(const st3_gqa_shape* shape, const st3_rows
     } else {
         if (D == 128) block_store_kernel<128, ST3_BLOCK_E4M3><<<grid, kThreads, 0, st>>>(a);
         else block_store_kernel<64, ST3_BLOCK_E4M3><<<grid, kThreads, 0, st>>>(a);
+    }
+    return check_launch();
+}
+
+extern "C" st3_status st3_block_append(const st3_gqa_shape* shape, const st3_rows* k, const st3_rows* v, const int32_t* cu_len, int32_t total,
+                                       int32_t max_new, const st3_block_cache* cache, int32_t max_len, const st3_rotary* rotary, void* stream) {
+    using namespace st3;
+    st3_status s = check_gqa_shape(shape);
+    if (s != ST3_OK) return s;
+    if ((s = check_block_cache(shape, cache)) != ST3_OK) return s;
+    const int Hk = shape->kv_heads, D = shape->head_dim;
+    if (!cu_len || total < 0 || max_new < 0 || max_new > total || max_len < 0) return ST3_ERR_INVALID_ARG;
+    if (max_len > kMostRows) return ST3_ERR_UNSUPPORTED;
+    if (rotary && (s = check_rotary(rotary, D)) != ST3_OK) return s;
+    if (total == 0) return ST3_OK;          // (an empty tensor may have no address)
+    if ((s = check_rows(k, D, 2)) != ST3_OK || (s = check_rows(v, D, 2)) != ST3_OK) return s;
+    if (max_new == 0) return ST3_OK;
+    const int blocks = (int)(((int64_t)max_new + kBlk - 2) / kBlk) + 1;     // (new rows may begin with a block's last)
+    if (blocks > 65535) return ST3_ERR_UNSUPPORTED;
+    if (cache->table_blocks < max_len / kBlk) return ST3_ERR_INVALID_ARG;
+    const AppendArgs a{block_pages(cache), reinterpret_cast<const uint16_t*>(k->data), reinterpret_cast<const uint16_t*>(v->data), k->stride_t, k->stride_h,
+                       v->stride_t, v->stride_h, cu_len, rotation(rotary), total, max_new, max_len, Hk};
+    const dim3 grid(2 * Hk, blocks, shape->batch);
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    auto launch = [&](auto kernel) { kernel<<<grid, kThreads, 0, st>>>(a); };
+    auto turned = [&](auto still, auto halves, auto adjacent) {
+        if (!rotary) launch(still);
+        else if (rotary->layout == ST3_ROTARY_HALVES) launch(halves);
+        else launch(adjacent);
+    };
+    if (cache->code == ST3_BLOCK_INT8) {
+        if (D == 128) turned(block_append_kernel<128, ST3_BLOCK_INT8, kStill>, block_append_kernel<128, ST3_BLOCK_INT8, kHalves>, block_append_kernel<128, ST3_BLOCK_INT8, kAdjacent>);
+        else turned(block_append_kernel<64, ST3_BLOCK_INT8, kStill>, block_append_kernel<64, ST3_BLOCK_INT8, kHalves>, block_append_kernel<64, ST3_BLOCK_INT8, kAdjacent>);
+    } else {
+        if (D == 128) turned(block_append_kernel<128, ST3_BLOCK_E4M3, kStill>, block_append_kernel<128, ST3_BLOCK_E4M3, kHalves>, block_append_kernel<128, ST3_BLOCK_E4M3, kAdjacent>);
+        else turned(block_append_kernel<64, ST3_BLOCK_E4M3, kStill>, block_append_kernel<64, ST3_BLOCK_E4M3, kHalves>, block_append_kernel<64, ST3_BLOCK_E4M3, kAdjacent>);
     }
     return check_launch();
 }

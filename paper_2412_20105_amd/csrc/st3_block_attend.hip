@@ -1,0 +1,623 @@
+// Causal attention of several new tokens over a cache of 8-bit blocks, with grouped heads and accumulated weights.
+//
+// Rows.  The G query heads that share a key head are rows of one matrix, as for packed prompts: row x of a (sequence, key head) pair is head x % G of new
+// token x / G.  A workgroup's four waves have 16 QC rows each and walk the blocks of 64 keys together; 8-bit codes, loaded a block ahead into
+// registers, become bf16 on their way into LDS, once for all rows (codes have at most 8 significant bits: exact), and the scale of a block multiplies
+// the logits and the weights.
+//   S^T = K Q^T    (A: lane (c, g) holds A[c][8g..8g+7], B: B[8g..8g+7][c], C: C[4g..4g+3][c]) product t of four: row 4g'+i of A is key 16 g' + 4 t + i, so
+//                  that lane (c, g) of C ends with keys 16 g .. 16 g + 15 of row c.
+//   O^T = V^T P^T  the lane's 16 keys are the contraction slots 8g..8g+7 of two steps: P^T is where S^T left it.
+// No value crosses lanes but the maximum.  Where row tiles are too few to fill the card, a strip's blocks are cut into pieces, and a second launch joins them.
+#include <algorithm>
+#include <type_traits>
+
+#include "st3_block.h"
+
+namespace st3 {
+namespace {
+
+struct ChunkArgs {
+    BlockPages c;
+    const uint16_t* q; uint16_t* out;
+    int64_t q_st, q_sh, o_st, o_sh;
+    const int32_t* cu;
+    int32_t B, total, max_new, max_len, H, Hk, G;
+    int32_t piece, pieces;          // blocks of a piece; pieces of the longest strip (1: whole strips)
+    float scale_l2;
+    float* score; int64_t s_sb, s_sh;
+    int32_t window;
+    float2* ml;                     // [total][H] maximum, and one over the sum; null: no score
+    float* part_o;                  // [total][H][pieces][D]
+    float2* part_ml;                // [total][H][pieces]
+};
+
+// A sequence's new rows, the rows in front of them (negative: an empty place), and what it attends.
+struct Turn {
+    int start, m, n;
+    __device__ __forceinline__ int rows() const { return n < 0 ? 0 : n + m; }
+    __device__ __forceinline__ int sees(int t) const { return n < 0 ? -1 : n + t; }        // the last row that new row t sees
+};
+__device__ __forceinline__ Turn turn_of(const ChunkArgs& a, int b) {
+    const int s = max(0, min(a.cu[b], a.total)), e = max(s, min(a.cu[b + 1], a.total)), n = a.c.len[b];
+    return Turn{s, min(min(e - s, a.max_new), n < 0 ? a.max_new : max(a.max_len - n, 0)), n};
+}
+
+// Workgroup -> (sequence, key head, row tile).  Key heads run fastest (they go round-robin to the 8 XCDs); every wave finds its place, a lane for each of 64
+// sequences at a time.
+template <int ROWS>
+__device__ __forceinline__ bool place(const ChunkArgs& a, int lane, int& b, int& kh, int& tile, Turn& sq) {
+    kh = blockIdx.x % a.Hk;
+    int x = blockIdx.x / a.Hk;
+    for (int i0 = 0; i0 < a.B; i0 += kWave) {
+        Turn its = {0, 0, 0};
+        int mine = 0;
+        if (i0 + lane < a.B) {
+            its = turn_of(a, i0 + lane);
+            mine = (int)(((int64_t)its.m * a.G + ROWS - 1) / ROWS);
+        }
+        const int upto = wave_prefix(mine), all = __builtin_amdgcn_readlane(upto, 63);
+        if (x < all) {
+            const int at = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(x < upto)) - 1);
+            b = i0 + at;
+            tile = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_readlane(upto, at) - 1 - x);
+            sq = Turn{__builtin_amdgcn_readlane(its.start, at), __builtin_amdgcn_readlane(its.m, at), __builtin_amdgcn_readlane(its.n, at)};
+            return true;
+        }
+        x -= all;
+    }
+    return false;
+}
+
+// A block in LDS: K as 64 rows of D bf16, V as D rows (columns of V) of 64.  Unit u (16 bytes) of row r lies at u ^ swz(r): the 16 rows that a fragment's
+// lanes read lie in 16 different units of the banks.
+template <int D> struct Tile {
+    static constexpr int K = kBlk * D, BYTES = 4 * K;       // elements of K, and of V; bytes of both
+    __device__ static __forceinline__ int k_swz(int row) {
+        return D == 128 ? (row >> 4 & 3) << 2 | (row & 3) : (row >> 4 & 3) << 1 | (row >> 1 & 1);
+    }
+    __device__ static __forceinline__ int v_swz(int row) { return row >> 1 & 7; }
+};
+
+__device__ __forceinline__ void lds_write16(uint32_t at, u32x4 x) { *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(at) = x; }
+
+// A block's codes on their way from memory to LDS.
+template <int D, int CODE, int THREADS>
+struct Codes {
+    static constexpr int N = kBlk * D / 16 / THREADS;
+    u32x4 k[N], v[N];
+    __device__ __forceinline__ void load(const BlockPages& c, int64_t at, int tid) {
+        const u32x4* kp = reinterpret_cast<const u32x4*>(c.k_codes + at * (kBlk * D));
+        const u32x4* vp = reinterpret_cast<const u32x4*>(c.v_codes + at * (kBlk * D));
+#pragma unroll
+        for (int i = 0; i < N; ++i) k[i] = kp[tid + i * THREADS];
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = vp[tid + i * THREADS];
+    }
+    __device__ __forceinline__ void store(uint32_t lds, int tid) const {
+        using F = BlockCode<CODE>;
+        auto put = [](uint32_t row_at, int unit, int swz, const u32x4& w) {
+            const uint2 a = F::to_bf16(w.x), b = F::to_bf16(w.y), c = F::to_bf16(w.z), d = F::to_bf16(w.w);
+            lds_write16(row_at + 16 * (unit ^ swz), u32x4{a.x, a.y, b.x, b.y});
+            lds_write16(row_at + 16 * ((unit + 1) ^ swz), u32x4{c.x, c.y, d.x, d.y});
+        };
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = tid + i * THREADS, kr = p / (D / 16), vr = p / (kBlk / 16);
+            put(lds + 2 * D * kr, 2 * (p % (D / 16)), Tile<D>::k_swz(kr), k[i]);
+            put(lds + 2 * Tile<D>::K + 2 * kBlk * vr, 2 * (p % (kBlk / 16)), Tile<D>::v_swz(vr), v[i]);
+        }
+    }
+};
+
+// The tail, `rows` rows in 16 bits, into LDS; the rows behind them are zeros, whatever their bits are.
+template <int D, int THREADS>
+__device__ __forceinline__ void tail_to_lds(const BlockPages& c, int64_t strip, int rows, uint32_t lds, int tid) {
+    const u32x4* kp = reinterpret_cast<const u32x4*>(c.k_tail + strip * (kBlk * D));
+    const u32x4* vp = reinterpret_cast<const u32x4*>(c.v_tail + strip * (kBlk * D));
+    constexpr int N = kBlk * D / 8 / THREADS;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int p = tid + i * THREADS, kr = p / (D / 8), vr = p / (kBlk / 8);
+        const u32x4 k = kp[p];
+        lds_write16(lds + 2 * D * kr + 16 * (p % (D / 8) ^ Tile<D>::k_swz(kr)), kr < rows ? k : u32x4{0, 0, 0, 0});
+        Frag f;
+        f.u4 = vp[p];
+        const int key = 8 * (p % (kBlk / 8));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f.w[j] &= (key + 2 * j < rows ? 0xffffu : 0u) | (key + 2 * j + 1 < rows ? 0xffff0000u : 0u);
+        lds_write16(lds + 2 * Tile<D>::K + 2 * kBlk * vr + 16 * (p % (kBlk / 8) ^ Tile<D>::v_swz(vr)), f.u4);
+    }
+}
+
+// A wave's 16 QC rows, as QC columns of 16: lane (c, g) holds row 16 qc + c of each, and of its output the columns 16 dt + 4 g .. + 3.
+template <int D, int QC>
+struct Rows {
+    f32x4 o[D / 16][QC];
+    float m[QC], l[QC];
+    int pos[QC];            // the last of the sequence's rows that the row sees
+    __device__ __forceinline__ void init() {
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) {
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) o[dt][qc] = f32x4{0.f, 0.f, 0.f, 0.f};
+            m[qc] = -3.402823466e38f; l[qc] = 0.f;
+        }
+    }
+};
+
+// 64 keys for one wave; ks: the block's scale of K times that of the logits (in the log2 domain), vs: of V.  MASKED: some row does not see some
+// of the keys.  CAREFUL: V may hold infinities or NaN, and a weight of 0 does not silence those; row by row, V's keys that the row does not see count as 0.
+template <int D, int QC, bool MASKED, bool CAREFUL = false>
+__device__ __forceinline__ void chunk_step(uint32_t k_at, uint32_t v_at, const Frag (&qf)[QC][D / 32], Rows<D, QC>& st, float ks, float vs, int g, int k0) {
+    constexpr int KS = D / 32, DT = D / 16;
+    f32x4 s[4][QC];
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        Frag ka[KS];
+#pragma unroll
+        for (int x = 0; x < KS; ++x) ka[x].u4 = lds_read16((k_at ^ (64 * x)) + 8 * D * t);
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) {
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < KS; ++x) y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[x].v, qf[qc][x].v, y, 0, 0, 0);
+            s[t][qc] = y;
+        }
+    }
+    __builtin_amdgcn_s_setprio(0);
+    // (a block's scale may be 0, and -infinity times 0 is no number: masks come behind the scale)
+    if (MASKED) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int qc = 0; qc < QC; ++qc) {
+                s[t][qc] *= ks;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (k0 + 16 * g + 4 * t + i > st.pos[qc]) s[t][qc][i] = -INFINITY;
+            }
+    }
+    const float by = MASKED ? 1.0f : ks;
+    // the reference point of the exponents follows the maximum only when that has moved by more than kLazy (weights reach 2^kLazy at most)
+    constexpr float kLazy = 8.0f;
+    float mx[QC];
+    bool moved = false;
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc) {
+        float x = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) x = fmaxf(x, fmaxf(fmaxf(s[t][qc][0], s[t][qc][1]), fmaxf(s[t][qc][2], s[t][qc][3])));
+        mx[qc] = x * by;
+        moved |= mx[qc] - st.m[qc] > kLazy;
+    }
+    if (__any(moved)) {
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) {
+            const float cand = fmaxf(st.m[qc], wave_max_from<16>(mx[qc]));
+            const float m_new = cand - st.m[qc] > kLazy ? cand : st.m[qc];
+            const float alpha = exp2_fast(st.m[qc] - m_new);
+            st.m[qc] = m_new;
+            st.l[qc] *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) st.o[dt][qc] *= alpha;
+        }
+    }
+    // A weight times V's scale is rounded to bf16 once, to nearest: an error of 2^-8 of it at most and without bias, beside the output's own rounding by as
+    // much; the sum is of the unrounded ones.
+    Frag pb[2][QC];
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float s0 = s[2 * x + j / 2][qc][2 * (j & 1)], s1 = s[2 * x + j / 2][qc][2 * (j & 1) + 1];
+                const float p0 = exp2_fast(fmaf(s0, by, -st.m[qc])), p1 = exp2_fast(fmaf(s1, by, -st.m[qc]));
+                st.l[qc] += p0 + p1;
+                const f32x2 w = {p0 * vs, p1 * vs};
+                pb[x][qc].w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(w, bf16x2));
+            }
+    if constexpr (CAREFUL) {
+        const int c = threadIdx.x & 15;
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc)
+            for (int row = 0; row < 16; ++row) {
+                const int pos = __builtin_amdgcn_readlane(st.pos[qc], row);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    Frag seen;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int key = k0 + 16 * g + 8 * x + 2 * j;
+                        seen.w[j] = (key <= pos ? 0xffffu : 0u) | (key < pos ? 0xffff0000u : 0u);
+                    }
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        Frag va;
+                        va.u4 = lds_read16((v_at ^ (16 * x)) + 32 * kBlk * dt);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) va.w[j] &= seen.w[j];
+                        const f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va.v, pb[x][qc].v, st.o[dt][qc], 0, 0, 0);
+                        st.o[dt][qc] = c == row ? o : st.o[dt][qc];
+                    }
+                }
+            }
+        return;
+    }
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+        Frag va[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) va[x].u4 = lds_read16((v_at ^ (16 * x)) + 32 * kBlk * dt);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int qc = 0; qc < QC; ++qc) st.o[dt][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[x].v, pb[x][qc].v, st.o[dt][qc], 0, 0, 0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+}
+
+template <int D, int CODE, int QC>
+__global__ __launch_bounds__(256, 2) void block_chunk_kernel(ChunkArgs a) {
+    constexpr int kThr = 256, kRows = 64 * QC, KS = D / 32, DT = D / 16, OSTR = D + 8;
+    using L = Tile<D>;
+    constexpr int kOut = 2 * 4 * 16 * QC * OSTR;            // bytes
+    __shared__ __attribute__((aligned(1024))) uint8_t buf[2 * L::BYTES > kOut ? 2 * L::BYTES : kOut];
+    __shared__ int redo;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15, ch = blockIdx.y;
+    int b, kh, tile;
+    Turn sq;
+    if (!place<kRows>(a, lane, b, kh, tile, sq)) return;
+    const int rows = sq.m * a.G, r0 = tile * kRows + wave * 16 * QC;        // the wave's first row
+    const int last = sq.sees((min(rows, (tile + 1) * kRows) - 1) / a.G);    // the last row that the workgroup sees
+    const int u_begin = ch * a.piece, u_end = min((last + kBlk) / kBlk, u_begin + a.piece), blocks = sq.rows() / kBlk;     // (last may be -1)
+    if (ch > 0 && u_begin >= u_end) return;
+    if (tid == 0) redo = 0;
+    const int64_t strip = (int64_t)b * a.Hk + kh;
+    const uint32_t lds0 = lds_addr(buf);
+    Rows<D, QC> st;
+    st.init();
+    Frag qf[QC][KS];
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc) {
+        const int r = min(r0 + 16 * qc + c, rows - 1), t = r / a.G;
+        st.pos[qc] = sq.sees(t);
+        const uint16_t* row = a.q + (int64_t)(sq.start + t) * a.q_st + (int64_t)(kh * a.G + r - t * a.G) * a.q_sh;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[qc][s].u4 = *reinterpret_cast<const u32x4*>(row + 32 * s + 8 * g);
+    }
+    const int p_first = sq.sees(min(r0, rows - 1) / a.G), p_last = sq.sees((min(r0 + 16 * QC, rows) - 1) / a.G);      // what the wave's first and last rows see
+    const bool idle = r0 >= rows;
+    const int krow = 16 * (c >> 2) + (c & 3);
+    const uint32_t k_lane = (uint32_t)(2 * D * krow + 16 * (g ^ L::k_swz(krow))), v_lane = (uint32_t)(2 * L::K + 2 * kBlk * c + 16 * (2 * g ^ L::v_swz(c)));
+    // lane i has the page and the scales of block `base` + i
+    int base = 0, page_l = -1;
+    float ks_l = 0.f, vs_l = 0.f;
+    auto look_up = [&](int from) {
+        base = from;
+        const int u = from + lane;
+        page_l = u < u_end && u < blocks ? page_of(a.c, b, u) : -1;
+        ks_l = vs_l = 0.f;
+        if (page_l >= 0) {
+            const int64_t at = (int64_t)page_l * a.Hk + kh;
+            ks_l = a.c.k_scale[at];
+            vs_l = a.c.v_scale[at];
+        }
+    };
+    auto walk = [&](auto careful) {
+        constexpr bool kCareful = decltype(careful)::value;
+        Codes<D, CODE, kThr> codes;
+        look_up(u_begin);
+        auto page_at = [&](int u) {
+            if (u >= base + kWave) look_up(u);
+            return __builtin_amdgcn_readlane(page_l, u - base);
+        };
+        int u = u_begin, slot = 0;
+        const int u_stop = min(u_end, blocks);
+        int page = u < u_stop ? page_at(u) : -1;
+        if (page >= 0) codes.load(a.c, (int64_t)page * a.Hk + kh, tid);
+        for (; u < u_stop; ++u, slot ^= 1) {
+            const bool there = page >= 0;                   // (a block without a page is passed over)
+            const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), u - base)) * a.scale_l2;
+            const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_l), u - base));
+            const uint32_t at = lds0 + slot * L::BYTES;
+            if (there) codes.store(at, tid);
+            __syncthreads();
+            if (u + 1 < u_stop) {
+                page = page_at(u + 1);
+                if (page >= 0) codes.load(a.c, (int64_t)page * a.Hk + kh, tid);
+            }
+            if (!there || idle) continue;
+            if (u * kBlk + kBlk - 1 <= p_first) chunk_step<D, QC, false>(at + k_lane, at + v_lane, qf, st, ks, vs, g, u * kBlk);
+            else if (u * kBlk <= p_last) chunk_step<D, QC, true, kCareful>(at + k_lane, at + v_lane, qf, st, ks, vs, g, u * kBlk);
+        }
+        if (blocks >= u_begin && blocks < u_end) {          // the rows in 16 bits
+            const uint32_t at = lds0 + slot * L::BYTES;
+            tail_to_lds<D, kThr>(a.c, strip, sq.rows() % kBlk, at, tid);
+            __syncthreads();
+            if (!idle && blocks * kBlk <= p_last) chunk_step<D, QC, true, kCareful>(at + k_lane, at + v_lane, qf, st, a.scale_l2, 1.0f, g, blocks * kBlk);
+        }
+    };
+    walk(std::false_type{});
+    // Anything but finite: it may be from V of keys that a row does not see (0 times infinity).  Once more, such V left out.
+    float odd = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) odd = fmaf(st.o[dt][qc][i], 0.f, odd);
+    if (odd != 0.f) redo = 1;
+    __syncthreads();
+    if (redo) {
+        st.init();
+        walk(std::true_type{});
+        __syncthreads();
+    }
+    if (a.pieces > 1) {
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) {
+            const float l = wave_sum_from<16>(st.l[qc]);
+            const int r = r0 + 16 * qc + c, t = r / a.G;
+            if (r >= rows) continue;
+            const int64_t part = ((int64_t)(sq.start + t) * a.H + kh * a.G + r - t * a.G) * a.pieces + ch;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(a.part_o + part * D + 16 * dt + 4 * g) = st.o[dt][qc];
+            if (g == 0) a.part_ml[part] = make_float2(st.m[qc], l);
+        }
+        return;
+    }
+    // ---- normalise; the block of outputs goes through LDS and leaves as whole rows ----------------------------------------------
+    uint16_t* ob = reinterpret_cast<uint16_t*>(buf) + wave * 16 * QC * OSTR;
+    constexpr int VPR = D / 8, RPI = 64 / VPR;
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc) {
+        const float l = wave_sum_from<16>(st.l[qc]), rl = l == 0.f ? 0.f : 1.0f / l;      // (a sum of NaN stays one)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const f32x4 o = st.o[dt][qc] * rl;
+            const f32x2 o01 = {o[0], o[1]}, o23 = {o[2], o[3]};
+            uint2 pk;
+            pk.x = __builtin_bit_cast(uint32_t, __builtin_convertvector(o01, bf16x2));
+            pk.y = __builtin_bit_cast(uint32_t, __builtin_convertvector(o23, bf16x2));
+            *reinterpret_cast<uint2*>(ob + (16 * qc + c) * OSTR + 16 * dt + 4 * g) = pk;
+        }
+        const int r = r0 + 16 * qc + c, t = r / a.G;
+        if (a.ml != nullptr && g == 0 && r < rows) a.ml[(int64_t)(sq.start + t) * a.H + kh * a.G + r - t * a.G] = make_float2(st.m[qc], rl);
+    }
+#pragma unroll
+    for (int i = 0; i < 16 * QC / RPI; ++i) {
+        const int x = i * RPI + lane / VPR, r = r0 + x;
+        const u32x4 val = *reinterpret_cast<const u32x4*>(ob + x * OSTR + (lane % VPR) * 8);
+        if (r < rows) {
+            const int t = r / a.G;
+            *reinterpret_cast<u32x4*>(a.out + (int64_t)(sq.start + t) * a.o_st + (int64_t)(kh * a.G + r - t * a.G) * a.o_sh + (lane % VPR) * 8) = val;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// Behind the pieces: a wave joins a row's parts.
+// ---------------------------------------------------------------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t x = (int64_t)blockIdx.x * 4 + wave;
+    const int row = (int)(x / a.H), h = (int)(x % a.H);
+    if (row >= a.total) return;
+    // whose row it is: the sequence that begins last among those that begin at it or before (empty ones begin where the next one does)
+    int b = -1, start = 0;
+    for (int i0 = 0; i0 < a.B; i0 += kWave) {
+        const int s = i0 + lane < a.B ? max(0, min(a.cu[i0 + lane], a.total)) : 0x7fffffff;
+        const uint64_t before = __ballot(s <= row);
+        if (before == 0) break;
+        b = i0 + 63 - __clzll(before);
+        start = __builtin_amdgcn_readlane(s, 63 - __clzll(before));
+        if (before != ~0ull) break;
+    }
+    if (b < 0) return;
+    const Turn sq = turn_of(a, b);
+    if (row - start >= sq.m) return;
+    const int units = (sq.sees(row - start) + kBlk) / kBlk, parts = max(1, (units + a.piece - 1) / a.piece);
+    const int64_t at = ((int64_t)row * a.H + h) * a.pieces;
+    float top = -3.402823466e38f;
+    for (int i = lane; i < parts; i += kWave) top = fmaxf(top, a.part_ml[at + i].x);
+    top = wave_max_from<1>(top);
+    float sum = 0.f;
+    constexpr int PER = D / 64;
+    float v[PER] = {};
+    for (int i = 0; i < parts; ++i) {
+        const float2 ml = a.part_ml[at + i];
+        const float f = exp2_fast(ml.x - top);
+        sum = fmaf(ml.y, f, sum);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) v[e] = fmaf(a.part_o[(at + i) * D + PER * lane + e], f, v[e]);
+    }
+    const float rl = sum == 0.f ? 0.f : 1.0f / sum;
+    uint16_t* out = a.out + (int64_t)row * a.o_st + (int64_t)h * a.o_sh + PER * lane;
+    if constexpr (PER == 2) {
+        const f32x2 o = {v[0] * rl, v[1] * rl};
+        *reinterpret_cast<uint32_t*>(out) = __builtin_bit_cast(uint32_t, __builtin_convertvector(o, bf16x2));
+    } else {
+        const f32x2 o = {v[0] * rl, 0.f};
+        *out = (uint16_t)__builtin_bit_cast(uint32_t, __builtin_convertvector(o, bf16x2));
+    }
+    if (a.ml != nullptr && lane == 0) a.ml[(int64_t)row * a.H + h] = make_float2(top, rl);
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// Scores: the logits of the window's rows are formed again.  Workgroup (key head, block, sequence): each of the four waves has the block's 64 keys in
+// registers and takes 16 rows in turn, straight from memory; a lane adds up what its 16 keys get.
+// ---------------------------------------------------------------------------------------------------------------------------------
+template <int D, int CODE>
+__global__ __launch_bounds__(256) void chunk_score_kernel(ChunkArgs a) {
+    using F = BlockCode<CODE>;
+    constexpr int KS = D / 32, KH = D / 64;
+    __shared__ float part[4][kBlk];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
+    const int kh = blockIdx.x, u = blockIdx.y, b = blockIdx.z;
+    const Turn sq = turn_of(a, b);
+    const int keys = sq.rows(), blocks = keys / kBlk;
+    if (sq.n < 0 || sq.m <= 0 || u * kBlk >= keys) return;
+    const int page = u < blocks ? page_of(a.c, b, u) : -1;
+    const bool there = u == blocks || page >= 0;
+    f32x4 sum[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) sum[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (there) {
+        // key 16 x + c; a lane's columns are 64 y + 16 g .. + 15, in two steps
+        Frag kf[4][KS];
+        float scale = a.scale_l2;
+        if (u < blocks) {
+            const int64_t at = (int64_t)page * a.Hk + kh;
+            const uint8_t* codes = a.c.k_codes + at * (kBlk * D);
+            scale *= a.c.k_scale[at];
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int y = 0; y < KH; ++y) {
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(codes + (16 * x + c) * D + 64 * y + 16 * g);
+                    const uint2 w0 = F::to_bf16(w.x), w1 = F::to_bf16(w.y), w2 = F::to_bf16(w.z), w3 = F::to_bf16(w.w);
+                    kf[x][2 * y].u4 = u32x4{w0.x, w0.y, w1.x, w1.y};
+                    kf[x][2 * y + 1].u4 = u32x4{w2.x, w2.y, w3.x, w3.y};
+                }
+        } else {
+            const uint16_t* tail = a.c.k_tail + ((int64_t)b * a.Hk + kh) * (kBlk * D);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kf[x][s].u4 = *reinterpret_cast<const u32x4*>(tail + (16 * x + c) * D + 64 * (s / 2) + 16 * g + 8 * (s & 1));
+        }
+        const int rows = sq.m * a.G, from = max(max(0, sq.m - a.window), u * kBlk - sq.n);      // (rows in front see none of these keys)
+        for (int r0 = from * a.G + 16 * wave; r0 < rows; r0 += 64) {
+            const int r = min(r0 + c, rows - 1), t = r / a.G, head = kh * a.G + r - t * a.G;
+            const uint16_t* row = a.q + (int64_t)(sq.start + t) * a.q_st + (int64_t)head * a.q_sh;
+            Frag qf[KS];
+#pragma unroll
+            for (int s = 0; s < KS; ++s) qf[s].u4 = *reinterpret_cast<const u32x4*>(row + 64 * (s / 2) + 16 * g + 8 * (s & 1));
+            const float2 ml = a.ml[(int64_t)(sq.start + t) * a.H + head];
+            const int pos = r0 + c < rows ? sq.n + t : -1;      // (a row that does not exist sees nothing)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < KS; ++s) y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x][s].v, qf[s].v, y, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p = exp2_fast(fmaf(y[i], scale, -ml.x)) * ml.y;
+                    sum[x][i] += u * kBlk + 16 * x + 4 * g + i > pos ? 0.f : p;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[x][i] = group_sum<16>(sum[x][i]);
+    if (c == 0) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4*>(&part[wave][16 * x + 4 * g]) = sum[x];
+    }
+    __syncthreads();
+    const int key = u * kBlk + tid;
+    if (tid < kBlk && key < keys) {
+        float* to = a.score + b * a.s_sb + kh * a.s_sh + key;
+        const float got = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
+        *to = key < sq.n ? *to + got : got;
+    }
+}
+
+// How a call is cut: columns of 16 rows a wave, blocks of a piece, pieces.
+struct ChunkCut { int cols, piece, pieces; };
+constexpr int kEnough = 512, kWanted = 1024, kLeastPiece = 4;
+
+// No more row tiles than this, whatever the lengths are: each sequence has one that is not full.
+inline int64_t chunk_tiles(const st3_gqa_shape* s, int total, int max_new, int rows) {
+    const int G = s->heads / s->kv_heads;
+    return std::min((int64_t)total * G / rows + std::min(s->batch, total), ((int64_t)max_new * G + rows - 1) / rows * s->batch);
+}
+inline ChunkCut chunk_cut(const st3_gqa_shape* s, int total, int max_new, int max_len) {
+    const int G = s->heads / s->kv_heads, cols = (int64_t)max_new * G <= 64 ? 1 : 2;
+    const int64_t tiles = chunk_tiles(s, total, max_new, 64 * cols) * s->kv_heads, units = max_len / kBlk + 1;
+    if (tiles >= kEnough || tiles == 0) return ChunkCut{cols, (int)units, 1};
+    const int64_t pieces = std::min((kWanted + tiles - 1) / tiles, (units + kLeastPiece - 1) / kLeastPiece);
+    const int64_t piece = (units + pieces - 1) / pieces;
+    return ChunkCut{cols, (int)piece, (int)((units + piece - 1) / piece)};
+}
+
+struct ChunkWs { size_t ml, part_o, part_ml, total; };
+// Room for as many parts as a launch of any smaller sizes may leave: kWanted tiles of 128 rows and one part more for each row, or one for every kLeastPiece blocks.
+inline ChunkWs chunk_ws(const st3_gqa_shape* s, int total, int max_len) {
+    const int64_t rows = (int64_t)total * s->heads, units = max_len / kBlk + 1;
+    const int64_t parts = std::min((int64_t)kWanted * 128 + rows, rows * ((units + kLeastPiece - 1) / kLeastPiece));
+    ChunkWs w{};
+    size_t off = 0;
+    w.ml = off;      off = align_up(off + rows * sizeof(float2), 256);
+    w.part_o = off;  off = align_up(off + parts * s->head_dim * sizeof(float), 256);
+    w.part_ml = off; off = align_up(off + parts * sizeof(float2), 256);
+    w.total = off;
+    return w;
+}
+
+template <int D, int CODE>
+void launch_chunk(const ChunkArgs& a, int cols, unsigned grid, hipStream_t st) {
+    if (cols == 1) block_chunk_kernel<D, CODE, 1><<<dim3(grid, a.pieces), 256, 0, st>>>(a);
+    else block_chunk_kernel<D, CODE, 2><<<dim3(grid, a.pieces), 256, 0, st>>>(a);
+    if (a.pieces > 1) chunk_join_kernel<D><<<(unsigned)(((int64_t)a.total * a.H + 3) / 4), 256, 0, st>>>(a);
+    if (a.score && a.max_len > 0) chunk_score_kernel<D, CODE><<<dim3(a.Hk, (a.max_len + kBlk - 1) / kBlk, a.B), 256, 0, st>>>(a);
+}
+
+}  // namespace
+}  // namespace st3
+
+extern "C" size_t st3_block_attend_workspace_bytes(const st3_gqa_shape* shape, int32_t total, int32_t max_new, int32_t max_len) {
+    if (st3::check_gqa_shape(shape) != ST3_OK || total < 0 || max_new < 0 || max_len < 0) return 0;
+    return std::max<size_t>(256, st3::chunk_ws(shape, total, max_len).total);
+}
+
+extern "C" st3_status st3_block_attend(const st3_gqa_shape* shape, const st3_rows* q, const int32_t* cu_len, int32_t total, int32_t max_new,
+                                       const st3_block_cache* cache, int32_t max_len, const st3_rows* out, int32_t window, float* score,
+                                       int64_t score_stride_b, int64_t score_stride_h, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace st3;
+    st3_status s = check_gqa_shape(shape);
+    if (s != ST3_OK) return s;
+    if ((s = check_block_cache(shape, cache)) != ST3_OK) return s;
+    const int B = shape->batch, H = shape->heads, Hk = shape->kv_heads, D = shape->head_dim, G = H / Hk;
+    if (!cu_len || total < 0 || max_new < 0 || max_new > total || max_len < 0 || window < 0) return ST3_ERR_INVALID_ARG;
+    if (max_len > kMostRows || (int64_t)max_new * G > kMostRows) return ST3_ERR_UNSUPPORTED;
+    if (total == 0) return ST3_OK;          // (an empty tensor may have no address)
+    if ((s = check_rows(q, D, 2)) != ST3_OK || (s = check_output(out, H, total, D, 2)) != ST3_OK) return s;
+    if (max_new == 0) return ST3_OK;
+    if (cache->table_blocks < max_len / kBlk) return ST3_ERR_INVALID_ARG;
+    if (packed_rows_meet(q, H, out, H, total, D, 2)) return ST3_ERR_INVALID_ARG;
+    if (score && (window < 1 || score_stride_h < max_len || (B > 1 && score_stride_b < max_len))) return ST3_ERR_INVALID_ARG;
+    if (!workspace || !aligned16(workspace)) return ST3_ERR_INVALID_ARG;
+    const ChunkCut cut = chunk_cut(shape, total, max_new, max_len);
+    const int64_t grid = chunk_tiles(shape, total, max_new, 64 * cut.cols) * Hk;
+    if (!grid_fits(grid, 256, cut.pieces) || !grid_fits(((int64_t)total * H + 3) / 4, 256, 1) || (score && (max_len + kBlk - 1) / kBlk > 65535)) return ST3_ERR_UNSUPPORTED;
+    const ChunkWs wl = chunk_ws(shape, total, max_len);
+    if (workspace_bytes < st3_block_attend_workspace_bytes(shape, total, max_new, max_len)) return ST3_ERR_WORKSPACE_TOO_SMALL;
+    char* ws = reinterpret_cast<char*>(workspace);
+    ChunkArgs a{};
+    a.c = block_pages(cache);
+    a.q = reinterpret_cast<const uint16_t*>(q->data); a.out = reinterpret_cast<uint16_t*>(out->data);
+    a.q_st = q->stride_t; a.q_sh = q->stride_h; a.o_st = out->stride_t; a.o_sh = out->stride_h;
+    a.cu = cu_len; a.B = B; a.total = total; a.max_new = max_new; a.max_len = max_len; a.H = H; a.Hk = Hk; a.G = G;
+    a.piece = cut.piece; a.pieces = cut.pieces;
+    a.scale_l2 = gqa_scale_log2(shape);
+    a.score = score; a.s_sb = score_stride_b; a.s_sh = score_stride_h; a.window = window;
+    a.ml = score ? reinterpret_cast<float2*>(ws + wl.ml) : nullptr;
+    a.part_o = reinterpret_cast<float*>(ws + wl.part_o);
+    a.part_ml = reinterpret_cast<float2*>(ws + wl.part_ml);
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    if (cache->code == ST3_BLOCK_INT8) {
+        if (D == 128) launch_chunk<128, ST3_BLOCK_INT8>(a, cut.cols, (unsigned)grid, st);
+        else launch_chunk<64, ST3_BLOCK_INT8>(a, cut.cols, (unsigned)grid, st);
+    } else {
+        if (D == 128) launch_chunk<128, ST3_BLOCK_E4M3>(a, cut.cols, (unsigned)grid, st);
+        else launch_chunk<64, ST3_BLOCK_E4M3>(a, cut.cols, (unsigned)grid, st);
+    }
+    return check_launch();
+}
