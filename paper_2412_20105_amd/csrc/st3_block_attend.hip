@@ -448,84 +448,157 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Scores: the logits of the window's rows are formed again.  Workgroup (key head, block, sequence): each of the four waves has the block's 64 keys in
-// registers and takes 16 rows in turn, straight from memory; a lane adds up what its 16 keys get.
+// Scores: the logits of the window's rows are formed again.  Workgroup (key head, strip of 4 x rounds blocks, sequence): the rows, up to kScoreRows of them, lie in
+// LDS; a wave has the 64 keys of a block in registers, the next block's codes on their way, meets 16 rows at a time, and a lane adds up what its
+// 16 keys get.
 // ---------------------------------------------------------------------------------------------------------------------------------
+constexpr int kScoreRows = 256;         // rows in LDS at a time: 64 KB at d = 128
+
+// Rows in LDS, of a launch whose windows hold `rows` at most.
+inline int score_rows(int64_t rows) { return (int)std::min<int64_t>((rows + 15) / 16 * 16, kScoreRows); }
+
 template <int D, int CODE>
-__global__ __launch_bounds__(256) void chunk_score_kernel(ChunkArgs a) {
+__global__ __launch_bounds__(256, 2) void chunk_score_kernel(ChunkArgs a, int rounds, int fit) {
     using F = BlockCode<CODE>;
-    constexpr int KS = D / 32, KH = D / 64;
+    constexpr int KS = D / 32, KH = D / 64, UPR = D / 8;    // contraction steps; 16-byte pieces of codes in a key's row for a lane; units of a row
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ float part[4][kBlk];
+    u32x4* sm_q = reinterpret_cast<u32x4*>(lds);            // [fit][UPR], unit u of row r at u ^ r: 16 rows' units lie in 16 units of the banks
+    float2* sm_ml = reinterpret_cast<float2*>(lds + (size_t)fit * 2 * D);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-    const int kh = blockIdx.x, u = blockIdx.y, b = blockIdx.z;
+    const int kh = blockIdx.x, u0 = blockIdx.y * (4 * rounds), b = blockIdx.z;
     const Turn sq = turn_of(a, b);
-    const int keys = sq.rows(), blocks = keys / kBlk;
-    if (sq.n < 0 || sq.m <= 0 || u * kBlk >= keys) return;
-    const int page = u < blocks ? page_of(a.c, b, u) : -1;
-    const bool there = u == blocks || page >= 0;
-    f32x4 sum[4];
+    const int keys = sq.rows(), blocks = keys / kBlk, units = (keys + kBlk - 1) / kBlk;
+    if (sq.n < 0 || sq.m <= 0 || u0 >= units) return;
+    const int64_t strip = (int64_t)b * a.Hk + kh;
+    const int u_end = min(units, u0 + 4 * rounds);
+    // lane i has the page and the scale of the wave's i-th block
+    int page_l = -1;
+    float ks_l = 0.f;
+    {
+        const int u = u0 + wave + 4 * lane;
+        if (lane < rounds && u < u_end && u < blocks) page_l = page_of(a.c, b, u);
+        if (page_l >= 0) ks_l = a.c.k_scale[(int64_t)page_l * a.Hk + kh];
+    }
+    // key 16 x + c; a lane's columns are 64 y + 16 g .. + 15, in two steps
+    u32x4 raw[4][KH];
+    const uint32_t k_lane = (uint32_t)(c * D + 16 * g);
+    auto fetch = [&](int i) {                               // (page -1: whatever; it is not used)
+        const int page = max(__builtin_amdgcn_readlane(page_l, i), 0);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(a.c.k_codes + ((int64_t)page * a.Hk + kh) * (kBlk * D), 0, kBlk * D, 0x00020000);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) sum[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (there) {
-        // key 16 x + c; a lane's columns are 64 y + 16 g .. + 15, in two steps
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int y = 0; y < KH; ++y) raw[x][y] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, k_lane, 16 * x * D + 64 * y, 0);
+    };
+    fetch(0);
+    const int rows = sq.m * a.G, first = max(0, sq.m - a.window) * a.G;
+    auto stage = [&](int r0) {                              // rows r0 .. into LDS
+#pragma unroll 4
+        for (int e = tid; e < fit * UPR; e += 256) {
+            const int x = e / UPR, r = min(r0 + x, rows - 1), t = r / a.G;
+            const uint16_t* row = a.q + (int64_t)(sq.start + t) * a.q_st + (int64_t)(kh * a.G + r - t * a.G) * a.q_sh;
+            sm_q[x * UPR + (e % UPR ^ (D == 128 ? x & 15 : x >> 1 & 7))] = reinterpret_cast<const u32x4*>(row)[e % UPR];
+        }
+#pragma unroll 1
+        for (int x = tid; x < fit; x += 256) {
+            const int r = min(r0 + x, rows - 1), t = r / a.G;
+            sm_ml[x] = r0 + x < rows ? a.ml[(int64_t)(sq.start + t) * a.H + kh * a.G + r - t * a.G] : make_float2(0.f, 0.f);
+        }
+    };
+    stage(first);
+    __syncthreads();
+    const bool all_fit = rows - first <= fit;               // (else every round takes the rows piece by piece)
+#pragma unroll 1
+    for (int i = 0; i < rounds; ++i) {
+        const int u = u0 + wave + 4 * i;
+        if (all_fit && u >= u_end) break;
+        const bool tail = u == blocks && u < u_end, there = tail || __builtin_amdgcn_readlane(page_l, i) >= 0;
+        const float ks = tail ? a.scale_l2 : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), i)) * a.scale_l2;
         Frag kf[4][KS];
-        float scale = a.scale_l2;
-        if (u < blocks) {
-            const int64_t at = (int64_t)page * a.Hk + kh;
-            const uint8_t* codes = a.c.k_codes + at * (kBlk * D);
-            scale *= a.c.k_scale[at];
+        if (tail) {
+            const uint16_t* from = a.c.k_tail + strip * (kBlk * D);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kf[x][s].u4 = *reinterpret_cast<const u32x4*>(from + (16 * x + c) * D + 64 * (s / 2) + 16 * g + 8 * (s & 1));
+        } else {
 #pragma unroll
             for (int x = 0; x < 4; ++x)
 #pragma unroll
                 for (int y = 0; y < KH; ++y) {
-                    const u32x4 w = *reinterpret_cast<const u32x4*>(codes + (16 * x + c) * D + 64 * y + 16 * g);
+                    const u32x4 w = raw[x][y];
                     const uint2 w0 = F::to_bf16(w.x), w1 = F::to_bf16(w.y), w2 = F::to_bf16(w.z), w3 = F::to_bf16(w.w);
                     kf[x][2 * y].u4 = u32x4{w0.x, w0.y, w1.x, w1.y};
                     kf[x][2 * y + 1].u4 = u32x4{w2.x, w2.y, w3.x, w3.y};
                 }
-        } else {
-            const uint16_t* tail = a.c.k_tail + ((int64_t)b * a.Hk + kh) * (kBlk * D);
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-#pragma unroll
-                for (int s = 0; s < KS; ++s) kf[x][s].u4 = *reinterpret_cast<const u32x4*>(tail + (16 * x + c) * D + 64 * (s / 2) + 16 * g + 8 * (s & 1));
         }
-        const int rows = sq.m * a.G, from = max(max(0, sq.m - a.window), u * kBlk - sq.n);      // (rows in front see none of these keys)
-        for (int r0 = from * a.G + 16 * wave; r0 < rows; r0 += 64) {
-            const int r = min(r0 + c, rows - 1), t = r / a.G, head = kh * a.G + r - t * a.G;
-            const uint16_t* row = a.q + (int64_t)(sq.start + t) * a.q_st + (int64_t)head * a.q_sh;
-            Frag qf[KS];
+        __builtin_amdgcn_sched_barrier(0);
+        if (i + 1 < rounds) fetch(i + 1);
+        const int key = u * kBlk + lane;
+        float* to = a.score + b * a.s_sb + kh * a.s_sh + key;
+        const float old = u < u_end && key < sq.n ? *to : 0.f;
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 sum[4];
 #pragma unroll
-            for (int s = 0; s < KS; ++s) qf[s].u4 = *reinterpret_cast<const u32x4*>(row + 64 * (s / 2) + 16 * g + 8 * (s & 1));
-            const float2 ml = a.ml[(int64_t)(sq.start + t) * a.H + head];
-            const int pos = r0 + c < rows ? sq.n + t : -1;      // (a row that does not exist sees nothing)
+        for (int x = 0; x < 4; ++x) sum[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int r0 = first;;) {
+            const int here = min(fit, rows - r0);
+            if (there) {
+                // 16 rows, this lane's the one of column c: logits, weights
+                auto add = [&](int x0, auto masked) {
+                    const float2 ml = sm_ml[x0 + c];
+                    const int pos = sq.n + (r0 + x0 + c) / a.G;
+                    Frag qf[KS];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                f32x4 y = {0.f, 0.f, 0.f, 0.f};
+                    for (int s = 0; s < KS; ++s)
+                        qf[s].u4 = sm_q[(x0 + c) * UPR + ((8 * (s / 2) + 2 * g + (s & 1)) ^ (D == 128 ? c : (x0 + c) >> 1 & 7))];
 #pragma unroll
-                for (int s = 0; s < KS; ++s) y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x][s].v, qf[s].v, y, 0, 0, 0);
+                    for (int x = 0; x < 4; ++x) {
+                        f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = exp2_fast(fmaf(y[i], scale, -ml.x)) * ml.y;
-                    sum[x][i] += u * kBlk + 16 * x + 4 * g + i > pos ? 0.f : p;
+                        for (int s = 0; s < KS; ++s) y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x][s].v, qf[s].v, y, 0, 0, 0);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float p = exp2_fast(fmaf(y[j], ks, -ml.x));
+                            if constexpr (decltype(masked)::value) {
+                                const bool seen = u * kBlk + 16 * x + 4 * g + j <= pos && x0 + c < here;      // (a row that does not exist sees nothing)
+                                sum[x][j] += seen ? p * ml.y : 0.f;
+                            } else {
+                                sum[x][j] = fmaf(p, ml.y, sum[x][j]);
+                            }
+                        }
+                        if (x & 1) __builtin_amdgcn_sched_barrier(0);       // (else all products are kept at once)
+                    }
+                };
+#pragma unroll 1
+                for (int x0 = 0; x0 < here; x0 += 16) {
+                    if (x0 + 16 <= here && u * kBlk + kBlk - 1 <= sq.n + (r0 + x0) / a.G) add(x0, std::false_type{});
+                    else add(x0, std::true_type{});
                 }
             }
+            r0 += fit;
+            if (r0 >= rows) break;
+            __syncthreads();
+            stage(r0);
+            __syncthreads();
         }
-    }
+        if (!all_fit && i + 1 < rounds) {                   // the next round begins with the first rows again
+            __syncthreads();
+            stage(first);
+            __syncthreads();
+        }
+        if (u >= u_end) continue;
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
+        for (int x = 0; x < 4; ++x)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[x][i] = group_sum<16>(sum[x][i]);
-    if (c == 0) {
+            for (int j = 0; j < 4; ++j) sum[x][j] = group_sum<16>(sum[x][j]);
+        if (c == 0) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4*>(&part[wave][16 * x + 4 * g]) = sum[x];
-    }
-    __syncthreads();
-    const int key = u * kBlk + tid;
-    if (tid < kBlk && key < keys) {
-        float* to = a.score + b * a.s_sb + kh * a.s_sh + key;
-        const float got = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
-        *to = key < sq.n ? *to + got : got;
+            for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4*>(&part[wave][16 * x + 4 * g]) = sum[x];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        if (key < keys) *to = old + part[wave][lane];       // (written by this wave)
     }
 }
 
@@ -547,6 +620,13 @@ inline ChunkCut chunk_cut(const st3_gqa_shape* s, int total, int max_new, int ma
     return ChunkCut{cols, (int)piece, (int)((units + piece - 1) / piece)};
 }
 
+// Blocks that a wave of the scores' launch takes one behind the other.
+constexpr int kScoreWgs = 2048, kMostRounds = 16;
+inline int score_rounds(int64_t units, int Hk, int B) {
+    const int64_t want = units * Hk * B / (4 * kScoreWgs);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(want, kMostRounds));
+}
+
 struct ChunkWs { size_t ml, part_o, part_ml, total; };
 // Room for as many parts as a launch of any smaller sizes may leave: kWanted tiles of 128 rows and one part more for each row, or one for every kLeastPiece blocks.
 inline ChunkWs chunk_ws(const st3_gqa_shape* s, int total, int max_len) {
@@ -566,7 +646,9 @@ void launch_chunk(const ChunkArgs& a, int cols, unsigned grid, hipStream_t st) {
     if (cols == 1) block_chunk_kernel<D, CODE, 1><<<dim3(grid, a.pieces), 256, 0, st>>>(a);
     else block_chunk_kernel<D, CODE, 2><<<dim3(grid, a.pieces), 256, 0, st>>>(a);
     if (a.pieces > 1) chunk_join_kernel<D><<<(unsigned)(((int64_t)a.total * a.H + 3) / 4), 256, 0, st>>>(a);
-    if (a.score && a.max_len > 0) chunk_score_kernel<D, CODE><<<dim3(a.Hk, (a.max_len + kBlk - 1) / kBlk, a.B), 256, 0, st>>>(a);
+    if (!a.score || a.max_len == 0) return;
+    const int fit = score_rows((int64_t)std::min(a.window, a.max_new) * a.G), units = (a.max_len + kBlk - 1) / kBlk, rounds = score_rounds(units, a.Hk, a.B);
+    chunk_score_kernel<D, CODE><<<dim3(a.Hk, (units + 4 * rounds - 1) / (4 * rounds), a.B), 256, fit * (2 * D + sizeof(float2)), st>>>(a, rounds, fit);
 }
 
 }  // namespace
@@ -596,7 +678,7 @@ extern "C" st3_status st3_block_attend(const st3_gqa_shape* shape, const st3_row
     if (!workspace || !aligned16(workspace)) return ST3_ERR_INVALID_ARG;
     const ChunkCut cut = chunk_cut(shape, total, max_new, max_len);
     const int64_t grid = chunk_tiles(shape, total, max_new, 64 * cut.cols) * Hk;
-    if (!grid_fits(grid, 256, cut.pieces) || !grid_fits(((int64_t)total * H + 3) / 4, 256, 1) || (score && (max_len + kBlk - 1) / kBlk > 65535)) return ST3_ERR_UNSUPPORTED;
+    if (!grid_fits(grid, 256, cut.pieces) || !grid_fits(((int64_t)total * H + 3) / 4, 256, 1) || (score && (max_len + 4 * kBlk - 1) / (4 * kBlk) > 65535)) return ST3_ERR_UNSUPPORTED;
     const ChunkWs wl = chunk_ws(shape, total, max_len);
     if (workspace_bytes < st3_block_attend_workspace_bytes(shape, total, max_new, max_len)) return ST3_ERR_WORKSPACE_TOO_SMALL;
     char* ws = reinterpret_cast<char*>(workspace);
