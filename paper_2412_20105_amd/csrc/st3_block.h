@@ -115,6 +115,12 @@ __device__ __forceinline__ int wave_most(int x) {
     return __builtin_amdgcn_readlane(x, 63);
 }
 
+// Two float32 as two bf16, rounded to nearest even (NaN stays NaN).
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    const f32x2 v = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+
 // Page of block j of sequence b; -1: there is none.
 __device__ __forceinline__ int page_of(const BlockPages& c, int b, int j) {
     if (j >= c.table_blocks) return -1;

@@ -16,12 +16,19 @@
 namespace st3 {
 namespace {
 
+#ifndef KAHEAD1
+#define KAHEAD1 3
+#define VAHEAD1 4
+#endif
+constexpr int kChunkWaves = 8, kChunkThreads = 64 * kChunkWaves;
+
 struct ChunkArgs {
     BlockPages c;
     const uint16_t* q; uint16_t* out;
     int64_t q_st, q_sh, o_st, o_sh;
     const int32_t* cu;
     int32_t B, total, max_new, max_len, H, Hk, G;
+    int32_t tile;                   // rows of a row tile: a multiple of 16
     int32_t piece, pieces;          // blocks of a piece; pieces of the longest strip (1: whole strips)
     float scale_l2;
     float* score; int64_t s_sb, s_sh;
@@ -42,30 +49,44 @@ __device__ __forceinline__ Turn turn_of(const ChunkArgs& a, int b) {
     return Turn{s, min(min(e - s, a.max_new), n < 0 ? a.max_new : max(a.max_len - n, 0)), n};
 }
 
-// Workgroup -> (sequence, key head, row tile).  Key heads run fastest (they go round-robin to the 8 XCDs); every wave finds its place, a lane for each of 64
-// sequences at a time.
-template <int ROWS>
+// Workgroup -> (sequence, key head, row tile).  Key heads run fastest (they go round-robin to the 8 XCDs), longest sequences come first, so that the launch
+// ends with its shortest workgroups; more than 64 keep their own order.  Lengths are known to the device only: every wave finds its place, a lane for
+// each sequence.
 __device__ __forceinline__ bool place(const ChunkArgs& a, int lane, int& b, int& kh, int& tile, Turn& sq) {
     kh = blockIdx.x % a.Hk;
     int x = blockIdx.x / a.Hk;
-    for (int i0 = 0; i0 < a.B; i0 += kWave) {
-        Turn its = {0, 0, 0};
-        int mine = 0;
-        if (i0 + lane < a.B) {
-            its = turn_of(a, i0 + lane);
-            mine = (int)(((int64_t)its.m * a.G + ROWS - 1) / ROWS);
+    Turn its = {0, 0, 0};
+    auto tiles_of = [&](int i) {
+        if (i < a.B) its = turn_of(a, i);
+        return i < a.B ? (its.m * a.G + a.tile - 1) / a.tile : 0;
+    };
+    auto found = [&](int first, int at, int t) {        // (lane `at` has sequence first + at)
+        at = __builtin_amdgcn_readfirstlane(at);
+        b = first + at;
+        tile = __builtin_amdgcn_readfirstlane(t);
+        sq = Turn{__builtin_amdgcn_readlane(its.start, at), __builtin_amdgcn_readlane(its.m, at), __builtin_amdgcn_readlane(its.n, at)};
+        return true;
+    };
+    if (a.B > kWave) {
+        for (int i0 = 0; i0 < a.B; i0 += kWave) {
+            const int mine = tiles_of(i0 + lane), upto = wave_prefix(mine), all = __builtin_amdgcn_readlane(upto, 63);
+            if (x < all) {
+                const int at = __ffsll((unsigned long long)__ballot(x < upto)) - 1;
+                return found(i0, at, __builtin_amdgcn_readlane(upto, at) - 1 - x);
+            }
+            x -= all;
         }
-        const int upto = wave_prefix(mine), all = __builtin_amdgcn_readlane(upto, 63);
-        if (x < all) {
-            const int at = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(x < upto)) - 1);
-            b = i0 + at;
-            tile = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_readlane(upto, at) - 1 - x);
-            sq = Turn{__builtin_amdgcn_readlane(its.start, at), __builtin_amdgcn_readlane(its.m, at), __builtin_amdgcn_readlane(its.n, at)};
-            return true;
-        }
-        x -= all;
+        return false;
     }
-    return false;
+    const int mine = tiles_of(lane), rows = its.rows();
+    if (x >= wave_total(mine)) return false;
+    int before = 0;                     // tiles of the sequences in front of this one
+    for (int i = 0; i < a.B; ++i) {
+        const int other = __builtin_amdgcn_readlane(rows, i);
+        before += other > rows || (other == rows && i < lane) ? __builtin_amdgcn_readlane(mine, i) : 0;
+    }
+    const int at = __ffsll((unsigned long long)__ballot(mine > 0 && before <= x && x < before + mine)) - 1;
+    return found(0, at, __builtin_amdgcn_readlane(before + mine, at) - 1 - x);
 }
 
 // A block in LDS: K as 64 rows of D bf16, V as D rows (columns of V) of 64.  Unit u (16 bytes) of row r lies at u ^ swz(r): the 16 rows that a fragment's
@@ -80,31 +101,30 @@ template <int D> struct Tile {
 
 __device__ __forceinline__ void lds_write16(uint32_t at, u32x4 x) { *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(at) = x; }
 
-// A block's codes on their way from memory to LDS.
+// A block's codes on their way from memory to LDS: pieces of 16 bytes, those of K and then those of V, dealt to the threads.
 template <int D, int CODE, int THREADS>
 struct Codes {
-    static constexpr int N = kBlk * D / 16 / THREADS;
-    u32x4 k[N], v[N];
+    static constexpr int PIECES = kBlk * D / 16, N = 2 * PIECES / THREADS;
+    static_assert(N * THREADS == 2 * PIECES && PIECES % kWave == 0, "whole waves take pieces of K, or of V");
+    u32x4 w[N];
     __device__ __forceinline__ void load(const BlockPages& c, int64_t at, int tid) {
-        const u32x4* kp = reinterpret_cast<const u32x4*>(c.k_codes + at * (kBlk * D));
-        const u32x4* vp = reinterpret_cast<const u32x4*>(c.v_codes + at * (kBlk * D));
 #pragma unroll
-        for (int i = 0; i < N; ++i) k[i] = kp[tid + i * THREADS];
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = vp[tid + i * THREADS];
+        for (int i = 0; i < N; ++i) {
+            const int p = tid + i * THREADS;
+            const uint8_t* codes = p < PIECES ? c.k_codes : c.v_codes;
+            w[i] = reinterpret_cast<const u32x4*>(codes + at * (kBlk * D))[p < PIECES ? p : p - PIECES];
+        }
     }
     __device__ __forceinline__ void store(uint32_t lds, int tid) const {
         using F = BlockCode<CODE>;
-        auto put = [](uint32_t row_at, int unit, int swz, const u32x4& w) {
-            const uint2 a = F::to_bf16(w.x), b = F::to_bf16(w.y), c = F::to_bf16(w.z), d = F::to_bf16(w.w);
-            lds_write16(row_at + 16 * (unit ^ swz), u32x4{a.x, a.y, b.x, b.y});
-            lds_write16(row_at + 16 * ((unit + 1) ^ swz), u32x4{c.x, c.y, d.x, d.y});
-        };
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int p = tid + i * THREADS, kr = p / (D / 16), vr = p / (kBlk / 16);
-            put(lds + 2 * D * kr, 2 * (p % (D / 16)), Tile<D>::k_swz(kr), k[i]);
-            put(lds + 2 * Tile<D>::K + 2 * kBlk * vr, 2 * (p % (kBlk / 16)), Tile<D>::v_swz(vr), v[i]);
+            const int p = tid + i * THREADS, kr = p / (D / 16), vr = (p - PIECES) / (kBlk / 16);
+            const uint32_t row_at = p < PIECES ? lds + 2 * D * kr : lds + 2 * Tile<D>::K + 2 * kBlk * vr;
+            const int swz = p < PIECES ? Tile<D>::k_swz(kr) : Tile<D>::v_swz(vr), unit = p < PIECES ? 2 * (p % (D / 16)) : 2 * (p % (kBlk / 16));
+            const uint2 a = F::to_bf16(w[i].x), b = F::to_bf16(w[i].y), c = F::to_bf16(w[i].z), d = F::to_bf16(w[i].w);
+            lds_write16(row_at + 16 * (unit ^ swz), u32x4{a.x, a.y, b.x, b.y});
+            lds_write16(row_at + 16 * ((unit + 1) ^ swz), u32x4{c.x, c.y, d.x, d.y});
         }
     }
 };
@@ -115,6 +135,7 @@ __device__ __forceinline__ void tail_to_lds(const BlockPages& c, int64_t strip, 
     const u32x4* kp = reinterpret_cast<const u32x4*>(c.k_tail + strip * (kBlk * D));
     const u32x4* vp = reinterpret_cast<const u32x4*>(c.v_tail + strip * (kBlk * D));
     constexpr int N = kBlk * D / 8 / THREADS;
+    static_assert(N * THREADS == kBlk * D / 8, "all of the tail");
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int p = tid + i * THREADS, kr = p / (D / 8), vr = p / (kBlk / 8);
@@ -145,50 +166,83 @@ struct Rows {
     }
 };
 
-// 64 keys for one wave; ks: the block's scale of K times that of the logits (in the log2 domain), vs: of V.  MASKED: some row does not see some
-// of the keys.  CAREFUL: V may hold infinities or NaN, and a weight of 0 does not silence those; row by row, V's keys that the row does not see count as 0.
-template <int D, int QC, bool MASKED, bool CAREFUL = false>
-__device__ __forceinline__ void chunk_step(uint32_t k_at, uint32_t v_at, const Frag (&qf)[QC][D / 32], Rows<D, QC>& st, float ks, float vs, int g, int k0) {
-    constexpr int KS = D / 32, DT = D / 16;
-    f32x4 s[4][QC];
-    __builtin_amdgcn_s_setprio(1);
+// S^T = K Q^T of 64 keys.
+template <int D, int QC>
+__device__ __forceinline__ void chunk_logits(uint32_t k_at, const Frag (&qf)[QC][D / 32], f32x4 (&s)[4][QC]) {
+    constexpr int KS = D / 32;
+    constexpr int AHEAD = QC == 1 ? KAHEAD1 : 1;
+    Frag ka[AHEAD + 1][KS];
+    auto load = [&](int t) {
+#pragma unroll
+        for (int x = 0; x < KS; ++x) ka[t % (AHEAD + 1)][x].u4 = lds_read16((k_at ^ (64 * x)) + 8 * D * t);
+    };
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) load(t);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        Frag ka[KS];
+        if (t + AHEAD < 4) load(t + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int x = 0; x < KS; ++x) ka[x].u4 = lds_read16((k_at ^ (64 * x)) + 8 * D * t);
+        for (int qc = 0; qc < QC; ++qc) s[t][qc] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < KS; ++x)
+#pragma unroll
+            for (int qc = 0; qc < QC; ++qc) s[t][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[t % (AHEAD + 1)][x].v, qf[qc][x].v, s[t][qc], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// O^T += V^T P^T of 64 keys.
+template <int D, int QC>
+__device__ __forceinline__ void chunk_values(uint32_t v_at, const Frag (&pb)[2][QC], Rows<D, QC>& st) {
+    constexpr int DT = D / 16, AHEAD = QC == 1 ? VAHEAD1 : 2;
+    Frag va[AHEAD + 1][2];
+    auto load = [&](int dt) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) va[dt % (AHEAD + 1)][x].u4 = lds_read16((v_at ^ (16 * x)) + 32 * kBlk * dt);
+    };
+#pragma unroll
+    for (int dt = 0; dt < AHEAD; ++dt) load(dt);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+        if (dt + AHEAD < DT) load(dt + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int qc = 0; qc < QC; ++qc) st.o[dt][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[dt % (AHEAD + 1)][x].v, pb[x][qc].v, st.o[dt][qc], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// 64 keys for one wave, some of which some row may not see; ks: the block's scale of K times that of the logits (in the log2 domain), vs: of V.
+// CAREFUL: V may hold infinities or NaN, and a weight of 0 does not silence those; row by row, V's keys that the row does not see count as 0.
+// A weight times V's scale is rounded to bf16 once, to nearest: an error of 2^-8 of it at most and without bias, beside the output's own rounding by as
+// much; the sum is of the unrounded ones.
+template <int D, int QC, bool CAREFUL = false>
+__device__ __forceinline__ void chunk_step(uint32_t k_at, uint32_t v_at, const Frag (&qf)[QC][D / 32], Rows<D, QC>& st, float ks, float vs, int g, int k0) {
+    constexpr int DT = D / 16;
+    f32x4 s[4][QC];
+    chunk_logits<D, QC>(k_at, qf, s);
+    // (a block's scale may be 0, and -infinity times 0 is no number: masks come behind the scale)
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int qc = 0; qc < QC; ++qc) {
-            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+            s[t][qc] *= ks;
 #pragma unroll
-            for (int x = 0; x < KS; ++x) y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[x].v, qf[qc][x].v, y, 0, 0, 0);
-            s[t][qc] = y;
+            for (int i = 0; i < 4; ++i)
+                if (k0 + 16 * g + 4 * t + i > st.pos[qc]) s[t][qc][i] = -INFINITY;
         }
-    }
-    __builtin_amdgcn_s_setprio(0);
-    // (a block's scale may be 0, and -infinity times 0 is no number: masks come behind the scale)
-    if (MASKED) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int qc = 0; qc < QC; ++qc) {
-                s[t][qc] *= ks;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (k0 + 16 * g + 4 * t + i > st.pos[qc]) s[t][qc][i] = -INFINITY;
-            }
-    }
-    const float by = MASKED ? 1.0f : ks;
-    // the reference point of the exponents follows the maximum only when that has moved by more than kLazy (weights reach 2^kLazy at most)
+    // the reference point of the exponents follows the maximum only when that has moved by more than kLazy
     constexpr float kLazy = 8.0f;
     float mx[QC];
     bool moved = false;
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc) {
-        float x = -INFINITY;
+        mx[qc] = -INFINITY;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) x = fmaxf(x, fmaxf(fmaxf(s[t][qc][0], s[t][qc][1]), fmaxf(s[t][qc][2], s[t][qc][3])));
-        mx[qc] = x * by;
+        for (int t = 0; t < 4; ++t) mx[qc] = fmaxf(mx[qc], fmaxf(fmaxf(s[t][qc][0], s[t][qc][1]), fmaxf(s[t][qc][2], s[t][qc][3])));
         moved |= mx[qc] - st.m[qc] > kLazy;
     }
     if (__any(moved)) {
@@ -203,8 +257,6 @@ __device__ __forceinline__ void chunk_step(uint32_t k_at, uint32_t v_at, const F
             for (int dt = 0; dt < DT; ++dt) st.o[dt][qc] *= alpha;
         }
     }
-    // A weight times V's scale is rounded to bf16 once, to nearest: an error of 2^-8 of it at most and without bias, beside the output's own rounding by as
-    // much; the sum is of the unrounded ones.
     Frag pb[2][QC];
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc)
@@ -212,16 +264,16 @@ __device__ __forceinline__ void chunk_step(uint32_t k_at, uint32_t v_at, const F
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float s0 = s[2 * x + j / 2][qc][2 * (j & 1)], s1 = s[2 * x + j / 2][qc][2 * (j & 1) + 1];
-                const float p0 = exp2_fast(fmaf(s0, by, -st.m[qc])), p1 = exp2_fast(fmaf(s1, by, -st.m[qc]));
+                const f32x4 y = s[2 * x + j / 2][qc];
+                const float p0 = exp2_fast(y[2 * (j & 1)] - st.m[qc]), p1 = exp2_fast(y[2 * (j & 1) + 1] - st.m[qc]);
                 st.l[qc] += p0 + p1;
-                const f32x2 w = {p0 * vs, p1 * vs};
-                pb[x][qc].w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(w, bf16x2));
+                pb[x][qc].w[j] = bf16_pair(p0 * vs, p1 * vs);
             }
     if constexpr (CAREFUL) {
         const int c = threadIdx.x & 15;
 #pragma unroll
         for (int qc = 0; qc < QC; ++qc)
+#pragma unroll 1
             for (int row = 0; row < 16; ++row) {
                 const int pos = __builtin_amdgcn_readlane(st.pos[qc], row);
 #pragma unroll
@@ -240,42 +292,69 @@ __device__ __forceinline__ void chunk_step(uint32_t k_at, uint32_t v_at, const F
                         for (int j = 0; j < 4; ++j) va.w[j] &= seen.w[j];
                         const f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va.v, pb[x][qc].v, st.o[dt][qc], 0, 0, 0);
                         st.o[dt][qc] = c == row ? o : st.o[dt][qc];
+                        __builtin_amdgcn_sched_barrier(0);
                     }
                 }
             }
         return;
     }
+    chunk_values<D, QC>(v_at, pb, st);
+}
+
+// The same of a block that every row sees whole, nearly all of them.  The reference point stays where it is (weights are floating point, in bf16 too: nothing is
+// lost as long as none of them grows large), and V's scale comes with the exponent: exp2(s ks - m + log2 vs); what a lane adds to the sum is that
+// divided by vs.  False, and nothing done, where weights have grown above kMost, are no numbers, or vs has no logarithm (lvs is NaN then).
+template <int D, int QC>
+__device__ __forceinline__ bool chunk_step_whole(uint32_t k_at, uint32_t v_at, const Frag (&qf)[QC][D / 32], Rows<D, QC>& st, float ks, float lvs, float rvs) {
+    constexpr float kMost = 4096.0f;
+    f32x4 s[4][QC];
     __builtin_amdgcn_s_setprio(1);
+    chunk_logits<D, QC>(k_at, qf, s);
+    __builtin_amdgcn_s_setprio(0);
+    Frag pb[2][QC];
+    float sum[QC];
+    bool large = false;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-        Frag va[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) va[x].u4 = lds_read16((v_at ^ (16 * x)) + 32 * kBlk * dt);
+    for (int qc = 0; qc < QC; ++qc) {
+        const float off = lvs - st.m[qc];
+        sum[qc] = 0.f;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int qc = 0; qc < QC; ++qc) st.o[dt][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[x].v, pb[x][qc].v, st.o[dt][qc], 0, 0, 0);
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 y = s[2 * x + j / 2][qc];
+                const float w0 = exp2_fast(fmaf(y[2 * (j & 1)], ks, off)), w1 = exp2_fast(fmaf(y[2 * (j & 1) + 1], ks, off));
+                sum[qc] += w0 + w1;
+                pb[x][qc].w[j] = bf16_pair(w0, w1);
+            }
+        sum[qc] *= rvs;
+        large |= !(sum[qc] <= kMost);
     }
+    if (__any(large)) return false;
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc) st.l[qc] += sum[qc];
+    __builtin_amdgcn_s_setprio(1);
+    chunk_values<D, QC>(v_at, pb, st);
     __builtin_amdgcn_s_setprio(0);
+    return true;
 }
 
-template <int D, int CODE, int QC>
-__global__ __launch_bounds__(256, 2) void block_chunk_kernel(ChunkArgs a) {
-    constexpr int kThr = 256, kRows = 64 * QC, KS = D / 32, DT = D / 16, OSTR = D + 8;
-    using L = Tile<D>;
-    constexpr int kOut = 2 * 4 * 16 * QC * OSTR;            // bytes
-    __shared__ __attribute__((aligned(1024))) uint8_t buf[2 * L::BYTES > kOut ? 2 * L::BYTES : kOut];
-    __shared__ int redo;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15, ch = blockIdx.y;
-    int b, kh, tile;
+// What a workgroup works on.
+struct Work {
     Turn sq;
-    if (!place<kRows>(a, lane, b, kh, tile, sq)) return;
-    const int rows = sq.m * a.G, r0 = tile * kRows + wave * 16 * QC;        // the wave's first row
-    const int last = sq.sees((min(rows, (tile + 1) * kRows) - 1) / a.G);    // the last row that the workgroup sees
-    const int u_begin = ch * a.piece, u_end = min((last + kBlk) / kBlk, u_begin + a.piece), blocks = sq.rows() / kBlk;     // (last may be -1)
-    if (ch > 0 && u_begin >= u_end) return;
-    if (tid == 0) redo = 0;
-    const int64_t strip = (int64_t)b * a.Hk + kh;
+    int64_t strip;
+    int kh, ch, b, rows, u_begin, u_end;
+};
+
+// One wave's part of it: 16 QC rows from row r0 on (idle: none).  Every wave of a workgroup meets the same barriers, whatever its QC.
+template <int D, int CODE, int QC, int COLS>
+__device__ __forceinline__ void chunk_wave(const ChunkArgs& a, const Work& w, uint8_t* buf, int* redo, int r0, bool idle) {
+    constexpr int kThr = kChunkThreads, KS = D / 32, DT = D / 16, OSTR = D + 8;
+    using L = Tile<D>;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
+    const int rows = w.rows, kh = w.kh, b = w.b, ch = w.ch, u_begin = w.u_begin, u_end = w.u_end, blocks = w.sq.rows() / kBlk;
+    const Turn& sq = w.sq;
+    const int64_t strip = w.strip;
     const uint32_t lds0 = lds_addr(buf);
     Rows<D, QC> st;
     st.init();
@@ -289,12 +368,11 @@ __global__ __launch_bounds__(256, 2) void block_chunk_kernel(ChunkArgs a) {
         for (int s = 0; s < KS; ++s) qf[qc][s].u4 = *reinterpret_cast<const u32x4*>(row + 32 * s + 8 * g);
     }
     const int p_first = sq.sees(min(r0, rows - 1) / a.G), p_last = sq.sees((min(r0 + 16 * QC, rows) - 1) / a.G);      // what the wave's first and last rows see
-    const bool idle = r0 >= rows;
     const int krow = 16 * (c >> 2) + (c & 3);
     const uint32_t k_lane = (uint32_t)(2 * D * krow + 16 * (g ^ L::k_swz(krow))), v_lane = (uint32_t)(2 * L::K + 2 * kBlk * c + 16 * (2 * g ^ L::v_swz(c)));
     // lane i has the page and the scales of block `base` + i
     int base = 0, page_l = -1;
-    float ks_l = 0.f, vs_l = 0.f;
+    float ks_l = 0.f, vs_l = 0.f, lvs_l = 0.f, rvs_l = 0.f;
     auto look_up = [&](int from) {
         base = from;
         const int u = from + lane;
@@ -302,42 +380,52 @@ __global__ __launch_bounds__(256, 2) void block_chunk_kernel(ChunkArgs a) {
         ks_l = vs_l = 0.f;
         if (page_l >= 0) {
             const int64_t at = (int64_t)page_l * a.Hk + kh;
-            ks_l = a.c.k_scale[at];
+            ks_l = a.c.k_scale[at] * a.scale_l2;
             vs_l = a.c.v_scale[at];
         }
+        // (0, and scales so small or large that weights times them leave the normal range, have no logarithm here)
+        lvs_l = vs_l > 0x1p-90f && vs_l < 0x1p90f ? __builtin_amdgcn_logf(vs_l) : __uint_as_float(0x7fc00000u);
+        rvs_l = 1.0f / vs_l;
     };
+    auto lane_value = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
+    const int u_stop = min(u_end, blocks);
+    // A block on its way, and its scales; two of them, one for even and one for odd steps.
+    struct Next { Codes<D, CODE, kThr> codes; int page; float ks, vs, lvs, rvs; };
     auto walk = [&](auto careful) {
         constexpr bool kCareful = decltype(careful)::value;
-        Codes<D, CODE, kThr> codes;
-        look_up(u_begin);
-        auto page_at = [&](int u) {
+        Next next[2];
+        auto fetch = [&](int u, Next& x) {
+            if (u >= u_stop) return;
             if (u >= base + kWave) look_up(u);
-            return __builtin_amdgcn_readlane(page_l, u - base);
+            const int i = u - base;
+            x.page = __builtin_amdgcn_readlane(page_l, i);
+            x.ks = lane_value(ks_l, i); x.vs = lane_value(vs_l, i); x.lvs = lane_value(lvs_l, i); x.rvs = lane_value(rvs_l, i);
+            if (x.page >= 0) x.codes.load(a.c, (int64_t)x.page * a.Hk + kh, tid);
         };
-        int u = u_begin, slot = 0;
-        const int u_stop = min(u_end, blocks);
-        int page = u < u_stop ? page_at(u) : -1;
-        if (page >= 0) codes.load(a.c, (int64_t)page * a.Hk + kh, tid);
-        for (; u < u_stop; ++u, slot ^= 1) {
-            const bool there = page >= 0;                   // (a block without a page is passed over)
-            const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), u - base)) * a.scale_l2;
-            const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_l), u - base));
-            const uint32_t at = lds0 + slot * L::BYTES;
-            if (there) codes.store(at, tid);
+        auto step = [&](int u, Next& x, uint32_t at) {
+            const bool there = x.page >= 0;                 // (a block without a page is passed over)
+            const float ks = x.ks, vs = x.vs, lvs = x.lvs, rvs = x.rvs;
+            if (there) x.codes.store(at, tid);
             __syncthreads();
-            if (u + 1 < u_stop) {
-                page = page_at(u + 1);
-                if (page >= 0) codes.load(a.c, (int64_t)page * a.Hk + kh, tid);
-            }
-            if (!there || idle) continue;
-            if (u * kBlk + kBlk - 1 <= p_first) chunk_step<D, QC, false>(at + k_lane, at + v_lane, qf, st, ks, vs, g, u * kBlk);
-            else if (u * kBlk <= p_last) chunk_step<D, QC, true, kCareful>(at + k_lane, at + v_lane, qf, st, ks, vs, g, u * kBlk);
+            fetch(u + 2, x);
+            if (!there || idle || u * kBlk > p_last) return;
+            if (u * kBlk + kBlk - 1 <= p_first && chunk_step_whole<D, QC>(at + k_lane, at + v_lane, qf, st, ks, lvs, rvs)) return;
+            chunk_step<D, QC, kCareful>(at + k_lane, at + v_lane, qf, st, ks, vs, g, u * kBlk);
+        };
+        look_up(u_begin);
+        fetch(u_begin, next[0]);
+        fetch(u_begin + 1, next[1]);
+        int u = u_begin;
+        for (; u + 1 < u_stop; u += 2) {
+            step(u, next[0], lds0);
+            step(u + 1, next[1], lds0 + L::BYTES);
         }
+        if (u < u_stop) step(u, next[0], lds0);
         if (blocks >= u_begin && blocks < u_end) {          // the rows in 16 bits
-            const uint32_t at = lds0 + slot * L::BYTES;
+            const uint32_t at = lds0 + (u < u_stop ? L::BYTES : 0);
             tail_to_lds<D, kThr>(a.c, strip, sq.rows() % kBlk, at, tid);
             __syncthreads();
-            if (!idle && blocks * kBlk <= p_last) chunk_step<D, QC, true, kCareful>(at + k_lane, at + v_lane, qf, st, a.scale_l2, 1.0f, g, blocks * kBlk);
+            if (!idle && blocks * kBlk <= p_last) chunk_step<D, QC, kCareful>(at + k_lane, at + v_lane, qf, st, a.scale_l2, 1.0f, g, blocks * kBlk);
         }
     };
     walk(std::false_type{});
@@ -349,9 +437,9 @@ __global__ __launch_bounds__(256, 2) void block_chunk_kernel(ChunkArgs a) {
         for (int qc = 0; qc < QC; ++qc)
 #pragma unroll
             for (int i = 0; i < 4; ++i) odd = fmaf(st.o[dt][qc][i], 0.f, odd);
-    if (odd != 0.f) redo = 1;
+    if (odd != 0.f) *redo = 1;
     __syncthreads();
-    if (redo) {
+    if (*redo) {
         st.init();
         walk(std::true_type{});
         __syncthreads();
@@ -361,7 +449,7 @@ __global__ __launch_bounds__(256, 2) void block_chunk_kernel(ChunkArgs a) {
         for (int qc = 0; qc < QC; ++qc) {
             const float l = wave_sum_from<16>(st.l[qc]);
             const int r = r0 + 16 * qc + c, t = r / a.G;
-            if (r >= rows) continue;
+            if (r >= rows || idle) continue;
             const int64_t part = ((int64_t)(sq.start + t) * a.H + kh * a.G + r - t * a.G) * a.pieces + ch;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(a.part_o + part * D + 16 * dt + 4 * g) = st.o[dt][qc];
@@ -370,7 +458,8 @@ __global__ __launch_bounds__(256, 2) void block_chunk_kernel(ChunkArgs a) {
         return;
     }
     // ---- normalise; the block of outputs goes through LDS and leaves as whole rows ----------------------------------------------
-    uint16_t* ob = reinterpret_cast<uint16_t*>(buf) + wave * 16 * QC * OSTR;
+    if (idle) return;
+    uint16_t* ob = reinterpret_cast<uint16_t*>(buf) + wave * 16 * COLS * OSTR;
     constexpr int VPR = D / 8, RPI = 64 / VPR;
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc) {
@@ -378,10 +467,9 @@ __global__ __launch_bounds__(256, 2) void block_chunk_kernel(ChunkArgs a) {
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
             const f32x4 o = st.o[dt][qc] * rl;
-            const f32x2 o01 = {o[0], o[1]}, o23 = {o[2], o[3]};
             uint2 pk;
-            pk.x = __builtin_bit_cast(uint32_t, __builtin_convertvector(o01, bf16x2));
-            pk.y = __builtin_bit_cast(uint32_t, __builtin_convertvector(o23, bf16x2));
+            pk.x = bf16_pair(o[0], o[1]);
+            pk.y = bf16_pair(o[2], o[3]);
             *reinterpret_cast<uint2*>(ob + (16 * qc + c) * OSTR + 16 * dt + 4 * g) = pk;
         }
         const int r = r0 + 16 * qc + c, t = r / a.G;
@@ -396,6 +484,35 @@ __global__ __launch_bounds__(256, 2) void block_chunk_kernel(ChunkArgs a) {
             *reinterpret_cast<u32x4*>(a.out + (int64_t)(sq.start + t) * a.o_st + (int64_t)(kh * a.G + r - t * a.G) * a.o_sh + (lane % VPR) * 8) = val;
         }
     }
+}
+
+// A tile's columns of 16 rows are dealt to the waves as evenly as they go: one column a wave (COLS 1), or one or two.
+template <int D, int CODE, int COLS>
+__global__ __launch_bounds__(kChunkThreads, 2) void block_chunk_kernel(ChunkArgs a) {
+    constexpr int kOut = 2 * kChunkWaves * 16 * COLS * (D + 8), kTiles = 2 * Tile<D>::BYTES;        // bytes
+    __shared__ __attribute__((aligned(1024))) uint8_t buf[kTiles > kOut ? kTiles : kOut];
+    __shared__ int redo;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Work w;
+    int tile;
+    if (!place(a, lane, w.b, w.kh, tile, w.sq)) return;
+    w.ch = blockIdx.y;
+    w.rows = w.sq.m * a.G;
+    const int first = tile * a.tile, cols = (min(a.tile, w.rows - first) + 15) / 16;
+    const int last = w.sq.sees((min(w.rows, first + a.tile) - 1) / a.G);                     // the last row that the workgroup sees (-1: none)
+    w.u_begin = w.ch * a.piece;
+    w.u_end = min((last + kBlk) / kBlk, w.u_begin + a.piece);
+    if (w.ch > 0 && w.u_begin >= w.u_end) return;
+    w.strip = (int64_t)w.b * a.Hk + w.kh;
+    if (threadIdx.x == 0) redo = 0;
+    const int from = wave * cols / kChunkWaves, n = (wave + 1) * cols / kChunkWaves - from, r0 = first + 16 * from;
+    if constexpr (COLS == 2) {
+        if (n == 2) {
+            chunk_wave<D, CODE, 2, COLS>(a, w, buf, &redo, r0, false);
+            return;
+        }
+    }
+    chunk_wave<D, CODE, 1, COLS>(a, w, buf, &redo, r0, n == 0);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
@@ -437,13 +554,8 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a) {
     }
     const float rl = sum == 0.f ? 0.f : 1.0f / sum;
     uint16_t* out = a.out + (int64_t)row * a.o_st + (int64_t)h * a.o_sh + PER * lane;
-    if constexpr (PER == 2) {
-        const f32x2 o = {v[0] * rl, v[1] * rl};
-        *reinterpret_cast<uint32_t*>(out) = __builtin_bit_cast(uint32_t, __builtin_convertvector(o, bf16x2));
-    } else {
-        const f32x2 o = {v[0] * rl, 0.f};
-        *out = (uint16_t)__builtin_bit_cast(uint32_t, __builtin_convertvector(o, bf16x2));
-    }
+    if constexpr (PER == 2) *reinterpret_cast<uint32_t*>(out) = bf16_pair(v[0] * rl, v[1] * rl);
+    else *out = (uint16_t)bf16_pair(v[0] * rl, 0.f);
     if (a.ml != nullptr && lane == 0) a.ml[(int64_t)row * a.H + h] = make_float2(top, rl);
 }
 
@@ -602,22 +714,29 @@ __global__ __launch_bounds__(256, 2) void chunk_score_kernel(ChunkArgs a, int ro
     }
 }
 
-// How a call is cut: columns of 16 rows a wave, blocks of a piece, pieces.
-struct ChunkCut { int cols, piece, pieces; };
-constexpr int kEnough = 512, kWanted = 1024, kLeastPiece = 4;
+// How a call is cut: rows of a tile, blocks of a piece, pieces.
+struct ChunkCut { int rows, piece, pieces; };
+constexpr int kMostRowsOfTile = 32 * kChunkWaves;
+constexpr int kWanted = 512;            // workgroups that a cut aims at: two for a compute unit
+constexpr int kLeastPiece = 4;
 
 // No more row tiles than this, whatever the lengths are: each sequence has one that is not full.
 inline int64_t chunk_tiles(const st3_gqa_shape* s, int total, int max_new, int rows) {
     const int G = s->heads / s->kv_heads;
     return std::min((int64_t)total * G / rows + std::min(s->batch, total), ((int64_t)max_new * G + rows - 1) / rows * s->batch);
 }
+// The longest sequence's rows in as few tiles as hold them, all alike.
+inline int tile_rows(int64_t most) {
+    const int64_t tiles = (most + kMostRowsOfTile - 1) / kMostRowsOfTile;
+    return tiles == 0 ? 16 : (int)((most + 16 * tiles - 1) / (16 * tiles) * 16);
+}
 inline ChunkCut chunk_cut(const st3_gqa_shape* s, int total, int max_new, int max_len) {
-    const int G = s->heads / s->kv_heads, cols = (int64_t)max_new * G <= 64 ? 1 : 2;
-    const int64_t tiles = chunk_tiles(s, total, max_new, 64 * cols) * s->kv_heads, units = max_len / kBlk + 1;
-    if (tiles >= kEnough || tiles == 0) return ChunkCut{cols, (int)units, 1};
+    const int rows = tile_rows((int64_t)max_new * (s->heads / s->kv_heads));
+    const int64_t tiles = chunk_tiles(s, total, max_new, rows) * s->kv_heads, units = max_len / kBlk + 1;
+    if (2 * tiles >= kWanted || tiles == 0) return ChunkCut{rows, (int)units, 1};
     const int64_t pieces = std::min((kWanted + tiles - 1) / tiles, (units + kLeastPiece - 1) / kLeastPiece);
     const int64_t piece = (units + pieces - 1) / pieces;
-    return ChunkCut{cols, (int)piece, (int)((units + piece - 1) / piece)};
+    return ChunkCut{rows, (int)piece, (int)((units + piece - 1) / piece)};
 }
 
 // Blocks that a wave of the scores' launch takes one behind the other.
@@ -627,12 +746,14 @@ inline int score_rounds(int64_t units, int Hk, int B) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(want, kMostRounds));
 }
 
-struct ChunkWs { size_t ml, part_o, part_ml, total; };
-// Room for as many parts as a launch of any smaller sizes may leave: kWanted tiles of 128 rows and one part more for each row, or one for every kLeastPiece blocks.
+struct ChunkWs { size_t ml, part_o, part_ml, total; int64_t parts; };
+// Room for as many parts as a launch of these or any smaller sizes may leave.  Tiles hold all rows, so less than kWanted / tiles + 1 pieces are less
+// than kWanted tiles of parts and one more for each row; nor are there more than one for every kLeastPiece blocks.
 inline ChunkWs chunk_ws(const st3_gqa_shape* s, int total, int max_len) {
     const int64_t rows = (int64_t)total * s->heads, units = max_len / kBlk + 1;
-    const int64_t parts = std::min((int64_t)kWanted * 128 + rows, rows * ((units + kLeastPiece - 1) / kLeastPiece));
+    const int64_t parts = std::min((int64_t)kWanted * kMostRowsOfTile + rows, rows * ((units + kLeastPiece - 1) / kLeastPiece));
     ChunkWs w{};
+    w.parts = parts;
     size_t off = 0;
     w.ml = off;      off = align_up(off + rows * sizeof(float2), 256);
     w.part_o = off;  off = align_up(off + parts * s->head_dim * sizeof(float), 256);
@@ -642,9 +763,9 @@ inline ChunkWs chunk_ws(const st3_gqa_shape* s, int total, int max_len) {
 }
 
 template <int D, int CODE>
-void launch_chunk(const ChunkArgs& a, int cols, unsigned grid, hipStream_t st) {
-    if (cols == 1) block_chunk_kernel<D, CODE, 1><<<dim3(grid, a.pieces), 256, 0, st>>>(a);
-    else block_chunk_kernel<D, CODE, 2><<<dim3(grid, a.pieces), 256, 0, st>>>(a);
+void launch_chunk(const ChunkArgs& a, unsigned grid, hipStream_t st) {
+    if (a.tile <= 16 * kChunkWaves) block_chunk_kernel<D, CODE, 1><<<dim3(grid, a.pieces), kChunkThreads, 0, st>>>(a);
+    else block_chunk_kernel<D, CODE, 2><<<dim3(grid, a.pieces), kChunkThreads, 0, st>>>(a);
     if (a.pieces > 1) chunk_join_kernel<D><<<(unsigned)(((int64_t)a.total * a.H + 3) / 4), 256, 0, st>>>(a);
     if (!a.score || a.max_len == 0) return;
     const int fit = score_rows((int64_t)std::min(a.window, a.max_new) * a.G), units = (a.max_len + kBlk - 1) / kBlk, rounds = score_rounds(units, a.Hk, a.B);
@@ -677,9 +798,10 @@ extern "C" st3_status st3_block_attend(const st3_gqa_shape* shape, const st3_row
     if (score && (window < 1 || score_stride_h < max_len || (B > 1 && score_stride_b < max_len))) return ST3_ERR_INVALID_ARG;
     if (!workspace || !aligned16(workspace)) return ST3_ERR_INVALID_ARG;
     const ChunkCut cut = chunk_cut(shape, total, max_new, max_len);
-    const int64_t grid = chunk_tiles(shape, total, max_new, 64 * cut.cols) * Hk;
-    if (!grid_fits(grid, 256, cut.pieces) || !grid_fits(((int64_t)total * H + 3) / 4, 256, 1) || (score && (max_len + 4 * kBlk - 1) / (4 * kBlk) > 65535)) return ST3_ERR_UNSUPPORTED;
+    const int64_t grid = chunk_tiles(shape, total, max_new, cut.rows) * Hk;
+    if (!grid_fits(grid, kChunkThreads, cut.pieces) || !grid_fits(((int64_t)total * H + 3) / 4, 256, 1) || (score && (max_len + 4 * kBlk - 1) / (4 * kBlk) > 65535)) return ST3_ERR_UNSUPPORTED;
     const ChunkWs wl = chunk_ws(shape, total, max_len);
+    if (cut.pieces > 1 && (int64_t)total * H * cut.pieces > wl.parts) return ST3_ERR_UNSUPPORTED;    // (never, by the rule above)
     if (workspace_bytes < st3_block_attend_workspace_bytes(shape, total, max_new, max_len)) return ST3_ERR_WORKSPACE_TOO_SMALL;
     char* ws = reinterpret_cast<char*>(workspace);
     ChunkArgs a{};
@@ -687,7 +809,7 @@ extern "C" st3_status st3_block_attend(const st3_gqa_shape* shape, const st3_row
     a.q = reinterpret_cast<const uint16_t*>(q->data); a.out = reinterpret_cast<uint16_t*>(out->data);
     a.q_st = q->stride_t; a.q_sh = q->stride_h; a.o_st = out->stride_t; a.o_sh = out->stride_h;
     a.cu = cu_len; a.B = B; a.total = total; a.max_new = max_new; a.max_len = max_len; a.H = H; a.Hk = Hk; a.G = G;
-    a.piece = cut.piece; a.pieces = cut.pieces;
+    a.tile = cut.rows; a.piece = cut.piece; a.pieces = cut.pieces;
     a.scale_l2 = gqa_scale_log2(shape);
     a.score = score; a.s_sb = score_stride_b; a.s_sh = score_stride_h; a.window = window;
     a.ml = score ? reinterpret_cast<float2*>(ws + wl.ml) : nullptr;
@@ -695,11 +817,11 @@ extern "C" st3_status st3_block_attend(const st3_gqa_shape* shape, const st3_row
     a.part_ml = reinterpret_cast<float2*>(ws + wl.part_ml);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     if (cache->code == ST3_BLOCK_INT8) {
-        if (D == 128) launch_chunk<128, ST3_BLOCK_INT8>(a, cut.cols, (unsigned)grid, st);
-        else launch_chunk<64, ST3_BLOCK_INT8>(a, cut.cols, (unsigned)grid, st);
+        if (D == 128) launch_chunk<128, ST3_BLOCK_INT8>(a, (unsigned)grid, st);
+        else launch_chunk<64, ST3_BLOCK_INT8>(a, (unsigned)grid, st);
     } else {
-        if (D == 128) launch_chunk<128, ST3_BLOCK_E4M3>(a, cut.cols, (unsigned)grid, st);
-        else launch_chunk<64, ST3_BLOCK_E4M3>(a, cut.cols, (unsigned)grid, st);
+        if (D == 128) launch_chunk<128, ST3_BLOCK_E4M3>(a, (unsigned)grid, st);
+        else launch_chunk<64, ST3_BLOCK_E4M3>(a, (unsigned)grid, st);
     }
     return check_launch();
 }

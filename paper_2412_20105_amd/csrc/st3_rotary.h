@@ -39,11 +39,6 @@ __device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
     b = bc + as;
 }
 
-__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
-    const f32x2 v = {lo, hi};
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-}
-
 // A vector of 16 bytes from float32, rounded to nearest even.
 template <typename T> __device__ __forceinline__ uint4 packed(const float* f);
 template <> __device__ __forceinline__ uint4 packed<float>(const float* f) { return ElemTraits<float>::pack(f); }
