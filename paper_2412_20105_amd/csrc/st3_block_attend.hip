@@ -16,10 +16,6 @@
 namespace st3 {
 namespace {
 
-#ifndef KAHEAD1
-#define KAHEAD1 3
-#define VAHEAD1 4
-#endif
 constexpr int kChunkWaves = 8, kChunkThreads = 64 * kChunkWaves;
 
 struct ChunkArgs {
@@ -89,14 +85,15 @@ __device__ __forceinline__ bool place(const ChunkArgs& a, int lane, int& b, int&
     return found(0, at, __builtin_amdgcn_readlane(before + mine, at) - 1 - x);
 }
 
-// A block in LDS: K as 64 rows of D bf16, V as D rows (columns of V) of 64.  Unit u (16 bytes) of row r lies at u ^ swz(r): the 16 rows that a fragment's
-// lanes read lie in 16 different units of the banks.
+// A block in LDS: K as 64 rows of D bf16, V as D rows (columns of V) of 64.  Unit u (16 bytes) of a row r of K lies at u ^ k_swz(r), of V at v_place(u) ^ v_swz(r):
+// lanes that are served together (16 of them, of rows 0 .. 3 and 12 .. 15 of one g and 4 .. 11 of the next) read 16 different units of the banks.
 template <int D> struct Tile {
     static constexpr int K = kBlk * D, BYTES = 4 * K;       // elements of K, and of V; bytes of both
     __device__ static __forceinline__ int k_swz(int row) {
         return D == 128 ? (row >> 4 & 3) << 2 | (row & 3) : (row >> 4 & 3) << 1 | (row >> 1 & 1);
     }
     __device__ static __forceinline__ int v_swz(int row) { return row >> 1 & 7; }
+    __device__ static __forceinline__ int v_place(int unit) { return unit >> 1 | (unit & 1) << 2; }
 };
 
 __device__ __forceinline__ void lds_write16(uint32_t at, u32x4 x) { *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(at) = x; }
@@ -121,10 +118,11 @@ struct Codes {
         for (int i = 0; i < N; ++i) {
             const int p = tid + i * THREADS, kr = p / (D / 16), vr = (p - PIECES) / (kBlk / 16);
             const uint32_t row_at = p < PIECES ? lds + 2 * D * kr : lds + 2 * Tile<D>::K + 2 * kBlk * vr;
-            const int swz = p < PIECES ? Tile<D>::k_swz(kr) : Tile<D>::v_swz(vr), unit = p < PIECES ? 2 * (p % (D / 16)) : 2 * (p % (kBlk / 16));
+            const int swz = p < PIECES ? Tile<D>::k_swz(kr) : Tile<D>::v_swz(vr);
+            const int first = p < PIECES ? 2 * (p % (D / 16)) : p % (kBlk / 16), second = first + (p < PIECES ? 1 : 4);       // (v_place of 2 u and 2 u + 1)
             const uint2 a = F::to_bf16(w[i].x), b = F::to_bf16(w[i].y), c = F::to_bf16(w[i].z), d = F::to_bf16(w[i].w);
-            lds_write16(row_at + 16 * (unit ^ swz), u32x4{a.x, a.y, b.x, b.y});
-            lds_write16(row_at + 16 * ((unit + 1) ^ swz), u32x4{c.x, c.y, d.x, d.y});
+            lds_write16(row_at + 16 * (first ^ swz), u32x4{a.x, a.y, b.x, b.y});
+            lds_write16(row_at + 16 * (second ^ swz), u32x4{c.x, c.y, d.x, d.y});
         }
     }
 };
@@ -132,6 +130,7 @@ struct Codes {
 // The tail, `rows` rows in 16 bits, into LDS; the rows behind them are zeros, whatever their bits are.
 template <int D, int THREADS>
 __device__ __forceinline__ void tail_to_lds(const BlockPages& c, int64_t strip, int rows, uint32_t lds, int tid) {
+    asm volatile("" : "+v"(tid));                           // (opaque, as below: else what follows from it is kept in registers through a walk that needs it once)
     const u32x4* kp = reinterpret_cast<const u32x4*>(c.k_tail + strip * (kBlk * D));
     const u32x4* vp = reinterpret_cast<const u32x4*>(c.v_tail + strip * (kBlk * D));
     constexpr int N = kBlk * D / 8 / THREADS;
@@ -146,7 +145,7 @@ __device__ __forceinline__ void tail_to_lds(const BlockPages& c, int64_t strip, 
         const int key = 8 * (p % (kBlk / 8));
 #pragma unroll
         for (int j = 0; j < 4; ++j) f.w[j] &= (key + 2 * j < rows ? 0xffffu : 0u) | (key + 2 * j + 1 < rows ? 0xffff0000u : 0u);
-        lds_write16(lds + 2 * Tile<D>::K + 2 * kBlk * vr + 16 * (p % (kBlk / 8) ^ Tile<D>::v_swz(vr)), f.u4);
+        lds_write16(lds + 2 * Tile<D>::K + 2 * kBlk * vr + 16 * (Tile<D>::v_place(p % (kBlk / 8)) ^ Tile<D>::v_swz(vr)), f.u4);
     }
 }
 
@@ -166,64 +165,56 @@ struct Rows {
     }
 };
 
-// S^T = K Q^T of 64 keys.
+// A wave's products, O^T += V^T P^T of one block and S^T = K Q^T of the next; fragments are read from LDS a few products ahead (and no more: the scheduling
+// barriers keep the compiler from holding more of them than there are registers for).
 template <int D, int QC>
-__device__ __forceinline__ void chunk_logits(uint32_t k_at, const Frag (&qf)[QC][D / 32], f32x4 (&s)[4][QC]) {
-    constexpr int KS = D / 32;
-    constexpr int AHEAD = QC == 1 ? KAHEAD1 : 1;
-    Frag ka[AHEAD + 1][KS];
-    auto load = [&](int t) {
+struct Products {
+    static constexpr int KS = D / 32, DT = D / 16, kAhead = 2;
+    Frag va[kAhead + 1][2], ka[2][KS];
+    __device__ __forceinline__ void read_v(int dt, uint32_t v_at) {
 #pragma unroll
-        for (int x = 0; x < KS; ++x) ka[t % (AHEAD + 1)][x].u4 = lds_read16((k_at ^ (64 * x)) + 8 * D * t);
-    };
-#pragma unroll
-    for (int t = 0; t < AHEAD; ++t) load(t);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        if (t + AHEAD < 4) load(t + AHEAD);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int qc = 0; qc < QC; ++qc) s[t][qc] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int x = 0; x < KS; ++x)
-#pragma unroll
-            for (int qc = 0; qc < QC; ++qc) s[t][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[t % (AHEAD + 1)][x].v, qf[qc][x].v, s[t][qc], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int x = 0; x < 2; ++x) va[dt % (kAhead + 1)][x].u4 = lds_read16((v_at ^ (64 * x)) + 32 * kBlk * dt);
     }
-}
-
-// O^T += V^T P^T of 64 keys.
-template <int D, int QC>
-__device__ __forceinline__ void chunk_values(uint32_t v_at, const Frag (&pb)[2][QC], Rows<D, QC>& st) {
-    constexpr int DT = D / 16, AHEAD = QC == 1 ? VAHEAD1 : 2;
-    Frag va[AHEAD + 1][2];
-    auto load = [&](int dt) {
+    __device__ __forceinline__ void read_k(int t, uint32_t k_at) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) va[dt % (AHEAD + 1)][x].u4 = lds_read16((v_at ^ (16 * x)) + 32 * kBlk * dt);
-    };
-#pragma unroll
-    for (int dt = 0; dt < AHEAD; ++dt) load(dt);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-        if (dt + AHEAD < DT) load(dt + AHEAD);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int qc = 0; qc < QC; ++qc) st.o[dt][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[dt % (AHEAD + 1)][x].v, pb[x][qc].v, st.o[dt][qc], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int x = 0; x < KS; ++x) ka[t & 1][x].u4 = lds_read16((k_at ^ (64 * x)) + 8 * D * t);
     }
-}
+    __device__ __forceinline__ void values(uint32_t v_at, const Frag (&pb)[2][QC], Rows<D, QC>& st) {
+#pragma unroll
+        for (int dt = 0; dt < kAhead; ++dt) read_v(dt, v_at);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            if (dt + kAhead < DT) read_v(dt + kAhead, v_at);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int qc = 0; qc < QC; ++qc) st.o[dt][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[dt % (kAhead + 1)][x].v, pb[x][qc].v, st.o[dt][qc], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    __device__ __forceinline__ void logits(uint32_t k_at, const Frag (&qf)[QC][KS], f32x4 (&s)[4][QC]) {
+        read_k(0, k_at);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            if (t + 1 < 4) read_k(t + 1, k_at);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int x = 0; x < KS; ++x)
+#pragma unroll
+                for (int qc = 0; qc < QC; ++qc)
+                    s[t][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[t & 1][x].v, qf[qc][x].v, x == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t][qc], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+};
 
-// 64 keys for one wave, some of which some row may not see; ks: the block's scale of K times that of the logits (in the log2 domain), vs: of V.
-// CAREFUL: V may hold infinities or NaN, and a weight of 0 does not silence those; row by row, V's keys that the row does not see count as 0.
+// Weights of 64 keys, some of which some row may not see; ks: the block's scale of K times that of the logits (in the log2 domain), vs: of V.
 // A weight times V's scale is rounded to bf16 once, to nearest: an error of 2^-8 of it at most and without bias, beside the output's own rounding by as
 // much; the sum is of the unrounded ones.
-template <int D, int QC, bool CAREFUL = false>
-__device__ __forceinline__ void chunk_step(uint32_t k_at, uint32_t v_at, const Frag (&qf)[QC][D / 32], Rows<D, QC>& st, float ks, float vs, int g, int k0) {
-    constexpr int DT = D / 16;
-    f32x4 s[4][QC];
-    chunk_logits<D, QC>(k_at, qf, s);
+template <int D, int QC>
+__device__ __forceinline__ void chunk_weights(f32x4 (&s)[4][QC], Rows<D, QC>& st, float ks, float vs, int g, int k0, Frag (&pb)[2][QC]) {
+    asm volatile("" : "+v"(g));
     // (a block's scale may be 0, and -infinity times 0 is no number: masks come behind the scale)
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -254,10 +245,9 @@ __device__ __forceinline__ void chunk_step(uint32_t k_at, uint32_t v_at, const F
             st.m[qc] = m_new;
             st.l[qc] *= alpha;
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) st.o[dt][qc] *= alpha;
+            for (int dt = 0; dt < D / 16; ++dt) st.o[dt][qc] *= alpha;
         }
     }
-    Frag pb[2][QC];
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc)
 #pragma unroll
@@ -269,49 +259,14 @@ __device__ __forceinline__ void chunk_step(uint32_t k_at, uint32_t v_at, const F
                 st.l[qc] += p0 + p1;
                 pb[x][qc].w[j] = bf16_pair(p0 * vs, p1 * vs);
             }
-    if constexpr (CAREFUL) {
-        const int c = threadIdx.x & 15;
-#pragma unroll
-        for (int qc = 0; qc < QC; ++qc)
-#pragma unroll 1
-            for (int row = 0; row < 16; ++row) {
-                const int pos = __builtin_amdgcn_readlane(st.pos[qc], row);
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    Frag seen;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int key = k0 + 16 * g + 8 * x + 2 * j;
-                        seen.w[j] = (key <= pos ? 0xffffu : 0u) | (key < pos ? 0xffff0000u : 0u);
-                    }
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        Frag va;
-                        va.u4 = lds_read16((v_at ^ (16 * x)) + 32 * kBlk * dt);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) va.w[j] &= seen.w[j];
-                        const f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va.v, pb[x][qc].v, st.o[dt][qc], 0, 0, 0);
-                        st.o[dt][qc] = c == row ? o : st.o[dt][qc];
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                }
-            }
-        return;
-    }
-    chunk_values<D, QC>(v_at, pb, st);
 }
 
 // The same of a block that every row sees whole, nearly all of them.  The reference point stays where it is (weights are floating point, in bf16 too: nothing is
 // lost as long as none of them grows large), and V's scale comes with the exponent: exp2(s ks - m + log2 vs); what a lane adds to the sum is that
 // divided by vs.  False, and nothing done, where weights have grown above kMost, are no numbers, or vs has no logarithm (lvs is NaN then).
 template <int D, int QC>
-__device__ __forceinline__ bool chunk_step_whole(uint32_t k_at, uint32_t v_at, const Frag (&qf)[QC][D / 32], Rows<D, QC>& st, float ks, float lvs, float rvs) {
+__device__ __forceinline__ bool chunk_weights_whole(const f32x4 (&s)[4][QC], Rows<D, QC>& st, float ks, float lvs, float rvs, Frag (&pb)[2][QC]) {
     constexpr float kMost = 4096.0f;
-    f32x4 s[4][QC];
-    __builtin_amdgcn_s_setprio(1);
-    chunk_logits<D, QC>(k_at, qf, s);
-    __builtin_amdgcn_s_setprio(0);
-    Frag pb[2][QC];
     float sum[QC];
     bool large = false;
 #pragma unroll
@@ -333,10 +288,49 @@ __device__ __forceinline__ bool chunk_step_whole(uint32_t k_at, uint32_t v_at, c
     if (__any(large)) return false;
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc) st.l[qc] += sum[qc];
-    __builtin_amdgcn_s_setprio(1);
-    chunk_values<D, QC>(v_at, pb, st);
-    __builtin_amdgcn_s_setprio(0);
     return true;
+}
+
+// 64 keys for one wave where V may hold infinities or NaN, which a weight of 0 does not silence: row by row, V's keys that the row does not see count as 0.
+template <int D, int QC>
+__device__ __forceinline__ void chunk_step_careful(uint32_t k_at, uint32_t v_at, const Frag (&qf)[QC][D / 32], Rows<D, QC>& st, float ks, float vs, int g, int k0) {
+    f32x4 s[4][QC];
+    Frag pb[2][QC];
+    Products<D, QC>{}.logits(k_at, qf, s);
+    chunk_weights<D, QC>(s, st, ks, vs, g, k0, pb);
+    const int c = threadIdx.x & 15;
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc)
+#pragma unroll 1
+        for (int row = 0; row < 16; ++row) {
+            const int pos = __builtin_amdgcn_readlane(st.pos[qc], row);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                Frag seen;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int key = k0 + 16 * g + 8 * x + 2 * j;
+                    seen.w[j] = (key <= pos ? 0xffffu : 0u) | (key < pos ? 0xffff0000u : 0u);
+                }
+#pragma unroll
+                for (int dt = 0; dt < D / 16; ++dt) {
+                    Frag va;
+                    va.u4 = lds_read16((v_at ^ (64 * x)) + 32 * kBlk * dt);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) va.w[j] &= seen.w[j];
+                    const f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va.v, pb[x][qc].v, st.o[dt][qc], 0, 0, 0);
+                    st.o[dt][qc] = c == row ? o : st.o[dt][qc];
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+}
+
+// A barrier that nothing is moved across.
+__device__ __forceinline__ void meet() {
+    __builtin_amdgcn_sched_barrier(0);
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // What a workgroup works on.
@@ -369,7 +363,7 @@ __device__ __forceinline__ void chunk_wave(const ChunkArgs& a, const Work& w, ui
     }
     const int p_first = sq.sees(min(r0, rows - 1) / a.G), p_last = sq.sees((min(r0 + 16 * QC, rows) - 1) / a.G);      // what the wave's first and last rows see
     const int krow = 16 * (c >> 2) + (c & 3);
-    const uint32_t k_lane = (uint32_t)(2 * D * krow + 16 * (g ^ L::k_swz(krow))), v_lane = (uint32_t)(2 * L::K + 2 * kBlk * c + 16 * (2 * g ^ L::v_swz(c)));
+    const uint32_t k_lane = (uint32_t)(2 * D * krow + 16 * (g ^ L::k_swz(krow))), v_lane = (uint32_t)(2 * L::K + 2 * kBlk * c + 16 * (g ^ L::v_swz(c)));
     // lane i has the page and the scales of block `base` + i
     int base = 0, page_l = -1;
     float ks_l = 0.f, vs_l = 0.f, lvs_l = 0.f, rvs_l = 0.f;
@@ -388,47 +382,89 @@ __device__ __forceinline__ void chunk_wave(const ChunkArgs& a, const Work& w, ui
         rvs_l = 1.0f / vs_l;
     };
     auto lane_value = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
-    const int u_stop = min(u_end, blocks);
-    // A block on its way, and its scales; two of them, one for even and one for odd steps.
-    struct Next { Codes<D, CODE, kThr> codes; int page; float ks, vs, lvs, rvs; };
-    auto walk = [&](auto careful) {
-        constexpr bool kCareful = decltype(careful)::value;
-        Next next[2];
-        auto fetch = [&](int u, Next& x) {
-            if (u >= u_stop) return;
-            if (u >= base + kWave) look_up(u);
-            const int i = u - base;
-            x.page = __builtin_amdgcn_readlane(page_l, i);
-            x.ks = lane_value(ks_l, i); x.vs = lane_value(vs_l, i); x.lvs = lane_value(lvs_l, i); x.rvs = lane_value(rvs_l, i);
-            if (x.page >= 0) x.codes.load(a.c, (int64_t)x.page * a.Hk + kh, tid);
-        };
-        auto step = [&](int u, Next& x, uint32_t at) {
-            const bool there = x.page >= 0;                 // (a block without a page is passed over)
-            const float ks = x.ks, vs = x.vs, lvs = x.lvs, rvs = x.rvs;
-            if (there) x.codes.store(at, tid);
-            __syncthreads();
-            fetch(u + 2, x);
-            if (!there || idle || u * kBlk > p_last) return;
-            if (u * kBlk + kBlk - 1 <= p_first && chunk_step_whole<D, QC>(at + k_lane, at + v_lane, qf, st, ks, lvs, rvs)) return;
-            chunk_step<D, QC, kCareful>(at + k_lane, at + v_lane, qf, st, ks, vs, g, u * kBlk);
-        };
-        look_up(u_begin);
-        fetch(u_begin, next[0]);
-        fetch(u_begin + 1, next[1]);
-        int u = u_begin;
-        for (; u + 1 < u_stop; u += 2) {
-            step(u, next[0], lds0);
-            step(u + 1, next[1], lds0 + L::BYTES);
-        }
-        if (u < u_stop) step(u, next[0], lds0);
-        if (blocks >= u_begin && blocks < u_end) {          // the rows in 16 bits
-            const uint32_t at = lds0 + (u < u_stop ? L::BYTES : 0);
-            tail_to_lds<D, kThr>(a.c, strip, sq.rows() % kBlk, at, tid);
-            __syncthreads();
-            if (!idle && blocks * kBlk <= p_last) chunk_step<D, QC, kCareful>(at + k_lane, at + v_lane, qf, st, a.scale_l2, 1.0f, g, blocks * kBlk);
-        }
+    const int u_stop = min(u_end, blocks), units = max(u_end - u_begin, 0);     // (one behind u_stop: the rows in 16 bits)
+    // A block's scales, and whether there is one.
+    struct Scales { bool there; float ks, vs, lvs, rvs; };
+    auto scales_of = [&](int u) {
+        if (u >= u_stop) return Scales{u < u_end, a.scale_l2, 1.0f, 0.0f, 1.0f};
+        if (u >= base + kWave) look_up(u);
+        const int i = u - base;
+        return Scales{__builtin_amdgcn_readlane(page_l, i) >= 0, lane_value(ks_l, i), lane_value(vs_l, i), lane_value(lvs_l, i), lane_value(rvs_l, i)};
     };
-    walk(std::false_type{});
+    // Blocks' codes on their way: codes[x] and page[x] those of the i-th from u_begin on, x = i & 1.
+    Codes<D, CODE, kThr> codes[2];
+    int page[2] = {-1, -1};
+    int ahead = 0, page_ahead = -1;                         // lane i has the page of block `ahead` + i (codes are fetched further ahead than scales)
+    auto fetch = [&](int i, int x) {
+        const int u = u_begin + i;
+        if (u >= ahead + kWave) {
+            ahead = u;
+            page_ahead = u + lane < u_stop ? page_of(a.c, b, u + lane) : -1;
+        }
+        page[x] = __builtin_amdgcn_readlane(page_ahead, u - ahead);
+        codes[x].load(a.c, (int64_t)max(page[x], 0) * a.Hk + kh, tid);     // (always: where loads hang on a condition, those behind them are waited for too)
+    };
+    auto store = [&](int i, int x) {
+        const uint32_t at = lds0 + (i & 3) * L::BYTES;
+        const int u = u_begin + i;
+        if (page[x] >= 0) codes[x].store(at, tid);
+        else if (u < u_end) tail_to_lds<D, kThr>(a.c, strip, u >= u_stop ? sq.rows() % kBlk : 0, at, tid);      // (a block without a page: zeros, without weight)
+    };
+    // A step of a wave is a half on the matrix units (the values of one block, the logits of the next) and one on the others (weights; a block's codes
+    // into LDS, two steps ahead).  The two waves of a SIMD are half a step apart: while one keeps the matrix units busy, the other computes weights.
+    const int mine = idle || p_last < u_begin * kBlk ? 0 : min(units, p_last / kBlk - u_begin + 1);     // steps in which this wave has rows that see something
+    auto v_of = [&](int i) { return lds0 + (i & 3) * L::BYTES + v_lane; };
+    auto k_of = [&](int i) { return lds0 + (i & 3) * L::BYTES + k_lane; };
+    look_up(u_begin);
+    ahead = u_begin;
+    page_ahead = page_l;
+    fetch(0, 0);
+    fetch(1, 1);
+    store(0, 0);
+    fetch(2, 0);
+    store(1, 1);
+    fetch(3, 1);
+    meet();
+    const bool second = wave >= kChunkWaves / 2;
+    if (second) meet();
+    if (mine > 0) {
+        f32x4 s[4][QC];
+        Frag pb[2][QC];
+        Products<D, QC> products;
+        products.logits(k_of(0), qf, s);
+        meet();
+        auto others = [&](int i, int x) {
+            const int u = u_begin + i;
+            const Scales w = scales_of(u);
+            if (u >= u_stop || !w.there || u * kBlk + kBlk - 1 > p_first || !chunk_weights_whole<D, QC>(s, st, w.ks, w.lvs, w.rvs, pb))
+                chunk_weights<D, QC>(s, st, w.ks, w.vs, g, w.there ? u * kBlk : 0x7fffff00, pb);        // (a block without a page lies behind all rows)
+            store(i + 2, x);
+            fetch(i + 4, x);
+            meet();
+            __builtin_amdgcn_s_setprio(1);
+            products.values(v_of(i), pb, st);
+            if (i + 1 == mine) return false;
+            products.logits(k_of(i + 1), qf, s);
+            __builtin_amdgcn_s_setprio(0);
+            meet();
+            return true;
+        };
+        for (int i = 0; others(i, 0) && others(i + 1, 1); i += 2) {}
+        __builtin_amdgcn_s_setprio(0);
+    }
+    auto idle_step = [&](int i, int x) {
+        meet();
+        store(i + 2, x);
+        fetch(i + 4, x);
+        meet();
+    };
+    int i = mine;
+    if (i < units && (i & 1)) idle_step(i++, 1);
+    for (; i < units; i += 2) {
+        idle_step(i, 0);
+        if (i + 1 < units) idle_step(i + 1, 1);
+    }
+    if (!second) meet();
     // Anything but finite: it may be from V of keys that a row does not see (0 times infinity).  Once more, such V left out.
     float odd = 0.f;
 #pragma unroll
@@ -441,7 +477,18 @@ __device__ __forceinline__ void chunk_wave(const ChunkArgs& a, const Work& w, ui
     __syncthreads();
     if (*redo) {
         st.init();
-        walk(std::true_type{});
+        look_up(u_begin);
+        for (int u = u_begin; u < u_end; ++u) {
+            __syncthreads();
+            const Scales x = scales_of(u);
+            if (u >= u_stop) tail_to_lds<D, kThr>(a.c, strip, sq.rows() % kBlk, lds0, tid);
+            else if (x.there) {
+                codes[0].load(a.c, (int64_t)__builtin_amdgcn_readlane(page_l, u - base) * a.Hk + kh, tid);
+                codes[0].store(lds0, tid);
+            }
+            __syncthreads();
+            if (x.there && !idle && u * kBlk <= p_last) chunk_step_careful<D, QC>(lds0 + k_lane, lds0 + v_lane, qf, st, x.ks, x.vs, g, u * kBlk);
+        }
         __syncthreads();
     }
     if (a.pieces > 1) {
@@ -489,7 +536,7 @@ __device__ __forceinline__ void chunk_wave(const ChunkArgs& a, const Work& w, ui
 // A tile's columns of 16 rows are dealt to the waves as evenly as they go: one column a wave (COLS 1), or one or two.
 template <int D, int CODE, int COLS>
 __global__ __launch_bounds__(kChunkThreads, 2) void block_chunk_kernel(ChunkArgs a) {
-    constexpr int kOut = 2 * kChunkWaves * 16 * COLS * (D + 8), kTiles = 2 * Tile<D>::BYTES;        // bytes
+    constexpr int kOut = 2 * kChunkWaves * 16 * COLS * (D + 8), kTiles = 4 * Tile<D>::BYTES;        // bytes
     __shared__ __attribute__((aligned(1024))) uint8_t buf[kTiles > kOut ? kTiles : kOut];
     __shared__ int redo;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
