@@ -112,18 +112,20 @@ struct Codes {
             w[i] = reinterpret_cast<const u32x4*>(codes + at * (kBlk * D))[p < PIECES ? p : p - PIECES];
         }
     }
-    __device__ __forceinline__ void store(uint32_t lds, int tid) const {
+    // half a piece: 8 codes
+    static constexpr int HALVES = 2 * N;
+    __device__ __forceinline__ void store_half(int h, uint32_t lds, int tid) const {
         using F = BlockCode<CODE>;
+        const int i = h / 2, p = tid + i * THREADS, kr = p / (D / 16), vr = (p - PIECES) / (kBlk / 16);
+        const uint32_t row_at = p < PIECES ? 2 * D * kr : 2 * Tile<D>::K + 2 * kBlk * vr;
+        const int swz = p < PIECES ? Tile<D>::k_swz(kr) : Tile<D>::v_swz(vr);
+        const int first = p < PIECES ? 2 * (p % (D / 16)) : p % (kBlk / 16), second = first + (p < PIECES ? 1 : 4);       // (v_place of 2 u and 2 u + 1)
+        const uint2 a = F::to_bf16(h & 1 ? w[i].z : w[i].x), b = F::to_bf16(h & 1 ? w[i].w : w[i].y);
+        lds_write16(lds + (row_at + 16 * ((h & 1 ? second : first) ^ swz)), u32x4{a.x, a.y, b.x, b.y});
+    }
+    __device__ __forceinline__ void store(uint32_t lds, int tid) const {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int p = tid + i * THREADS, kr = p / (D / 16), vr = (p - PIECES) / (kBlk / 16);
-            const uint32_t row_at = p < PIECES ? lds + 2 * D * kr : lds + 2 * Tile<D>::K + 2 * kBlk * vr;
-            const int swz = p < PIECES ? Tile<D>::k_swz(kr) : Tile<D>::v_swz(vr);
-            const int first = p < PIECES ? 2 * (p % (D / 16)) : p % (kBlk / 16), second = first + (p < PIECES ? 1 : 4);       // (v_place of 2 u and 2 u + 1)
-            const uint2 a = F::to_bf16(w[i].x), b = F::to_bf16(w[i].y), c = F::to_bf16(w[i].z), d = F::to_bf16(w[i].w);
-            lds_write16(row_at + 16 * (first ^ swz), u32x4{a.x, a.y, b.x, b.y});
-            lds_write16(row_at + 16 * (second ^ swz), u32x4{c.x, c.y, d.x, d.y});
-        }
+        for (int h = 0; h < HALVES; ++h) store_half(h, lds, tid);
     }
 };
 
@@ -193,17 +195,25 @@ struct Products {
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    __device__ __forceinline__ void logits(uint32_t k_at, const Frag (&qf)[QC][KS], f32x4 (&s)[4][QC]) {
+    // beside(t): what else is done between the products, a quarter of it (VALU instructions and a write to LDS)
+    template <typename Beside>
+    __device__ __forceinline__ void logits(uint32_t k_at, const Frag (&qf)[QC][KS], f32x4 (&s)[4][QC], const Beside& beside) {
         read_k(0, k_at);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             if (t + 1 < 4) read_k(t + 1, k_at);
             __builtin_amdgcn_sched_barrier(0);
+            beside(t);
 #pragma unroll
             for (int x = 0; x < KS; ++x)
 #pragma unroll
                 for (int qc = 0; qc < QC; ++qc)
                     s[t][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[t & 1][x].v, qf[qc][x].v, x == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t][qc], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < KS * QC; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);          // a product, two others
+                __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -296,7 +306,7 @@ template <int D, int QC>
 __device__ __forceinline__ void chunk_step_careful(uint32_t k_at, uint32_t v_at, const Frag (&qf)[QC][D / 32], Rows<D, QC>& st, float ks, float vs, int g, int k0) {
     f32x4 s[4][QC];
     Frag pb[2][QC];
-    Products<D, QC>{}.logits(k_at, qf, s);
+    Products<D, QC>{}.logits(k_at, qf, s, [](int) {});
     chunk_weights<D, QC>(s, st, ks, vs, g, k0, pb);
     const int c = threadIdx.x & 15;
 #pragma unroll
@@ -404,14 +414,19 @@ __device__ __forceinline__ void chunk_wave(const ChunkArgs& a, const Work& w, ui
         page[x] = __builtin_amdgcn_readlane(page_ahead, u - ahead);
         codes[x].load(a.c, (int64_t)max(page[x], 0) * a.Hk + kh, tid);     // (always: where loads hang on a condition, those behind them are waited for too)
     };
-    auto store = [&](int i, int x) {
-        const uint32_t at = lds0 + (i & 3) * L::BYTES;
+    // The i-th block into LDS; what is no block of codes comes behind it, and the codes (those of page 0) then go where nothing is yet, into the next one's place.
+    auto place_of = [&](int i, int x) { return lds0 + ((page[x] >= 0 ? i : i + 1) & 3) * L::BYTES; };
+    auto others_of = [&](int i, int x) {
         const int u = u_begin + i;
-        if (page[x] >= 0) codes[x].store(at, tid);
-        else if (u < u_end) tail_to_lds<D, kThr>(a.c, strip, u >= u_stop ? sq.rows() % kBlk : 0, at, tid);      // (a block without a page: zeros, without weight)
+        if (page[x] < 0 && u < u_end) tail_to_lds<D, kThr>(a.c, strip, u >= u_stop ? sq.rows() % kBlk : 0, lds0 + (i & 3) * L::BYTES, tid);    // (a block without a page: zeros, without weight)
     };
-    // A step of a wave is a half on the matrix units (the values of one block, the logits of the next) and one on the others (weights; a block's codes
-    // into LDS, two steps ahead).  The two waves of a SIMD are half a step apart: while one keeps the matrix units busy, the other computes weights.
+    auto store = [&](int i, int x) {
+        codes[x].store(place_of(i, x), tid);
+        others_of(i, x);
+    };
+    // A step of a wave is a half on the matrix units (the values of one block and the logits of the next; beside them codes of the one behind go into
+    // LDS) and one on the others (weights).  The two waves of a SIMD are half a step apart: while one keeps the matrix units busy, the other
+    // computes weights.
     const int mine = idle || p_last < u_begin * kBlk ? 0 : min(units, p_last / kBlk - u_begin + 1);     // steps in which this wave has rows that see something
     auto v_of = [&](int i) { return lds0 + (i & 3) * L::BYTES + v_lane; };
     auto k_of = [&](int i) { return lds0 + (i & 3) * L::BYTES + k_lane; };
@@ -422,8 +437,6 @@ __device__ __forceinline__ void chunk_wave(const ChunkArgs& a, const Work& w, ui
     fetch(1, 1);
     store(0, 0);
     fetch(2, 0);
-    store(1, 1);
-    fetch(3, 1);
     meet();
     const bool second = wave >= kChunkWaves / 2;
     if (second) meet();
@@ -431,38 +444,45 @@ __device__ __forceinline__ void chunk_wave(const ChunkArgs& a, const Work& w, ui
         f32x4 s[4][QC];
         Frag pb[2][QC];
         Products<D, QC> products;
-        products.logits(k_of(0), qf, s);
+        auto multiply = [&](int i, int x) {                 // logits of the i-th block; codes[x]: those of the next
+            const uint32_t at = place_of(i + 1, x);
+            products.logits(k_of(i), qf, s, [&](int t) {
+                constexpr int H = Codes<D, CODE, kThr>::HALVES;
+                if (t < H) codes[x].store_half(t, at, tid);
+            });
+            others_of(i + 1, x);
+            fetch(i + 3, x);
+        };
+        multiply(0, 1);
         meet();
-        auto others = [&](int i, int x) {
+        auto step = [&](int i, int x) {
             const int u = u_begin + i;
             const Scales w = scales_of(u);
             if (u >= u_stop || !w.there || u * kBlk + kBlk - 1 > p_first || !chunk_weights_whole<D, QC>(s, st, w.ks, w.lvs, w.rvs, pb))
                 chunk_weights<D, QC>(s, st, w.ks, w.vs, g, w.there ? u * kBlk : 0x7fffff00, pb);        // (a block without a page lies behind all rows)
-            store(i + 2, x);
-            fetch(i + 4, x);
             meet();
             __builtin_amdgcn_s_setprio(1);
             products.values(v_of(i), pb, st);
             if (i + 1 == mine) return false;
-            products.logits(k_of(i + 1), qf, s);
+            multiply(i + 1, x);
             __builtin_amdgcn_s_setprio(0);
             meet();
             return true;
         };
-        for (int i = 0; others(i, 0) && others(i + 1, 1); i += 2) {}
+        for (int i = 0; step(i, 0) && step(i + 1, 1); i += 2) {}
         __builtin_amdgcn_s_setprio(0);
     }
-    auto idle_step = [&](int i, int x) {
+    auto idle_step = [&](int i, int x) {                    // codes[x]: those of block i + 1
+        store(i + 1, x);
+        fetch(i + 3, x);
         meet();
-        store(i + 2, x);
-        fetch(i + 4, x);
         meet();
     };
     int i = mine;
-    if (i < units && (i & 1)) idle_step(i++, 1);
+    if (i < units && (i & 1)) idle_step(i++, 0);
     for (; i < units; i += 2) {
-        idle_step(i, 0);
-        if (i + 1 < units) idle_step(i + 1, 1);
+        idle_step(i, 1);
+        if (i + 1 < units) idle_step(i + 1, 0);
     }
     if (!second) meet();
     // Anything but finite: it may be from V of keys that a row does not see (0 times infinity).  Once more, such V left out.
