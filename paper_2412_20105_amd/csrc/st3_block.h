@@ -121,6 +121,13 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
+// A block's K lies in a wave's own LDS, rows of D bytes, the 16-byte units of a row permuted: unit u of row r is at u ^ swz(r), so that the 16 rows
+// that a fragment's lanes read (16 (c / 4) + c % 4 + 4 t) lie in 16 different units of the banks.
+template <int D> struct KeyTile {
+    static constexpr int UPR = D / 16, RPI = 1024 / D, NI = kBlk / RPI;     // units of a row; rows of a wave-wide load; loads of a block
+    __device__ static __forceinline__ int swz(int row) { return D == 128 ? ((row >> 4 & 3) << 1 | (row >> 1 & 1)) : row >> 4 & 3; }
+};
+
 // Page of block j of sequence b; -1: there is none.
 __device__ __forceinline__ int page_of(const BlockPages& c, int b, int j) {
     if (j >= c.table_blocks) return -1;

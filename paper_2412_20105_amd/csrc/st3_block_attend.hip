@@ -583,6 +583,363 @@ __global__ __launch_bounds__(kChunkThreads, 2) void block_chunk_kernel(ChunkArgs
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
+// Few rows (16 QC of them at most: a token or a few drafted ones): every wave has them all, and takes the blocks in turn, each by itself, as the
+// attention of single tokens does: K straight to its own LDS, V straight into registers, 16 codes of a lane's operand at once, the rows in 16 bits by the
+// first waves, 32 keys at a time.  The waves' parts are joined in LDS.  WHOLE: a workgroup takes a whole strip; with room for the logits in LDS (stage:
+// rows of a strip there; 0: none) it adds the weights too.
+// ---------------------------------------------------------------------------------------------------------------------------------
+constexpr float kNoPage = -3.402823466e38f;     // in place of a logit: no page, no weight
+
+template <int D>
+inline size_t few_lds(int waves, int cols, int64_t stage) {
+    const size_t keys = (size_t)waves * kBlk * D, parts = sizeof(float) * waves * cols * (D + 4);
+    return std::max(keys, parts) + sizeof(float) * (2 * waves * cols + 2 * cols + (size_t)cols * stage);
+}
+
+template <int D, int CODE, int QC, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(ChunkArgs a, int stage) {
+    using F = BlockCode<CODE>;
+    using L = KeyTile<D>;
+    constexpr int KS = D / 32, DT = D / 16, KH = D / 64, kThr = WAVES * 64, OS = D + 4, kKeys = WAVES * kBlk * D / 4;
+    extern __shared__ __attribute__((aligned(16))) float few[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
+    const int kh = blockIdx.x, ch = blockIdx.y, b = blockIdx.z, cols = a.tile;
+    const Turn got = turn_of(a, b);
+    const Turn sq{__builtin_amdgcn_readfirstlane(got.start), __builtin_amdgcn_readfirstlane(got.m), __builtin_amdgcn_readfirstlane(got.n)};
+    if (sq.m <= 0) return;
+    const int rows = sq.m * a.G, keys = sq.rows(), blocks = keys / kBlk, units = (keys + kBlk - 1) / kBlk;
+    const int u_begin = WHOLE ? 0 : ch * a.piece, u_end = WHOLE ? units : min(units, u_begin + a.piece);
+    if (!WHOLE && ch > 0 && u_begin >= units) return;
+    float* sm_o = few;
+    float* sm_m = few + max(kKeys, WAVES * cols * OS);
+    float* sm_l = sm_m + WAVES * cols;
+    float* sm_h = sm_l + WAVES * cols;                      // a row's maximum, and one over its sum
+    float* staged = sm_h + 2 * cols;                        // [cols][stage]
+    const int64_t strip = (int64_t)b * a.Hk + kh;
+    const int krow = 16 * (c >> 2) + (c & 3);               // + 4 t: the key of row c of product t
+    const uint32_t v_lane = (uint32_t)(c * kBlk + 16 * g);
+    uint8_t* own = reinterpret_cast<uint8_t*>(few) + wave * (kBlk * D);
+    const uint32_t k_lane = (uint32_t)(lane / L::UPR * D + 16 * ((lane % L::UPR) ^ L::swz(lane / L::UPR)));
+    const uint32_t own_at = __builtin_amdgcn_readfirstlane(lds_addr(own));
+    u32x4 vr[DT];
+    auto load_k = [&](int page) {
+        const uint8_t* p = a.c.k_codes + ((int64_t)page * a.Hk + kh) * (kBlk * D);
+#pragma unroll
+        for (int i = 0; i < L::NI; ++i)                     // (what the first row adds to the permutation of a lane's row comes on top of it)
+            direct_load16_stream(p + 1024 * i, k_lane ^ (16 * L::swz(i * L::RPI)), own_at + 1024 * i);
+    };
+    auto load_v = [&](int page) {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(a.c.v_codes + ((int64_t)page * a.Hk + kh) * (kBlk * D), 0, kBlk * D, 0x00020000);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vr[dt] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, v_lane, 16 * dt * kBlk, 2);       // (nt: read once)
+    };
+    // Position i of a wave: first the halves of the tail, where it belongs to the piece, then the piece's blocks.  Lane i has the page and the scales of
+    // the block at the wave's i-th position (the launcher sees to it that there are no more of them).
+    const bool with_tail = units > blocks && blocks >= u_begin && blocks < u_end;
+    const int tail_rows = keys % kBlk, halves = !with_tail ? 0 : tail_rows > 32 ? 2 : 1, u_stop = min(u_end, blocks);
+    auto unit_at = [&](int i) { return u_begin + wave + WAVES * i - halves; };
+    int page_l = -1;
+    float ks_l = 0.f, vs_l = 0.f;
+    {
+        const int u = unit_at(lane);
+        page_l = u >= u_begin && u < u_stop ? page_of(a.c, b, u) : -1;
+        if (page_l >= 0) {
+            const int64_t at = (int64_t)page_l * a.Hk + kh;
+            ks_l = a.c.k_scale[at] * a.scale_l2;
+            vs_l = a.c.v_scale[at];
+        }
+    }
+    Frag qf[QC][KS];
+    Rows<D, QC> st;
+    st.init();
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc) {
+        const int r = min(16 * qc + c, rows - 1), t = r / a.G;
+        st.pos[qc] = sq.sees(t);
+        const uint16_t* row = a.q + (int64_t)(sq.start + t) * a.q_st + (int64_t)(kh * a.G + r - t * a.G) * a.q_sh;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[qc][s].u4 = *reinterpret_cast<const u32x4*>(row + 64 * (s / 2) + 16 * g + 8 * (s & 1));
+    }
+    auto keep = [&](int qc, const f32x4& s, int key) {      // logits of keys key .. + 3, of those of the strip
+        if (WHOLE && stage > 0 && 16 * qc + c < rows) *reinterpret_cast<f32x4*>(staged + (16 * qc + c) * stage + key) = s;
+    };
+    // the reference point of the exponents: follows the maximum only when that has moved by more than kLazy
+    auto follow = [&](const float (&mx)[QC]) {
+        constexpr float kLazy = 8.0f;
+        bool moved = false;
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) moved |= mx[qc] - st.m[qc] > kLazy;
+        if (!__any(moved)) return;
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) {
+            const float cand = fmaxf(st.m[qc], wave_max_from<16>(mx[qc])), m_new = cand - st.m[qc] > kLazy ? cand : st.m[qc];
+            const float alpha = exp2_fast(st.m[qc] - m_new);
+            st.m[qc] = m_new;
+            st.l[qc] *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) st.o[dt][qc] *= alpha;
+        }
+    };
+    auto weigh = [&](int qc, const f32x4& s0, const f32x4& s1, float vs) {      // (rounded to bf16 once, as in chunk_weights)
+        Frag f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const f32x4& y = j < 2 ? s0 : s1;
+            const float p0 = exp2_fast(y[2 * (j & 1)] - st.m[qc]), p1 = exp2_fast(y[2 * (j & 1) + 1] - st.m[qc]);
+            st.l[qc] += p0 + p1;
+            f.w[j] = bf16_pair(p0 * vs, p1 * vs);
+        }
+        return f;
+    };
+    // O^T += V^T P^T where V of keys that a row does not see may be infinite or no number: row by row, such V left out.  f: keys key .. + 7.
+    auto careful = [&](int dt, const Frag& f, const Frag (&p)[QC], int key) {
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc)
+#pragma unroll 1
+            for (int row = 0; row < 16; ++row) {
+                const int pos = __builtin_amdgcn_readlane(st.pos[qc], row);
+                Frag v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v.w[j] = f.w[j] & ((key + 2 * j <= pos ? 0xffffu : 0u) | (key + 2 * j < pos ? 0xffff0000u : 0u));
+                const f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, p[qc].v, st.o[dt][qc], 0, 0, 0);
+                st.o[dt][qc] = c == row ? o : st.o[dt][qc];
+            }
+    };
+    uint64_t left = __ballot(page_l >= 0);                  // the wave's positions whose blocks are to come
+    if (left != 0) load_k(__builtin_amdgcn_readlane(page_l, __ffsll((unsigned long long)left) - 1));     // (on its way beside the tail)
+    __builtin_amdgcn_sched_barrier(0);
+    if (wave < halves) {                                    // product t of two: row 4g'+i of A is key 8 g' + 4 t + i
+        const int first = 32 * wave, key0 = blocks * kBlk + first;
+        const uint16_t* kt = a.c.k_tail + strip * (kBlk * D);
+        const uint16_t* vt = a.c.v_tail + strip * (kBlk * D);
+        Frag tk[2][KS], tv[DT];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+                tk[t][i].u4 = *reinterpret_cast<const u32x4*>(kt + (first + 8 * (c >> 2) + (c & 3) + 4 * t) * D + 64 * (i / 2) + 16 * g + 8 * (i & 1));
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) tv[dt].u4 = *reinterpret_cast<const u32x4*>(vt + (16 * dt + c) * kBlk + first + 8 * g);
+        __builtin_amdgcn_sched_barrier(0);                  // (all of that is on its way)
+        f32x4 s[2][QC];
+        float mx[QC];
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) {
+            mx[qc] = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < KS; ++i) y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tk[t][i].v, qf[qc][i].v, y, 0, 0, 0);
+                y *= a.scale_l2;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (key0 + 8 * g + 4 * t + i > st.pos[qc]) y[i] = -INFINITY;       // (rows that hold nothing lie behind all rows)
+                    mx[qc] = fmaxf(mx[qc], y[i]);
+                }
+                s[t][qc] = y;
+                keep(qc, y, key0 + 8 * g + 4 * t);
+            }
+        }
+        follow(mx);
+        Frag pb[QC];
+#pragma unroll
+        for (int qc = 0; qc < QC; ++qc) pb[qc] = weigh(qc, s[0][qc], s[1][qc], 1.0f);
+        bool odd = false;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {                   // rows that hold nothing weigh nothing, whatever their bits are
+                const int row = first + 8 * g + 2 * j;
+                tv[dt].w[j] &= (row < tail_rows ? 0xffffu : 0u) | (row + 1 < tail_rows ? 0xffff0000u : 0u);
+                odd |= (tv[dt].w[j] & 0x7f80u) == 0x7f80u || (tv[dt].w[j] & 0x7f800000u) == 0x7f800000u;
+            }
+        if (__any(odd)) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) careful(dt, tv[dt], pb, key0 + 8 * g);
+        } else {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int qc = 0; qc < QC; ++qc) st.o[dt][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tv[dt].v, pb[qc].v, st.o[dt][qc], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    auto lane_value = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
+    if (WHOLE && stage > 0) {
+        const int unit_l = unit_at(lane);
+        for (uint64_t gone = __ballot(page_l < 0 && unit_l >= u_begin && unit_l < u_stop); gone != 0; gone &= gone - 1) {
+            const int u = unit_at(__ffsll((unsigned long long)gone) - 1);
+#pragma unroll
+            for (int qc = 0; qc < QC; ++qc)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) keep(qc, f32x4{kNoPage, kNoPage, kNoPage, kNoPage}, u * kBlk + 16 * g + 4 * t);
+        }
+    }
+    if (left != 0) {
+        int i = __ffsll((unsigned long long)left) - 1;
+        load_v(__builtin_amdgcn_readlane(page_l, i));
+        while (true) {
+            left &= left - 1;
+            const int next = left != 0 ? __ffsll((unsigned long long)left) - 1 : -1;
+            const int k0 = unit_at(i) * kBlk;
+            wait_direct_loads_but<DT>();                    // K is there: all of the wave's loads but V's, which came behind
+            asm volatile("" ::: "memory");
+            f32x4 s[4][QC];
+            u32x4 kr[2][4];
+            auto fetch = [&](int x) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) kr[x & 1][t] = *reinterpret_cast<const u32x4*>(own + (krow + 4 * t) * D + 16 * ((4 * x + g) ^ L::swz(krow)));
+            };
+            fetch(0);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int qc = 0; qc < QC; ++qc) s[t][qc] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < KH; ++x) {
+                if (x + 1 < KH) fetch(x + 1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const u32x4 w = kr[x & 1][t];
+                    const uint2 w0 = F::to_bf16(w.x), w1 = F::to_bf16(w.y), w2 = F::to_bf16(w.z), w3 = F::to_bf16(w.w);
+                    Frag f0, f1;
+                    f0.u4 = u32x4{w0.x, w0.y, w1.x, w1.y};
+                    f1.u4 = u32x4{w2.x, w2.y, w3.x, w3.y};
+#pragma unroll
+                    for (int qc = 0; qc < QC; ++qc) s[t][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f0.v, qf[qc][2 * x].v, s[t][qc], 0, 0, 0);
+#pragma unroll
+                    for (int qc = 0; qc < QC; ++qc) s[t][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f1.v, qf[qc][2 * x + 1].v, s[t][qc], 0, 0, 0);
+                    if (t & 1) __builtin_amdgcn_sched_barrier(0);   // (else all codes are converted ahead, into more registers than there are)
+                }
+            }
+            const float ks = lane_value(ks_l, i), vs = lane_value(vs_l, i);
+            const bool masked = k0 + kBlk - 1 > sq.n;       // (row n is the first token's own)
+            float mx[QC];
+#pragma unroll
+            for (int qc = 0; qc < QC; ++qc) {
+                mx[qc] = -INFINITY;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    s[t][qc] *= ks;
+                    if (masked) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (k0 + 16 * g + 4 * t + j > st.pos[qc]) s[t][qc][j] = -INFINITY;
+                    }
+                    mx[qc] = fmaxf(mx[qc], fmaxf(fmaxf(s[t][qc][0], s[t][qc][1]), fmaxf(s[t][qc][2], s[t][qc][3])));
+                    keep(qc, s[t][qc], k0 + 16 * g + 4 * t);
+                }
+            }
+            follow(mx);
+            // V is there.  Only now may the next K follow it: the compiler does not see direct loads, and would wait for them where it waits for V.
+            wait_direct_loads();
+            __builtin_amdgcn_sched_barrier(0);
+            if (next >= 0) load_k(__builtin_amdgcn_readlane(page_l, next));
+            __builtin_amdgcn_sched_barrier(0);
+            bool odd = false;
+            if (CODE == ST3_BLOCK_E4M3 && masked) {
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) odd |= (((vr[dt][j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;        // (a code that is no number)
+            }
+            const bool slow = __any(odd);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                Frag pb[QC];
+#pragma unroll
+                for (int qc = 0; qc < QC; ++qc) pb[qc] = weigh(qc, s[2 * x][qc], s[2 * x + 1][qc], vs);
+                __builtin_amdgcn_sched_barrier(0);
+                if (slow) {
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) {
+                        const uint2 w0 = F::to_bf16(vr[dt][2 * x]), w1 = F::to_bf16(vr[dt][2 * x + 1]);
+                        Frag f;
+                        f.u4 = u32x4{w0.x, w0.y, w1.x, w1.y};
+                        careful(dt, f, pb, k0 + 16 * g + 8 * x);
+                    }
+                    continue;
+                }
+#pragma unroll
+                for (int d2 = 0; d2 < DT; d2 += 2) {        // two chains of products at a time
+                    Frag f[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const uint2 w0 = F::to_bf16(vr[d2 + y][2 * x]), w1 = F::to_bf16(vr[d2 + y][2 * x + 1]);
+                        f[y].u4 = u32x4{w0.x, w0.y, w1.x, w1.y};
+                    }
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                        for (int qc = 0; qc < QC; ++qc) st.o[d2 + y][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[y].v, pb[qc].v, st.o[d2 + y][qc], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if (next < 0) break;
+            load_v(__builtin_amdgcn_readlane(page_l, next));
+            __builtin_amdgcn_sched_barrier(0);
+            i = next;
+        }
+    }
+    // ---- the waves' parts ---------------------------------------------------------------------------------------------------------
+    __syncthreads();                                        // (no wave reads its keys any more)
+#pragma unroll
+    for (int qc = 0; qc < QC; ++qc) {
+        const float l = wave_sum_from<16>(st.l[qc]);
+        const int col = 16 * qc + c;
+        if (col >= rows) continue;
+        if (g == 0) { sm_m[wave * cols + col] = st.m[qc]; sm_l[wave * cols + col] = l; }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(sm_o + (wave * cols + col) * OS + 16 * dt + 4 * g) = st.o[dt][qc];
+    }
+    __syncthreads();
+    for (int e = tid; e < rows * (D / 2); e += kThr) {      // two columns of a row
+        const int col = e / (D / 2), dim = 2 * (e % (D / 2)), t = col / a.G, h = kh * a.G + col - t * a.G;
+        float top = sm_m[col];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sm_m[w * cols + col]);
+        float sum = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = exp2_fast(sm_m[w * cols + col] - top);
+            const f32x2 o = *reinterpret_cast<const f32x2*>(sm_o + (w * cols + col) * OS + dim);
+            sum = fmaf(sm_l[w * cols + col], f, sum);
+            x = fmaf(o.x, f, x);
+            y = fmaf(o.y, f, y);
+        }
+        const int64_t row = (int64_t)(sq.start + t) * a.H + h;
+        if constexpr (WHOLE) {
+            const float rl = sum == 0.f ? 0.f : 1.0f / sum;     // (a sum of NaN stays one)
+            *reinterpret_cast<uint32_t*>(a.out + (int64_t)(sq.start + t) * a.o_st + (int64_t)h * a.o_sh + dim) = bf16_pair(x * rl, y * rl);
+            if (dim == 0) {
+                sm_h[col] = top;
+                sm_h[cols + col] = rl;
+                if (stage == 0 && a.ml != nullptr) a.ml[row] = make_float2(top, rl);
+            }
+        } else {
+            *reinterpret_cast<f32x2*>(a.part_o + (row * a.pieces + ch) * D + dim) = f32x2{x, y};
+            if (dim == 0) a.part_ml[row * a.pieces + ch] = make_float2(top, sum);
+        }
+    }
+    if (!WHOLE || stage == 0) return;
+    __syncthreads();
+    float* score = a.score + b * a.s_sb + kh * a.s_sh;
+    const int t_first = max(0, sq.m - a.window);
+    for (int key = tid; key < keys; key += kThr) {
+        const float old = key < sq.n ? score[key] : 0.f;
+        float w = 0.f;
+        for (int t = max(t_first, key - sq.n); t < sq.m; ++t)          // (the tokens that see the key)
+            for (int col = t * a.G; col < (t + 1) * a.G; ++col) {
+                const float s = staged[col * stage + key];
+                if (s != kNoPage) w = fmaf(exp2_fast(s - sm_h[col]), sm_h[cols + col], w);
+            }
+        score[key] = old + w;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------------
 // Behind the pieces: a wave joins a row's parts.
 // ---------------------------------------------------------------------------------------------------------------------------------
 template <int D>
@@ -781,11 +1138,25 @@ __global__ __launch_bounds__(256, 2) void chunk_score_kernel(ChunkArgs a, int ro
     }
 }
 
-// How a call is cut: rows of a tile, blocks of a piece, pieces.
-struct ChunkCut { int rows, piece, pieces; };
-constexpr int kMostRowsOfTile = 32 * kChunkWaves;
+// How a call is cut: rows of a tile, blocks of a piece, pieces; waves of a workgroup where rows are few (else 0), and rows of a strip whose logits fit in LDS.
+struct ChunkCut { int rows, piece, pieces, few, stage; };
+constexpr int kMostRowsOfTile = 32 * kChunkWaves, kFewRows = 32;
 constexpr int kWanted = 512;            // workgroups that a cut aims at: two for a compute unit
 constexpr int kLeastPiece = 4;
+constexpr int kWholeStrips = 192, kShortUnits = 20, kManyStrips = 256, kFewWgs = 768, kMostPiece = 4 * kWave - 2;
+
+template <int D>
+inline ChunkCut few_cut(int64_t strips, int cols, int max_len, bool scored) {
+    constexpr size_t kLds = 160 << 10;
+    const int64_t units = max_len / kBlk + 1;
+    const int waves = strips > kManyStrips ? 4 : cols <= 16 ? 12 : 8;
+    if (units + 2 <= waves * kWave && (strips >= kWholeStrips || units <= kShortUnits)) {
+        const bool staged = scored && few_lds<D>(waves, cols, units * kBlk) <= kLds;
+        return ChunkCut{cols, (int)units, 1, waves, staged ? (int)units * kBlk : 0};
+    }
+    const int64_t piece = std::max<int64_t>(kLeastPiece, std::min<int64_t>((units * strips + kFewWgs - 1) / kFewWgs, kMostPiece));
+    return ChunkCut{cols, (int)piece, (int)((units + piece - 1) / piece), 4, 0};
+}
 
 // No more row tiles than this, whatever the lengths are: each sequence has one that is not full.
 inline int64_t chunk_tiles(const st3_gqa_shape* s, int total, int max_new, int rows) {
@@ -797,13 +1168,15 @@ inline int tile_rows(int64_t most) {
     const int64_t tiles = (most + kMostRowsOfTile - 1) / kMostRowsOfTile;
     return tiles == 0 ? 16 : (int)((most + 16 * tiles - 1) / (16 * tiles) * 16);
 }
-inline ChunkCut chunk_cut(const st3_gqa_shape* s, int total, int max_new, int max_len) {
-    const int rows = tile_rows((int64_t)max_new * (s->heads / s->kv_heads));
+inline ChunkCut chunk_cut(const st3_gqa_shape* s, int total, int max_new, int max_len, bool scored) {
+    const int64_t most = (int64_t)max_new * (s->heads / s->kv_heads), strips = (int64_t)s->batch * s->kv_heads;
+    if (most <= kFewRows && most > 0) return s->head_dim == 128 ? few_cut<128>(strips, (int)most, max_len, scored) : few_cut<64>(strips, (int)most, max_len, scored);
+    const int rows = tile_rows(most);
     const int64_t tiles = chunk_tiles(s, total, max_new, rows) * s->kv_heads, units = max_len / kBlk + 1;
-    if (2 * tiles >= kWanted || tiles == 0) return ChunkCut{rows, (int)units, 1};
+    if (2 * tiles >= kWanted || tiles == 0) return ChunkCut{rows, (int)units, 1, 0, 0};
     const int64_t pieces = std::min((kWanted + tiles - 1) / tiles, (units + kLeastPiece - 1) / kLeastPiece);
     const int64_t piece = (units + pieces - 1) / pieces;
-    return ChunkCut{rows, (int)piece, (int)((units + piece - 1) / piece)};
+    return ChunkCut{rows, (int)piece, (int)((units + piece - 1) / piece), 0, 0};
 }
 
 // Blocks that a wave of the scores' launch takes one behind the other.
@@ -815,10 +1188,11 @@ inline int score_rounds(int64_t units, int Hk, int B) {
 
 struct ChunkWs { size_t ml, part_o, part_ml, total; int64_t parts; };
 // Room for as many parts as a launch of these or any smaller sizes may leave.  Tiles hold all rows, so less than kWanted / tiles + 1 pieces are less
-// than kWanted tiles of parts and one more for each row; nor are there more than one for every kLeastPiece blocks.
+// than kWanted tiles of parts and one more for each row (with few rows: than kFewWgs of them, or one for every kMostPiece blocks); nor are there more than
+// one for every kLeastPiece blocks.
 inline ChunkWs chunk_ws(const st3_gqa_shape* s, int total, int max_len) {
     const int64_t rows = (int64_t)total * s->heads, units = max_len / kBlk + 1;
-    const int64_t parts = std::min((int64_t)kWanted * kMostRowsOfTile + rows, rows * ((units + kLeastPiece - 1) / kLeastPiece));
+    const int64_t parts = std::min((int64_t)kWanted * kMostRowsOfTile + rows * (1 + (units + kMostPiece - 1) / kMostPiece), rows * ((units + kLeastPiece - 1) / kLeastPiece));
     ChunkWs w{};
     w.parts = parts;
     size_t off = 0;
@@ -829,12 +1203,23 @@ inline ChunkWs chunk_ws(const st3_gqa_shape* s, int total, int max_len) {
     return w;
 }
 
+template <int D, int CODE, int QC>
+void launch_few(const ChunkArgs& a, const ChunkCut& cut, hipStream_t st) {
+    const size_t lds = few_lds<D>(cut.few, a.tile, cut.stage);
+    const dim3 grid(a.Hk, a.pieces, a.B);
+    constexpr int kMost = QC == 1 ? 12 : 8;
+    if (a.pieces > 1) chunk_few_kernel<D, CODE, QC, 4, false><<<grid, 256, lds, st>>>(a, 0);
+    else if (cut.few == kMost) chunk_few_kernel<D, CODE, QC, kMost, true><<<grid, 64 * kMost, lds, st>>>(a, cut.stage);
+    else chunk_few_kernel<D, CODE, QC, 4, true><<<grid, 256, lds, st>>>(a, cut.stage);
+}
+
 template <int D, int CODE>
-void launch_chunk(const ChunkArgs& a, unsigned grid, hipStream_t st) {
-    if (a.tile <= 16 * kChunkWaves) block_chunk_kernel<D, CODE, 1><<<dim3(grid, a.pieces), kChunkThreads, 0, st>>>(a);
+void launch_chunk(const ChunkArgs& a, const ChunkCut& cut, unsigned grid, hipStream_t st) {
+    if (cut.few > 0) a.tile <= 16 ? launch_few<D, CODE, 1>(a, cut, st) : launch_few<D, CODE, 2>(a, cut, st);
+    else if (a.tile <= 16 * kChunkWaves) block_chunk_kernel<D, CODE, 1><<<dim3(grid, a.pieces), kChunkThreads, 0, st>>>(a);
     else block_chunk_kernel<D, CODE, 2><<<dim3(grid, a.pieces), kChunkThreads, 0, st>>>(a);
     if (a.pieces > 1) chunk_join_kernel<D><<<(unsigned)(((int64_t)a.total * a.H + 3) / 4), 256, 0, st>>>(a);
-    if (!a.score || a.max_len == 0) return;
+    if (!a.score || a.max_len == 0 || cut.stage > 0) return;
     const int fit = score_rows((int64_t)std::min(a.window, a.max_new) * a.G), units = (a.max_len + kBlk - 1) / kBlk, rounds = score_rounds(units, a.Hk, a.B);
     chunk_score_kernel<D, CODE><<<dim3(a.Hk, (units + 4 * rounds - 1) / (4 * rounds), a.B), 256, fit * (2 * D + sizeof(float2)), st>>>(a, rounds, fit);
 }
@@ -864,8 +1249,8 @@ extern "C" st3_status st3_block_attend(const st3_gqa_shape* shape, const st3_row
     if (packed_rows_meet(q, H, out, H, total, D, 2)) return ST3_ERR_INVALID_ARG;
     if (score && (window < 1 || score_stride_h < max_len || (B > 1 && score_stride_b < max_len))) return ST3_ERR_INVALID_ARG;
     if (!workspace || !aligned16(workspace)) return ST3_ERR_INVALID_ARG;
-    const ChunkCut cut = chunk_cut(shape, total, max_new, max_len);
-    const int64_t grid = chunk_tiles(shape, total, max_new, cut.rows) * Hk;
+    const ChunkCut cut = chunk_cut(shape, total, max_new, max_len, score != nullptr);
+    const int64_t grid = cut.few > 0 ? Hk : chunk_tiles(shape, total, max_new, cut.rows) * Hk;
     if (!grid_fits(grid, kChunkThreads, cut.pieces) || !grid_fits(((int64_t)total * H + 3) / 4, 256, 1) || (score && (max_len + 4 * kBlk - 1) / (4 * kBlk) > 65535)) return ST3_ERR_UNSUPPORTED;
     const ChunkWs wl = chunk_ws(shape, total, max_len);
     if (cut.pieces > 1 && (int64_t)total * H * cut.pieces > wl.parts) return ST3_ERR_UNSUPPORTED;    // (never, by the rule above)
@@ -884,11 +1269,11 @@ extern "C" st3_status st3_block_attend(const st3_gqa_shape* shape, const st3_row
     a.part_ml = reinterpret_cast<float2*>(ws + wl.part_ml);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     if (cache->code == ST3_BLOCK_INT8) {
-        if (D == 128) launch_chunk<128, ST3_BLOCK_INT8>(a, (unsigned)grid, st);
-        else launch_chunk<64, ST3_BLOCK_INT8>(a, (unsigned)grid, st);
+        if (D == 128) launch_chunk<128, ST3_BLOCK_INT8>(a, cut, (unsigned)grid, st);
+        else launch_chunk<64, ST3_BLOCK_INT8>(a, cut, (unsigned)grid, st);
     } else {
-        if (D == 128) launch_chunk<128, ST3_BLOCK_E4M3>(a, (unsigned)grid, st);
-        else launch_chunk<64, ST3_BLOCK_E4M3>(a, (unsigned)grid, st);
+        if (D == 128) launch_chunk<128, ST3_BLOCK_E4M3>(a, cut, (unsigned)grid, st);
+        else launch_chunk<64, ST3_BLOCK_E4M3>(a, cut, (unsigned)grid, st);
     }
     return check_launch();
 }

@@ -37,13 +37,6 @@ struct BlockDecodeArgs {
 // Blocks that hold rows to attend (the last one may be the tail).
 __device__ __forceinline__ int units_of(int n, bool fresh) { return n / kBlk + (n % kBlk + (fresh ? 1 : 0) > 0 ? 1 : 0); }
 
-// A block's K lies in a wave's own LDS, rows of D bytes, the 16-byte units of a row permuted: unit u of row r is at u ^ swz(r), so that the 16 rows
-// that a fragment's lanes read (16 (c / 4) + c % 4 + 4 t) lie in 16 different units of the banks.
-template <int D> struct KeyTile {
-    static constexpr int UPR = D / 16, RPI = 1024 / D, NI = kBlk / RPI;     // units of a row; rows of a wave-wide load; loads of a block
-    __device__ static __forceinline__ int swz(int row) { return D == 128 ? ((row >> 4 & 3) << 1 | (row >> 1 & 1)) : row >> 4 & 3; }
-};
-
 // Dynamic LDS: the waves' K blocks, and where those were the waves' outputs [waves][columns][D + 4], their maxima and sums [2][waves][16], the heads'
 // [2][16], and in a launch of whole strips the logits [columns][rows].
 template <int D>
