@@ -359,14 +359,20 @@ def block_cache(k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Ten
     return c
 
 
-def rotary(table: torch.Tensor, layout: int = ST3_ROTARY_HALVES) -> Rotary:
-    """A rotation of packed rows by table [rows, pairs, 2] (float32: cosine, sine), as st3_rotary_table fills it; its rows may be those of a wider tensor."""
-    if table.dim() != 3 or table.shape[2] != 2 or (table.numel() and (table.stride(2) != 1 or table.stride(1) != 2)):
-        raise ValueError(f"table: [rows, pairs, 2], cosine and sine side by side, expected; {tuple(table.shape)} given")
+def _table(table: torch.Tensor):
+    """(rows, pairs, stride of a row) of a table [rows, pairs, 2]."""
+    size, steps = table.shape, table.stride()
+    if len(size) != 3 or size[2] != 2 or (size[0] * size[1] > 0 and (steps[2] != 1 or (steps[1] != 2 and size[1] > 1))):
+        raise ValueError(f"table: [rows, pairs, 2], cosine and sine side by side, expected; {tuple(size)} given")
     if table.dtype != torch.float32 or not table.is_cuda:
         raise TypeError(f"table: float32 on the device expected, {table.dtype} on {table.device} given")
-    rows, pairs, _ = table.shape
-    r = Rotary(table.data_ptr(), table.stride(0) if rows > 1 else 2 * pairs, pairs, layout)
+    return size[0], size[1], steps[0] if size[0] > 1 else 2 * size[1]
+
+
+def rotary(table: torch.Tensor, layout: int = ST3_ROTARY_HALVES) -> Rotary:
+    """A rotation of packed rows by table [rows, pairs, 2] (float32: cosine, sine), as st3_rotary_table fills it; its rows may be those of a wider tensor."""
+    rows, pairs, stride = _table(table)
+    r = Rotary(table.data_ptr(), stride, pairs, layout)
     r._refs = (table,)
     r._rows = rows
     return r
@@ -617,23 +623,22 @@ def st3_block_evict(shape: GqaShape, src: BlockCache, dst: BlockCache, max_len: 
 def st3_rotary_table(positions, inv_freq, axis, table, stream=None) -> None:
     """table [T, pairs, 2] <- cosines and sines.  positions int32 [axes, T] or [T]; inv_freq float32 [pairs]; axis: the component that turns each
     pair, a sequence of pairs integers, or None where there is one."""
-    pos = positions if positions.dim() == 2 else positions[None]
-    axes, total = pos.shape
-    t = rotary(table)
-    if t._rows != total or inv_freq.shape != (t.pairs,) or not inv_freq.is_contiguous():
-        raise ValueError(f"{total} positions and {tuple(inv_freq.shape)} frequencies for a table of {tuple(table.shape)}")
+    size, steps = positions.shape, positions.stride()
+    if not 1 <= len(size) <= 2:
+        raise ValueError(f"positions: [axes, T] or [T] expected, {tuple(size)} given")
+    axes, total, apart = (1, size[0], size[0]) if len(size) == 1 else (size[0], size[1], max(steps[0], size[1]))
+    rows, pairs, stride = _table(table)
+    if rows != total or inv_freq.shape != (pairs,) or inv_freq.stride(0) != 1:
+        raise ValueError(f"{total} positions and {tuple(inv_freq.shape)} frequencies, side by side, for a table of {tuple(table.shape)}")
     if inv_freq.dtype != torch.float32 or not inv_freq.is_cuda:
         raise TypeError(f"inv_freq: float32 on the device expected, {inv_freq.dtype} on {inv_freq.device} given")
-    if total > 1 and pos.stride(1) != 1:
+    if total > 1 and steps[-1] != 1:
         raise ValueError("the positions of an axis follow each other")
-    of = None
-    if axis is not None:
-        axis = [int(i) for i in axis]
-        if len(axis) != t.pairs or not all(0 <= i < axes for i in axis):
-            raise ValueError(f"axis: {t.pairs} of 0 .. {axes - 1} expected, {axis} given")
-        of = bytes(axis)
-    _check(lib().st3_rotary_table(axes, t.pairs, of, inv_freq.data_ptr(), _ints(pos, "positions"), max(pos.stride(0), total) if axes > 1 else total, total,
-                                  t.table, t.stride_t, _stream(stream)), "st3_rotary_table")
+    of = None if axis is None else bytes(axis)
+    if of is not None and (len(of) != pairs or max(of) >= axes):
+        raise ValueError(f"axis: {pairs} of 0 .. {axes - 1} expected, {axis} given")
+    _check(lib().st3_rotary_table(axes, pairs, of, inv_freq.data_ptr(), _ints(positions, "positions"), apart, total, table.data_ptr(), stride, _stream(stream)),
+           "st3_rotary_table")
 
 
 def st3_rotate_rows(x, out, rotary: Rotary, inverse: bool = False, stream=None) -> None:

@@ -29,8 +29,9 @@ struct Place {
 };
 
 // Codes a block of K (COLUMNS: of V) from the threads' values v [row][column] into a page (past the caches: 16 prompts into pages 20.3 -> 18.7 us).
-template <int D, int CODE, bool COLUMNS>
-__device__ __forceinline__ void write_block(float (&v)[4][D / 16], const BlockPages& c, int64_t at, uint32_t* sm, int tid) {
+// SPLIT (K only): the thread's columns are two runs, from `first` and from `second` on.
+template <int D, int CODE, bool COLUMNS, bool SPLIT = false>
+__device__ __forceinline__ void write_block(float (&v)[4][D / 16], const BlockPages& c, int64_t at, uint32_t* sm, int tid, int first = 0, int second = 0) {
     using F = BlockCode<CODE>;
     constexpr int W = D / 16;
     const Place<D, COLUMNS> my(tid);
@@ -63,6 +64,20 @@ __device__ __forceinline__ void write_block(float (&v)[4][D / 16], const BlockPa
         for (int e = 0; e < W; ++e) {
             const float x[4] = {v[0][e], v[1][e], v[2][e], v[3][e]};
             __builtin_nontemporal_store(F::code4(x, divide), reinterpret_cast<uint32_t*>(codes + (my.col + e) * kBlk + my.row));
+        }
+    } else if constexpr (SPLIT) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            uint8_t* to = codes + (my.row + r) * D;
+            const float rear[4] = {v[r][W / 2], v[r][W / 2 + 1], W == 8 ? v[r][W - 2] : 0.f, W == 8 ? v[r][W - 1] : 0.f};
+            if constexpr (W == 8) {
+                __builtin_nontemporal_store(F::code4(v[r], divide), reinterpret_cast<uint32_t*>(to + first));
+                __builtin_nontemporal_store(F::code4(rear, divide), reinterpret_cast<uint32_t*>(to + second));
+            } else {                                        // two codes each
+                const uint32_t w = F::code4(v[r], divide);
+                *reinterpret_cast<uint16_t*>(to + first) = (uint16_t)w;
+                *reinterpret_cast<uint16_t*>(to + second) = (uint16_t)(w >> 16);
+            }
         }
     } else {
 #pragma unroll
@@ -162,117 +177,154 @@ struct AppendArgs {
     int32_t total, max_new, max_len, Hk;
 };
 
-// Rows row .. + 3 (of those of the sequence) of a thread's columns, 16 bits each, turned on the way; rows outside [0, m) read the nearest.
+// A thread's columns, two runs of D / 32.  Where the halves of a row turn against each other they are a pair's two sides, and those of the last threads
+// the columns that do not turn; else they follow each other.
 enum Turn { kStill, kHalves, kAdjacent };
-template <int D, bool COLUMNS, int TURN>
-__device__ __forceinline__ void new_rows(const AppendArgs& a, int kh, int start, int m, int row, int col, uint32_t (&raw)[4][D / 32]) {
-    constexpr int W = D / 16;
-    const uint16_t* src = COLUMNS ? a.v + kh * a.v_sh : a.k + kh * a.k_sh;
-    const int64_t stride = COLUMNS ? a.v_st : a.k_st;
-    const uint16_t* at[4];
-    int t[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        t[r] = start + max(0, min(row + r, m - 1));
-        at[r] = src + t[r] * stride;
-        load_bf16<W>(at[r] + col, raw[r]);
+template <int D, int TURN>
+struct Runs {
+    static constexpr int R = D / 32;
+    int first, second;
+    __device__ __forceinline__ Runs(int fast, int pairs) {
+        if (TURN == kHalves && fast < pairs / R) {
+            first = R * fast;
+            second = first + pairs;
+        } else {
+            first = 2 * R * fast;
+            second = first + R;
+        }
     }
-    if constexpr (TURN != kStill && !COLUMNS) {
-        if (col >= 2 * a.r.pairs) return;
-        if constexpr (TURN == kAdjacent) {
+};
+
+// Four rows of a thread's columns on their way, with the cosines and sines that turn them; rows outside [0, m) are the nearest.
+template <int D, bool COLUMNS, int TURN>
+struct NewRows {
+    static constexpr int R = D / 32;                        // columns of a run, pairs of a thread
+    uint32_t raw[4][R];                                     // two bf16 each: the first run, the second
+    float4 cs[4][R / 2];
+    bool turns;
+    __device__ __forceinline__ void load(const AppendArgs& a, const Runs<D, TURN>& my, int kh, int start, int m, int row) {
+        const uint16_t* src = COLUMNS ? a.v + kh * a.v_sh : a.k + kh * a.k_sh;
+        const int64_t stride = COLUMNS ? a.v_st : a.k_st;
+        turns = TURN != kStill && !COLUMNS && my.first < (TURN == kHalves ? a.r.pairs : 2 * a.r.pairs);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float4* cs = reinterpret_cast<const float4*>(a.r.table + t[r] * a.r.stride + col);
-#pragma unroll
-                for (int e = 0; e < W; e += 4) {
-                    const float4 x = cs[e / 4];
-                    float p[4] = {bf16_lo(raw[r][e / 2]), bf16_hi(raw[r][e / 2]), bf16_lo(raw[r][e / 2 + 1]), bf16_hi(raw[r][e / 2 + 1])};
-                    turn(p[0], p[1], x.x, x.y);
-                    turn(p[2], p[3], x.z, x.w);
-                    raw[r][e / 2] = bf16_pair(p[0], p[1]);
-                    raw[r][e / 2 + 1] = bf16_pair(p[2], p[3]);
-                }
+        for (int r = 0; r < 4; ++r) {
+            const int t = start + max(0, min(row + r, m - 1));
+            const uint16_t* at = src + t * stride;
+            if constexpr (TURN == kHalves && !COLUMNS) {
+                run(at + my.first, raw[r]);
+                run(at + my.second, raw[r] + R / 2);
+            } else {
+                load_bf16<2 * R>(at + my.first, raw[r]);
             }
-        } else {                                            // the other half's columns are another thread's: read here too
-            const bool upper = col >= a.r.pairs;
-            const int c = upper ? col - a.r.pairs : col;
-            uint32_t other[4][W / 2];
+            if constexpr (TURN != kStill && !COLUMNS) {
+                const float4* from = reinterpret_cast<const float4*>(a.r.table + t * a.r.stride + (turns ? (TURN == kHalves ? 2 * my.first : my.first) : 0));
 #pragma unroll
-            for (int r = 0; r < 4; ++r) load_bf16<W>(at[r] + (upper ? c : c + a.r.pairs), other[r]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float4* cs = reinterpret_cast<const float4*>(a.r.table + t[r] * a.r.stride + 2 * c);
-#pragma unroll
-                for (int e = 0; e < W; e += 2) {
-                    const float4 x = cs[e / 2];
-                    float p0 = bf16_lo(raw[r][e / 2]), p1 = bf16_hi(raw[r][e / 2]), q0 = bf16_lo(other[r][e / 2]), q1 = bf16_hi(other[r][e / 2]);
-                    // (b cos + a sin is a cos - b sin with the pair and the sine's sign exchanged)
-                    turn(p0, q0, x.x, upper ? -x.y : x.y);
-                    turn(p1, q1, x.z, upper ? -x.w : x.w);
-                    raw[r][e / 2] = bf16_pair(p0, p1);
-                }
+                for (int e = 0; e < R / 2; ++e) cs[r][e] = from[e];
             }
         }
     }
-}
+    __device__ __forceinline__ static void run(const uint16_t* p, uint32_t* to) {
+        if constexpr (R == 4) {
+            const uint2 q = *reinterpret_cast<const uint2*>(p);
+            to[0] = q.x;
+            to[1] = q.y;
+        } else {
+            to[0] = *reinterpret_cast<const uint32_t*>(p);
+        }
+    }
+    __device__ __forceinline__ void turn_all() {
+        if (!turns) return;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < R / 2; ++e) {               // two pairs
+                const float4 x = cs[r][e];
+                uint32_t& u = raw[r][TURN == kHalves ? e : 2 * e];
+                uint32_t& w = raw[r][TURN == kHalves ? R / 2 + e : 2 * e + 1];
+                float p[4] = {bf16_lo(u), bf16_hi(u), bf16_lo(w), bf16_hi(w)};
+                if constexpr (TURN == kHalves) {
+                    turn(p[0], p[2], x.x, x.y);
+                    turn(p[1], p[3], x.z, x.w);
+                } else {
+                    turn(p[0], p[1], x.x, x.y);
+                    turn(p[2], p[3], x.z, x.w);
+                }
+                u = bf16_pair(p[0], p[1]);
+                w = bf16_pair(p[2], p[3]);
+            }
+    }
+    __device__ __forceinline__ uint16_t bits(int r, int e) const { return (uint16_t)(raw[r][e / 2] >> (16 * (e & 1))); }
+};
 
 template <int D, int CODE, bool COLUMNS, int TURN>
 __device__ __forceinline__ void append_block(const AppendArgs& a, int kh, int j, int b, uint32_t* sm) {
-    constexpr int W = D / 16;
+    constexpr int W = D / 16, R = W / 2, kTurn = COLUMNS ? kStill : TURN;
     const int tid = threadIdx.x;
-    const Place<D, COLUMNS> my(tid);
+    const int row = 4 * (COLUMNS ? tid & 15 : tid >> 4);    // (Place)
+    const Runs<D, kTurn> my(COLUMNS ? tid >> 4 : tid & 15, a.r.pairs);
+    auto column = [&](int e) { return e < R ? my.first + e : my.second + e - R; };
     const int n = a.c.len[b], start = max(0, min(a.cu[b], a.total));
     const int m = min(min(max(start, min(a.cu[b + 1], a.total)) - start, a.max_new), a.max_len - n);
     if (n < 0 || n >= a.max_len || m <= 0) return;
-    const int first = n / kBlk, at = (first + j) * kBlk, total = n + m, rest = total % kBlk;
+    const int first = n / kBlk, at = (first + j) * kBlk, total = n + m, rest = total % kBlk, held = j == 0 ? n % kBlk : 0;
     const int64_t strip = (int64_t)b * a.Hk + kh;
     if (at >= total || (j > 0 && at + kBlk > total)) return;        // (the last, partial block is the first workgroup's)
-    uint32_t raw[4][W / 2], behind[4][W / 2];
-    new_rows<D, COLUMNS, TURN>(a, kh, start, m, at + my.row - n, my.col, raw);
     const bool whole = at + kBlk <= total, more = j == 0 && whole && rest > 0;
-    if (more) new_rows<D, COLUMNS, TURN>(a, kh, start, m, total - rest + my.row - n, my.col, behind);
-    auto bits = [](const uint32_t (&x)[4][W / 2], int r, int e) { return (uint16_t)(x[r][e / 2] >> (16 * (e & 1))); };
-    if (whole) {
-        if (j == 0 && my.row < n % kBlk) {                  // the block's rows that are in the tail
-            const uint16_t* tail = (COLUMNS ? a.c.v_tail : a.c.k_tail) + strip * (kBlk * D);
-            if constexpr (COLUMNS) {
+    const int page = whole ? page_of(a.c, b, first + j) : -1;
+    uint16_t* tail = (COLUMNS ? a.c.v_tail : a.c.k_tail) + strip * (kBlk * D);
+    NewRows<D, COLUMNS, kTurn> now, behind;
+    now.load(a, my, kh, start, m, at + row - n);
+    if (more) behind.load(a, my, kh, start, m, total - rest + row - n);
+    uint32_t old[4][R];
+    if (whole && row < held) {                              // the block's rows that are in the tail
+        if constexpr (COLUMNS) {
+            uint32_t pair[W][2];
 #pragma unroll
-                for (int e = 0; e < W; ++e) {
-                    const uint2 x = *reinterpret_cast<const uint2*>(tail + (my.col + e) * kBlk + my.row);
-                    const uint32_t half[4] = {x.x & 0xffffu, x.x >> 16, x.y & 0xffffu, x.y >> 16};
+            for (int e = 0; e < W; ++e) {
+                const uint2 x = *reinterpret_cast<const uint2*>(tail + column(e) * kBlk + row);
+                pair[e][0] = x.x;
+                pair[e][1] = x.y;
+            }
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (my.row + r < n % kBlk) raw[r][e / 2] = e & 1 ? (raw[r][e / 2] & 0xffffu) | half[r] << 16 : (raw[r][e / 2] & 0xffff0000u) | half[r];
-                }
-            } else {
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (my.row + r < n % kBlk) load_bf16<W>(tail + (my.row + r) * D + my.col, raw[r]);
+                for (int e = 0; e < W; e += 2)
+                    old[r][e / 2] = __builtin_amdgcn_perm(pair[e + 1][r / 2], pair[e][r / 2], r & 1 ? 0x07060302u : 0x05040100u);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                NewRows<D, COLUMNS, kTurn>::run(tail + (row + r) * D + my.first, old[r]);
+                NewRows<D, COLUMNS, kTurn>::run(tail + (row + r) * D + my.second, old[r] + R / 2);
             }
         }
-        const int page = page_of(a.c, b, first + j);
+    }
+    now.turn_all();
+    if (whole) {
+        if (row < held) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < R; ++e) now.raw[r][e] = row + r < held ? old[r][e] : now.raw[r][e];
+        }
         if (page >= 0) {
             float v[4][W];
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int e = 0; e < W; e += 2) { v[r][e] = bf16_lo(raw[r][e / 2]); v[r][e + 1] = bf16_hi(raw[r][e / 2]); }
-            write_block<D, CODE, COLUMNS>(v, a.c, (int64_t)page * a.Hk + kh, sm, tid);
+                for (int e = 0; e < W; e += 2) { v[r][e] = bf16_lo(now.raw[r][e / 2]); v[r][e + 1] = bf16_hi(now.raw[r][e / 2]); }
+            write_block<D, CODE, COLUMNS, kTurn == kHalves>(v, a.c, (int64_t)page * a.Hk + kh, sm, tid, my.first, my.second);
         }
-        if (more) {
-            __syncthreads();                                // (all have read the tail)
-            write_tail<D, COLUMNS>([&](int r, int e) { return bits(behind, r, e); }, a.c, strip, rest, tid);
-        }
-        return;
+        if (!more) return;
+        behind.turn_all();
+        __syncthreads();                                    // (all have read the tail)
     }
-    const int from = n % kBlk;                              // the new rows stay in the tail, behind those that are there
-    const Place<D, COLUMNS> p(tid);
-    uint16_t* tail = (COLUMNS ? a.c.v_tail : a.c.k_tail) + strip * (kBlk * D);
+    const NewRows<D, COLUMNS, kTurn>& x = more ? behind : now;      // rows of the tail, behind those that stay
+    const int from = more ? 0 : held;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        if (p.row + r < from || p.row + r >= rest) continue;
+        if (row + r < from || row + r >= rest) continue;
 #pragma unroll
-        for (int e = 0; e < W; ++e) tail[COLUMNS ? (p.col + e) * kBlk + p.row + r : (p.row + r) * D + p.col + e] = bits(raw, r, e);
+        for (int e = 0; e < W; ++e) tail[COLUMNS ? column(e) * kBlk + row + r : (row + r) * D + column(e)] = x.bits(r, e);
     }
 }
 

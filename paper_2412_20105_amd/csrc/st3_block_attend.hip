@@ -883,6 +883,14 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
             i = next;
         }
     }
+    // what the first rows have received so far, on its way while the waves' parts are joined
+    constexpr int kAhead = 4;
+    float* score = a.score + b * a.s_sb + kh * a.s_sh;
+    float old[kAhead] = {};
+    if (WHOLE && stage > 0 && sq.n > 0) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) old[j] = score[min(tid + j * kThr, sq.n - 1)];
+    }
     // ---- the waves' parts ---------------------------------------------------------------------------------------------------------
     __syncthreads();                                        // (no wave reads its keys any more)
 #pragma unroll
@@ -914,8 +922,8 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
             const float rl = sum == 0.f ? 0.f : 1.0f / sum;     // (a sum of NaN stays one)
             *reinterpret_cast<uint32_t*>(a.out + (int64_t)(sq.start + t) * a.o_st + (int64_t)h * a.o_sh + dim) = bf16_pair(x * rl, y * rl);
             if (dim == 0) {
-                sm_h[col] = top;
-                sm_h[cols + col] = rl;
+                sm_h[2 * col] = top;
+                sm_h[2 * col + 1] = rl;
                 if (stage == 0 && a.ml != nullptr) a.ml[row] = make_float2(top, rl);
             }
         } else {
@@ -925,18 +933,25 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
     }
     if (!WHOLE || stage == 0) return;
     __syncthreads();
-    float* score = a.score + b * a.s_sb + kh * a.s_sh;
-    const int t_first = max(0, sq.m - a.window);
-    for (int key = tid; key < keys; key += kThr) {
-        const float old = key < sq.n ? score[key] : 0.f;
+    const int first = max(0, sq.m - a.window) * a.G;
+    auto weight = [&](int key) {
+        const int from = (key - sq.n) * a.G;                // (the rows of the tokens that see the key)
         float w = 0.f;
-        for (int t = max(t_first, key - sq.n); t < sq.m; ++t)          // (the tokens that see the key)
-            for (int col = t * a.G; col < (t + 1) * a.G; ++col) {
-                const float s = staged[col * stage + key];
-                if (s != kNoPage) w = fmaf(exp2_fast(s - sm_h[col]), sm_h[cols + col], w);
-            }
-        score[key] = old + w;
+#pragma unroll 4
+        for (int col = first; col < rows; ++col) {
+            const float s = staged[col * stage + key];
+            const f32x2 h = *reinterpret_cast<const f32x2*>(sm_h + 2 * col);
+            const float p = exp2_fast(s - h.x) * h.y;
+            w += col < from || s == kNoPage ? 0.f : p;
+        }
+        return w;
+    };
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+        const int key = tid + j * kThr;
+        if (key < keys) score[key] = (key < sq.n ? old[j] : 0.f) + weight(key);
     }
+    for (int key = tid + kAhead * kThr; key < keys; key += kThr) score[key] = (key < sq.n ? score[key] : 0.f) + weight(key);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
