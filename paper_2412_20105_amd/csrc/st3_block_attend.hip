@@ -955,7 +955,7 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Behind the pieces: a wave joins a row's parts.
+// Behind the pieces: a wave joins a row's parts, eight loads on their way (1952 rows of up to 32 parts 9.8 us, one load at a time 15.6).
 // ---------------------------------------------------------------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a) {
@@ -981,16 +981,22 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a) {
     float top = -3.402823466e38f;
     for (int i = lane; i < parts; i += kWave) top = fmaxf(top, a.part_ml[at + i].x);
     top = wave_max_from<1>(top);
-    float sum = 0.f;
     constexpr int PER = D / 64;
-    float v[PER] = {};
-    for (int i = 0; i < parts; ++i) {
-        const float2 ml = a.part_ml[at + i];
-        const float f = exp2_fast(ml.x - top);
-        sum = fmaf(ml.y, f, sum);
+    float sum = 0.f, v[PER] = {};
+    for (int i0 = 0; i0 < parts; i0 += kWave) {             // lane i has part i0 + i's factor; the parts' loads go out eight at a time
+        const int here = min(kWave, parts - i0);
+        const float2 ml = lane < here ? a.part_ml[at + i0 + lane] : make_float2(top, 0.f);
+        const float f_l = exp2_fast(ml.x - top);
+        sum = fmaf(ml.y, f_l, sum);
+        const float* from = a.part_o + (at + i0) * D + PER * lane;
+#pragma unroll 8
+        for (int i = 0; i < here; ++i) {
+            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f_l), i));
 #pragma unroll
-        for (int e = 0; e < PER; ++e) v[e] = fmaf(a.part_o[(at + i) * D + PER * lane + e], f, v[e]);
+            for (int e = 0; e < PER; ++e) v[e] = fmaf(from[(int64_t)i * D + e], f, v[e]);
+        }
     }
+    sum = wave_sum_from<1>(sum);
     const float rl = sum == 0.f ? 0.f : 1.0f / sum;
     uint16_t* out = a.out + (int64_t)row * a.o_st + (int64_t)h * a.o_sh + PER * lane;
     if constexpr (PER == 2) *reinterpret_cast<uint32_t*>(out) = bf16_pair(v[0] * rl, v[1] * rl);
@@ -1000,8 +1006,8 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a) {
 
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Scores: the logits of the window's rows are formed again.  Workgroup (key head, strip of 4 x rounds blocks, sequence): the rows, up to kScoreRows of them, lie in
-// LDS; a wave has the 64 keys of a block in registers, the next block's codes on their way, meets 16 rows at a time, and a lane adds up what its
-// 16 keys get.
+// LDS; a wave has the 64 keys of a block in registers, meets 16 rows at a time, and a lane adds up what its 16 keys get.  Three waves of a SIMD hide each
+// other's loads of codes better than two that have the next block's codes on their way (those need the registers): a call with 16 tokens' windows over 202000 rows took 303 us so, 314 before.
 // ---------------------------------------------------------------------------------------------------------------------------------
 constexpr int kScoreRows = 256;         // rows in LDS at a time: 64 KB at d = 128
 
@@ -1009,7 +1015,7 @@ constexpr int kScoreRows = 256;         // rows in LDS at a time: 64 KB at d = 1
 inline int score_rows(int64_t rows) { return (int)std::min<int64_t>((rows + 15) / 16 * 16, kScoreRows); }
 
 template <int D, int CODE>
-__global__ __launch_bounds__(256, 2) void chunk_score_kernel(ChunkArgs a, int rounds, int fit) {
+__global__ __launch_bounds__(256, 3) void chunk_score_kernel(ChunkArgs a, int rounds, int fit) {
     using F = BlockCode<CODE>;
     constexpr int KS = D / 32, KH = D / 64, UPR = D / 8;    // contraction steps; 16-byte pieces of codes in a key's row for a lane; units of a row
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -1042,10 +1048,9 @@ __global__ __launch_bounds__(256, 2) void chunk_score_kernel(ChunkArgs a, int ro
 #pragma unroll
             for (int y = 0; y < KH; ++y) raw[x][y] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, k_lane, 16 * x * D + 64 * y, 0);
     };
-    fetch(0);
     const int rows = sq.m * a.G, first = max(0, sq.m - a.window) * a.G;
     auto stage = [&](int r0) {                              // rows r0 .. into LDS
-#pragma unroll 4
+#pragma unroll 2
         for (int e = tid; e < fit * UPR; e += 256) {
             const int x = e / UPR, r = min(r0 + x, rows - 1), t = r / a.G;
             const uint16_t* row = a.q + (int64_t)(sq.start + t) * a.q_st + (int64_t)(kh * a.G + r - t * a.G) * a.q_sh;
@@ -1066,6 +1071,7 @@ __global__ __launch_bounds__(256, 2) void chunk_score_kernel(ChunkArgs a, int ro
         if (all_fit && u >= u_end) break;
         const bool tail = u == blocks && u < u_end, there = tail || __builtin_amdgcn_readlane(page_l, i) >= 0;
         const float ks = tail ? a.scale_l2 : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), i)) * a.scale_l2;
+        fetch(i);
         Frag kf[4][KS];
         if (tail) {
             const uint16_t* from = a.c.k_tail + strip * (kBlk * D);
@@ -1085,7 +1091,6 @@ __global__ __launch_bounds__(256, 2) void chunk_score_kernel(ChunkArgs a, int ro
                 }
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (i + 1 < rounds) fetch(i + 1);
         const int key = u * kBlk + lane;
         float* to = a.score + b * a.s_sb + kh * a.s_sh + key;
         const float old = u < u_end && key < sq.n ? *to : 0.f;
@@ -1099,7 +1104,8 @@ __global__ __launch_bounds__(256, 2) void chunk_score_kernel(ChunkArgs a, int ro
                 // 16 rows, this lane's the one of column c: logits, weights
                 auto add = [&](int x0, auto masked) {
                     const float2 ml = sm_ml[x0 + c];
-                    const int pos = sq.n + (r0 + x0 + c) / a.G;
+                    // keys of the block that the row sees, those of this lane's first (a row that does not exist sees none)
+                    const int seen = !decltype(masked)::value ? 0 : x0 + c < here ? sq.n + (r0 + x0 + c) / a.G + 1 - u * kBlk - 4 * g : -kBlk;
                     Frag qf[KS];
 #pragma unroll
                     for (int s = 0; s < KS; ++s)
@@ -1113,8 +1119,7 @@ __global__ __launch_bounds__(256, 2) void chunk_score_kernel(ChunkArgs a, int ro
                         for (int j = 0; j < 4; ++j) {
                             const float p = exp2_fast(fmaf(y[j], ks, -ml.x));
                             if constexpr (decltype(masked)::value) {
-                                const bool seen = u * kBlk + 16 * x + 4 * g + j <= pos && x0 + c < here;      // (a row that does not exist sees nothing)
-                                sum[x][j] += seen ? p * ml.y : 0.f;
+                                sum[x][j] += 16 * x + j < seen ? p * ml.y : 0.f;
                             } else {
                                 sum[x][j] = fmaf(p, ml.y, sum[x][j]);
                             }
@@ -1122,11 +1127,13 @@ __global__ __launch_bounds__(256, 2) void chunk_score_kernel(ChunkArgs a, int ro
                         if (x & 1) __builtin_amdgcn_sched_barrier(0);       // (else all products are kept at once)
                     }
                 };
+                int x0 = 0;
+                if (u * kBlk + kBlk - 1 <= sq.n + r0 / a.G) {       // every row sees the whole block
 #pragma unroll 1
-                for (int x0 = 0; x0 < here; x0 += 16) {
-                    if (x0 + 16 <= here && u * kBlk + kBlk - 1 <= sq.n + (r0 + x0) / a.G) add(x0, std::false_type{});
-                    else add(x0, std::true_type{});
+                    for (; x0 + 16 <= here; x0 += 16) add(x0, std::false_type{});
                 }
+#pragma unroll 1
+                for (; x0 < here; x0 += 16) add(x0, std::true_type{});
             }
             r0 += fit;
             if (r0 >= rows) break;
@@ -1154,14 +1161,24 @@ __global__ __launch_bounds__(256, 2) void chunk_score_kernel(ChunkArgs a, int ro
 }
 
 // How a call is cut: rows of a tile, blocks of a piece, pieces; waves of a workgroup where rows are few (else 0), and rows of a strip whose logits fit in LDS.
+// No more workgroups than compute units: a second one would wait for the first, with products of its own to begin and to join (33 tokens over 131072 rows:
+// 178 us with 512 of them, 158 with 256; 64 over 30000: 91 and 68).
 struct ChunkCut { int rows, piece, pieces, few, stage; };
 constexpr int kMostRowsOfTile = 32 * kChunkWaves, kFewRows = 32;
-constexpr int kWanted = 512;            // workgroups that a cut aims at: two for a compute unit
+constexpr int kWanted = 256;            // workgroups that a cut aims at: one has a compute unit's LDS to itself
 constexpr int kLeastPiece = 4;
 constexpr int kWholeStrips = 192, kShortUnits = 20, kManyStrips = 256, kFewWgs = 768, kMostPiece = 4 * kWave - 2;
 
+// Room for as many parts as a launch of these or any smaller sizes may leave.  Tiles hold all rows, so kWanted / tiles pieces are no more than kWanted
+// tiles of parts (with few rows: than kFewWgs of them, or one for every kMostPiece blocks); nor are there more than
+// one for every kLeastPiece blocks.  (A batch with many more rows than its sequences have is cut into fewer pieces instead.)
+inline int64_t chunk_parts(int64_t rows, int64_t units) {
+    return std::min((int64_t)kWanted * kMostRowsOfTile + rows * (1 + (units + kMostPiece - 1) / kMostPiece), rows * ((units + kLeastPiece - 1) / kLeastPiece));
+}
+
+// most_pieces: that there is room for
 template <int D>
-inline ChunkCut few_cut(int64_t strips, int cols, int max_len, bool scored) {
+inline ChunkCut few_cut(int64_t strips, int cols, int max_len, bool scored, int64_t most_pieces) {
     constexpr size_t kLds = 160 << 10;
     const int64_t units = max_len / kBlk + 1;
     const int waves = strips > kManyStrips ? 4 : cols <= 16 ? 12 : 8;
@@ -1169,7 +1186,8 @@ inline ChunkCut few_cut(int64_t strips, int cols, int max_len, bool scored) {
         const bool staged = scored && few_lds<D>(waves, cols, units * kBlk) <= kLds;
         return ChunkCut{cols, (int)units, 1, waves, staged ? (int)units * kBlk : 0};
     }
-    const int64_t piece = std::max<int64_t>(kLeastPiece, std::min<int64_t>((units * strips + kFewWgs - 1) / kFewWgs, kMostPiece));
+    const int64_t want = std::max<int64_t>(kLeastPiece, std::min<int64_t>((units * strips + kFewWgs - 1) / kFewWgs, kMostPiece));
+    const int64_t piece = std::max(want, (units + most_pieces - 1) / most_pieces);
     return ChunkCut{cols, (int)piece, (int)((units + piece - 1) / piece), 4, 0};
 }
 
@@ -1183,33 +1201,30 @@ inline int tile_rows(int64_t most) {
     const int64_t tiles = (most + kMostRowsOfTile - 1) / kMostRowsOfTile;
     return tiles == 0 ? 16 : (int)((most + 16 * tiles - 1) / (16 * tiles) * 16);
 }
+// (total and max_new above zero)
 inline ChunkCut chunk_cut(const st3_gqa_shape* s, int total, int max_new, int max_len, bool scored) {
     const int64_t most = (int64_t)max_new * (s->heads / s->kv_heads), strips = (int64_t)s->batch * s->kv_heads;
-    if (most <= kFewRows && most > 0) return s->head_dim == 128 ? few_cut<128>(strips, (int)most, max_len, scored) : few_cut<64>(strips, (int)most, max_len, scored);
+    const int64_t units = max_len / kBlk + 1, most_pieces = chunk_parts((int64_t)total * s->heads, units) / ((int64_t)total * s->heads);
+    if (most <= kFewRows) return s->head_dim == 128 ? few_cut<128>(strips, (int)most, max_len, scored, most_pieces) : few_cut<64>(strips, (int)most, max_len, scored, most_pieces);
     const int rows = tile_rows(most);
-    const int64_t tiles = chunk_tiles(s, total, max_new, rows) * s->kv_heads, units = max_len / kBlk + 1;
-    if (2 * tiles >= kWanted || tiles == 0) return ChunkCut{rows, (int)units, 1, 0, 0};
-    const int64_t pieces = std::min((kWanted + tiles - 1) / tiles, (units + kLeastPiece - 1) / kLeastPiece);
+    const int64_t tiles = chunk_tiles(s, total, max_new, rows) * s->kv_heads;
+    if (2 * tiles >= kWanted) return ChunkCut{rows, (int)units, 1, 0, 0};
+    const int64_t pieces = std::min({kWanted / tiles, (units + kLeastPiece - 1) / kLeastPiece, most_pieces});
     const int64_t piece = (units + pieces - 1) / pieces;
     return ChunkCut{rows, (int)piece, (int)((units + piece - 1) / piece), 0, 0};
 }
 
 // Blocks that a wave of the scores' launch takes one behind the other.
-constexpr int kScoreWgs = 2048, kMostRounds = 16;
+constexpr int kScoreWgs = 1024, kMostRounds = 16;
 inline int score_rounds(int64_t units, int Hk, int B) {
     const int64_t want = units * Hk * B / (4 * kScoreWgs);
     return (int)std::max<int64_t>(1, std::min<int64_t>(want, kMostRounds));
 }
 
-struct ChunkWs { size_t ml, part_o, part_ml, total; int64_t parts; };
-// Room for as many parts as a launch of these or any smaller sizes may leave.  Tiles hold all rows, so less than kWanted / tiles + 1 pieces are less
-// than kWanted tiles of parts and one more for each row (with few rows: than kFewWgs of them, or one for every kMostPiece blocks); nor are there more than
-// one for every kLeastPiece blocks.
+struct ChunkWs { size_t ml, part_o, part_ml, total; };
 inline ChunkWs chunk_ws(const st3_gqa_shape* s, int total, int max_len) {
-    const int64_t rows = (int64_t)total * s->heads, units = max_len / kBlk + 1;
-    const int64_t parts = std::min((int64_t)kWanted * kMostRowsOfTile + rows * (1 + (units + kMostPiece - 1) / kMostPiece), rows * ((units + kLeastPiece - 1) / kLeastPiece));
+    const int64_t rows = (int64_t)total * s->heads, parts = chunk_parts(rows, max_len / kBlk + 1);
     ChunkWs w{};
-    w.parts = parts;
     size_t off = 0;
     w.ml = off;      off = align_up(off + rows * sizeof(float2), 256);
     w.part_o = off;  off = align_up(off + parts * s->head_dim * sizeof(float), 256);
@@ -1268,7 +1283,6 @@ extern "C" st3_status st3_block_attend(const st3_gqa_shape* shape, const st3_row
     const int64_t grid = cut.few > 0 ? Hk : chunk_tiles(shape, total, max_new, cut.rows) * Hk;
     if (!grid_fits(grid, kChunkThreads, cut.pieces) || !grid_fits(((int64_t)total * H + 3) / 4, 256, 1) || (score && (max_len + 4 * kBlk - 1) / (4 * kBlk) > 65535)) return ST3_ERR_UNSUPPORTED;
     const ChunkWs wl = chunk_ws(shape, total, max_len);
-    if (cut.pieces > 1 && (int64_t)total * H * cut.pieces > wl.parts) return ST3_ERR_UNSUPPORTED;    // (never, by the rule above)
     if (workspace_bytes < st3_block_attend_workspace_bytes(shape, total, max_new, max_len)) return ST3_ERR_WORKSPACE_TOO_SMALL;
     char* ws = reinterpret_cast<char*>(workspace);
     ChunkArgs a{};
