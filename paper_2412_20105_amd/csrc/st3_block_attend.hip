@@ -1,13 +1,16 @@
 // Causal attention of several new tokens over a cache of 8-bit blocks, with grouped heads and accumulated weights.
 //
 // Rows.  The G query heads that share a key head are rows of one matrix, as for packed prompts: row x of a (sequence, key head) pair is head x % G of new
-// token x / G.  A workgroup's four waves have 16 QC rows each and walk the blocks of 64 keys together; 8-bit codes, loaded a block ahead into
-// registers, become bf16 on their way into LDS, once for all rows (codes have at most 8 significant bits: exact), and the scale of a block multiplies
-// the logits and the weights.
+// token x / G.  A workgroup's eight waves have up to 32 rows each (more would not fit the registers: 48 and 64 spill, and take 2 and 4 times as long) and
+// walk the blocks of 64 keys together; 8-bit codes, loaded two blocks ahead into registers, become bf16 on their way into LDS, once for all rows (codes have
+// at most 8 significant bits: exact), and the scale of a block multiplies the logits and the weights.  By waves of four the conversion costs twice as
+// much: 1138 us against 1005 for 2048 tokens over 30000 rows (32 heads, 8 key heads, d = 128).
 //   S^T = K Q^T    (A: lane (c, g) holds A[c][8g..8g+7], B: B[8g..8g+7][c], C: C[4g..4g+3][c]) product t of four: row 4g'+i of A is key 16 g' + 4 t + i, so
 //                  that lane (c, g) of C ends with keys 16 g .. 16 g + 15 of row c.
 //   O^T = V^T P^T  the lane's 16 keys are the contraction slots 8g..8g+7 of two steps: P^T is where S^T left it.
 // No value crosses lanes but the maximum.  Where row tiles are too few to fill the card, a strip's blocks are cut into pieces, and a second launch joins them.
+// What bounds it: the matrix units with many rows (2048 tokens over 30000 rows 895 us, 1180 TFLOP/s); with few, the chain from a block's codes through both
+// products to its barrier (1.3 us a block of 64 keys with 36 rows, 1.8 with 256), so that rows up to kFewRows go another way, below, bound by memory.
 #include <algorithm>
 #include <type_traits>
 
@@ -426,7 +429,7 @@ __device__ __forceinline__ void chunk_wave(const ChunkArgs& a, const Work& w, ui
     };
     // A step of a wave is a half on the matrix units (the values of one block and the logits of the next; beside them codes of the one behind go into
     // LDS) and one on the others (weights).  The two waves of a SIMD are half a step apart: while one keeps the matrix units busy, the other
-    // computes weights.
+    // computes weights (2048 tokens over 30000 rows: 1045 us in step, 958 so; with the codes' conversion between the products 895).
     const int mine = idle || p_last < u_begin * kBlk ? 0 : min(units, p_last / kBlk - u_begin + 1);     // steps in which this wave has rows that see something
     auto v_of = [&](int i) { return lds0 + (i & 3) * L::BYTES + v_lane; };
     auto k_of = [&](int i) { return lds0 + (i & 3) * L::BYTES + k_lane; };
@@ -955,7 +958,7 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Behind the pieces: a wave joins a row's parts, eight loads on their way (1952 rows of up to 32 parts 9.8 us, one load at a time 15.6).
+// Behind the pieces: a wave joins a row's parts, eight loads on their way (1952 rows of up to 16 parts: 9.8 us).
 // ---------------------------------------------------------------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a) {
@@ -1164,13 +1167,21 @@ __global__ __launch_bounds__(256, 3) void chunk_score_kernel(ChunkArgs a, int ro
 // No more workgroups than compute units: a second one would wait for the first, with products of its own to begin and to join (33 tokens over 131072 rows:
 // 178 us with 512 of them, 158 with 256; 64 over 30000: 91 and 68).
 struct ChunkCut { int rows, piece, pieces, few, stage; };
-constexpr int kMostRowsOfTile = 32 * kChunkWaves, kFewRows = 32;
+constexpr int kMostRowsOfTile = 32 * kChunkWaves;
 constexpr int kWanted = 256;            // workgroups that a cut aims at: one has a compute unit's LDS to itself
 constexpr int kLeastPiece = 4;
-constexpr int kWholeStrips = 192, kShortUnits = 20, kManyStrips = 256, kFewWgs = 768, kMostPiece = 4 * kWave - 2;
+// Few rows, up to kFewRows: every wave has them all (8 key heads, d = 128: 4 tokens of 32 sequences over 611 to 3136 rows 30 us, by tiles 52; 8 of one over
+// 30000 rows 22 and 37).
+//   whole strips, without a join, and with the weights added at once, where there are kWholeStrips of them or they have no more than kShortUnits blocks: 64
+//     sequences of 1000 to 3000 rows 50 us, in pieces 65; one of 744 rows 15.2 and 18.7; 16 sequences 35.0, in pieces 33.7.
+//     By 12 waves (8 with more than 16 rows), by 4 where there are more than kManyStrips: 32 sequences 30 us by 12 and 43 by 4, 64 sequences 51 and 50.
+//   pieces by 4 waves: of no more than kWanted / 4 strips one for each compute unit (one sequence of 30000 rows 22 us, three times as many pieces 39; eight
+//     of them 74 and 91), of more strips, whose lengths differ, three times as many (15 sequences of 1000 to 9000 rows 39 us, two pieces each 49).
+//     A wave's blocks are lanes of a register: no more than kMostPiece.
+constexpr int kFewRows = 32, kWholeStrips = 192, kShortUnits = 20, kManyStrips = 256, kMostPiece = 4 * kWave - 2;
 
 // Room for as many parts as a launch of these or any smaller sizes may leave.  Tiles hold all rows, so kWanted / tiles pieces are no more than kWanted
-// tiles of parts (with few rows: than kFewWgs of them, or one for every kMostPiece blocks); nor are there more than
+// tiles of parts (with few rows: than three times as many of 32, or one for every kMostPiece blocks); nor are there more than
 // one for every kLeastPiece blocks.  (A batch with many more rows than its sequences have is cut into fewer pieces instead.)
 inline int64_t chunk_parts(int64_t rows, int64_t units) {
     return std::min((int64_t)kWanted * kMostRowsOfTile + rows * (1 + (units + kMostPiece - 1) / kMostPiece), rows * ((units + kLeastPiece - 1) / kLeastPiece));
@@ -1186,7 +1197,8 @@ inline ChunkCut few_cut(int64_t strips, int cols, int max_len, bool scored, int6
         const bool staged = scored && few_lds<D>(waves, cols, units * kBlk) <= kLds;
         return ChunkCut{cols, (int)units, 1, waves, staged ? (int)units * kBlk : 0};
     }
-    const int64_t want = std::max<int64_t>(kLeastPiece, std::min<int64_t>((units * strips + kFewWgs - 1) / kFewWgs, kMostPiece));
+    const int64_t even = strips <= kWanted / 4 ? (units + kWanted / strips - 1) / (kWanted / strips) : (units * strips + 3 * kWanted - 1) / (3 * kWanted);
+    const int64_t want = std::max<int64_t>(kLeastPiece, std::min<int64_t>(even, kMostPiece));
     const int64_t piece = std::max(want, (units + most_pieces - 1) / most_pieces);
     return ChunkCut{cols, (int)piece, (int)((units + piece - 1) / piece), 4, 0};
 }
