@@ -1226,8 +1226,10 @@ inline ChunkCut chunk_cut(const st3_gqa_shape* s, int total, int max_new, int ma
     return ChunkCut{rows, (int)piece, (int)((units + piece - 1) / piece), 0, 0};
 }
 
-// Blocks that a wave of the scores' launch takes one behind the other.
-constexpr int kScoreWgs = 1024, kMostRounds = 16;
+// Blocks that a wave of the scores' launch takes one behind the other: as many as leave three workgroups for each compute unit, which hold its registers
+// (9 to 33 tokens over 70000 to 131072 rows 274 us, with four 284, with two 286); their pages are lanes of a register (4 x 130000 rows 297 us, no more
+// than 16 blocks a wave 311).
+constexpr int kScoreWgs = 768, kMostRounds = kWave;
 inline int score_rounds(int64_t units, int Hk, int B) {
     const int64_t want = units * Hk * B / (4 * kScoreWgs);
     return (int)std::max<int64_t>(1, std::min<int64_t>(want, kMostRounds));

@@ -7,7 +7,7 @@ import torch
 
 import test_gpu_block_append as append
 import test_gpu_block_attend as attend
-from block_util import BLOCK, filled
+from block_util import BLOCK, DeviceCache, filled
 from gpu_util import DEV, rand_values
 from paper_2412_20105_amd import binding as st3
 
@@ -90,6 +90,41 @@ def test_strides_beyond_32_bits(new):
         assert torch.equal(getattr(caches[0], name), getattr(caches[1], name))
     for name in ("k_codes", "v_codes", "k_scale", "v_scale"):
         assert torch.equal(getattr(caches[0], name)[full], getattr(caches[1], name)[full])
+
+
+@pytest.mark.parametrize("new", [2, 20])
+def test_a_long_batch_is_its_sequences_alone(new):
+    """Waves that walk up to 64 blocks for the scores, and few: the same sums."""
+    rng, B, Hk, H, d = np.random.default_rng(11), 4, 8, 16, 128
+    old = [130000, 129990, 100000, 64]
+    blocks = (max(old) + new) // BLOCK + 1
+    dev = DeviceCache(rng, B, Hk, d, "int8", blocks, pages=B * blocks)
+    for x in (dev.k_scale, dev.v_scale):
+        x.copy_(torch.rand(x.shape, device=DEV) * 0.02 + 0.001)
+    for x in (dev.k_tail, dev.v_tail):
+        x.copy_(torch.randn(x.shape, device=DEV))
+    dev.set_len(old)
+    q = torch.from_numpy(rand_values(rng, (B * new, H, d), "bf16", 1.0)).to(DEV).bfloat16()
+    top = max(old) + new
+
+    def go(tokens, c, batch):
+        shape, out, score = st3.gqa_shape(batch, H, Hk, d), torch.empty_like(tokens), torch.zeros((batch, Hk, top), device=DEV)
+        cu = torch.arange(0, batch * new + 1, new, dtype=torch.int32, device=DEV)
+        ws = torch.empty(st3.st3_block_attend_workspace_bytes(shape, batch * new, new, top), dtype=torch.uint8, device=DEV)
+        st3.st3_block_attend(shape, tokens, cu, new, c, top, out, new, score, ws)
+        torch.cuda.synchronize()
+        return out.double(), score.double()
+
+    out, score = go(q, dev.c, B)
+    v_most = float(dev.v_scale.max()) * 128 + float(dev.v_tail.abs().max())
+    for b in range(B):
+        c = st3.block_cache(dev.k_codes, dev.v_codes, dev.k_scale, dev.v_scale, dev.k_tail[b:b + 1], dev.v_tail[b:b + 1], dev.table[b:b + 1], dev.len[b:b + 1])
+        o, s = go(q[b * new:(b + 1) * new], c, 1)
+        # either sum of up to `top` weights in float32, in another order
+        assert bool(((score[b] - s[0]).abs() <= 2 * (top + 32) * 2.0 ** -24 * s[0] + 1e-30).all())
+        assert float((score[b, :, :old[b] + new].sum(-1) / (new * H // Hk) - 1).abs().max()) <= 2 * (top + 32) * 2.0 ** -24
+        assert not score[b, :, old[b] + new:].any()
+        assert bool(((out[b * new:(b + 1) * new] - o).abs() <= 2 * attend.HALF * 1.01 * (o.abs() + v_most)).all())
 
 
 def test_two_at_once_and_two_graphs():
