@@ -586,7 +586,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void block_chunk_kernel(ChunkArgs
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Few rows (16 QC of them at most: a token or a few drafted ones): every wave has them all, and takes the blocks in turn, each by itself, as the
+// Few rows (a token or a few drafted ones; a workgroup has 16 QC of them at most): every wave has them all, and takes the blocks in turn, each by itself, as the
 // attention of single tokens does: K straight to its own LDS, V straight into registers, 16 codes of a lane's operand at once, the rows in 16 bits by the
 // first waves, 32 keys at a time.  The waves' parts are joined in LDS.  WHOLE: a workgroup takes a whole strip; with room for the logits in LDS (stage:
 // rows of a strip there; 0: none) it adds the weights too.
@@ -606,11 +606,11 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
     constexpr int KS = D / 32, DT = D / 16, KH = D / 64, kThr = WAVES * 64, OS = D + 4, kKeys = WAVES * kBlk * D / 4;
     extern __shared__ __attribute__((aligned(16))) float few[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-    const int kh = blockIdx.x, ch = blockIdx.y, b = blockIdx.z, cols = a.tile;
+    const int kh = blockIdx.x % a.Hk, ch = blockIdx.y, b = blockIdx.z, cols = a.tile, r0 = blockIdx.x / a.Hk * cols;
     const Turn got = turn_of(a, b);
     const Turn sq{__builtin_amdgcn_readfirstlane(got.start), __builtin_amdgcn_readfirstlane(got.m), __builtin_amdgcn_readfirstlane(got.n)};
-    if (sq.m <= 0) return;
-    const int rows = sq.m * a.G, keys = sq.rows(), blocks = keys / kBlk, units = (keys + kBlk - 1) / kBlk;
+    if (sq.m * a.G <= r0) return;
+    const int rows = min(sq.m * a.G - r0, cols), keys = sq.rows(), blocks = keys / kBlk, units = (keys + kBlk - 1) / kBlk;
     const int u_begin = WHOLE ? 0 : ch * a.piece, u_end = WHOLE ? units : min(units, u_begin + a.piece);
     if (!WHOLE && ch > 0 && u_begin >= units) return;
     float* sm_o = few;
@@ -657,7 +657,7 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
     st.init();
 #pragma unroll
     for (int qc = 0; qc < QC; ++qc) {
-        const int r = min(16 * qc + c, rows - 1), t = r / a.G;
+        const int r = r0 + min(16 * qc + c, rows - 1), t = r / a.G;
         st.pos[qc] = sq.sees(t);
         const uint16_t* row = a.q + (int64_t)(sq.start + t) * a.q_st + (int64_t)(kh * a.G + r - t * a.G) * a.q_sh;
 #pragma unroll
@@ -907,7 +907,7 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
     }
     __syncthreads();
     for (int e = tid; e < rows * (D / 2); e += kThr) {      // two columns of a row
-        const int col = e / (D / 2), dim = 2 * (e % (D / 2)), t = col / a.G, h = kh * a.G + col - t * a.G;
+        const int col = e / (D / 2), dim = 2 * (e % (D / 2)), t = (r0 + col) / a.G, h = kh * a.G + r0 + col - t * a.G;
         float top = sm_m[col];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sm_m[w * cols + col]);
@@ -1166,41 +1166,45 @@ __global__ __launch_bounds__(256, 3) void chunk_score_kernel(ChunkArgs a, int ro
 // How a call is cut: rows of a tile, blocks of a piece, pieces; waves of a workgroup where rows are few (else 0), and rows of a strip whose logits fit in LDS.
 // No more workgroups than compute units: a second one would wait for the first, with products of its own to begin and to join (33 tokens over 131072 rows:
 // 178 us with 512 of them, 158 with 256; 64 over 30000: 91 and 68).
-struct ChunkCut { int rows, piece, pieces, few, stage; };
+struct ChunkCut { int rows, piece, pieces, few, stage, groups; };
 constexpr int kMostRowsOfTile = 32 * kChunkWaves;
 constexpr int kWanted = 256;            // workgroups that a cut aims at: one has a compute unit's LDS to itself
 constexpr int kLeastPiece = 4;
-// Few rows, up to kFewRows: every wave has them all (8 key heads, d = 128: 4 tokens of 32 sequences over 611 to 3136 rows 30 us, by tiles 52; 8 of one over
-// 30000 rows 22 and 37).
-//   whole strips, without a join, and with the weights added at once, where there are kWholeStrips of them or they have no more than kShortUnits blocks: 64
-//     sequences of 1000 to 3000 rows 50 us, in pieces 65; one of 744 rows 15.2 and 18.7; 16 sequences 35.0, in pieces 33.7.
+// Few rows, up to kFewRows: every wave has those of its group, kFewGroup at most (8 key heads, d = 128: 4 tokens of 32 sequences over 611 to 3136 rows 30 us,
+// by tiles 52; 8 of one over 30000 rows 22 and 37).  Two groups read a strip twice, the second time from L2: 16 tokens (64 rows) of 8 sequences over 20000 to
+// 30000 rows 130 us, by tiles 159; three would not pay (24 tokens of them 199, by tiles 155).
+//   whole strips, without a join, and with one group's weights added at once, where there are kWholeStrips of them or they have no more than kShortUnits
+//     blocks: 64 sequences of 1000 to 3000 rows 50 us, in pieces 65; one of 744 rows 15.2 and 18.7; 16 sequences 35.0, in pieces 33.7.
 //     By 12 waves (8 with more than 16 rows), by 4 where there are more than kManyStrips: 32 sequences 30 us by 12 and 43 by 4, 64 sequences 51 and 50.
 //   pieces by 4 waves: of no more than kWanted / 4 strips one for each compute unit (one sequence of 30000 rows 22 us, three times as many pieces 39; eight
-//     of them 74 and 91), of more strips, whose lengths differ, three times as many (15 sequences of 1000 to 9000 rows 39 us, two pieces each 49).
-//     A wave's blocks are lanes of a register: no more than kMostPiece.
-constexpr int kFewRows = 32, kWholeStrips = 192, kShortUnits = 20, kManyStrips = 256, kMostPiece = 4 * kWave - 2;
+//     of them 74 and 91), of more strips, whose lengths differ, three times as many (15 sequences of 1000 to 9000 rows 37 us, two pieces each 49).
+//     A wave's blocks are lanes of a register, no more than kMostPiece; longer strips in twice, three times as many pieces (4 tokens of 8 sequences over
+//     70000 to 131072 rows 276 us, in as few as hold them 302).
+constexpr int kFewGroup = 32, kFewRows = 64, kWholeStrips = 192, kShortUnits = 20, kManyStrips = 256, kMostPiece = 4 * kWave - 2;
 
 // Room for as many parts as a launch of these or any smaller sizes may leave.  Tiles hold all rows, so kWanted / tiles pieces are no more than kWanted
-// tiles of parts (with few rows: than three times as many of 32, or one for every kMostPiece blocks); nor are there more than
-// one for every kLeastPiece blocks.  (A batch with many more rows than its sequences have is cut into fewer pieces instead.)
+// tiles of parts (with few rows: than three times as many of kFewGroup, or a few for every kMostPiece blocks); nor are there more than
+// one for every kLeastPiece blocks.  (Where that is not enough, as for a batch with many
+// more rows than its sequences have, there are fewer pieces.)
 inline int64_t chunk_parts(int64_t rows, int64_t units) {
     return std::min((int64_t)kWanted * kMostRowsOfTile + rows * (1 + (units + kMostPiece - 1) / kMostPiece), rows * ((units + kLeastPiece - 1) / kLeastPiece));
 }
 
 // most_pieces: that there is room for
 template <int D>
-inline ChunkCut few_cut(int64_t strips, int cols, int max_len, bool scored, int64_t most_pieces) {
+inline ChunkCut few_cut(int64_t strips, int most, int max_len, bool scored, int64_t most_pieces) {
     constexpr size_t kLds = 160 << 10;
     const int64_t units = max_len / kBlk + 1;
+    const int groups = (most + kFewGroup - 1) / kFewGroup, cols = (most + groups - 1) / groups;
+    strips *= groups;                       // (workgroups of a whole launch)
     const int waves = strips > kManyStrips ? 4 : cols <= 16 ? 12 : 8;
     if (units + 2 <= waves * kWave && (strips >= kWholeStrips || units <= kShortUnits)) {
-        const bool staged = scored && few_lds<D>(waves, cols, units * kBlk) <= kLds;
-        return ChunkCut{cols, (int)units, 1, waves, staged ? (int)units * kBlk : 0};
+        const bool staged = scored && groups == 1 && few_lds<D>(waves, cols, units * kBlk) <= kLds;
+        return ChunkCut{cols, (int)units, 1, waves, staged ? (int)units * kBlk : 0, groups};
     }
-    const int64_t even = strips <= kWanted / 4 ? (units + kWanted / strips - 1) / (kWanted / strips) : (units * strips + 3 * kWanted - 1) / (3 * kWanted);
-    const int64_t want = std::max<int64_t>(kLeastPiece, std::min<int64_t>(even, kMostPiece));
-    const int64_t piece = std::max(want, (units + most_pieces - 1) / most_pieces);
-    return ChunkCut{cols, (int)piece, (int)((units + piece - 1) / piece), 4, 0};
+    const int64_t even = strips <= kWanted / 4 ? kWanted / strips : (3 * kWanted + strips - 1) / strips, pieces = even * ((units + even * kMostPiece - 1) / (even * kMostPiece));
+    const int64_t piece = std::max((int64_t)kLeastPiece, (units + std::min(pieces, most_pieces) - 1) / std::min(pieces, most_pieces));
+    return ChunkCut{cols, (int)piece, (int)((units + piece - 1) / piece), 4, 0, groups};
 }
 
 // No more row tiles than this, whatever the lengths are: each sequence has one that is not full.
@@ -1220,10 +1224,10 @@ inline ChunkCut chunk_cut(const st3_gqa_shape* s, int total, int max_new, int ma
     if (most <= kFewRows) return s->head_dim == 128 ? few_cut<128>(strips, (int)most, max_len, scored, most_pieces) : few_cut<64>(strips, (int)most, max_len, scored, most_pieces);
     const int rows = tile_rows(most);
     const int64_t tiles = chunk_tiles(s, total, max_new, rows) * s->kv_heads;
-    if (2 * tiles >= kWanted) return ChunkCut{rows, (int)units, 1, 0, 0};
+    if (2 * tiles >= kWanted) return ChunkCut{rows, (int)units, 1, 0, 0, 0};
     const int64_t pieces = std::min({kWanted / tiles, (units + kLeastPiece - 1) / kLeastPiece, most_pieces});
     const int64_t piece = (units + pieces - 1) / pieces;
-    return ChunkCut{rows, (int)piece, (int)((units + piece - 1) / piece), 0, 0};
+    return ChunkCut{rows, (int)piece, (int)((units + piece - 1) / piece), 0, 0, 0};
 }
 
 // Blocks that a wave of the scores' launch takes one behind the other: as many as leave three workgroups for each compute unit, which hold its registers
@@ -1250,7 +1254,7 @@ inline ChunkWs chunk_ws(const st3_gqa_shape* s, int total, int max_len) {
 template <int D, int CODE, int QC>
 void launch_few(const ChunkArgs& a, const ChunkCut& cut, hipStream_t st) {
     const size_t lds = few_lds<D>(cut.few, a.tile, cut.stage);
-    const dim3 grid(a.Hk, a.pieces, a.B);
+    const dim3 grid(a.Hk * cut.groups, a.pieces, a.B);
     constexpr int kMost = QC == 1 ? 12 : 8;
     if (a.pieces > 1) chunk_few_kernel<D, CODE, QC, 4, false><<<grid, 256, lds, st>>>(a, 0);
     else if (cut.few == kMost) chunk_few_kernel<D, CODE, QC, kMost, true><<<grid, 64 * kMost, lds, st>>>(a, cut.stage);
@@ -1294,7 +1298,7 @@ extern "C" st3_status st3_block_attend(const st3_gqa_shape* shape, const st3_row
     if (score && (window < 1 || score_stride_h < max_len || (B > 1 && score_stride_b < max_len))) return ST3_ERR_INVALID_ARG;
     if (!workspace || !aligned16(workspace)) return ST3_ERR_INVALID_ARG;
     const ChunkCut cut = chunk_cut(shape, total, max_new, max_len, score != nullptr);
-    const int64_t grid = cut.few > 0 ? Hk : chunk_tiles(shape, total, max_new, cut.rows) * Hk;
+    const int64_t grid = cut.few > 0 ? Hk * cut.groups : chunk_tiles(shape, total, max_new, cut.rows) * Hk;
     if (!grid_fits(grid, kChunkThreads, cut.pieces) || !grid_fits(((int64_t)total * H + 3) / 4, 256, 1) || (score && (max_len + 4 * kBlk - 1) / (4 * kBlk) > 65535)) return ST3_ERR_UNSUPPORTED;
     const ChunkWs wl = chunk_ws(shape, total, max_len);
     if (workspace_bytes < st3_block_attend_workspace_bytes(shape, total, max_new, max_len)) return ST3_ERR_WORKSPACE_TOO_SMALL;

@@ -32,10 +32,11 @@ def test_parts_of_a_large_batch():
 
 
 @pytest.mark.parametrize("old,new,B,H,Hk", [(1251, 8, 1, 8, 2), (1250, 3, 2, 4, 4), (1290, 3, 2, 4, 4), (600, 1, 65, 8, 4), (600, 5, 60, 16, 4), (100, 32, 2, 2, 2),
-                                            (100, 33, 2, 2, 2), (5000, 16, 5, 4, 2), (2000, 4, 200, 2, 1), (17000, 1, 200, 1, 1)])
+                                            (100, 33, 2, 2, 2), (5000, 16, 5, 4, 2), (1251, 9, 1, 8, 2),
+                                            (600, 9, 3, 7, 1), (5000, 16, 2, 8, 2), (17000, 9, 2, 28, 4), (700, 13, 70, 15, 3), (1000, 65, 2, 3, 3), (2000, 4, 200, 2, 1), (17000, 1, 200, 1, 1)])
 @pytest.mark.parametrize("window", [0, 2, 50])
 def test_either_side_of_every_cut(old, new, B, H, Hk, window):
-    """Few rows: by 4, 8 and 12 waves, whole and in pieces, with their logits in LDS and formed again."""
+    """Few rows: by 4, 8 and 12 waves, whole and in pieces, with their logits in LDS and formed again, in one group and in two (which may part a token's heads)."""
     rng = np.random.default_rng(old + new + B)
     olds = [old] * B
     for b in range(1, B):
@@ -92,7 +93,7 @@ def test_strides_beyond_32_bits(new):
         assert torch.equal(getattr(caches[0], name)[full], getattr(caches[1], name)[full])
 
 
-@pytest.mark.parametrize("new", [2, 20])
+@pytest.mark.parametrize("new", [2, 20, 40])
 def test_a_long_batch_is_its_sequences_alone(new):
     """Waves that walk up to 64 blocks for the scores, and few: the same sums."""
     rng, B, Hk, H, d = np.random.default_rng(11), 4, 8, 16, 128
