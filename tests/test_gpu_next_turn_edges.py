@@ -190,3 +190,17 @@ def test_several_pieces_give_what_one_call_gives():
     assert bool(((one - two).abs() <= 2 * attend.HALF * 1.01 * (one.abs() + v_most)).all())
     # sums of 4 x 4 weights of at most 1 in float32, each within a slack far below 2^-16
     assert float((results[0][1] - results[1][1]).abs().max()) <= 2 * 16 * 2.0 ** -16
+
+
+@pytest.mark.parametrize("pairs", [8, 24, 40, 64])
+@pytest.mark.parametrize("more", [0, 1, 13])
+def test_a_large_table_is_that_of_its_halves(pairs, more):
+    rng = np.random.default_rng(12)
+    T = 2 ** 20 // pairs + more                     # (from 2^20 pairs on threads make several tokens)
+    positions = torch.from_numpy(rng.integers(-1000, 200000, (2, T)).astype(np.int32)).to(DEV)
+    f, axis = torch.rand(pairs, device=DEV), rng.integers(0, 2, pairs).tolist()
+    whole, halves = (torch.full((T + 70, pairs, 2), 7.0, device=DEV) for _ in range(2))
+    st3.st3_rotary_table(positions, f, axis, whole[:T])
+    for a, b in ((0, T // 2), (T // 2, T)):
+        st3.st3_rotary_table(positions[:, a:b], f, axis, halves[a:b])
+    assert torch.equal(whole, halves) and bool((whole[T:] == 7.0).all()) and not bool((whole[:T] == 7.0).any())
