@@ -626,7 +626,10 @@ def st3_rotary_table(positions, inv_freq, axis, table, stream=None) -> None:
     size, steps = positions.shape, positions.stride()
     if not 1 <= len(size) <= 2:
         raise ValueError(f"positions: [axes, T] or [T] expected, {tuple(size)} given")
-    axes, total, apart = (1, size[0], size[0]) if len(size) == 1 else (size[0], size[1], max(steps[0], size[1]))
+    axes, total = (1, size[0]) if len(size) == 1 else size
+    apart = steps[0] if axes > 1 else total
+    if axes > 1 and 0 != apart < total:
+        raise ValueError("the axes' positions lie one behind the other, or are the same")
     rows, pairs, stride = _table(table)
     if rows != total or inv_freq.shape != (pairs,) or inv_freq.stride(0) != 1:
         raise ValueError(f"{total} positions and {tuple(inv_freq.shape)} frequencies, side by side, for a table of {tuple(table.shape)}")

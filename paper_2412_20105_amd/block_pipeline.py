@@ -76,9 +76,14 @@ class BlockGeneration:
         self._prompt_ws = torch.empty((0,), dtype=torch.uint8, device=device)
         self._out = torch.empty((layers, batch, heads, head_dim), **half)
         self.lens: List[int] = [-1] * batch     # host copies; negative: an empty place
-        self.new: Optional[List[int]] = None    # rows that the turn adds, while one is open
         self._turn_ws = torch.empty((0,), dtype=torch.uint8, device=device)
         self.evictions = 0
+
+    new: Optional[List[int]] = None             # rows that the turn adds, while one is open
+
+    def _no_turn(self) -> None:
+        if self.new is not None:
+            raise ValueError("a turn is open: finish_turn() comes first")
 
     # ------------------------------------------------------------------------------------
     def begin(self, prompt_lens: Sequence[int]) -> None:
@@ -106,6 +111,7 @@ class BlockGeneration:
     def prefill_layer(self, l: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Packed prompts (slices of a fused projection's output are fine) of layer l: attended, and stored.  As many rows
         as the lengths that begin() was told have together."""
+        self._no_turn()
         if not q.shape[0] == k.shape[0] == v.shape[0] == self.total:
             raise ValueError(f"{q.shape[0]}, {k.shape[0]} and {v.shape[0]} rows of q, k and v: {self.total} expected, the lengths' sum")
         if out is None:
@@ -118,25 +124,25 @@ class BlockGeneration:
 
     def begin_step(self) -> None:
         """Makes room where a sequence has none left for the step's row."""
-        if self.new is not None:
-            raise ValueError("a turn is open: finish_turn() comes first")
+        self._no_turn()
         if self.longest >= self.capacity:
             self.evict()
 
     def decode_layer(self, l: int, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor) -> torch.Tensor:
         """The step's token of every sequence in layer l; empty places get 0.  The result is valid until this layer's next step."""
+        self._no_turn()
         st3.st3_block_decode(self.shape, q, k_new, v_new, self._sets[self._of[l]], self.longest, self._out[l], self.score[l], self._ws)
         return self._out[l]
 
     def finish_step(self) -> None:
+        self._no_turn()
         self.len.add_(self.live)
         self.lens = [n + 1 if n >= 0 else n for n in self.lens]
 
     # ------------------------------------------------------------------------------------
     def begin_turn(self, new_lens: Sequence[int]) -> None:
         """A turn of so many new tokens of each sequence (an empty place has none); makes room where a sequence has too little."""
-        if self.new is not None:
-            raise ValueError("a turn is open: finish_turn() comes first")
+        self._no_turn()
         new = [int(m) for m in new_lens]
         if len(new) != self.B or min(new) < 0 or any(m and n < 0 for n, m in zip(self.lens, new)):
             raise ValueError(f"{self.B} numbers of new tokens, none for an empty place, expected; {new} given")
@@ -189,6 +195,7 @@ class BlockGeneration:
 
     def evict(self) -> None:
         """Every layer keeps `budget` rows of each longer sequence; `kept[l]` names them by the rows they had."""
+        self._no_turn()
         if self.longest == 0:
             return
         for l in range(self.L):

@@ -153,7 +153,7 @@ extern "C" st3_status st3_rotary_table(int32_t axes, int32_t pairs, const uint8_
     }
     if (!inv_freq || (reinterpret_cast<uintptr_t>(inv_freq) & 7) != 0) return ST3_ERR_INVALID_ARG;
     if (total == 0) return ST3_OK;          // (an empty tensor may have no address)
-    if (!positions || !table || !aligned16(table) || (axes > 1 && position_stride < total)) return ST3_ERR_INVALID_ARG;
+    if (!positions || !table || !aligned16(table) || (axes > 1 && position_stride != 0 && position_stride < total)) return ST3_ERR_INVALID_ARG;
     if (table_stride % 4 != 0 || table_stride < 2 * pairs) return ST3_ERR_INVALID_ARG;
     a.inv_freq = inv_freq; a.positions = positions; a.p_stride = position_stride; a.table = table; a.t_stride = table_stride;
     a.total = total; a.pairs = pairs; a.per = pairs / 2; a.rows = kThreads / a.per;

@@ -204,3 +204,12 @@ def test_a_large_table_is_that_of_its_halves(pairs, more):
     for a, b in ((0, T // 2), (T // 2, T)):
         st3.st3_rotary_table(positions[:, a:b], f, axis, halves[a:b])
     assert torch.equal(whole, halves) and bool((whole[T:] == 7.0).all()) and not bool((whole[:T] == 7.0).any())
+
+
+def test_components_that_are_all_the_same():
+    """One row of positions stretched over the axes, without a copy: the table of one axis."""
+    pos, f = torch.arange(50, 117, dtype=torch.int32, device=DEV), torch.rand(32, device=DEV)
+    one, three = (torch.zeros((67, 32, 2), device=DEV) for _ in range(2))
+    st3.st3_rotary_table(pos, f, None, one)
+    st3.st3_rotary_table(pos.expand(3, 67), f, [c % 3 for c in range(32)], three)
+    assert torch.equal(one, three)

@@ -40,7 +40,7 @@ def table(axes=1, pairs=64, axis=None, freq=FAKE, pos=FAKE, ps=10, total=10, out
     (dict(axes=0), INVALID), (dict(axes=5), UNSUPPORTED), (dict(pairs=0), INVALID), (dict(pairs=12), UNSUPPORTED), (dict(pairs=72, st=144), UNSUPPORTED),
     (dict(axis=bytes([0] * 63 + [1])), INVALID), (dict(axes=2, axis=bytes([2] + [0] * 63)), INVALID), (dict(freq=None), INVALID), (dict(freq=FAKE + 4), INVALID),
     (dict(pos=None), INVALID), (dict(axes=2, ps=9), INVALID), (dict(total=-1), INVALID), (dict(out=None), INVALID), (dict(out=FAKE + 8), INVALID),
-    (dict(st=127), INVALID), (dict(st=126), INVALID), (dict(st=130), INVALID), (dict(total=0, pos=None, out=None), OK)], ids=str)
+    (dict(axes=2, ps=-10), INVALID), (dict(st=127), INVALID), (dict(st=126), INVALID), (dict(st=130), INVALID), (dict(total=0, pos=None, out=None), OK)], ids=str)
 def test_table_refuses(bad, want):
     assert table(**bad) == want
 
@@ -216,3 +216,23 @@ def test_turns_of_a_generation():
     gen.lens[2], gen.live[2], gen.len[2] = -1, 0, -1            # retired before the turn's end
     gen.finish_turn()
     assert gen.lens == [129, -1, -1] and gen.len.tolist() == gen.lens
+
+
+def test_nothing_else_while_a_turn_is_open():
+    gen = a_generation([20, -1, 30])
+    del gen.evict
+    gen.begin_turn([5, 0, 9])
+    rows = torch.zeros(14, 1, 1)
+    for call in (gen.begin_step, gen.finish_step, gen.evict, lambda: gen.begin_turn([0, 0, 0]), lambda: gen.prefill_layer(0, rows, rows, rows),
+                 lambda: gen.decode_layer(0, rows, rows, rows)):
+        with pytest.raises(ValueError):
+            call()
+    assert gen.lens == [20, -1, 30] and gen.len.tolist() == gen.lens
+    gen.finish_turn()
+    assert gen.lens == [25, -1, 39]
+
+
+def test_positions_that_overlap_are_refused():
+    for positions in (torch.zeros(12, dtype=torch.int32).as_strided((3, 8), (2, 1)), torch.zeros(30, dtype=torch.int32).as_strided((2, 8), (1, 2))):
+        with pytest.raises(ValueError, match="axes"):
+            st3.st3_rotary_table(positions, torch.zeros(8), None, torch.zeros(8, 8, 2))
