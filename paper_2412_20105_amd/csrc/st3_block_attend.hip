@@ -1299,7 +1299,7 @@ extern "C" st3_status st3_block_attend(const st3_gqa_shape* shape, const st3_row
     if (!workspace || !aligned16(workspace)) return ST3_ERR_INVALID_ARG;
     const ChunkCut cut = chunk_cut(shape, total, max_new, max_len, score != nullptr);
     const int64_t grid = cut.few > 0 ? Hk * cut.groups : chunk_tiles(shape, total, max_new, cut.rows) * Hk;
-    if (!grid_fits(grid, kChunkThreads, cut.pieces) || !grid_fits(((int64_t)total * H + 3) / 4, 256, 1) || (score && (max_len + 4 * kBlk - 1) / (4 * kBlk) > 65535)) return ST3_ERR_UNSUPPORTED;
+    if (!grid_fits(grid, kChunkThreads, cut.pieces) || (cut.pieces > 1 && !grid_fits(((int64_t)total * H + 3) / 4, 256, 1)) || (score && (max_len + 4 * kBlk - 1) / (4 * kBlk) > 65535)) return ST3_ERR_UNSUPPORTED;
     const ChunkWs wl = chunk_ws(shape, total, max_len);
     if (workspace_bytes < st3_block_attend_workspace_bytes(shape, total, max_new, max_len)) return ST3_ERR_WORKSPACE_TOO_SMALL;
     char* ws = reinterpret_cast<char*>(workspace);

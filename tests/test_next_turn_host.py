@@ -236,3 +236,24 @@ def test_positions_that_overlap_are_refused():
     for positions in (torch.zeros(12, dtype=torch.int32).as_strided((3, 8), (2, 1)), torch.zeros(30, dtype=torch.int32).as_strided((2, 8), (1, 2))):
         with pytest.raises(ValueError, match="axes"):
             st3.st3_rotary_table(positions, torch.zeros(8), None, torch.zeros(8, 8, 2))
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_any_sizes_are_cut_into_a_launch(seed):
+    """From one token to the largest sizes, batches with far more rows than their sequences have among them: the only thing missing is workspace.  (Parts
+    of more than 2^26 rows and heads, most of them no sequence's, are no launch.)"""
+    rng = np.random.default_rng(seed)
+    pick = lambda most: int(np.exp(rng.uniform(0, np.log(most))))  # noqa: E731
+    for _ in range(500):
+        Hk, batch = pick(64), pick(300)
+        H = Hk * pick(16)
+        new = pick(4096)
+        total = max(new, pick(200000) if rng.integers(2) else int(batch * new * rng.uniform(0.2, 1)))
+        both = new + pick(2 ** 20) - 1
+        blocks = both // 64 + 1
+        d = int(rng.choice([64, 128]))
+        s = C.byref(st3.gqa_shape(batch, H, Hk, d))
+        got = st3.lib().st3_block_attend(s, rows(st=H * d, sh=d), FAKE, total, new, cache(table_blocks=blocks, table_stride=blocks), both, rows(1 << 50, H * d, d), 3,
+                                         FAKE, Hk * both, both, FAKE, 0, None)
+        assert got == SMALL or got == UNSUPPORTED and total * H > 2 ** 26 and batch * new < total, (batch, H, Hk, d, total, new, both, got)
+        assert st3.st3_block_attend_workspace_bytes(st3.gqa_shape(batch, H, Hk, d), total, new, both) > 0
