@@ -1008,9 +1008,10 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Scores: the logits of the window's rows are formed again.  Workgroup (key head, strip of 4 x rounds blocks, sequence): the rows, up to kScoreRows of them, lie in
-// LDS; a wave has the 64 keys of a block in registers, meets 16 rows at a time, and a lane adds up what its 16 keys get.  Three waves of a SIMD hide each
-// other's loads of codes better than two that have the next block's codes on their way (those need the registers): a call with 16 tokens' windows over 202000 rows took 303 us so, 314 before.
+// Scores: the logits of the window's rows are formed again.  Workgroup (key head, strip of 4 x rounds blocks, sequence): the rows, up to kScoreRows of them,
+// lie in LDS; a wave has the 64 keys of a block in registers, meets 16 rows at a time, and a lane adds up what its 16 keys get.  Three waves of a SIMD hide
+// each other's loads of codes better than two that have the next block's codes on their way (those need the registers): a call with 16 tokens' windows over
+// 202000 rows took 303 us so, 314 before.
 // ---------------------------------------------------------------------------------------------------------------------------------
 constexpr int kScoreRows = 256;         // rows in LDS at a time: 64 KB at d = 128
 
@@ -1053,7 +1054,7 @@ __global__ __launch_bounds__(256, 3) void chunk_score_kernel(ChunkArgs a, int ro
     };
     const int rows = sq.m * a.G, first = max(0, sq.m - a.window) * a.G;
     auto stage = [&](int r0) {                              // rows r0 .. into LDS
-#pragma unroll 2
+#pragma unroll 4
         for (int e = tid; e < fit * UPR; e += 256) {
             const int x = e / UPR, r = min(r0 + x, rows - 1), t = r / a.G;
             const uint16_t* row = a.q + (int64_t)(sq.start + t) * a.q_st + (int64_t)(kh * a.G + r - t * a.G) * a.q_sh;
@@ -1182,10 +1183,9 @@ constexpr int kLeastPiece = 4;
 //     70000 to 131072 rows 276 us, in as few as hold them 302).
 constexpr int kFewGroup = 32, kFewRows = 64, kWholeStrips = 192, kShortUnits = 20, kManyStrips = 256, kMostPiece = 4 * kWave - 2;
 
-// Room for as many parts as a launch of these or any smaller sizes may leave.  Tiles hold all rows, so kWanted / tiles pieces are no more than kWanted
-// tiles of parts (with few rows: than three times as many of kFewGroup, or a few for every kMostPiece blocks); nor are there more than
-// one for every kLeastPiece blocks.  (Where that is not enough, as for a batch with many
-// more rows than its sequences have, there are fewer pieces.)
+// Room for as many parts as a launch of these or any smaller sizes may leave.  Tiles hold all rows, so kWanted / tiles pieces are no more than kWanted tiles
+// of parts (with few rows: than three times as many of kFewGroup, or a few for every kMostPiece blocks); nor are there more than one for every kLeastPiece
+// blocks.  (Where that is not enough, as for a batch with many more rows than its sequences have, there are fewer pieces.)
 inline int64_t chunk_parts(int64_t rows, int64_t units) {
     return std::min((int64_t)kWanted * kMostRowsOfTile + rows * (1 + (units + kMostPiece - 1) / kMostPiece), rows * ((units + kLeastPiece - 1) / kLeastPiece));
 }
