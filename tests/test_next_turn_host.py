@@ -257,3 +257,21 @@ def test_any_sizes_are_cut_into_a_launch(seed):
                                          FAKE, Hk * both, both, FAKE, 0, None)
         assert got == SMALL or got == UNSUPPORTED and total * H > 2 ** 26 and batch * new < total, (batch, H, Hk, d, total, new, both, got)
         assert st3.st3_block_attend_workspace_bytes(st3.gqa_shape(batch, H, Hk, d), total, new, both) > 0
+
+
+def test_the_rotation_has_the_header_s_layout(tmp_path):
+    import os
+    import shutil
+    import subprocess
+
+    from conftest import ROOT
+    if shutil.which("gcc") is None:
+        pytest.skip("no C compiler")
+    names = [n for n, _ in st3.Rotary._fields_]
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "st3.h"\nint main(void) {\n  printf("%zu", sizeof(st3_rotary));\n' +
+                   "".join(f'  printf(" %zu", offsetof(st3_rotary, {n}));\n' for n in names) +
+                   '  printf(" %d %d", ST3_ROTARY_HALVES, ST3_ROTARY_ADJACENT);\n  return 0;\n}\n')
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    got = [int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
+    assert got == [C.sizeof(st3.Rotary), *(getattr(st3.Rotary, n).offset for n in names), st3.ST3_ROTARY_HALVES, st3.ST3_ROTARY_ADJACENT]
