@@ -1009,7 +1009,8 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a) {
 
 // ---------------------------------------------------------------------------------------------------------------------------------
 // Scores: the logits of the window's rows are formed again.  Workgroup (key head, strip of 4 x rounds blocks, sequence): the rows, up to kScoreRows of them,
-// lie in LDS; a wave has the 64 keys of a block in registers, meets 16 rows at a time, and a lane adds up what its 16 keys get.  Three waves of a SIMD hide
+// lie in LDS; a wave has the 64 keys of a block in registers, meets 16 rows at a time, and a lane adds up what its 16 keys get.  SHARED: a workgroup has one
+// block, and its waves every fourth 16 of the rows; their sums are added in one order.  Three waves of a SIMD hide
 // each other's loads of codes better than two that have the next block's codes on their way (those need the registers): a call with 16 tokens' windows over
 // 202000 rows took 303 us so, 314 before.
 // ---------------------------------------------------------------------------------------------------------------------------------
@@ -1018,7 +1019,7 @@ constexpr int kScoreRows = 256;         // rows in LDS at a time: 64 KB at d = 1
 // Rows in LDS, of a launch whose windows hold `rows` at most.
 inline int score_rows(int64_t rows) { return (int)std::min<int64_t>((rows + 15) / 16 * 16, kScoreRows); }
 
-template <int D, int CODE>
+template <int D, int CODE, bool SHARED>
 __global__ __launch_bounds__(256, 3) void chunk_score_kernel(ChunkArgs a, int rounds, int fit) {
     using F = BlockCode<CODE>;
     constexpr int KS = D / 32, KH = D / 64, UPR = D / 8;    // contraction steps; 16-byte pieces of codes in a key's row for a lane; units of a row
@@ -1027,17 +1028,17 @@ __global__ __launch_bounds__(256, 3) void chunk_score_kernel(ChunkArgs a, int ro
     u32x4* sm_q = reinterpret_cast<u32x4*>(lds);            // [fit][UPR], unit u of row r at u ^ r: 16 rows' units lie in 16 units of the banks
     float2* sm_ml = reinterpret_cast<float2*>(lds + (size_t)fit * 2 * D);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-    const int kh = blockIdx.x, u0 = blockIdx.y * (4 * rounds), b = blockIdx.z;
+    const int kh = blockIdx.x, n_units = SHARED ? 1 : 4 * rounds, u0 = blockIdx.y * n_units, b = blockIdx.z;
     const Turn sq = turn_of(a, b);
     const int keys = sq.rows(), blocks = keys / kBlk, units = (keys + kBlk - 1) / kBlk;
     if (sq.n < 0 || sq.m <= 0 || u0 >= units) return;
     const int64_t strip = (int64_t)b * a.Hk + kh;
-    const int u_end = min(units, u0 + 4 * rounds);
+    const int u_end = min(units, u0 + n_units);
     // lane i has the page and the scale of the wave's i-th block
     int page_l = -1;
     float ks_l = 0.f;
     {
-        const int u = u0 + wave + 4 * lane;
+        const int u = SHARED ? u0 : u0 + wave + 4 * lane;
         if (lane < rounds && u < u_end && u < blocks) page_l = page_of(a.c, b, u);
         if (page_l >= 0) ks_l = a.c.k_scale[(int64_t)page_l * a.Hk + kh];
     }
@@ -1071,7 +1072,7 @@ __global__ __launch_bounds__(256, 3) void chunk_score_kernel(ChunkArgs a, int ro
     const bool all_fit = rows - first <= fit;               // (else every round takes the rows piece by piece)
 #pragma unroll 1
     for (int i = 0; i < rounds; ++i) {
-        const int u = u0 + wave + 4 * i;
+        const int u = SHARED ? u0 : u0 + wave + 4 * i;
         if (all_fit && u >= u_end) break;
         const bool tail = u == blocks && u < u_end, there = tail || __builtin_amdgcn_readlane(page_l, i) >= 0;
         const float ks = tail ? a.scale_l2 : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), i)) * a.scale_l2;
@@ -1097,7 +1098,7 @@ __global__ __launch_bounds__(256, 3) void chunk_score_kernel(ChunkArgs a, int ro
         __builtin_amdgcn_sched_barrier(0);
         const int key = u * kBlk + lane;
         float* to = a.score + b * a.s_sb + kh * a.s_sh + key;
-        const float old = u < u_end && key < sq.n ? *to : 0.f;
+        const float old = u < u_end && key < sq.n && (!SHARED || wave == 0) ? *to : 0.f;
         __builtin_amdgcn_sched_barrier(0);
         f32x4 sum[4];
 #pragma unroll
@@ -1131,13 +1132,14 @@ __global__ __launch_bounds__(256, 3) void chunk_score_kernel(ChunkArgs a, int ro
                         if (x & 1) __builtin_amdgcn_sched_barrier(0);       // (else all products are kept at once)
                     }
                 };
-                int x0 = 0;
+                int x0 = SHARED ? 16 * wave : 0;
+                constexpr int kStep = SHARED ? 64 : 16;
                 if (u * kBlk + kBlk - 1 <= sq.n + r0 / a.G) {       // every row sees the whole block
 #pragma unroll 1
-                    for (; x0 + 16 <= here; x0 += 16) add(x0, std::false_type{});
+                    for (; x0 + 16 <= here; x0 += kStep) add(x0, std::false_type{});
                 }
 #pragma unroll 1
-                for (; x0 < here; x0 += 16) add(x0, std::true_type{});
+                for (; x0 < here; x0 += kStep) add(x0, std::true_type{});
             }
             r0 += fit;
             if (r0 >= rows) break;
@@ -1159,8 +1161,13 @@ __global__ __launch_bounds__(256, 3) void chunk_score_kernel(ChunkArgs a, int ro
 #pragma unroll
             for (int x = 0; x < 4; ++x) *reinterpret_cast<f32x4*>(&part[wave][16 * x + 4 * g]) = sum[x];
         }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        if (key < keys) *to = old + part[wave][lane];       // (written by this wave)
+        if constexpr (SHARED) {
+            __syncthreads();
+            if (wave == 0 && key < keys) *to = old + ((part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]));
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            if (key < keys) *to = old + part[wave][lane];   // (written by this wave)
+        }
     }
 }
 
@@ -1233,6 +1240,8 @@ inline ChunkCut chunk_cut(const st3_gqa_shape* s, int total, int max_new, int ma
 // Blocks that a wave of the scores' launch takes one behind the other: as many as leave three workgroups for each compute unit, which hold its registers
 // (9 to 33 tokens over 70000 to 131072 rows 274 us, with four 284, with two 286); their pages are lanes of a register (4 x 130000 rows 297 us, no more
 // than 16 blocks a wave 311).
+// Where there are fewer blocks than compute units, a workgroup's waves share one and deal out the rows (7 x 626 tokens, 1024 rows of each in the window: the
+// call 62 us, 85 by a block a wave; 100 tokens behind 1000 rows 29.4 and 31.0; with 576 blocks 41.1 and 40.1).
 constexpr int kScoreWgs = 768, kMostRounds = kWave;
 inline int score_rounds(int64_t units, int Hk, int B) {
     const int64_t want = units * Hk * B / (4 * kScoreWgs);
@@ -1269,7 +1278,9 @@ void launch_chunk(const ChunkArgs& a, const ChunkCut& cut, unsigned grid, hipStr
     if (a.pieces > 1) chunk_join_kernel<D><<<(unsigned)(((int64_t)a.total * a.H + 3) / 4), 256, 0, st>>>(a);
     if (!a.score || a.max_len == 0 || cut.stage > 0) return;
     const int fit = score_rows((int64_t)std::min(a.window, a.max_new) * a.G), units = (a.max_len + kBlk - 1) / kBlk, rounds = score_rounds(units, a.Hk, a.B);
-    chunk_score_kernel<D, CODE><<<dim3(a.Hk, (units + 4 * rounds - 1) / (4 * rounds), a.B), 256, fit * (2 * D + sizeof(float2)), st>>>(a, rounds, fit);
+    const size_t lds = fit * (2 * D + sizeof(float2));
+    if ((int64_t)units * a.Hk * a.B <= kWanted && fit > 16) chunk_score_kernel<D, CODE, true><<<dim3(a.Hk, units, a.B), 256, lds, st>>>(a, 1, fit);
+    else chunk_score_kernel<D, CODE, false><<<dim3(a.Hk, (units + 4 * rounds - 1) / (4 * rounds), a.B), 256, lds, st>>>(a, rounds, fit);
 }
 
 }  // namespace

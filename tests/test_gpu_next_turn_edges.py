@@ -36,12 +36,24 @@ def test_parts_of_a_large_batch():
                                             (600, 9, 3, 7, 1), (5000, 16, 2, 8, 2), (17000, 9, 2, 28, 4), (700, 13, 70, 15, 3), (1000, 65, 2, 3, 3), (2000, 4, 200, 2, 1), (17000, 1, 200, 1, 1)])
 @pytest.mark.parametrize("window", [0, 2, 50])
 def test_either_side_of_every_cut(old, new, B, H, Hk, window):
-    """Few rows: by 4, 8 and 12 waves, whole and in pieces, with their logits in LDS and formed again, in one group and in two (which may part a token's heads)."""
+    """Few rows: by 4, 8 and 12 waves, whole and in pieces, with their logits in LDS and formed again, in one group and in two (which may part a token's
+    heads)."""
     rng = np.random.default_rng(old + new + B)
     olds = [old] * B
     for b in range(1, B):
         olds[b] = int(rng.integers(-1, 200))
     attend.run(rng, olds, [new] * B, H, Hk, 64 if B > 100 else 128, "int8" if B % 2 else "e4m3", window)
+
+
+@pytest.mark.parametrize("B,old,new,H,Hk,d", [(1, 70, 40, 8, 2, 128), (3, 10, 300, 16, 1, 128), (5, 2, 90, 12, 4, 64), (1, 3000, 17, 4, 1, 128),
+                                              # (up to here no more than 256 blocks)
+                                              (40, 150, 40, 8, 2, 128), (30, 200, 30, 32, 2, 64), (60, 5, 300, 16, 1, 128)])
+@pytest.mark.parametrize("window", [5, 33, 1000])
+def test_scores_of_few_blocks_and_of_many(B, old, new, H, Hk, d, window):
+    """Windows of up to thousands of rows, which do not lie in LDS at once; a workgroup's waves with a block each, and with one together."""
+    rng = np.random.default_rng(B + old)
+    olds, news = [int(x) for x in rng.integers(0, old + 1, size=B)], [int(x) for x in rng.integers(1, new, size=B - 1)] + [new]
+    attend.run(rng, olds, news, H, Hk, d, "int8" if d == 64 else "e4m3", window)
 
 
 @pytest.mark.parametrize("old,new", [([200], [3]), ([130, 700], [4, 9]), ([20] * 110, [2] * 110)])
