@@ -80,6 +80,7 @@ class BlockGeneration:
         self.evictions = 0
 
     new: Optional[List[int]] = None             # rows that the turn adds, while one is open
+    prompts: bool = True                        # the rows are the prompts' and nothing has come behind them
 
     def _no_turn(self) -> None:
         if self.new is not None:
@@ -91,7 +92,7 @@ class BlockGeneration:
         lens = [int(n) for n in prompt_lens]
         if len(lens) != self.B or min(lens) < -1 or max(lens) > self.capacity:
             raise ValueError(f"{self.B} lengths, up to {self.capacity}, expected; {lens} given")
-        self.lens, self.evictions, self.new = lens, 0, None
+        self.lens, self.evictions, self.new, self.prompts = lens, 0, None, True
         starts = [0]
         for n in lens:
             starts.append(starts[-1] + max(n, 0))
@@ -110,8 +111,10 @@ class BlockGeneration:
 
     def prefill_layer(self, l: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Packed prompts (slices of a fused projection's output are fine) of layer l: attended, and stored.  As many rows
-        as the lengths that begin() was told have together."""
+        as the lengths that begin() was told have together, and before the first step's end, turn or eviction."""
         self._no_turn()
+        if not self.prompts:
+            raise ValueError("rows have come behind the prompts, or left them: begin() comes first")
         if not q.shape[0] == k.shape[0] == v.shape[0] == self.total:
             raise ValueError(f"{q.shape[0]}, {k.shape[0]} and {v.shape[0]} rows of q, k and v: {self.total} expected, the lengths' sum")
         if out is None:
@@ -136,6 +139,7 @@ class BlockGeneration:
 
     def finish_step(self) -> None:
         self._no_turn()
+        self.prompts = False
         self.len.add_(self.live)
         self.lens = [n + 1 if n >= 0 else n for n in self.lens]
 
@@ -154,6 +158,7 @@ class BlockGeneration:
         for m in new:
             starts.append(starts[-1] + m)
         image = torch.tensor(new + starts, dtype=torch.int32).to(self.device)
+        self.prompts = False
         self.new, self.total, self._added, self.cu = new, starts[-1], image[:self.B], image[self.B:]
         self._top = max(0, max(n + m for n, m in zip(self.lens, new)))
         need = st3.st3_block_attend_workspace_bytes(self.shape, self.total, max(new), self._top)
@@ -198,6 +203,7 @@ class BlockGeneration:
         self._no_turn()
         if self.longest == 0:
             return
+        self.prompts = False
         for l in range(self.L):
             st3.st3_block_evict(self.shape, self._sets[self._of[l]], self._sets[self._spare], self.longest, self.budget, self.n_sink, self.n_recent,
                                 self.score[l], self.score[l], self.kept[l])
