@@ -672,8 +672,8 @@ extern "C" st3_status st3_block_append(const st3_gqa_shape* shape, const st3_row
     const int Hk = shape->kv_heads, D = shape->head_dim;
     if (!cu_len || total < 0 || max_new < 0 || max_new > total || max_len < 0) return ST3_ERR_INVALID_ARG;
     if (max_len > kMostRows) return ST3_ERR_UNSUPPORTED;
-    if (rotary && (s = check_rotary(rotary, D)) != ST3_OK) return s;
     if (total == 0) return ST3_OK;          // (an empty tensor may have no address)
+    if (rotary && (s = check_rotary(rotary, D)) != ST3_OK) return s;
     if ((s = check_rows(k, D, 2)) != ST3_OK || (s = check_rows(v, D, 2)) != ST3_OK) return s;
     if (max_new == 0) return ST3_OK;
     const int blocks = (int)(((int64_t)max_new + kBlk - 2) / kBlk) + 1;     // (new rows may begin with a block's last)
