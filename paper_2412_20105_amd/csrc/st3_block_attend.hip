@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "st3_block.h"
+#include "st3_block_few.h"
 
 namespace st3 {
 namespace {
@@ -593,17 +594,11 @@ __global__ __launch_bounds__(kChunkThreads, 2) void block_chunk_kernel(ChunkArgs
 // ---------------------------------------------------------------------------------------------------------------------------------
 constexpr float kNoPage = -3.402823466e38f;     // in place of a logit: no page, no weight
 
-template <int D>
-inline size_t few_lds(int waves, int cols, int64_t stage) {
-    const size_t keys = (size_t)waves * kBlk * D, parts = sizeof(float) * waves * cols * (D + 4);
-    return std::max(keys, parts) + sizeof(float) * (2 * waves * cols + 2 * cols + (size_t)cols * stage);
-}
-
 template <int D, int CODE, int QC, int WAVES, bool WHOLE>
 __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(ChunkArgs a, int stage) {
     using F = BlockCode<CODE>;
     using L = KeyTile<D>;
-    constexpr int KS = D / 32, DT = D / 16, KH = D / 64, kThr = WAVES * 64, OS = D + 4, kKeys = WAVES * kBlk * D / 4;
+    constexpr int KS = D / 32, DT = D / 16, KH = D / 64, kThr = WAVES * 64, OS = D + 4;
     extern __shared__ __attribute__((aligned(16))) float few[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
     const int kh = blockIdx.x % a.Hk, ch = blockIdx.y, b = blockIdx.z, cols = a.tile, r0 = blockIdx.x / a.Hk * cols;
@@ -613,11 +608,12 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
     const int rows = min(sq.m * a.G - r0, cols), keys = sq.rows(), blocks = keys / kBlk, units = (keys + kBlk - 1) / kBlk;
     const int u_begin = WHOLE ? 0 : ch * a.piece, u_end = WHOLE ? units : min(units, u_begin + a.piece);
     if (!WHOLE && ch > 0 && u_begin >= units) return;
+    const FewLds<D> at(WAVES, cols);
     float* sm_o = few;
-    float* sm_m = few + max(kKeys, WAVES * cols * OS);
-    float* sm_l = sm_m + WAVES * cols;
-    float* sm_h = sm_l + WAVES * cols;                      // a row's maximum, and one over its sum
-    float* staged = sm_h + 2 * cols;                        // [cols][stage]
+    float* sm_m = few + at.maxima;
+    float* sm_l = few + at.sums;
+    float* sm_h = few + at.heads;                           // a row's maximum, and one over its sum
+    float* staged = few + at.staged;                        // [cols][stage]
     const int64_t strip = (int64_t)b * a.Hk + kh;
     const int krow = 16 * (c >> 2) + (c & 3);               // + 4 t: the key of row c of product t
     const uint32_t v_lane = (uint32_t)(c * kBlk + 16 * g);
@@ -1206,7 +1202,7 @@ inline ChunkCut few_cut(int64_t strips, int most, int max_len, bool scored, int6
     strips *= groups;                       // (workgroups of a whole launch)
     const int waves = strips > kManyStrips ? 4 : cols <= 16 ? 12 : 8;
     if (units + 2 <= waves * kWave && (strips >= kWholeStrips || units <= kShortUnits)) {
-        const bool staged = scored && groups == 1 && few_lds<D>(waves, cols, units * kBlk) <= kLds;
+        const bool staged = scored && groups == 1 && FewLds<D>(waves, cols).bytes(cols, units * kBlk) <= kLds;
         return ChunkCut{cols, (int)units, 1, waves, staged ? (int)units * kBlk : 0, groups};
     }
     const int64_t even = strips <= kWanted / 4 ? kWanted / strips : (3 * kWanted + strips - 1) / strips, pieces = even * ((units + even * kMostPiece - 1) / (even * kMostPiece));
@@ -1262,7 +1258,7 @@ inline ChunkWs chunk_ws(const st3_gqa_shape* s, int total, int max_len) {
 
 template <int D, int CODE, int QC>
 void launch_few(const ChunkArgs& a, const ChunkCut& cut, hipStream_t st) {
-    const size_t lds = few_lds<D>(cut.few, a.tile, cut.stage);
+    const size_t lds = FewLds<D>(cut.few, a.tile).bytes(a.tile, cut.stage);
     const dim3 grid(a.Hk * cut.groups, a.pieces, a.B);
     constexpr int kMost = QC == 1 ? 12 : 8;
     if (a.pieces > 1) chunk_few_kernel<D, CODE, QC, 4, false><<<grid, 256, lds, st>>>(a, 0);
