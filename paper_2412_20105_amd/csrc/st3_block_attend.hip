@@ -704,6 +704,9 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
                 st.o[dt][qc] = c == row ? o : st.o[dt][qc];
             }
     };
+    // bytes 0x7f and 0xff of four codes, by their highest bits
+    auto no_numbers = [](uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; };
+    uint64_t odd_at = 0;                                    // positions of masked blocks with such codes among V's
     uint64_t left = __ballot(page_l >= 0);                  // the wave's positions whose blocks are to come
     if (left != 0) load_k(__builtin_amdgcn_readlane(page_l, __ffsll((unsigned long long)left) - 1));     // (on its way beside the tail)
     __builtin_amdgcn_sched_barrier(0);
@@ -837,30 +840,29 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
             __builtin_amdgcn_sched_barrier(0);
             if (next >= 0) load_k(__builtin_amdgcn_readlane(page_l, next));
             __builtin_amdgcn_sched_barrier(0);
-            bool odd = false;
-            if (CODE == ST3_BLOCK_E4M3 && masked) {
+            if (CODE == ST3_BLOCK_E4M3 && masked) {         // codes that are no numbers count as 0 here, and below for the rows that see them
+                bool odd = false;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) odd |= (((vr[dt][j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;        // (a code that is no number)
+                    for (int j = 0; j < 4; ++j) odd |= no_numbers(vr[dt][j]) != 0;
+                if (__any(odd)) {
+                    odd_at |= 1ull << i;
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t top = no_numbers(vr[dt][j]);
+                            vr[dt][j] &= ~(top | (top - (top >> 7)));
+                        }
+                }
             }
-            const bool slow = __any(odd);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 Frag pb[QC];
 #pragma unroll
                 for (int qc = 0; qc < QC; ++qc) pb[qc] = weigh(qc, s[2 * x][qc], s[2 * x + 1][qc], vs);
                 __builtin_amdgcn_sched_barrier(0);
-                if (slow) {
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) {
-                        const uint2 w0 = F::to_bf16(vr[dt][2 * x]), w1 = F::to_bf16(vr[dt][2 * x + 1]);
-                        Frag f;
-                        f.u4 = u32x4{w0.x, w0.y, w1.x, w1.y};
-                        careful(dt, f, pb, k0 + 16 * g + 8 * x);
-                    }
-                    continue;
-                }
 #pragma unroll
                 for (int d2 = 0; d2 < DT; d2 += 2) {        // two chains of products at a time
                     Frag f[2];
@@ -881,6 +883,27 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
             __builtin_amdgcn_sched_barrier(0);
             i = next;
         }
+    }
+    // Such blocks once more, behind the loop: a row's output is NaN in a column whose first such code it sees.  (Products row by row within the loop cost it its
+    // registers, 5 to 29 spilled at d = 128: four tokens of 32 sequences over 611 to 3136 rows 29.7 us, 24.4 so; 8 of eight over 20000 to 30000 rows 188 and 115.)
+    for (; odd_at != 0; odd_at &= odd_at - 1) {
+        const int i = __ffsll((unsigned long long)odd_at) - 1, k0 = unit_at(i) * kBlk;
+        const uint8_t* v = a.c.v_codes + ((int64_t)__builtin_amdgcn_readlane(page_l, i) * a.Hk + kh) * (kBlk * D);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t* col = reinterpret_cast<const uint32_t*>(v + (16 * dt + 4 * g + j) * kBlk);
+                int from = 0x7fffffff;
+#pragma unroll 1
+                for (int w = kBlk / 4 - 1; w >= 0; --w) {
+                    const uint32_t top = no_numbers(col[w]);
+                    from = top != 0 ? k0 + 4 * w + (__ffs(top) - 1) / 8 : from;
+                }
+#pragma unroll
+                for (int qc = 0; qc < QC; ++qc)
+                    if (from <= st.pos[qc]) st.o[dt][qc][j] = __uint_as_float(0x7fc00000u);
+            }
     }
     // what the first rows have received so far, on its way while the waves' parts are joined
     constexpr int kAhead = 4;

@@ -165,3 +165,45 @@ def test_scales_at_either_end(form, code, value):
     out, score = call(state, q, 50)
     # below the smallest normal bf16 (2^-126) a rounding of a weight or of the output is a step of 2^-133 instead, or the value is lost
     check(dev, q, old, new, 50, out, score, state[-1], tiny=both * 127 * 2.0 ** -126)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("window", [0, 50])
+def test_values_that_are_no_numbers(form, window):
+    """Codes of NaN among V in blocks that new rows lie in, several in a column, and NaN in the tail: NaN for the rows that see one, in its column alone."""
+    old, new, H, Hk, d = FORMS[form]
+    both, rng = old + new, np.random.default_rng(5)
+    state = prepared(form, "e4m3", window, 6)
+    dev, q, last = state[4], state[1], both // BLOCK * BLOCK
+    nan = torch.zeros((Hk, both, d), dtype=torch.bool, device=DEV)
+    for j in [old, old + 1, last - 1, last - 2, last - 40, last - 64, both - 1, both - 2, *rng.integers(max(0, last - 64), both, 8).tolist()]:
+        h, col = int(rng.integers(Hk)), int(rng.integers(d))
+        for c in {col, 7}:
+            nan[h, j, c] = True
+            if j >= last:
+                dev.v_tail[0, h, c, j - last] = float("nan")
+            else:
+                dev.v_codes[int(dev.table[0, j // BLOCK]), h, c, j % BLOCK] = int(rng.choice([0x7f, 0xff]))
+    out, score = call(state, q, window) if window else (call_unscored(state, q), None)
+    k, v = rows_of(dev, both, "k"), rows_of(dev, both, "v")
+    assert torch.equal(torch.isnan(v), nan)
+    see = torch.arange(both, device=DEV) <= old + torch.arange(new, device=DEV)[:, None]
+    for h in range(H):
+        kh = h // (H // Hk)
+        x = q[:new, h].double()
+        p = torch.softmax((x @ k[kh].t() / np.sqrt(d)).masked_fill(~see, -torch.inf), -1)
+        slack = fp32_slack(float((x.abs() @ k[kh].abs().t()).max()) / np.sqrt(d), d, both)
+        odd, clean, got = (see.double() @ nan[kh].double()) > 0, v[kh].nan_to_num(nan=0.0), out[:new, h].double()
+        assert torch.equal(torch.isnan(got), odd), h
+        want, spread = p @ clean, p @ clean.abs()
+        assert bool(((got - want).abs() <= HALF * (want.abs() + spread) * 1.01 + slack * spread)[~odd].all())
+    if window:                                              # (weights have nothing to do with values)
+        assert bool(torch.isfinite(score).all())
+
+
+def call_unscored(state, q):
+    shape, _, at, most, dev, top, ws, _ = state
+    out = torch.full((q.shape[0], q.shape[1], dev.dim), 7.0, dtype=torch.bfloat16, device=DEV)
+    st3.st3_block_attend(shape, q, at, most, dev.c, top, out, 0, None, ws)
+    torch.cuda.synchronize()
+    return out
