@@ -673,7 +673,7 @@ def st3_block_attend_workspace_bytes(shape: GqaShape, total: int, max_new: int, 
 
 def st3_block_attend(shape: GqaShape, q, cu_len, max_new: int, cache: BlockCache, max_len: int, out, window: int, score, workspace, stream=None) -> None:
     """q, out [T, H, d]: new rows that the cache holds already, behind its lengths (max_len at most with them); score float32 [batch, Hk, >= max_len]
-    or None.  Weights are rounded to bf16 once in the product with v; everything else is float32."""
+    or None.  In the product with v weights are two bf16 terms where max_new * H / Hk <= 32, else rounded to bf16 once; everything else is float32."""
     _check_cache(shape, cache)
     total, H = q.shape[0], shape.heads
     sp, sb, sh = _scores(shape, score, "score", max_len)

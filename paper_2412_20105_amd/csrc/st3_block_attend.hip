@@ -594,7 +594,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void block_chunk_kernel(ChunkArgs
 // ---------------------------------------------------------------------------------------------------------------------------------
 constexpr float kNoPage = -3.402823466e38f;     // in place of a logit: no page, no weight
 
-template <int D, int CODE, int QC, int WAVES, bool WHOLE>
+template <int D, int CODE, int QC, int WAVES, bool WHOLE, bool TWO>
 __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(ChunkArgs a, int stage) {
     using F = BlockCode<CODE>;
     using L = KeyTile<D>;
@@ -679,19 +679,28 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
             for (int dt = 0; dt < DT; ++dt) st.o[dt][qc] *= alpha;
         }
     };
-    auto weigh = [&](int qc, const f32x4& s0, const f32x4& s1, float vs) {      // (rounded to bf16 once, as in chunk_weights)
-        Frag f;
+    // Weights times V's scale.  TWO, rows of one group: as two bf16 terms, cut off at 8 significant bits and the rest rounded to nearest: what is left out is
+    // 2^-16 of a weight at most, as for single tokens (five tokens over 739 rows 16.2 us, with one term 15.2; four of 32 sequences 27.5 and 26.3, of E4M3 24.8 and
+    // 24.4).  Two groups, whose matrix instructions are what their time goes into, have one, rounded to nearest (16 tokens of eight sequences over 20000 to
+    // 30000 rows 127 us, with two 141), as tiles have.
+    auto weigh = [&](int qc, const f32x4& s0, const f32x4& s1, float vs, Frag& hi, Frag& lo) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const f32x4& y = j < 2 ? s0 : s1;
             const float p0 = exp2_fast(y[2 * (j & 1)] - st.m[qc]), p1 = exp2_fast(y[2 * (j & 1) + 1] - st.m[qc]);
             st.l[qc] += p0 + p1;
-            f.w[j] = bf16_pair(p0 * vs, p1 * vs);
+            const float w0 = p0 * vs, w1 = p1 * vs;
+            if constexpr (TWO) {
+                const uint32_t b0 = __float_as_uint(w0), b1 = __float_as_uint(w1);
+                hi.w[j] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+                lo.w[j] = bf16_pair(w0 - __uint_as_float(b0 & 0xffff0000u), w1 - __uint_as_float(b1 & 0xffff0000u));
+            } else {
+                hi.w[j] = bf16_pair(w0, w1);
+            }
         }
-        return f;
     };
     // O^T += V^T P^T where V of keys that a row does not see may be infinite or no number: row by row, such V left out.  f: keys key .. + 7.
-    auto careful = [&](int dt, const Frag& f, const Frag (&p)[QC], int key) {
+    auto careful = [&](int dt, const Frag& f, const Frag (&hi)[QC], const Frag (&lo)[QC], int key) {
 #pragma unroll
         for (int qc = 0; qc < QC; ++qc)
 #pragma unroll 1
@@ -700,7 +709,8 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
                 Frag v;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v.w[j] = f.w[j] & ((key + 2 * j <= pos ? 0xffffu : 0u) | (key + 2 * j < pos ? 0xffff0000u : 0u));
-                const f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, p[qc].v, st.o[dt][qc], 0, 0, 0);
+                f32x4 o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, hi[qc].v, st.o[dt][qc], 0, 0, 0);
+                if constexpr (TWO) o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, lo[qc].v, o, 0, 0, 0);
                 st.o[dt][qc] = c == row ? o : st.o[dt][qc];
             }
     };
@@ -744,9 +754,9 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
             }
         }
         follow(mx);
-        Frag pb[QC];
+        Frag hi[QC], lo[QC];
 #pragma unroll
-        for (int qc = 0; qc < QC; ++qc) pb[qc] = weigh(qc, s[0][qc], s[1][qc], 1.0f);
+        for (int qc = 0; qc < QC; ++qc) weigh(qc, s[0][qc], s[1][qc], 1.0f, hi[qc], lo[qc]);
         bool odd = false;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -758,12 +768,15 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
             }
         if (__any(odd)) {
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) careful(dt, tv[dt], pb, key0 + 8 * g);
+            for (int dt = 0; dt < DT; ++dt) careful(dt, tv[dt], hi, lo, key0 + 8 * g);
         } else {
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                for (int qc = 0; qc < QC; ++qc) st.o[dt][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tv[dt].v, pb[qc].v, st.o[dt][qc], 0, 0, 0);
+                for (int qc = 0; qc < QC; ++qc) {
+                    st.o[dt][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tv[dt].v, hi[qc].v, st.o[dt][qc], 0, 0, 0);
+                    if constexpr (TWO) st.o[dt][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tv[dt].v, lo[qc].v, st.o[dt][qc], 0, 0, 0);
+                }
         }
         __builtin_amdgcn_sched_barrier(0);
     }
@@ -859,9 +872,9 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
             }
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                Frag pb[QC];
+                Frag hi[QC], lo[QC];
 #pragma unroll
-                for (int qc = 0; qc < QC; ++qc) pb[qc] = weigh(qc, s[2 * x][qc], s[2 * x + 1][qc], vs);
+                for (int qc = 0; qc < QC; ++qc) weigh(qc, s[2 * x][qc], s[2 * x + 1][qc], vs, hi[qc], lo[qc]);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int d2 = 0; d2 < DT; d2 += 2) {        // two chains of products at a time
@@ -874,7 +887,13 @@ __global__ __launch_bounds__(WAVES * 64, QC == 1 ? 3 : 2) void chunk_few_kernel(
 #pragma unroll
                     for (int y = 0; y < 2; ++y)
 #pragma unroll
-                        for (int qc = 0; qc < QC; ++qc) st.o[d2 + y][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[y].v, pb[qc].v, st.o[d2 + y][qc], 0, 0, 0);
+                        for (int qc = 0; qc < QC; ++qc) st.o[d2 + y][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[y].v, hi[qc].v, st.o[d2 + y][qc], 0, 0, 0);
+                    if constexpr (TWO) {
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+#pragma unroll
+                            for (int qc = 0; qc < QC; ++qc) st.o[d2 + y][qc] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[y].v, lo[qc].v, st.o[d2 + y][qc], 0, 0, 0);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -1279,19 +1298,20 @@ inline ChunkWs chunk_ws(const st3_gqa_shape* s, int total, int max_len) {
     return w;
 }
 
-template <int D, int CODE, int QC>
+template <int D, int CODE, int QC, bool TWO>
 void launch_few(const ChunkArgs& a, const ChunkCut& cut, hipStream_t st) {
     const size_t lds = FewLds<D>(cut.few, a.tile).bytes(a.tile, cut.stage);
     const dim3 grid(a.Hk * cut.groups, a.pieces, a.B);
     constexpr int kMost = QC == 1 ? 12 : 8;
-    if (a.pieces > 1) chunk_few_kernel<D, CODE, QC, 4, false><<<grid, 256, lds, st>>>(a, 0);
-    else if (cut.few == kMost) chunk_few_kernel<D, CODE, QC, kMost, true><<<grid, 64 * kMost, lds, st>>>(a, cut.stage);
-    else chunk_few_kernel<D, CODE, QC, 4, true><<<grid, 256, lds, st>>>(a, cut.stage);
+    if (a.pieces > 1) chunk_few_kernel<D, CODE, QC, 4, false, TWO><<<grid, 256, lds, st>>>(a, 0);
+    else if (cut.few == kMost) chunk_few_kernel<D, CODE, QC, kMost, true, TWO><<<grid, 64 * kMost, lds, st>>>(a, cut.stage);
+    else chunk_few_kernel<D, CODE, QC, 4, true, TWO><<<grid, 256, lds, st>>>(a, cut.stage);
 }
 
 template <int D, int CODE>
 void launch_chunk(const ChunkArgs& a, const ChunkCut& cut, unsigned grid, hipStream_t st) {
-    if (cut.few > 0) a.tile <= 16 ? launch_few<D, CODE, 1>(a, cut, st) : launch_few<D, CODE, 2>(a, cut, st);
+    if (cut.few > 0 && a.tile <= 16) launch_few<D, CODE, 1, true>(a, cut, st);          // (two groups have more than 16 each)
+    else if (cut.few > 0) cut.groups == 1 ? launch_few<D, CODE, 2, true>(a, cut, st) : launch_few<D, CODE, 2, false>(a, cut, st);
     else if (a.tile <= 16 * kChunkWaves) block_chunk_kernel<D, CODE, 1><<<dim3(grid, a.pieces), kChunkThreads, 0, st>>>(a);
     else block_chunk_kernel<D, CODE, 2><<<dim3(grid, a.pieces), kChunkThreads, 0, st>>>(a);
     if (a.pieces > 1) chunk_join_kernel<D><<<(unsigned)(((int64_t)a.total * a.H + 3) / 4), 256, 0, st>>>(a);

@@ -40,8 +40,8 @@ def rows_of(dev, length, name):
     return torch.cat([codes, tail[:, :length % BLOCK]], 1)
 
 
-def check(dev, q, old, new, window, out, score, before, tiny=1e-30):
-    """Against the definition in 64 bits: what is NaN, and how far the rest is off (the output's rounding, and that of every weight)."""
+def check(dev, q, old, new, window, out, score, before, tiny=1e-30, weight=HALF):
+    """Against the definition in 64 bits: what is NaN, and how far the rest is off (the output's rounding, and that of every weight: `weight` of it)."""
     both, H, Hk, d = old + new, q.shape[1], dev.kv_heads, dev.dim
     k, v = rows_of(dev, both, "k"), rows_of(dev, both, "v")
     see = torch.arange(both, device=DEV) <= old + torch.arange(new, device=DEV)[:, None]
@@ -62,7 +62,7 @@ def check(dev, q, old, new, window, out, score, before, tiny=1e-30):
             slack = max(slack, fp32_slack(worst, d, both))
             want, spread, got = p @ v[kh], p @ v[kh].abs(), out[:new, h].double()
             assert bool(torch.isnan(got[odd]).all()), (h, "a logit that is NaN or +infinity")
-            bound = HALF * (want.abs() + spread) * 1.01 + slack * spread + tiny
+            bound = (HALF * want.abs() + weight * spread) * 1.01 + slack * spread + tiny
             assert bool(((got - want).abs() <= bound)[~odd].all()), (h, float(((got - want).abs() / bound)[~odd].max()))
             given += p[counts & ~odd].sum(0)
             odd_keys |= see[counts & odd].any(0)

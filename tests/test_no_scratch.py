@@ -43,5 +43,5 @@ def test_attention_of_new_tokens_spills_nothing(tmp_path):
         pytest.skip("no llvm-readelf")
     st3.lib()
     used = {name: x for name, x in kernels(st3.LIB_PATH, tmp_path).items() if "chunk_" in name}
-    assert len(used) == 42                  # (24 for few rows, 8 for tiles, 8 for scores, 2 that join)
+    assert len(used) == 54                  # (36 for few rows, 8 for tiles, 8 for scores, 2 that join)
     assert not {name: x for name, x in used.items() if x != (0, 0)}
