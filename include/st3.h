@@ -664,7 +664,8 @@ ST3_EXPORT size_t st3_block_attend_workspace_bytes(const st3_gqa_shape* shape, i
  *   p_h[t] = softmax over those of (q_h[t] . k_{h/G}) * scale,   out[t,h,:] = sum_j p_h[t][j] v_{h/G}[j]
  *   score[b,kh,j] += sum_{h in group kh} sum_{t in the last `window` of the m rows, n + t >= j} p_h[t][j]  for j < n; = that sum for n <= j < n + m
  * q, out: [total, H, d] rows; the other arguments are those of st3_block_append and st3_packed_attention.  score may be NULL; its rows hold
- * max_len entries at least, a sequence without new rows keeps its own.  window >= 1 when a score is wanted.
+ * max_len entries at least, a sequence without new rows keeps its own.  (Rows that came in a call without scores have whatever their entries hold: a later
+ * call adds to that.)  window >= 1 when a score is wanted.
  * Logits, maxima, sums and scores are float32.  In the product with v a weight, times v's scale, is two bf16 terms (off by 2^-16 of itself at most) where
  * max_new * heads / kv_heads is 32 or less, and else rounded to bf16 once, to nearest (2^-8, without bias), beside the output's own rounding; sums of n + m
  * such products, weights of up to 2^8 on average, stay in float32 as long as no |v| is above 2^119 / (n + m).

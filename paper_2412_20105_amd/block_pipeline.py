@@ -34,7 +34,9 @@ class BlockGeneration:
     turned, as those of prefill_layer and decode_layer do.
     capacity: rows that a sequence may hold; when the longest has come to it, begin_step() has every key head of every layer keep
     `budget` rows of each longer sequence: the first n_sink, the last n_recent, and of the others those that have received the most
-    attention weight so far, counted from the prompt's last `window` rows on.
+    attention weight so far: from the prompt's last `window` rows, from every step's row, and from the last `window` rows of every turn that counts.
+    A prompt may come in pieces, as turns behind begin() with lengths of 0; where only the last of them counts, and has `window` rows, weights are those
+    of the prompt's last ones, wherever it was cut.
     Pages: a set of them for each layer and one to spare.  An eviction writes a layer's rows into the spare set, and the
     set that the layer leaves becomes the next one to spare.
     """
@@ -144,8 +146,9 @@ class BlockGeneration:
         self.lens = [n + 1 if n >= 0 else n for n in self.lens]
 
     # ------------------------------------------------------------------------------------
-    def begin_turn(self, new_lens: Sequence[int]) -> None:
-        """A turn of so many new tokens of each sequence (an empty place has none); makes room where a sequence has too little."""
+    def begin_turn(self, new_lens: Sequence[int], counts: bool = True) -> None:
+        """A turn of so many new tokens of each sequence (an empty place has none); makes room where a sequence has too little.  counts: whether what
+        the turn attends to counts as weight; where it does not, its own rows begin with none."""
         self._no_turn()
         new = [int(m) for m in new_lens]
         if len(new) != self.B or min(new) < 0 or any(m and n < 0 for n, m in zip(self.lens, new)):
@@ -158,16 +161,19 @@ class BlockGeneration:
         for m in new:
             starts.append(starts[-1] + m)
         image = torch.tensor(new + starts, dtype=torch.int32).to(self.device)
-        self.prompts = False
+        self.prompts, self.counts = False, counts
         self.new, self.total, self._added, self.cu = new, starts[-1], image[:self.B], image[self.B:]
         self._top = max(0, max(n + m for n, m in zip(self.lens, new)))
         need = st3.st3_block_attend_workspace_bytes(self.shape, self.total, max(new), self._top)
         if need > self._turn_ws.numel():
             self._turn_ws = torch.empty((need,), dtype=torch.uint8, device=self.device)
+        if not counts and self.total > 0:
+            rows = torch.arange(self._top, dtype=torch.int32, device=self.device) - self.len[:, None]
+            self.score[..., :self._top].masked_fill_(((rows >= 0) & (rows < self._added[:, None]))[:, None], 0.0)
 
     def extend_layer(self, l: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rotary: Optional[st3.Rotary] = None,
                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """The turn's packed rows in layer l: queries and keys turned, keys and values appended, queries attended; the scores go on."""
+        """The turn's packed rows in layer l: queries and keys turned, keys and values appended, queries attended; the scores go on where the turn counts."""
         if self.new is None:
             raise ValueError("no turn is open: begin_turn() comes first")
         if not q.shape[0] == k.shape[0] == v.shape[0] == self.total:
@@ -182,7 +188,7 @@ class BlockGeneration:
             turned = torch.empty((q.shape[0], self.H, self.d), dtype=q.dtype, device=q.device)
             st3.st3_rotate_rows(q, turned, rotary)
             q = turned
-        st3.st3_block_attend(self.shape, q, self.cu, most, cache, self._top, out, self.window, self.score[l], self._turn_ws)
+        st3.st3_block_attend(self.shape, q, self.cu, most, cache, self._top, out, self.window, self.score[l] if self.counts else None, self._turn_ws)
         return out
 
     def finish_turn(self) -> None:
