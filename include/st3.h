@@ -651,7 +651,9 @@ ST3_EXPORT st3_status st3_rotate_rows(const st3_rows* x, const st3_rows* out, in
  *   rows n .. n + m - 1 of sequence b <- rows cu_len[b] .. of k, turned by rotary where it is not NULL and rounded to bf16, and of v.
  * Blocks that are whole then are coded into their pages from rows of 16 bits, those in the tail among them, the rest goes into the tail: the
  * cache is the same, bit for bit, however the rows are cut into calls (st3_block_store, st3_block_decode and this one).
- * len still says n behind the call.  A place with a negative length stays as it is. */
+ * len still says n behind the call.  A place with a negative length stays as it is.
+ * A lower length does not take rows back once a block has filled: the tail then holds rows of the next one.  Rows that may not stay (drafted tokens) are
+ * appended to a cache with copies of the tails; the blocks that they fill go into pages that no length up to n reaches. */
 ST3_EXPORT st3_status st3_block_append(const st3_gqa_shape* shape, const st3_rows* k, const st3_rows* v, const int32_t* cu_len, int32_t total,
                                        int32_t max_new, const st3_block_cache* cache, int32_t max_len, const st3_rotary* rotary, void* stream);
 

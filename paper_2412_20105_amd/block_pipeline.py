@@ -25,7 +25,7 @@ class BlockGeneration:
             for l in range(layers):
                 out = gen.decode_layer(l, q, k_new, v_new)  # [batch, heads or kv_heads, d]
             gen.finish_step()
-        gen.begin_turn(new_lens)                            # several new tokens at once: the next question, drafted tokens
+        gen.begin_turn(new_lens)                            # several new tokens at once: the next question, a piece of a long prompt
         for l in range(layers):
             out = gen.extend_layer(l, q, k, v, rotary)      # [T, heads or kv_heads, d], packed like prompts
         gen.finish_turn()
@@ -37,6 +37,8 @@ class BlockGeneration:
     attention weight so far: from the prompt's last `window` rows, from every step's row, and from the last `window` rows of every turn that counts.
     A prompt may come in pieces, as turns behind begin() with lengths of 0; where only the last of them counts, and has `window` rows, weights are those
     of the prompt's last ones, wherever it was cut.
+    Drafted tokens are checked in a turn that does not stay: it attends like any other and leaves the sequences as they were (but for an eviction that
+    makes room).  Those that are accepted then come in a turn of their own, with the same rows of q, k and v.
     Pages: a set of them for each layer and one to spare.  An eviction writes a layer's rows into the spare set, and the
     set that the layer leaves becomes the next one to spare.
     """
@@ -79,6 +81,7 @@ class BlockGeneration:
         self._out = torch.empty((layers, batch, heads, head_dim), **half)
         self.lens: List[int] = [-1] * batch     # host copies; negative: an empty place
         self._turn_ws = torch.empty((0,), dtype=torch.uint8, device=device)
+        self._copies: List[st3.BlockCache] = []
         self.evictions = 0
 
     new: Optional[List[int]] = None             # rows that the turn adds, while one is open
@@ -146,9 +149,10 @@ class BlockGeneration:
         self.lens = [n + 1 if n >= 0 else n for n in self.lens]
 
     # ------------------------------------------------------------------------------------
-    def begin_turn(self, new_lens: Sequence[int], counts: bool = True) -> None:
+    def begin_turn(self, new_lens: Sequence[int], counts: bool = True, stays: bool = True) -> None:
         """A turn of so many new tokens of each sequence (an empty place has none); makes room where a sequence has too little.  counts: whether what
-        the turn attends to counts as weight; where it does not, its own rows begin with none."""
+        the turn attends to counts as weight; where it does not, its own rows begin with none.  stays: whether the sequences have its rows behind
+        finish_turn(); where they do not, nothing of it counts either."""
         self._no_turn()
         new = [int(m) for m in new_lens]
         if len(new) != self.B or min(new) < 0 or any(m and n < 0 for n, m in zip(self.lens, new)):
@@ -161,13 +165,13 @@ class BlockGeneration:
         for m in new:
             starts.append(starts[-1] + m)
         image = torch.tensor(new + starts, dtype=torch.int32).to(self.device)
-        self.prompts, self.counts = False, counts
+        self.prompts, self.counts, self.stays = False, counts and stays, stays
         self.new, self.total, self._added, self.cu = new, starts[-1], image[:self.B], image[self.B:]
         self._top = max(0, max(n + m for n, m in zip(self.lens, new)))
         need = st3.st3_block_attend_workspace_bytes(self.shape, self.total, max(new), self._top)
         if need > self._turn_ws.numel():
             self._turn_ws = torch.empty((need,), dtype=torch.uint8, device=self.device)
-        if not counts and self.total > 0:
+        if stays and not counts and self.total > 0:
             rows = torch.arange(self._top, dtype=torch.int32, device=self.device) - self.len[:, None]
             self.score[..., :self._top].masked_fill_(((rows >= 0) & (rows < self._added[:, None]))[:, None], 0.0)
 
@@ -182,7 +186,7 @@ class BlockGeneration:
             out = torch.empty((q.shape[0], self.H, self.d), dtype=q.dtype, device=q.device)
         if self.total == 0:
             return out
-        most, cache = max(self.new), self._sets[self._of[l]]
+        most, cache = max(self.new), self._sets[self._of[l]] if self.stays else self._copied_tails(self._of[l])
         st3.st3_block_append(self.shape, k, v, self.cu, most, cache, self._top, rotary)
         if rotary is not None:
             turned = torch.empty((q.shape[0], self.H, self.d), dtype=q.dtype, device=q.device)
@@ -191,11 +195,22 @@ class BlockGeneration:
         st3.st3_block_attend(self.shape, q, self.cu, most, cache, self._top, out, self.window, self.score[l] if self.counts else None, self._turn_ws)
         return out
 
+    def _copied_tails(self, i: int) -> st3.BlockCache:
+        """Set i's cache with copies of its tails.  Rows appended to it leave the set as it is: blocks that they fill go into pages that none of its
+        lengths reach, but a tail that overflows is lost (so a lower length alone would not bring it back)."""
+        if not self._copies:
+            self._copied = torch.empty_like(self.k_tail[0]), torch.empty_like(self.v_tail[0])
+            self._copies = [st3.block_cache(self.k_codes, self.v_codes, self.k_scale, self.v_scale, *self._copied, t, self.len) for t in self.tables]
+        self._copied[0].copy_(self.k_tail[i])
+        self._copied[1].copy_(self.v_tail[i])
+        return self._copies[i]
+
     def finish_turn(self) -> None:
         if self.new is None:
             raise ValueError("no turn is open: begin_turn() comes first")
-        self.len.add_(self._added * self.live)
-        self.lens = [n + m if n >= 0 else n for n, m in zip(self.lens, self.new)]
+        if self.stays:
+            self.len.add_(self._added * self.live)
+            self.lens = [n + m if n >= 0 else n for n, m in zip(self.lens, self.new)]
         self.new = None
 
     def retire(self, b: int) -> None:
