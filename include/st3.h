@@ -622,7 +622,7 @@ ST3_EXPORT st3_status st3_block_evict(const st3_gqa_shape* shape, const st3_bloc
 /* table[t][c] = (cos, sin) of positions[axis[c]][t] * inv_freq[c]: the angle by which pair c of token t's columns turns.
  * positions: DEVICE int32, [axes][total], a token's components (time, height, width ...) in rows position_stride entries apart, at least total, or 0
  * where all components are the same; 1 to 4 axes.
- * axis: HOST [pairs], each below axes, or NULL where all are 0.  inv_freq: DEVICE float32 [pairs].  pairs: 8 to 64, a multiple of 8.
+ * axis: HOST [pairs], each below axes, or NULL where all are 0.  inv_freq: DEVICE float32 [pairs], 8-byte aligned.  pairs: 8 to 64, a multiple of 8.
  * table: DEVICE float32, row t at table + t*table_stride (at least 2*pairs, a multiple of 4; 16-byte aligned): cosine, sine, pair by pair.
  * Angles are formed and reduced in 64 bits, so a far position costs nothing: cosine and sine are off by 2^-23 at most, up to
  * angles of 2^40 either way.  An inv_freq that is not finite gives NaN. */

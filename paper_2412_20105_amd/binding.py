@@ -621,7 +621,7 @@ def st3_block_evict(shape: GqaShape, src: BlockCache, dst: BlockCache, max_len: 
 
 # -- the next turn: positions, rotation, further rows of a cache, attention over it ---------------
 def st3_rotary_table(positions, inv_freq, axis, table, stream=None) -> None:
-    """table [T, pairs, 2] <- cosines and sines.  positions int32 [axes, T] or [T]; inv_freq float32 [pairs]; axis: the component that turns each
+    """table [T, pairs, 2] <- cosines and sines.  positions int32 [axes, T] or [T]; inv_freq float32 [pairs], 8-byte aligned; axis: the component that turns each
     pair, a sequence of pairs integers, or None where there is one."""
     size, steps = positions.shape, positions.stride()
     if not 1 <= len(size) <= 2:
