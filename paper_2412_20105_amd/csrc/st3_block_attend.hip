@@ -9,8 +9,9 @@
 //                  that lane (c, g) of C ends with keys 16 g .. 16 g + 15 of row c.
 //   O^T = V^T P^T  the lane's 16 keys are the contraction slots 8g..8g+7 of two steps: P^T is where S^T left it.
 // No value crosses lanes but the maximum.  Where row tiles are too few to fill the card, a strip's blocks are cut into pieces, and a second launch joins them.
-// What bounds it: the matrix units with many rows (2048 tokens over 30000 rows 895 us, 1180 TFLOP/s); with few, the chain from a block's codes through both
-// products to its barrier (1.3 us a block of 64 keys with 36 rows, 1.8 with 256), so that rows up to kFewRows go another way, below, bound by memory.
+// What bounds it: the matrix units with many rows (2048 tokens over 30000 rows 895 to 930 us, 1140 to 1180 TFLOP/s); with few, the chain from a block's codes
+// through both products to its barrier (1.3 us a block of 64 keys with 36 rows, 1.8 with 256), so that rows up to kFewRows go another way, below, bound by
+// memory.
 #include <algorithm>
 #include <type_traits>
 
@@ -1050,7 +1051,8 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a) {
 // lie in LDS; a wave has the 64 keys of a block in registers, meets 16 rows at a time, and a lane adds up what its 16 keys get.  SHARED: a workgroup has one
 // block, and its waves every fourth 16 of the rows; their sums are added in one order.  Three waves of a SIMD hide
 // each other's loads of codes better than two that have the next block's codes on their way (those need the registers): a call with 16 tokens' windows over
-// 202000 rows took 303 us so, 314 before.
+// 202000 rows took 303 us so and 314 with two, before its other launches became as fast as they are (274).  At d = 128 LDS has room for three workgroups of up to
+// 192 rows each; with more, as in windows of 64 tokens of groups of 4, there are two (2048 tokens over 30000 rows: 31 to 36 us of scores).
 // ---------------------------------------------------------------------------------------------------------------------------------
 constexpr int kScoreRows = 256;         // rows in LDS at a time: 64 KB at d = 128
 
@@ -1216,16 +1218,17 @@ struct ChunkCut { int rows, piece, pieces, few, stage, groups; };
 constexpr int kMostRowsOfTile = 32 * kChunkWaves;
 constexpr int kWanted = 256;            // workgroups that a cut aims at: one has a compute unit's LDS to itself
 constexpr int kLeastPiece = 4;
-// Few rows, up to kFewRows: every wave has those of its group, kFewGroup at most (8 key heads, d = 128: 4 tokens of 32 sequences over 611 to 3136 rows 30 us,
-// by tiles 52; 8 of one over 30000 rows 22 and 37).  Two groups read a strip twice, the second time from L2: 16 tokens (64 rows) of 8 sequences over 20000 to
-// 30000 rows 130 us, by tiles 159; three would not pay (24 tokens of them 199, by tiles 155).
+// Few rows, up to kFewRows: every wave has those of its group, kFewGroup at most (8 key heads, d = 128: 4 tokens of 32 sequences over 611 to 3136 rows 27 us,
+// by tiles 56; 8 of one over 30000 rows 23 and 37).  Two groups read a strip twice, the second time from L2: 16 tokens (64 rows) of 8 sequences over 20000 to
+// 30000 rows 127 us, by tiles 159; three would not pay (24 tokens of them 199, by tiles 155).
 //   whole strips, without a join, and with one group's weights added at once, where there are kWholeStrips of them or they have no more than kShortUnits
-//     blocks: 64 sequences of 1000 to 3000 rows 50 us, in pieces 65; one of 744 rows 15.2 and 18.7; 16 sequences 35.0, in pieces 33.7.
-//     By 12 waves (8 with more than 16 rows), by 4 where there are more than kManyStrips: 32 sequences 30 us by 12 and 43 by 4, 64 sequences 51 and 50.
-//   pieces by 4 waves: of no more than kWanted / 4 strips one for each compute unit (one sequence of 30000 rows 22 us, three times as many pieces 39; eight
-//     of them 74 and 91), of more strips, whose lengths differ, three times as many (15 sequences of 1000 to 9000 rows 37 us, two pieces each 49).
+//     blocks: 4 tokens of 64 sequences of 1000 to 3000 rows 51 us, in pieces 57; 5 of one of 744 rows 16.2 and 19.3; 4 of 16 sequences 36.3, in pieces 34.4.
+//     By 12 waves (8 with more than 16 rows), by 4 where there are more than kManyStrips: 32 sequences 27.5 us by 12 and 28.6 by 4, 64 sequences 52.3 and
+//     51.0, with 8 tokens 65 and 61.
+//   pieces by 4 waves: of no more than kWanted / 4 strips one for each compute unit (8 tokens over 30000 rows 23 us, three times as many pieces 40; of eight
+//     sequences 82 and 95), of more strips, whose lengths differ, three times as many (4 tokens of 15 sequences of 1000 to 9000 rows 38.8 us, two pieces each 39.7).
 //     A wave's blocks are lanes of a register, no more than kMostPiece; longer strips in twice, three times as many pieces (4 tokens of 8 sequences over
-//     70000 to 131072 rows 276 us, in as few as hold them 302).
+//     70000 to 131072 rows 276 us, in as few as hold them 302, measured with one term of weights).
 constexpr int kFewGroup = 32, kFewRows = 64, kWholeStrips = 192, kShortUnits = 20, kManyStrips = 256, kMostPiece = 4 * kWave - 2;
 
 // Room for as many parts as a launch of these or any smaller sizes may leave.  Tiles hold all rows, so kWanted / tiles pieces are no more than kWanted tiles
